@@ -361,6 +361,136 @@ typedef struct {
 int mrp_module_set_prefix(mrp_ctx *ctx, const mrp_module_kv *layers, const int32_t *prefix_len, int32_t prefix_cap,
                           int32_t append);
 
+/*
+ * The attention of a block behind a PAGED key / value cache, for the layers around the drafting pass (Fig. 1(c): a
+ * block is decoded given the committed clean prefix; the paper leaves the cache to the engine): normalising and
+ * rotating queries and keys, storing keys and values in pages, reading them with the block's queries.  Unlike the
+ * prefix of mrp_module_set_prefix the sequences need no contiguous slab each, query heads may share key heads, and the
+ * positions, masks and lengths are those of decoding, of block diffusion and of prompts.
+ *
+ * The cache of a layer is a pool of pages
+ *     k, v   DEVICE [n_pages, n_kv_heads, page_size, head_dim], context dtype, 16-byte aligned, pages page_stride
+ *            elements apart (head-major, like the prefix caches: those are such a pool of max_seqs pages of prefix_cap
+ *            rows, and mrp_paged_attention can read them)
+ * and position p of sequence b lies in row p % page_size of page page_table[b, p / page_size].  Pools are named per
+ * call (one per layer); their geometry is attached once, with the workspace.  Rows and pages no sequence uses may hold
+ * anything, NaN included.
+ */
+typedef struct {
+    int32_t n_heads, n_kv_heads; /* query heads, key / value heads: n_heads % n_kv_heads == 0; query heads
+                                    [h g, (h + 1) g), g = n_heads / n_kv_heads, read key head h               */
+    int32_t head_dim;            /* multiple of 8, at most 256                                               */
+    int32_t page_size;           /* rows per page, >= 1                                                      */
+    int32_t n_pages;             /* pages of a pool (0: no cache, mrp_qk_norm_rotate only)                   */
+    int32_t max_pages;           /* entries of a page table row: a sequence holds at most max_pages *
+                                    page_size <= 2^30 positions                                              */
+    int64_t page_stride;         /* elements from a page to the next, a multiple of 8; 0 = pages one after
+                                    the other                                                                */
+    int32_t rot_dim;             /* leading features of a head that are rotated: even, 0..head_dim (0: none)  */
+    int32_t rot_interleaved;     /* pairs (j, j + rot_dim / 2) if 0, else (2 j, 2 j + 1)                     */
+    double rot_theta;            /* pair j of position p is turned by p * rot_theta^(-2 j / rot_dim), or, with */
+    const double *inv_freq;      /* inv_freq (HOST [rot_dim / 2], copied; NULL: rot_theta), by p * inv_freq[j] */
+    float norm_eps;              /* epsilon of the per-head RMSNorm                                          */
+} mrp_kv_config;
+
+/* Bytes of additional device workspace (0 on a bad configuration). */
+size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv);
+
+/*
+ * Attach a cache geometry to a context (workspace borrowed until mrp_destroy or the next attach: DEVICE, 256-byte
+ * aligned, at least mrp_kv_workspace_bytes; it must not serve another context too).  Like mrp_create this call may
+ * block (it clears the workspace's arrival counters); make it outside of any stream capture.  The three calls below run
+ * on the context's device and, like every call on a context, one after the other: a captured graph of them counts as a
+ * call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
+ */
+int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t workspace_bytes);
+
+/*
+ * The step's tokens: n_tokens rows, of which rows seq_start[b] .. seq_start[b + 1] - 1 are the new tokens of sequence b
+ * (any number, also none), at positions prefix_len[b], prefix_len[b] + 1, ... behind the prefix_len[b] positions the
+ * sequence has in the cache already.  All arrays DEVICE; the lengths are read on the device, so a captured call serves
+ * other lengths on replay.  A sequence whose rows or positions do not fit (0 <= seq_start[b] <= seq_start[b + 1] <=
+ * n_tokens, 0 <= prefix_len[b], prefix_len[b] + new tokens <= max_pages * page_size) raises MRP_DEV_BAD_INDEX and is
+ * skipped: nothing of it is stored or written.  Rows that belong to no sequence are left alone.  The rows of two
+ * sequences must not overlap.
+ */
+typedef struct {
+    const int32_t *seq_start;   /* [n_seqs + 1]                                                      */
+    const int32_t *prefix_len;  /* [n_seqs]                                                          */
+    const int32_t *page_table;  /* [n_seqs, max_pages]; only entries of pages in use are read; one outside
+                                   [0, n_pages) raises MRP_DEV_BAD_INDEX: keys and values are not stored in it, and
+                                   read as zeros                                                     */
+    const int32_t *positions;   /* [n_tokens] positions to rotate by, where they differ from the place in the
+                                   sequence; NULL: the place                                         */
+    int32_t n_seqs;             /* 0..max_seqs                                                       */
+    int32_t n_tokens;
+    int32_t max_new;            /* the largest number of new tokens of a sequence, as far as known on the host: it only
+                                   helps to choose a kernel, results do not depend on it being right */
+    int32_t *status;            /* optional device int32 receiving MRP_DEV_* bits                    */
+} mrp_kv_batch;
+
+/*
+ * Query, key and value rows [n_tokens, heads, head_dim] in the context dtype: the heads of a token side by side, tokens
+ * *_stride elements apart (the rows of a packed projection output; 16-byte aligned, strides multiples of 16 bytes).
+ * With gamma (DEVICE [head_dim], 16-byte aligned; NULL: no norm) a head x becomes x * rsqrt(mean(x^2) + norm_eps) *
+ * gamma, then its first rot_dim features are rotated.  Sums, angles and products in fp32 (the angle's turns exactly),
+ * one rounding at the end.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const void *gamma_q, *gamma_k;
+    void *q_out, *k_out;        /* may be the inputs themselves (with the same strides) */
+    int64_t q_out_stride, k_out_stride;
+} mrp_qkv_rows;
+
+/*
+ * Norms of queries and keys for each head with the rotation by positions[t] (DEVICE [n_tokens] int32, any sign; NULL
+ * where rot_dim is 0), one pass: q -> q_out, k -> k_out; either may be NULL; v is not read.
+ * Errors: INVALID_ARG, UNSUPPORTED (nothing attached), CUDA.
+ */
+int mrp_qk_norm_rotate(mrp_ctx *ctx, const int32_t *positions, int32_t n_tokens, const mrp_qkv_rows *rows,
+                       void *cuda_stream);
+
+/*
+ * Append the step's tokens to the cache: k normalised and rotated on the way, v as it is, into the pages of their
+ * sequences; with q, q is normalised and rotated into q_out in the same launch.  k_out is not used.  prefix_len is not
+ * changed: mrp_paged_attention of the same step takes the same batch, and the caller raises the lengths once the tokens
+ * are committed (a block that is decoded again overwrites its rows).  Pages shared by sequences may be read by all, but
+ * rows written by two sequences in one call hold either's.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int mrp_kv_append(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages, const mrp_qkv_rows *rows,
+                  void *cuda_stream);
+
+/* Which positions the new token at place i of a sequence (position p = prefix_len[b] + i) may see. */
+typedef enum {
+    MRP_ATTN_CAUSAL = 0,        /* 0 .. p                                                             */
+    MRP_ATTN_BLOCK = 1,         /* 0 .. prefix_len[b] + new tokens - 1: the block sees itself whole   */
+    MRP_ATTN_PREFIX = 2         /* 0 .. prefix_len[b] - 1: the cache alone                            */
+} mrp_attention_mask;
+
+typedef struct {
+    const void *q;              /* [n_tokens, n_heads, head_dim] rows, q_stride elements apart        */
+    void *out;                  /* the same shape and dtype, out_stride elements apart                */
+    int64_t q_stride, out_stride;
+    float *lse;                 /* optional [n_tokens, n_heads] fp32: log-sum-exp of the scaled scores */
+    int32_t mask;               /* mrp_attention_mask                                                 */
+    int32_t window;             /* > 0: of those only positions > p - window, and                     */
+    int32_t sinks;              /* the first `sinks` positions, which stay visible (read with a window only) */
+    float scale;                /* of the scores; 0 = 1 / sqrt(head_dim)                              */
+} mrp_attention_args;
+
+/*
+ * out = softmax(scale * q K^T) V over the visible positions of the token's sequence, per query head; a token that sees
+ * nothing gets zeros and lse = -inf.  (Two passes over disjoint sets of keys are joined by their lse: MRP_ATTN_PREFIX
+ * for the cache, and the block's own keys elsewhere.)  Scores, softmax statistics and sums in fp32; on bf16 contexts
+ * the probabilities are rounded to bf16 as an operand of the product with V.  What positions no token sees hold does not
+ * matter.  The work is split over the cache's length by the device from the lengths it finds; results do not depend on
+ * anything but the inputs (parts are joined in a fixed order).  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages,
+                        const mrp_attention_args *args, void *cuda_stream);
+
 typedef enum { MRP_SELECT_STATIC = 0, MRP_SELECT_DYNAMIC_REMASK = 1 } mrp_select_mode;
 
 typedef struct {

@@ -31,13 +31,15 @@ MRP_FLAG_NO_CTA_PAIRS = 256
 MRP_SELECT_STATIC, MRP_SELECT_DYNAMIC_REMASK = 0, 1
 MRP_DEV_NONFINITE, MRP_DEV_TIMEOUT, MRP_DEV_BAD_INDEX, MRP_DEV_RANGE = 1, 2, 4, 8
 MRP_RANGE_LIMIT = 32768.0
+MRP_ATTN_CAUSAL, MRP_ATTN_BLOCK, MRP_ATTN_PREFIX = 0, 1, 2
 
 EXPORTS = ("mrp_workspace_bytes", "mrp_create", "mrp_destroy", "mrp_draft", "mrp_reveal_remask",
            "mrp_verify", "mrp_last_launch_count", "mrp_kernel_family", "mrp_status_string",
            "mrp_profile_enable", "mrp_profile_read", "mrp_last_error",
            "mrp_reveal_remask_noalloc", "mrp_selftest_wait_timeout", "mrp_draft_from_hidden", "mrp_commit",
            "mrp_set_logits0_event", "mrp_set_input_rows", "mrp_fetch_status", "mrp_draft_kl", "mrp_draft_bf16_logits", "mrp_quantised_lm_head",
-           "mrp_module_workspace_bytes", "mrp_module_attach", "mrp_module_step", "mrp_module_set_prefix", "mrp_module_step_kl")
+           "mrp_module_workspace_bytes", "mrp_module_attach", "mrp_module_step", "mrp_module_set_prefix", "mrp_module_step_kl",
+           "mrp_kv_workspace_bytes", "mrp_kv_attach", "mrp_qk_norm_rotate", "mrp_kv_append", "mrp_paged_attention")
 MRP_NOALLOC_MAX_POSITIONS = 65536
 MRP_ERR_CAPACITY = 7
 
@@ -88,6 +90,32 @@ class mrp_module_weights(ctypes.Structure):
 
 class mrp_module_kv(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class mrp_kv_config(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("rot_dim", ctypes.c_int32), ("rot_interleaved", ctypes.c_int32),
+                ("rot_theta", ctypes.c_double), ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("norm_eps", ctypes.c_float)]
+
+
+class mrp_kv_batch(ctypes.Structure):
+    _fields_ = [("seq_start", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("status", ctypes.c_void_p)]
+
+
+class mrp_qkv_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("gamma_q", ctypes.c_void_p),
+                ("gamma_k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
+class mrp_attention_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("mask", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class mrp_block_state(ctypes.Structure):
@@ -165,6 +193,18 @@ def _load():
     lib.mrp_verify.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                ctypes.c_void_p, ctypes.c_void_p]
+    lib.mrp_kv_workspace_bytes.restype = ctypes.c_size_t
+    lib.mrp_kv_workspace_bytes.argtypes = [ctypes.POINTER(mrp_config), ctypes.POINTER(mrp_kv_config)]
+    lib.mrp_kv_attach.restype = ctypes.c_int
+    lib.mrp_kv_attach.argtypes = [ctypes.c_void_p, ctypes.POINTER(mrp_kv_config), ctypes.c_void_p, ctypes.c_size_t]
+    lib.mrp_qk_norm_rotate.restype = ctypes.c_int
+    lib.mrp_qk_norm_rotate.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(mrp_qkv_rows), ctypes.c_void_p]
+    lib.mrp_kv_append.restype = ctypes.c_int
+    lib.mrp_kv_append.argtypes = [ctypes.c_void_p, ctypes.POINTER(mrp_kv_batch), ctypes.POINTER(mrp_module_kv),
+                                  ctypes.POINTER(mrp_qkv_rows), ctypes.c_void_p]
+    lib.mrp_paged_attention.restype = ctypes.c_int
+    lib.mrp_paged_attention.argtypes = [ctypes.c_void_p, ctypes.POINTER(mrp_kv_batch), ctypes.POINTER(mrp_module_kv),
+                                        ctypes.POINTER(mrp_attention_args), ctypes.c_void_p]
     lib.mrp_profile_enable.restype = ctypes.c_int
     lib.mrp_profile_enable.argtypes = [ctypes.c_void_p, ctypes.c_int32]
     lib.mrp_profile_read.restype = ctypes.c_int
@@ -213,6 +253,7 @@ class Context:
     cfg: mrp_config
     keep: tuple           # weights + workspace kept alive for the context's lifetime
     guards: tuple = ()    # (buffer, workspace offset, workspace bytes, guard bytes) for workspace_guards_intact
+    kv: object = None     # geometry of the paged cache (mrp_kv_attach)
 
     @property
     def family(self) -> str:
@@ -395,6 +436,172 @@ def mrp_module_set_prefix(ctx: Context, caches, prefix_len, append=False) -> Non
     if rc != 0:
         raise MrpError("mrp_module_set_prefix", rc)
     ctx.prefix_keep = (caches, prefix_len)
+
+
+def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_pages=0, max_pages=0, page_stride=0, rot_dim=0,
+                  rot_theta=10000.0, rot_interleaved=False, inv_freq=None, norm_eps=1e-6) -> None:
+    """Attach the geometry of a paged key / value cache (mrp_kv_config); allocates its workspace (a torch tensor kept with
+    the context).  ``inv_freq``: rot_dim / 2 numbers instead of the powers of ``rot_theta``."""
+    freq = None
+    if inv_freq is not None:
+        vals = [float(x) for x in inv_freq]
+        if len(vals) != int(rot_dim) // 2:
+            raise ValueError("inv_freq holds rot_dim / 2 numbers")
+        freq = (ctypes.c_double * max(len(vals), 1))(*vals)
+    kv = mrp_kv_config(int(n_heads), int(n_kv_heads), int(head_dim), int(page_size), int(n_pages), int(max_pages),
+                       int(page_stride), int(rot_dim), int(bool(rot_interleaved)), float(rot_theta), freq, float(norm_eps))
+    nbytes = int(lib.mrp_kv_workspace_bytes(ctypes.byref(ctx.cfg), ctypes.byref(kv)))
+    if nbytes == 0:
+        raise MrpError("mrp_kv_workspace_bytes", 1)
+    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda:%d" % ctx.cfg.device)
+    off = (-ws.data_ptr()) % 256
+    rc = lib.mrp_kv_attach(ctx.handle, ctypes.byref(kv), ctypes.c_void_p(ws.data_ptr() + off), ctypes.c_size_t(nbytes))
+    if rc != 0:
+        raise MrpError("mrp_kv_attach", rc, lib.mrp_last_error(ctx.handle).decode())
+    dtype = torch.float32 if ctx.cfg.dtype == MRP_F32 else torch.bfloat16
+    page = kv.n_kv_heads * kv.page_size * kv.head_dim
+    ctx.kv = _KvShape(dtype, ctx.cfg.device, (kv.n_heads, kv.head_dim), (kv.n_kv_heads, kv.head_dim),
+                      (kv.n_pages, kv.n_kv_heads, kv.page_size, kv.head_dim),
+                      (kv.page_stride or page, kv.page_size * kv.head_dim, kv.head_dim, 1), kv.max_pages)
+    ctx.keep = tuple(ctx.keep) + (ws,)
+
+
+@dataclass
+class _KvShape:
+    dtype: torch.dtype
+    device: int
+    q_row: tuple              # (heads, head_dim)
+    k_row: tuple
+    pool: tuple               # shape and strides of a pool
+    pool_stride: tuple
+    max_pages: int
+
+
+class KvBatch:
+    """A step's tokens (mrp_kv_batch): ``seq_start`` [B + 1], ``prefix_len`` [B], ``page_table`` [B, max_pages], optionally
+    ``positions`` [n_tokens], ``status`` [1], all int32 on the device; made once per step, used by the calls of all layers."""
+
+    def __init__(self, seq_start, prefix_len, page_table, n_tokens, max_new, positions=None, status=None):
+        for t, nm in ((seq_start, "seq_start"), (prefix_len, "prefix_len"), (page_table, "page_table"), (positions, "positions"),
+                      (status, "status")):
+            _check(t, torch.int32, nm)
+            if t is not None and t.device != seq_start.device:
+                raise TypeError("%s is on another device than seq_start" % nm)
+        n_seqs = prefix_len.numel()
+        if seq_start.numel() != n_seqs + 1 or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+            raise ValueError("seq_start [B + 1], prefix_len [B], page_table [B, max_pages]")
+        if positions is not None and positions.numel() < int(n_tokens):
+            raise ValueError("positions [n_tokens]")
+        self.max_pages, self.n_tokens, self.device = int(page_table.shape[1]), int(n_tokens), seq_start.device.index
+        self.keep = (seq_start, prefix_len, page_table, positions, status)
+        self.c = mrp_kv_batch(seq_start.data_ptr(), prefix_len.data_ptr(), page_table.data_ptr(),
+                              None if positions is None else positions.data_ptr(), n_seqs, int(n_tokens), int(max_new),
+                              None if status is None else status.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def _kv_shape(ctx):
+    kv = getattr(ctx, "kv", None)
+    if kv is None:
+        raise MrpError("paged cache", 2, "mrp_kv_attach first")
+    return kv
+
+
+def _rows(kv, t, row, n_tokens, what):
+    """(address, token stride) of rows [>= n_tokens, heads, head_dim]: the heads of a token side by side."""
+    if t.dtype != kv.dtype or t.get_device() != kv.device:
+        raise TypeError("%s must be a CUDA tensor of %s on the context's device" % (what, kv.dtype))
+    st = t.stride()
+    if tuple(t.shape[1:]) != row or t.shape[0] < n_tokens or (n_tokens > 0 and (st[2] != 1 or (st[1] != row[1] and row[0] > 1))):
+        raise ValueError("%s is [tokens, %d, %d] with the heads of a token side by side" % (what, row[0], row[1]))
+    # the stride of a single row means nothing
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else row[0] * row[1]
+
+
+def _gamma(kv, t, what):
+    if t is None:
+        return None
+    if t.dtype != kv.dtype or t.get_device() != kv.device or t.numel() != kv.k_row[1] or not t.is_contiguous():
+        raise TypeError("%s is a contiguous CUDA tensor [head_dim] of %s" % (what, kv.dtype))
+    return t.data_ptr()
+
+
+def _pools(kv, batch, k_pages, v_pages):
+    for t in (k_pages, v_pages):
+        if t.dtype != kv.dtype or t.get_device() != kv.device:
+            raise TypeError("pools are CUDA tensors of %s on the context's device" % kv.dtype)
+        if tuple(t.shape) != kv.pool or t.stride() != kv.pool_stride:
+            raise ValueError("pools are [n_pages, n_kv_heads, page_size, head_dim] with the strides attached")
+    if batch.max_pages != kv.max_pages or batch.device != kv.device:
+        raise ValueError("the batch's page table is [B, max_pages] on the context's device")
+    return mrp_module_kv(k_pages.data_ptr(), v_pages.data_ptr())
+
+
+def _raw_stream(kv, stream):
+    return torch._C._cuda_getCurrentRawStream(kv.device) if stream is None else stream.cuda_stream
+
+
+def mrp_qk_norm_rotate(ctx: Context, positions, q, k, q_out, k_out, gamma_q=None, gamma_k=None, stream=None) -> None:
+    """Per-head RMSNorm (with gamma) and rotation by ``positions`` [tokens] int32 of query rows q [tokens, n_heads, head_dim]
+    and key rows k [tokens, n_kv_heads, head_dim], either None; rows may be strided (a packed projection), outputs the inputs."""
+    kv = _kv_shape(ctx)
+    n = (q if q is not None else k).shape[0]
+    r = mrp_qkv_rows()
+    if q is not None:
+        r.q, r.q_stride = _rows(kv, q, kv.q_row, n, "q")
+        r.q_out, r.q_out_stride = _rows(kv, q_out, kv.q_row, n, "q_out")
+    if k is not None:
+        r.k, r.k_stride = _rows(kv, k, kv.k_row, n, "k")
+        r.k_out, r.k_out_stride = _rows(kv, k_out, kv.k_row, n, "k_out")
+    r.gamma_q, r.gamma_k = _gamma(kv, gamma_q, "gamma_q"), _gamma(kv, gamma_k, "gamma_k")
+    if positions is not None:
+        _check(positions, torch.int32, "positions")
+        if positions.numel() < n or positions.get_device() != kv.device:
+            raise ValueError("positions [tokens] on the context's device")
+        positions = positions.data_ptr()
+    rc = lib.mrp_qk_norm_rotate(ctx.handle, positions, n, ctypes.byref(r), _raw_stream(kv, stream))
+    if rc != 0:
+        raise MrpError("mrp_qk_norm_rotate", rc, lib.mrp_last_error(ctx.handle).decode())
+
+
+def mrp_kv_append(ctx: Context, batch: KvBatch, k_pages, v_pages, k, v, gamma_k=None, q=None, q_out=None, gamma_q=None,
+                  stream=None) -> None:
+    """Store the batch's keys (normalised with gamma_k, rotated) and values in their sequences' pages; with ``q`` also
+    q -> q_out, normalised with gamma_q and rotated."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    pools = _pools(kv, batch, k_pages, v_pages)
+    r = mrp_qkv_rows()
+    r.k, r.k_stride = _rows(kv, k, kv.k_row, n, "k")
+    r.v, r.v_stride = _rows(kv, v, kv.k_row, n, "v")
+    r.gamma_k = _gamma(kv, gamma_k, "gamma_k")
+    if q is not None:
+        r.q, r.q_stride = _rows(kv, q, kv.q_row, n, "q")
+        r.q_out, r.q_out_stride = _rows(kv, q_out, kv.q_row, n, "q_out")
+        r.gamma_q = _gamma(kv, gamma_q, "gamma_q")
+    rc = lib.mrp_kv_append(ctx.handle, batch.ref, ctypes.byref(pools), ctypes.byref(r), _raw_stream(kv, stream))
+    if rc != 0:
+        raise MrpError("mrp_kv_append", rc, lib.mrp_last_error(ctx.handle).decode())
+
+
+def mrp_paged_attention(ctx: Context, batch: KvBatch, k_pages, v_pages, q, out, lse=None, mask=MRP_ATTN_CAUSAL, window=0,
+                        sinks=0, scale=0.0, stream=None) -> None:
+    """Attention of the batch's queries q [tokens, n_heads, head_dim] over their sequences' pages into ``out``; ``lse``
+    [tokens, n_heads] fp32 optional."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    pools = _pools(kv, batch, k_pages, v_pages)
+    a = mrp_attention_args()
+    a.q, a.q_stride = _rows(kv, q, kv.q_row, n, "q")
+    a.out, a.out_stride = _rows(kv, out, kv.q_row, n, "out")
+    if lse is not None:
+        if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != kv.device or lse.numel() < n * kv.q_row[0]:
+            raise TypeError("lse is a contiguous CUDA tensor [tokens, n_heads] of float32 on the context's device")
+        a.lse = lse.data_ptr()
+    a.mask, a.window, a.sinks, a.scale = mask, window, sinks, scale
+    rc = lib.mrp_paged_attention(ctx.handle, batch.ref, ctypes.byref(pools), ctypes.byref(a), _raw_stream(kv, stream))
+    if rc != 0:
+        raise MrpError("mrp_paged_attention", rc, lib.mrp_last_error(ctx.handle).decode())
 
 
 def mrp_set_input_rows(ctx: Context, n_rows: int) -> None:

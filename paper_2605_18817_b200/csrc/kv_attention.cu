@@ -1,0 +1,725 @@
+// Attention over the pages of a key / value cache: the kernel for few query rows per sequence (decoding), and for the
+// shapes the large-tile kernel does not take.
+//
+//   out_r = sum_j p_rj V_j / sum_j p_rj,  p_rj = exp2(scale log2(e) (q_r . K_j) - m_r)  over the visible positions j,
+// m_r the running maximum (raised only when a score exceeds it by 2^8, which keeps p and its sum well inside fp32 and
+// bf16 and spares most rescalings of the accumulator), p_rj and its sum in fp32.
+//
+// Decoding reads every K / V row once and does little else: memory bounds it.  The g = n_heads / n_kv_heads query heads
+// that share a key head and the new tokens of a sequence are the rows of one tile (row r = token r / g, head r % g; 16
+// rows), so a K / V row is read once for all of them.  The keys of a (sequence, row tile, key head) unit go in tiles of
+// 64, 16 for each of the CTA's four warps; a warp keeps its own ring of 16-key stages filled by cp.async ahead of its
+// products and meets the other warps only at the end of a unit.  All tiles of all units form one line that is cut into
+// equal pieces, one per CTA of a grid that fills the GPU: ragged batches balance to one tile, and a unit cut in two or
+// more pieces is joined by the CTA that finishes last (an arrival counter; nobody waits).  The lengths are read on the
+// device, so the cut is found there: every CTA sums the units' tiles itself.
+//
+// bf16: mma.sync m16n8k16, operands by ldmatrix from XOR-swizzled rows, probabilities rounded to bf16.
+// f32:  mma.sync m16n8k8 on tf32 operands split into two (x = hi + lo, three products: relative 2^-21).
+#include "kv_attention.cuh"
+
+namespace mrp {
+namespace {
+
+constexpr int kRows = 16;                  // query rows of a tile
+constexpr int kTile = 64;                  // keys of a tile
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kWarpKeys = kTile / kWarps;  // 16
+constexpr float kLazy = 8.f;               // log2 of the growth a running maximum may lag behind
+
+struct AttnParams {
+    KvBatch b;
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    int64_t q_stride, out_stride;
+    int H, Hk, g, D;
+    int mask, window, sinks;
+    float scale_log2;
+    KvPartials part;
+};
+
+__device__ __forceinline__ uint32_t s_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool read)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t r[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t r[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void mma16(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x = hi + lo, both tf32 (10 mantissa bits and a sign each): what is left out is below 2^-21 of x
+__device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo)
+{
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---- the line of tiles ---------------------------------------------------------------------------------------------
+// A row tile of a sequence: its rows, what they may see, its key tiles.  Tiles 0..first-1 hold the first positions that
+// stay visible beside the window, the others start at key tile `base`.
+struct RowTile {
+    int r0, rows;              // rows r0 .. r0 + rows - 1 of the sequence's n * g
+    int lo, hi, s1;            // some row sees positions [lo, hi), [0, s1)
+    int first, base, tiles;
+};
+__device__ __forceinline__ RowTile row_tile(const AttnParams &p, int n, int pre, int rt)
+{
+    RowTile t;
+    t.r0 = rt * kRows;
+    t.rows = min(kRows, n * p.g - t.r0);
+    const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
+    t.hi = p.mask == MRP_ATTN_CAUSAL ? pre + i1 + 1 : p.mask == MRP_ATTN_BLOCK ? pre + n : pre;
+    t.lo = p.window > 0 ? max(0, pre + i0 + 1 - p.window) : 0;
+    t.s1 = p.window > 0 ? min(min(p.sinks, t.lo), t.hi) : 0;
+    t.base = t.lo / kTile;
+    const int end = t.hi > t.lo ? (t.hi + kTile - 1) / kTile : t.base;
+    t.first = (t.s1 + kTile - 1) / kTile;
+    if (t.first >= t.base) {               // they meet: one run from position 0
+        t.tiles = max(end > t.base ? end : 0, t.first);
+        t.first = 0;
+        t.base = 0;
+    } else {
+        t.tiles = t.first + (end - t.base);
+    }
+    t.tiles = max(t.tiles, 1);             // rows that see nothing are still written
+    return t;
+}
+__device__ __forceinline__ int key_tile(const RowTile &t, int i) { return i < t.first ? i : t.base + i - t.first; }
+
+__device__ __forceinline__ long long sequence_tiles(const AttnParams &p, int s, bool report)
+{
+    int start, n, pre;
+    if (!kv_sequence(p.b, s, start, n, pre)) {
+        if (report) kv_bad_index(p.b);
+        return 0;
+    }
+    const int nrt = (n * p.g + kRows - 1) / kRows;
+    long long sum = 0;
+    for (int rt = 0; rt < nrt; ++rt) sum += row_tile(p, n, pre, rt).tiles;
+    return sum * p.Hk;
+}
+
+// A place on the line: tile `i` of unit (sequence s, row tile rt, key head h); `at` its offset on the line, `unit` the
+// offset of the unit's first tile.
+struct Cursor {
+    int s, rt, h, i;
+    int start, n, pre;
+    RowTile t;
+    long long at, unit;
+};
+__device__ __forceinline__ bool open_sequence(const AttnParams &p, Cursor &c)
+{
+    for (; c.s < p.b.n_seqs; ++c.s)
+        if (kv_sequence(p.b, c.s, c.start, c.n, c.pre) && c.n > 0) {
+            c.rt = 0; c.h = 0; c.i = 0;
+            c.t = row_tile(p, c.n, c.pre, 0);
+            return true;
+        }
+    return false;
+}
+__device__ __forceinline__ void advance(const AttnParams &p, Cursor &c)
+{
+    ++c.at;
+    if (++c.i < c.t.tiles) return;
+    c.i = 0;
+    c.unit = c.at;
+    if (++c.h < p.Hk) return;
+    c.h = 0;
+    if (++c.rt < (c.n * p.g + kRows - 1) / kRows) {
+        c.t = row_tile(p, c.n, c.pre, c.rt);
+        return;
+    }
+    ++c.s;
+    open_sequence(p, c);
+}
+
+// Sets `c` to the start of this CTA's piece and returns its length; `per` is the length of a full piece.
+__device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor &c, long long &per, long long *sh)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long *sh_warp = sh, *sh_found = sh + kWarps;      // [kWarps], [2]
+    long long total = 0, mine = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += kThreads) {
+        const int s = s0 + tid;
+        mine = s < p.b.n_seqs ? sequence_tiles(p, s, blockIdx.x == 0) : 0;
+        long long x = mine;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
+        __syncthreads();
+        if (lane == 0) sh_warp[warp] = x;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) total += sh_warp[w];
+    }
+    per = (total + gridDim.x - 1) / gridDim.x;
+    const long long begin = per * blockIdx.x, end = min(total, begin + per);
+    if (begin >= end) return 0;
+    long long done = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += kThreads) {
+        const int s = s0 + tid;
+        if (p.b.n_seqs > kThreads) mine = s < p.b.n_seqs ? sequence_tiles(p, s, false) : 0;
+        long long x = mine;                // inclusive sum over the lanes
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, w);
+            if (lane >= w) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) sh_warp[warp] = x;
+        __syncthreads();
+        long long before = done + x - mine;
+        for (int w = 0; w < warp; ++w) before += sh_warp[w];
+        for (int w = 0; w < kWarps; ++w) done += sh_warp[w];
+        if (mine > 0 && before <= begin && begin < before + mine) {
+            sh_found[0] = s;
+            sh_found[1] = before;
+        }
+        __syncthreads();
+        if (done > begin) break;
+    }
+    c.s = (int)sh_found[0];
+    c.at = sh_found[1];
+    open_sequence(p, c);
+    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
+        c.at += (long long)c.t.tiles * p.Hk;
+        c.t = row_tile(p, c.n, c.pre, ++c.rt);
+    }
+    const int in = (int)(begin - c.at);
+    c.h = in / c.t.tiles;
+    c.i = in - c.h * c.t.tiles;
+    c.at = begin;
+    c.unit = begin - c.i;
+    return end - begin;
+}
+
+// ---- element types -------------------------------------------------------------------------------------------------
+template <typename T, int DP> struct Geo;
+template <int DP> struct Geo<__nv_bfloat16, DP> {
+    static constexpr int kChunks = DP / 8;                 // 16-byte chunks of a row
+    static constexpr int kPitchK = DP * 2, kPitchV = DP * 2, kPitchQ = DP * 2;     // bytes; chunks XOR-swizzled
+    static constexpr int kStages = DP <= 128 ? 3 : 2;
+    static constexpr bool kSwizzle = true;
+};
+template <int DP> struct Geo<float, DP> {
+    static constexpr int kChunks = DP / 4;
+    static constexpr int kPitchK = DP * 4 + 32, kPitchV = DP * 4 + 16, kPitchQ = DP * 4 + 32;
+    static constexpr int kStages = DP <= 64 ? 3 : DP <= 128 ? 2 : 1;
+    static constexpr bool kSwizzle = false;
+};
+template <typename T, int DP> struct Smem {
+    typedef Geo<T, DP> G;
+    static constexpr int kStage = kWarpKeys * (G::kPitchK + G::kPitchV);
+    static constexpr int kRing = kWarps * G::kStages * kStage;
+    static constexpr int kQ = kRows * G::kPitchQ;
+    static constexpr int kRedPitch = DP + 4;               // floats
+    static constexpr int kRed = kWarps * kRows * kRedPitch * 4;
+    static constexpr int kMl = 2 * kWarps * kRows * 4;
+    static constexpr int kTotal = kRing + kQ + kRed + kMl;
+    static constexpr int kCtas = kTotal <= 113 * 1024 ? 2 : 1;
+};
+
+template <int DP>
+__device__ __forceinline__ uint32_t chunk_at(uint32_t base, int row, int chunk)    // bf16 rows
+{
+    return base + row * (DP * 2) + ((chunk ^ (row & 7)) << 4);
+}
+
+// Zeroes values that are not finite in rows that some but not all query rows see, after adding them to the rows that
+// do: 0 * inf must not reach the others.  p[nt][4]: the warp's probabilities; v: the warp's 16 value rows.
+template <typename T, int DP, int NF>
+__device__ __noinline__ void patch_nonfinite(uint32_t v, const float (&pr)[2][4], float (&o)[NF][4], int lane)
+{
+    constexpr int pitch = Geo<T, DP>::kPitchV;
+    bool bad = false;
+    const int key = lane >> 1;
+    for (int c = lane & 1; c < Geo<T, DP>::kChunks; c += 2) {
+        uint32_t w[4];
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + key * pitch + c * 16) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            bad |= sizeof(T) == 4 ? (w[i] & 0x7F800000u) == 0x7F800000u
+                                  : (w[i] & 0x7F800000u) == 0x7F800000u || (w[i] & 0x7F80u) == 0x7F80u;
+    }
+    uint32_t rows = __ballot_sync(0xffffffffu, bad);
+    while (rows) {
+        const int kk = (__ffs(rows) - 1) >> 1;
+        rows &= ~(3u << (2 * kk));
+        const int owner = (lane & ~3) | ((kk & 7) >> 1);
+        const float pa0 = __shfl_sync(0xffffffffu, pr[0][0], owner), pa1 = __shfl_sync(0xffffffffu, pr[0][1], owner);
+        const float pb0 = __shfl_sync(0xffffffffu, pr[0][2], owner), pb1 = __shfl_sync(0xffffffffu, pr[0][3], owner);
+        const float pc0 = __shfl_sync(0xffffffffu, pr[1][0], owner), pc1 = __shfl_sync(0xffffffffu, pr[1][1], owner);
+        const float pd0 = __shfl_sync(0xffffffffu, pr[1][2], owner), pd1 = __shfl_sync(0xffffffffu, pr[1][3], owner);
+        const float pu = kk < 8 ? (kk & 1 ? pa1 : pa0) : (kk & 1 ? pc1 : pc0);
+        const float pl = kk < 8 ? (kk & 1 ? pb1 : pb0) : (kk & 1 ? pd1 : pd0);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            const int e = f * 8 + 2 * (lane & 3);
+            float x0, x1;
+            if (sizeof(T) == 2) {
+                uint32_t w;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(chunk_at<DP>(v, kk, f) + 4 * (lane & 3)) : "memory");
+                x0 = __uint_as_float(w << 16);
+                x1 = __uint_as_float(w & 0xFFFF0000u);
+            } else {
+                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x0), "=f"(x1) : "r"(v + kk * pitch + e * 4) : "memory");
+            }
+            if (pu > 0.f) { o[f][0] = fmaf(pu, x0, o[f][0]); o[f][1] = fmaf(pu, x1, o[f][1]); }
+            if (pl > 0.f) { o[f][2] = fmaf(pl, x0, o[f][2]); o[f][3] = fmaf(pl, x1, o[f][3]); }
+        }
+        __syncwarp();
+        for (int c = lane; c < Geo<T, DP>::kChunks; c += 32)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + kk * pitch + c * 16), "r"(0u) : "memory");
+        __syncwarp();
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_kernel(const __grid_constant__ AttnParams p)
+{
+    typedef Geo<T, DP> G;
+    typedef Smem<T, DP> S;
+    constexpr bool kBf16 = sizeof(T) == 2;
+    constexpr int kStages = G::kStages;
+    constexpr int NF = DP / 8;                             // 8-feature blocks of the accumulator
+    constexpr bool kQRegs = kBf16 && DP <= 128;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ long long sh_find[kWarps + 2];
+    __shared__ int sh_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int gid = lane >> 2, tig = lane & 3;
+    const uint32_t ring = s_addr(smem) + warp * kStages * S::kStage;
+    const uint32_t sq = s_addr(smem) + S::kRing;
+    float *red = reinterpret_cast<float *>(smem + S::kRing + S::kQ);
+    float *red_m = reinterpret_cast<float *>(smem + S::kRing + S::kQ + S::kRed), *red_l = red_m + kWarps * kRows;
+    const T *kp = reinterpret_cast<const T *>(p.k), *vp = reinterpret_cast<const T *>(p.v);
+    const int P = p.b.page.d, chunks = kBf16 ? p.D / 8 : p.D / 4;
+
+    pdl_wait();
+    pdl_trigger();
+    Cursor cur;
+    long long per;
+    const long long len = find_piece(p, cur, per, sh_find);
+    if (len == 0) return;
+
+    // -- loads run kStages - 1 tiles ahead of the products, through their own cursor; the page of the lane's key is
+    //    fetched another tile ahead
+    Cursor ld = cur;
+    long long to_load = len;
+    int entry = 0, row_in_page = 0;
+    bool see = false;
+    auto look_up = [&]() {                                 // lanes l and l + 16: key l of the warp's 16
+        const int j = key_tile(ld.t, ld.i) * kTile + warp * kWarpKeys + (lane & 15);
+        see = j < ld.t.hi && (j >= ld.t.lo || j < ld.t.s1);
+        entry = 0;
+        row_in_page = 0;
+        if (see) {
+            const int pg = fast_div(j, p.b.page);
+            row_in_page = j - pg * P;
+            entry = __ldg(p.b.page_table + (size_t)ld.s * p.b.max_pages + pg);
+        }
+    };
+    auto load_tile = [&](int stage) {
+        if (to_load > 0) {
+            if (see && (unsigned)entry >= (unsigned)p.b.n_pages) {
+                see = false;
+                if (lane < 16) kv_bad_index(p.b);
+            }
+            const long long off = see ? (long long)entry * p.b.page_stride + ((long long)ld.h * P + row_in_page) * p.D : -1;
+            const uint32_t dk = ring + stage * S::kStage, dv = dk + kWarpKeys * G::kPitchK;
+            constexpr int per_row = G::kChunks;
+            constexpr int rows_at_once = per_row >= 32 ? 1 : 32 / per_row;
+            constexpr int reps = per_row >= 32 ? per_row / 32 : 1;
+#pragma unroll
+            for (int r = 0; r < kWarpKeys; r += rows_at_once) {
+                const int row = r + (per_row >= 32 ? 0 : lane / per_row);
+                const long long ro = __shfl_sync(0xffffffffu, off, row);
+#pragma unroll
+                for (int x = 0; x < reps; ++x) {
+                    const int ch = per_row >= 32 ? lane + 32 * x : lane % per_row;
+                    const bool on = ro >= 0 && ch < chunks;
+                    const long long src = on ? ro + ch * (16 / (int)sizeof(T)) : 0;
+                    const int dc = G::kSwizzle ? ch ^ (row & 7) : ch;
+                    cp16(dk + row * G::kPitchK + dc * 16, kp + src, on);
+                    cp16(dv + row * G::kPitchV + dc * 16, vp + src, on);
+                }
+            }
+            advance(p, ld);
+            if (--to_load > 0) look_up();
+        }
+        cp_commit();
+    };
+    look_up();
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) load_tile(s);
+
+    const long long piece_end = cur.at + len;
+    int stage = 0;
+    long long at = cur.at;
+    while (at < piece_end) {
+        // ---- a unit, or the part of it in this piece
+        const int begin_tile = cur.i;
+        const int count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        const RowTile t = cur.t;
+        // queries of the tile -> shared memory, zero beyond the rows and features there are
+        for (int i = tid; i < kRows * G::kChunks; i += kThreads) {
+            const int r = i / G::kChunks, ch = i - r * G::kChunks;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < t.rows && ch < chunks) {
+                const int row = t.r0 + r, tok = row / p.g, hg = row - tok * p.g;
+                x = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.q) + (int64_t)(cur.start + tok) * p.q_stride +
+                                                          (int64_t)(cur.h * p.g + hg) * p.D) + ch);
+            }
+            const uint32_t a = sq + r * G::kPitchQ + ((G::kSwizzle ? ch ^ (r & 7) : ch) << 4);
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        }
+        __syncthreads();
+        uint32_t qf[kQRegs ? DP / 16 : 1][4];
+        if constexpr (kQRegs) {
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) ldsm4(chunk_at<DP>(sq, lane & 15, 2 * ks + (lane >> 4)), qf[ks]);
+        }
+        // the two rows of this lane: what they see
+        int hi2[2], lo2[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int r = min(gid + 8 * x, t.rows - 1), pos = cur.pre + (t.r0 + r) / p.g;
+            hi2[x] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
+            lo2[x] = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+        }
+        const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
+        const int all_hi = p.mask == MRP_ATTN_CAUSAL ? cur.pre + i0 + 1 : t.hi;      // all rows see [all_lo, all_hi)
+        const int all_lo = p.window > 0 ? max(0, cur.pre + i1 + 1 - p.window) : 0;
+        const bool differ = i0 != i1 && (p.mask == MRP_ATTN_CAUSAL || p.window > 0);
+
+        float o[NF][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[f][x] = 0.f;
+
+        for (int n = 0; n < count; ++n) {
+            load_tile((stage + kStages - 1) % kStages);
+            cp_wait<kStages - 1>();
+            __syncwarp();
+            const uint32_t sk = ring + stage * S::kStage, sv = sk + kWarpKeys * G::kPitchK;
+            const int j0 = key_tile(t, begin_tile + n) * kTile + warp * kWarpKeys;
+            float s[2][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) s[x][y] = 0.f;
+            if constexpr (kBf16) {
+#pragma unroll
+                for (int ks = 0; ks < DP / 16; ++ks) {
+                    uint32_t b[4], a[4];
+                    ldsm4(chunk_at<DP>(sk, ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)), b);
+                    if constexpr (kQRegs) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) a[x] = qf[ks][x];
+                    } else {
+                        ldsm4(chunk_at<DP>(sq, lane & 15, 2 * ks + (lane >> 4)), a);
+                    }
+                    mma16(s[0], a, b[0], b[1]);
+                    mma16(s[1], a, b[2], b[3]);
+                }
+            } else {
+#pragma unroll 4
+                for (int ks = 0; ks < DP / 8; ++ks) {      // features 2 tig, 2 tig + 1 stand for k = tig, tig + 4
+                    float2 qa, qb;
+                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qa.x), "=f"(qa.y) : "r"(sq + gid * G::kPitchQ + (ks * 8 + 2 * tig) * 4) : "memory");
+                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qb.x), "=f"(qb.y) : "r"(sq + (gid + 8) * G::kPitchQ + (ks * 8 + 2 * tig) * 4) : "memory");
+                    uint32_t ah[4], al[4];
+                    split_tf32(qa.x, ah[0], al[0]);
+                    split_tf32(qb.x, ah[1], al[1]);
+                    split_tf32(qa.y, ah[2], al[2]);
+                    split_tf32(qb.y, ah[3], al[3]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        float2 kb;
+                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(kb.x), "=f"(kb.y) : "r"(sk + (x * 8 + gid) * G::kPitchK + (ks * 8 + 2 * tig) * 4) : "memory");
+                        uint32_t bh[2], bl[2];
+                        split_tf32(kb.x, bh[0], bl[0]);
+                        split_tf32(kb.y, bh[1], bl[1]);
+                        mma8(s[x], al, bh[0], bh[1]);
+                        mma8(s[x], ah, bl[0], bl[1]);
+                        mma8(s[x], ah, bh[0], bh[1]);
+                    }
+                }
+            }
+            // scores in units of log2; what a row does not see is -inf
+            const bool whole = j0 >= all_lo && j0 + kWarpKeys <= all_hi;
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    s[x][y] *= p.scale_log2;
+                    if (!whole) {
+                        const int j = j0 + x * 8 + 2 * tig + (y & 1);
+                        if (!(j < hi2[y >> 1] && (j >= lo2[y >> 1] || j < p.sinks))) s[x][y] = -INFINITY;
+                    }
+                    top[y >> 1] = fmaxf(top[y >> 1], s[x][y]);
+                }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 1));
+                top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 2));
+            }
+            if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float nm = fmaxf(m[x], top[x]);
+                    const float c = m[x] == nm ? 1.f : exp2_fast(m[x] - nm);       // (-inf before the first visible key: 0)
+                    l[x] *= c;
+#pragma unroll
+                    for (int f = 0; f < NF; ++f) { o[f][2 * x] *= c; o[f][2 * x + 1] *= c; }
+                    m[x] = nm;
+                }
+            }
+            const float mm[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    s[x][y] = exp2_fast(s[x][y] - mm[y >> 1]);
+                    l[y >> 1] += s[x][y];
+                }
+            if (!whole && differ) patch_nonfinite<T, DP, NF>(sv, s, o, lane);
+            if constexpr (kBf16) {
+                uint32_t a[4];
+                const __nv_bfloat162 h0 = __floats2bfloat162_rn(s[0][0], s[0][1]), h1 = __floats2bfloat162_rn(s[0][2], s[0][3]);
+                const __nv_bfloat162 h2 = __floats2bfloat162_rn(s[1][0], s[1][1]), h3 = __floats2bfloat162_rn(s[1][2], s[1][3]);
+                a[0] = *reinterpret_cast<const uint32_t *>(&h0);
+                a[1] = *reinterpret_cast<const uint32_t *>(&h1);
+                a[2] = *reinterpret_cast<const uint32_t *>(&h2);
+                a[3] = *reinterpret_cast<const uint32_t *>(&h3);
+#pragma unroll
+                for (int f = 0; f < NF; f += 2) {
+                    uint32_t b[4];
+                    ldsm4t(chunk_at<DP>(sv, (((lane >> 3) & 1) << 3) + (lane & 7), f + (lane >> 4)), b);
+                    mma16(o[f], a, b[0], b[1]);
+                    mma16(o[f + 1], a, b[2], b[3]);
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {              // keys 2 tig, 2 tig + 1 stand for k = tig, tig + 4
+                    uint32_t ah[4], al[4];
+                    split_tf32(s[x][0], ah[0], al[0]);
+                    split_tf32(s[x][2], ah[1], al[1]);
+                    split_tf32(s[x][1], ah[2], al[2]);
+                    split_tf32(s[x][3], ah[3], al[3]);
+#pragma unroll
+                    for (int f = 0; f < NF; ++f) {
+                        float v0, v1;
+                        const uint32_t a0 = sv + (x * 8 + 2 * tig) * G::kPitchV + (f * 8 + gid) * 4;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v0) : "r"(a0) : "memory");
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v1) : "r"(a0 + G::kPitchV) : "memory");
+                        uint32_t bh[2], bl[2];
+                        split_tf32(v0, bh[0], bl[0]);
+                        split_tf32(v1, bh[1], bl[1]);
+                        mma8(o[f], al, bh[0], bh[1]);
+                        mma8(o[f], ah, bl[0], bl[1]);
+                        mma8(o[f], ah, bh[0], bh[1]);
+                    }
+                }
+            }
+            __syncwarp();
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+
+        // ---- the four warps' parts meet
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+            if (tig == 0) {
+                red_m[warp * kRows + gid + 8 * x] = m[x];
+                red_l[warp * kRows + gid + 8 * x] = l[x];
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+                *reinterpret_cast<float2 *>(red + (size_t)(warp * kRows + gid + 8 * x) * S::kRedPitch + f * 8 + 2 * tig) =
+                    make_float2(o[f][2 * x], o[f][2 * x + 1]);
+        }
+        __syncthreads();
+        const bool whole_unit = count == t.tiles;
+        const int slot = 2 * blockIdx.x + (begin_tile == 0 ? 1 : 0);
+        constexpr int F4 = DP / 4;
+        auto put = [&](int r, int f4, float4 a, float M, float L) {       // final values of a row's four features
+            const int row = t.r0 + r, tok = row / p.g, head = cur.h * p.g + row - tok * p.g;
+            const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);   // (NaN goes through)
+            a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+            T *dst = reinterpret_cast<T *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D + f4 * 4;
+            if (f4 * 4 < p.D) {
+                if constexpr (kBf16) {
+                    const __nv_bfloat162 x0 = __floats2bfloat162_rn(a.x, a.y), x1 = __floats2bfloat162_rn(a.z, a.w);
+                    *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&x0), *reinterpret_cast<const uint32_t *>(&x1));
+                } else {
+                    *reinterpret_cast<float4 *>(dst) = a;
+                }
+            }
+            if (f4 == 0 && p.lse)
+                p.lse[(int64_t)(cur.start + tok) * p.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        };
+        for (int i = tid; i < t.rows * F4; i += kThreads) {
+            const int r = i / F4, f4 = i - r * F4;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red_m[w * kRows + r]);
+            float L = 0.f;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = red_m[w * kRows + r];
+                const float c = mw == -INFINITY ? 0.f : exp2_fast(mw - M);
+                if (mw == -INFINITY && red_l[w * kRows + r] == 0.f) continue;        // saw nothing
+                const float4 x = *reinterpret_cast<const float4 *>(red + (size_t)(w * kRows + r) * S::kRedPitch + f4 * 4);
+                L = fmaf(c, red_l[w * kRows + r], L);
+                a.x = fmaf(c, x.x, a.x); a.y = fmaf(c, x.y, a.y); a.z = fmaf(c, x.z, a.z); a.w = fmaf(c, x.w, a.w);
+            }
+            if (whole_unit) {
+                put(r, f4, a, M, L);
+            } else {
+                __stcg(reinterpret_cast<float4 *>(p.part.o + ((size_t)slot * kRows + r) * DP) + f4, a);
+                if (f4 == 0) __stcg(p.part.ml + (size_t)slot * kRows + r, make_float2(M, L));
+            }
+        }
+        if (!whole_unit) {
+            // ---- the pieces of a unit meet: the CTA that arrives last joins them in the order of the pieces
+            const int c0 = (int)(cur.unit / per), c1 = (int)((cur.unit + t.tiles - 1) / per);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) sh_last = atomicAdd(p.part.counters + c0, 1) == c1 - c0;
+            __syncthreads();
+            if (sh_last) {
+                __threadfence();
+                for (int i = tid; i < t.rows * F4; i += kThreads) {
+                    const int r = i / F4, f4 = i - r * F4;
+                    float M = -INFINITY;
+                    for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(p.part.ml + (size_t)(2 * c + (c == c0)) * kRows + r).x);
+                    float L = 0.f;
+                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) {
+                        const size_t sl = (size_t)(2 * c + (c == c0)) * kRows + r;
+                        const float2 ml = __ldcg(p.part.ml + sl);
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.part.o + sl * DP) + f4);
+                        if (ml.x == -INFINITY && ml.y == 0.f) continue;
+                        const float w = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - M);
+                        L = fmaf(w, ml.y, L);
+                        a.x = fmaf(w, x.x, a.x); a.y = fmaf(w, x.y, a.y); a.z = fmaf(w, x.z, a.z); a.w = fmaf(w, x.w, a.w);
+                    }
+                    put(r, f4, a, M, L);
+                }
+                if (tid == 0) p.part.counters[c0] = 0;
+            }
+        }
+        // ---- next unit
+        at += count;
+        if (at < piece_end) {
+            cur.i = t.tiles - 1;
+            cur.at = at - 1;
+            advance(p, cur);
+            __syncthreads();               // the queries and the parts of this unit are read
+        }
+    }
+    cp_wait<0>();
+}
+
+size_t slot_bytes() { return (size_t)kRows * (256 * 4 + 8); }
+
+template <typename T, int DP>
+cudaError_t prepare()
+{
+    return cudaFuncSetAttribute(kv_attention_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<T, DP>::kTotal);
+}
+template <typename T, int DP>
+cudaError_t launch(Ctx *c, const AttnParams &p, cudaStream_t st)
+{
+    const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
+    cudaError_t e = launch_k(kv_attention_kernel<T, DP>, dim3(sms * Smem<T, DP>::kCtas), dim3(kThreads), Smem<T, DP>::kTotal, st,
+                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
+    c->launches = 1;
+    return note_err(c, e, "kv_attention_kernel");
+}
+
+}  // namespace
+
+size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv)
+{
+    (void)cfg; (void)kv;
+    return kKvCounterBytes + (size_t)4 * kKvMaxSm * slot_bytes();
+}
+
+cudaError_t kv_attach(Ctx *c)
+{
+    cudaError_t e = cudaMemset(c->kv_ws, 0, kKvCounterBytes);
+    if (e != cudaSuccess) return e;
+    if (c->cfg.dtype == MRP_BF16) {
+        if ((e = prepare<__nv_bfloat16, 64>()) != cudaSuccess || (e = prepare<__nv_bfloat16, 128>()) != cudaSuccess) return e;
+        return prepare<__nv_bfloat16, 256>();
+    }
+    if ((e = prepare<float, 64>()) != cudaSuccess || (e = prepare<float, 128>()) != cudaSuccess) return e;
+    return prepare<float, 256>();
+}
+
+cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_module_kv &pages,
+                                   const mrp_attention_args &a, cudaStream_t st)
+{
+    const mrp_kv_config &kv = c->kv;
+    AttnParams p;
+    p.b.seq_start = batch.seq_start;
+    p.b.prefix_len = batch.prefix_len;
+    p.b.page_table = batch.page_table;
+    p.b.positions = nullptr;
+    p.b.n_seqs = batch.n_seqs;
+    p.b.n_tokens = batch.n_tokens;
+    p.b.n_pages = kv.n_pages;
+    p.b.max_pages = kv.max_pages;
+    p.b.cap = kv.max_pages * kv.page_size;
+    p.b.page = make_fastdiv(kv.page_size);
+    p.b.page_stride = kv.page_stride;
+    p.b.status = (int32_t *)(c->ws + c->lay.status);
+    p.b.user_status = batch.status;
+    p.q = a.q; p.k = pages.k; p.v = pages.v; p.out = a.out; p.lse = a.lse;
+    p.q_stride = a.q_stride; p.out_stride = a.out_stride;
+    p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
+    p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
+    p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
+    const size_t slots = (size_t)4 * kKvMaxSm;
+    p.part.counters = (int32_t *)c->kv_ws;
+    p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
+    p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * kRows * 8);
+    if (c->cfg.dtype == MRP_BF16)
+        return kv.head_dim <= 64 ? launch<__nv_bfloat16, 64>(c, p, st)
+             : kv.head_dim <= 128 ? launch<__nv_bfloat16, 128>(c, p, st) : launch<__nv_bfloat16, 256>(c, p, st);
+    return kv.head_dim <= 64 ? launch<float, 64>(c, p, st)
+         : kv.head_dim <= 128 ? launch<float, 128>(c, p, st) : launch<float, 256>(c, p, st);
+}
+
+}  // namespace mrp

@@ -1,4 +1,5 @@
 // C ABI of libmrp_b200.so: argument validation, workspace layout, launch sequencing.
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -441,6 +442,147 @@ int mrp_module_step_kl(mrp_ctx *ctx, const int32_t *tokens, const void *hidden0,
     if (!(ctx->c.cfg.flags & MRP_FLAG_TRAINING_KL) || ctx->c.use_fp8_lm) return MRP_ERR_UNSUPPORTED;
     if ((M > 0 && (!teacher || !kl)) || ((uintptr_t)teacher & 15u)) return MRP_ERR_INVALID_ARG;
     return module_call(ctx, tokens, hidden0, h_state, logits0, row_index, M, B, L, first_step, out, cuda_stream, teacher, kl);
+}
+
+// ---- the paged key / value cache ------------------------------------------------------------------------------------
+static bool kv_ok(const mrp_kv_config *kv)
+{
+    if (!kv || kv->n_heads < 1 || kv->n_kv_heads < 1 || kv->n_heads % kv->n_kv_heads || kv->n_heads > 65536) return false;
+    if (kv->head_dim < 8 || kv->head_dim > 256 || kv->head_dim % 8) return false;
+    if (kv->page_size < 1 || kv->n_pages < 0 || kv->max_pages < 0) return false;
+    if (kv->n_pages > 0 && (kv->max_pages < 1 || (long long)kv->max_pages * kv->page_size > (1ll << 30))) return false;
+    const long long page = (long long)kv->n_kv_heads * kv->page_size * kv->head_dim;
+    if (kv->page_stride != 0 && (kv->page_stride < page || kv->page_stride % 8)) return false;
+    if (kv->n_pages > 0 && (kv->page_stride ? kv->page_stride : page) > (1ll << 60) / kv->n_pages) return false;
+    if (kv->rot_dim < 0 || kv->rot_dim > kv->head_dim || kv->rot_dim % 2) return false;
+    if (kv->rot_dim > 0 && !kv->inv_freq && !(kv->rot_theta > 0 && isfinite(kv->rot_theta))) return false;
+    if (kv->rot_dim > 0 && kv->inv_freq)
+        for (int j = 0; j < kv->rot_dim / 2; ++j)
+            if (!isfinite(kv->inv_freq[j])) return false;
+    return kv->norm_eps >= 0.f;
+}
+
+size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv)
+{
+    if (!config_ok(cfg) || !kv_ok(kv)) return 0;
+    return kv_workspace_bytes(*cfg, *kv);
+}
+
+int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t workspace_bytes)
+{
+    if (!ctx || !workspace || ((uintptr_t)workspace & 255u) || !kv_ok(kv)) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (workspace_bytes < kv_workspace_bytes(c.cfg, *kv)) return MRP_ERR_NOMEM;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    c.has_kv = false;
+    c.kv = *kv;
+    c.kv.inv_freq = nullptr;
+    if (c.kv.page_stride == 0) c.kv.page_stride = (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim;
+    for (int j = 0; j < kv->rot_dim / 2; ++j) {
+        const double w = kv->inv_freq ? kv->inv_freq[j] : pow(kv->rot_theta, -2.0 * j / kv->rot_dim);
+        double turns = w / 6.283185307179586476925;       // of a turn per position; whole turns are dropped
+        turns -= floor(turns);
+        c.kv_turn[j] = turns >= 1.0 ? 0 : (uint64_t)(turns * 18446744073709551616.0);
+    }
+    c.kv_ws = (char *)workspace;
+    const cudaError_t e = kv_attach(&c);
+    if (e != cudaSuccess) {
+        note_err(&c, e, "mrp_kv_attach");
+        return MRP_ERR_CUDA;
+    }
+    c.has_kv = true;
+    return MRP_OK;
+}
+
+// rows of `heads` heads, `stride` elements apart: present, aligned, not overlapping
+static bool rows_ok(const Ctx &c, const void *ptr, int64_t stride, int heads)
+{
+    const int64_t size = c.cfg.dtype == MRP_BF16 ? 2 : 4;
+    return ptr && !((uintptr_t)ptr & 15u) && stride >= (int64_t)heads * c.kv.head_dim && stride <= (1ll << 40) && (stride * size) % 16 == 0;
+}
+
+static int kv_batch_status(const Ctx &c, const mrp_kv_batch *b)
+{
+    if (!b || b->n_seqs < 0 || b->n_seqs > c.cfg.max_seqs || b->n_tokens < 0 || b->max_new < 0) return MRP_ERR_INVALID_ARG;
+    if ((long long)b->n_tokens * c.kv.n_heads > (1ll << 30)) return MRP_ERR_INVALID_ARG;
+    if (b->n_seqs > 0 && b->n_tokens > 0 && (!b->seq_start || !b->prefix_len || !b->page_table)) return MRP_ERR_INVALID_ARG;
+    return MRP_OK;
+}
+
+static int qk_rows_status(const Ctx &c, const mrp_qkv_rows *r, bool need_k_out)
+{
+    if (r->q) {
+        if (!rows_ok(c, r->q, r->q_stride, c.kv.n_heads) || !rows_ok(c, r->q_out, r->q_out_stride, c.kv.n_heads)) return MRP_ERR_INVALID_ARG;
+        if (r->q == r->q_out && r->q_stride != r->q_out_stride) return MRP_ERR_INVALID_ARG;
+    }
+    if (r->k) {
+        if (!rows_ok(c, r->k, r->k_stride, c.kv.n_kv_heads)) return MRP_ERR_INVALID_ARG;
+        if (need_k_out && (!rows_ok(c, r->k_out, r->k_out_stride, c.kv.n_kv_heads) || (r->k == r->k_out && r->k_stride != r->k_out_stride)))
+            return MRP_ERR_INVALID_ARG;
+    }
+    if (((uintptr_t)r->gamma_q & 15u) || ((uintptr_t)r->gamma_k & 15u)) return MRP_ERR_INVALID_ARG;
+    return MRP_OK;
+}
+
+int mrp_qk_norm_rotate(mrp_ctx *ctx, const int32_t *positions, int32_t n_tokens, const mrp_qkv_rows *rows, void *cuda_stream)
+{
+    if (!ctx || !rows) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv) return MRP_ERR_UNSUPPORTED;
+    if (n_tokens < 0 || (long long)n_tokens * c.kv.n_heads > (1ll << 30)) return MRP_ERR_INVALID_ARG;
+    c.launches = 0;
+    if (n_tokens == 0 || (!rows->q && !rows->k)) return MRP_OK;
+    if (!positions && c.kv.rot_dim > 0) return MRP_ERR_INVALID_ARG;
+    const int bad = qk_rows_status(c, rows, true);
+    if (bad) return bad;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_qk_rows(&c, nullptr, nullptr, positions, n_tokens, *rows, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+static bool pools_ok(const mrp_module_kv *p)
+{
+    return p && p->k && p->v && !((uintptr_t)p->k & 15u) && !((uintptr_t)p->v & 15u);
+}
+
+int mrp_kv_append(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages, const mrp_qkv_rows *rows, void *cuda_stream)
+{
+    if (!ctx || !rows) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
+    int bad = kv_batch_status(c, batch);
+    if (bad) return bad;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!pools_ok(pages) || !rows->k || !rows_ok(c, rows->v, rows->v_stride, c.kv.n_kv_heads)) return MRP_ERR_INVALID_ARG;
+    if ((bad = qk_rows_status(c, rows, false)) != MRP_OK) return bad;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_qk_rows(&c, batch, pages, batch->positions, batch->n_tokens, *rows, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages, const mrp_attention_args *args,
+                        void *cuda_stream)
+{
+    if (!ctx || !args) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
+    const int bad = kv_batch_status(c, batch);
+    if (bad) return bad;
+    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !isfinite(args->scale))
+        return MRP_ERR_INVALID_ARG;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!pools_ok(pages) || !rows_ok(c, args->q, args->q_stride, c.kv.n_heads) || !rows_ok(c, args->out, args->out_stride, c.kv.n_heads))
+        return MRP_ERR_INVALID_ARG;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_paged_attention(&c, *batch, *pages, *args, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
 }
 
 int mrp_quantised_lm_head(mrp_ctx *ctx, const uint8_t **codes, const float **scales)

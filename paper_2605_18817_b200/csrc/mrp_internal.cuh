@@ -101,6 +101,12 @@ struct Ctx {
     const int32_t *prefix_len;
     int prefix_cap;
     bool prefix_append;
+    // the paged cache's geometry (mrp_kv_attach): copy, turn fractions of the rotation, workspace (kv_attention.cuh)
+    bool has_kv;
+    mrp_kv_config kv;
+    uint64_t kv_turn[128];     // 2^64 / (2 pi) * inv_freq[j] mod 2^64: position * kv_turn[j] is the exact angle in turns
+    char *kv_ws;
+    void *kv_encode;           // cuTensorMapEncodeTiled, or nullptr where the geometry does not take the TMA kernel
     char err[192];             // detail of the last failure ("" if none)
     bool prof_enabled;
     cudaEvent_t *prof_events;  // [kProfSlots][kProfMarks]
@@ -280,6 +286,14 @@ cudaError_t module_step(Ctx *c, const int32_t *tokens, const void *hidden0, floa
                         cudaStream_t st);
 size_t module_workspace_bytes(const mrp_config &cfg, int n_layers);
 size_t module_att_offset(const mrp_config &cfg);   // the clean-prefix attention's area of the module workspace
+
+// ---- the paged key / value cache (kv_rows.cu, kv_attention.cu, kv_attention_tc.cu) ------
+size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv);
+cudaError_t kv_attach(Ctx *c);               // after the kv fields are set: clears the counters, sets kernel attributes
+cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_kv *pages, const int32_t *positions,
+                           int n_tokens, const mrp_qkv_rows &rows, cudaStream_t st);
+cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_module_kv &pages,
+                                   const mrp_attention_args &a, cudaStream_t st);
 
 // Few-row variants (tc_skinny.cu): weight rows on the MMA M axis; rows <= 32.
 bool sk_rows_ok(int rows);          // LM head: row-steps incl. step 0
