@@ -14,7 +14,7 @@
 // more pieces is joined by the CTA that finishes last (an arrival counter; nobody waits).  The lengths are read on the
 // device, so the cut is found there: every CTA sums the units' tiles itself.
 //
-// bf16: mma.sync m16n8k16, operands by ldmatrix from XOR-swizzled rows, probabilities rounded to bf16.
+// bf16: mma.sync m16n8k16, operands by ldmatrix from XOR-swizzled rows, probabilities as bf16 hi + lo.
 // f32:  mma.sync m16n8k8 on tf32 operands split into two (x = hi + lo, three products: relative 2^-21).
 #include "kv_attention.cuh"
 
@@ -28,17 +28,6 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kWarpKeys = kTile / kWarps;  // 16
 constexpr float kLazy = 8.f;               // log2 of the growth a running maximum may lag behind
 
-struct AttnParams {
-    KvBatch b;
-    const void *q, *k, *v;
-    void *out;
-    float *lse;
-    int64_t q_stride, out_stride;
-    int H, Hk, g, D;
-    int mask, window, sinks;
-    float scale_log2;
-    KvPartials part;
-};
 
 __device__ __forceinline__ uint32_t s_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool read)
@@ -71,149 +60,19 @@ __device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo)
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
 }
+// hi = bf16(a, b); lo = bf16 of what the rounding left out
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint32_t &lo)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
+    lo = *reinterpret_cast<const uint32_t *>(&l);
+}
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// ---- the line of tiles ---------------------------------------------------------------------------------------------
-// A row tile of a sequence: its rows, what they may see, its key tiles.  Tiles 0..first-1 hold the first positions that
-// stay visible beside the window, the others start at key tile `base`.
-struct RowTile {
-    int r0, rows;              // rows r0 .. r0 + rows - 1 of the sequence's n * g
-    int lo, hi, s1;            // some row sees positions [lo, hi), [0, s1)
-    int first, base, tiles;
-};
-__device__ __forceinline__ RowTile row_tile(const AttnParams &p, int n, int pre, int rt)
-{
-    RowTile t;
-    t.r0 = rt * kRows;
-    t.rows = min(kRows, n * p.g - t.r0);
-    const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
-    t.hi = p.mask == MRP_ATTN_CAUSAL ? pre + i1 + 1 : p.mask == MRP_ATTN_BLOCK ? pre + n : pre;
-    t.lo = p.window > 0 ? max(0, pre + i0 + 1 - p.window) : 0;
-    t.s1 = p.window > 0 ? min(min(p.sinks, t.lo), t.hi) : 0;
-    t.base = t.lo / kTile;
-    const int end = t.hi > t.lo ? (t.hi + kTile - 1) / kTile : t.base;
-    t.first = (t.s1 + kTile - 1) / kTile;
-    if (t.first >= t.base) {               // they meet: one run from position 0
-        t.tiles = max(end > t.base ? end : 0, t.first);
-        t.first = 0;
-        t.base = 0;
-    } else {
-        t.tiles = t.first + (end - t.base);
-    }
-    t.tiles = max(t.tiles, 1);             // rows that see nothing are still written
-    return t;
-}
-__device__ __forceinline__ int key_tile(const RowTile &t, int i) { return i < t.first ? i : t.base + i - t.first; }
-
-__device__ __forceinline__ long long sequence_tiles(const AttnParams &p, int s, bool report)
-{
-    int start, n, pre;
-    if (!kv_sequence(p.b, s, start, n, pre)) {
-        if (report) kv_bad_index(p.b);
-        return 0;
-    }
-    const int nrt = (n * p.g + kRows - 1) / kRows;
-    long long sum = 0;
-    for (int rt = 0; rt < nrt; ++rt) sum += row_tile(p, n, pre, rt).tiles;
-    return sum * p.Hk;
-}
-
-// A place on the line: tile `i` of unit (sequence s, row tile rt, key head h); `at` its offset on the line, `unit` the
-// offset of the unit's first tile.
-struct Cursor {
-    int s, rt, h, i;
-    int start, n, pre;
-    RowTile t;
-    long long at, unit;
-};
-__device__ __forceinline__ bool open_sequence(const AttnParams &p, Cursor &c)
-{
-    for (; c.s < p.b.n_seqs; ++c.s)
-        if (kv_sequence(p.b, c.s, c.start, c.n, c.pre) && c.n > 0) {
-            c.rt = 0; c.h = 0; c.i = 0;
-            c.t = row_tile(p, c.n, c.pre, 0);
-            return true;
-        }
-    return false;
-}
-__device__ __forceinline__ void advance(const AttnParams &p, Cursor &c)
-{
-    ++c.at;
-    if (++c.i < c.t.tiles) return;
-    c.i = 0;
-    c.unit = c.at;
-    if (++c.h < p.Hk) return;
-    c.h = 0;
-    if (++c.rt < (c.n * p.g + kRows - 1) / kRows) {
-        c.t = row_tile(p, c.n, c.pre, c.rt);
-        return;
-    }
-    ++c.s;
-    open_sequence(p, c);
-}
-
-// Sets `c` to the start of this CTA's piece and returns its length; `per` is the length of a full piece.
-__device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor &c, long long &per, long long *sh)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    long long *sh_warp = sh, *sh_found = sh + kWarps;      // [kWarps], [2]
-    long long total = 0, mine = 0;
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += kThreads) {
-        const int s = s0 + tid;
-        mine = s < p.b.n_seqs ? sequence_tiles(p, s, blockIdx.x == 0) : 0;
-        long long x = mine;
-#pragma unroll
-        for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
-        __syncthreads();
-        if (lane == 0) sh_warp[warp] = x;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) total += sh_warp[w];
-    }
-    per = (total + gridDim.x - 1) / gridDim.x;
-    const long long begin = per * blockIdx.x, end = min(total, begin + per);
-    if (begin >= end) return 0;
-    long long done = 0;
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += kThreads) {
-        const int s = s0 + tid;
-        if (p.b.n_seqs > kThreads) mine = s < p.b.n_seqs ? sequence_tiles(p, s, false) : 0;
-        long long x = mine;                // inclusive sum over the lanes
-#pragma unroll
-        for (int w = 1; w < 32; w <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, w);
-            if (lane >= w) x += y;
-        }
-        __syncthreads();
-        if (lane == 31) sh_warp[warp] = x;
-        __syncthreads();
-        long long before = done + x - mine;
-        for (int w = 0; w < warp; ++w) before += sh_warp[w];
-        for (int w = 0; w < kWarps; ++w) done += sh_warp[w];
-        if (mine > 0 && before <= begin && begin < before + mine) {
-            sh_found[0] = s;
-            sh_found[1] = before;
-        }
-        __syncthreads();
-        if (done > begin) break;
-    }
-    c.s = (int)sh_found[0];
-    c.at = sh_found[1];
-    open_sequence(p, c);
-    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
-        c.at += (long long)c.t.tiles * p.Hk;
-        c.t = row_tile(p, c.n, c.pre, ++c.rt);
-    }
-    const int in = (int)(begin - c.at);
-    c.h = in / c.t.tiles;
-    c.i = in - c.h * c.t.tiles;
-    c.at = begin;
-    c.unit = begin - c.i;
-    return end - begin;
 }
 
 // ---- element types -------------------------------------------------------------------------------------------------
@@ -320,14 +179,15 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
 
     pdl_wait();
     pdl_trigger();
-    Cursor cur;
+    typedef RowTile<kRows, kTile> Tile;
+    Cursor<kRows, kTile> cur;
     long long per;
-    const long long len = find_piece(p, cur, per, sh_find);
+    const long long len = find_piece<kRows, kTile, kThreads>(p, cur, per, sh_find);
     if (len == 0) return;
 
     // -- loads run kStages - 1 tiles ahead of the products, through their own cursor; the page of the lane's key is
     //    fetched another tile ahead
-    Cursor ld = cur;
+    Cursor<kRows, kTile> ld = cur;
     long long to_load = len;
     int entry = 0, row_in_page = 0;
     bool see = false;
@@ -383,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
         // ---- a unit, or the part of it in this piece
         const int begin_tile = cur.i;
         const int count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
-        const RowTile t = cur.t;
+        const Tile t = cur.t;
         // queries of the tile -> shared memory, zero beyond the rows and features there are
         for (int i = tid; i < kRows * G::kChunks; i += kThreads) {
             const int r = i / G::kChunks, ch = i - r * G::kChunks;
@@ -465,25 +325,28 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                         uint32_t bh[2], bl[2];
                         split_tf32(kb.x, bh[0], bl[0]);
                         split_tf32(kb.y, bh[1], bl[1]);
-                        mma8(s[x], al, bh[0], bh[1]);
-                        mma8(s[x], ah, bl[0], bl[1]);
-                        mma8(s[x], ah, bh[0], bh[1]);
+                        // the tensor pipe cuts its sums off instead of rounding them: eight products at a time, added here
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
+                        mma8(d, al, bh[0], bh[1]);
+                        mma8(d, ah, bl[0], bl[1]);
+                        mma8(d, ah, bh[0], bh[1]);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) s[x][y] += d[y];
                     }
                 }
             }
-            // scores in units of log2; what a row does not see is -inf
+            // what a row does not see scores -inf in units of log2 (the scale may be negative)
             const bool whole = j0 >= all_lo && j0 + kWarpKeys <= all_hi;
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    s[x][y] *= p.scale_log2;
                     if (!whole) {
                         const int j = j0 + x * 8 + 2 * tig + (y & 1);
-                        if (!(j < hi2[y >> 1] && (j >= lo2[y >> 1] || j < p.sinks))) s[x][y] = -INFINITY;
+                        if (!(j < hi2[y >> 1] && (j >= lo2[y >> 1] || j < p.sinks))) s[x][y] = p.unseen;
                     }
-                    top[y >> 1] = fmaxf(top[y >> 1], s[x][y]);
+                    top[y >> 1] = fmaxf(top[y >> 1], s[x][y] * p.scale_log2);
                 }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -506,22 +369,23 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    s[x][y] = exp2_fast(s[x][y] - mm[y >> 1]);
+                    s[x][y] = exp2_fast(fmaf(s[x][y], p.scale_log2, -mm[y >> 1]));
                     l[y >> 1] += s[x][y];
                 }
             if (!whole && differ) patch_nonfinite<T, DP, NF>(sv, s, o, lane);
             if constexpr (kBf16) {
-                uint32_t a[4];
-                const __nv_bfloat162 h0 = __floats2bfloat162_rn(s[0][0], s[0][1]), h1 = __floats2bfloat162_rn(s[0][2], s[0][3]);
-                const __nv_bfloat162 h2 = __floats2bfloat162_rn(s[1][0], s[1][1]), h3 = __floats2bfloat162_rn(s[1][2], s[1][3]);
-                a[0] = *reinterpret_cast<const uint32_t *>(&h0);
-                a[1] = *reinterpret_cast<const uint32_t *>(&h1);
-                a[2] = *reinterpret_cast<const uint32_t *>(&h2);
-                a[3] = *reinterpret_cast<const uint32_t *>(&h3);
+                // probabilities as bf16 hi + lo (2^-17 together): with few rows the second product costs nothing that shows
+                uint32_t a[4], al[4];
+                split_bf16(s[0][0], s[0][1], a[0], al[0]);
+                split_bf16(s[0][2], s[0][3], a[1], al[1]);
+                split_bf16(s[1][0], s[1][1], a[2], al[2]);
+                split_bf16(s[1][2], s[1][3], a[3], al[3]);
 #pragma unroll
                 for (int f = 0; f < NF; f += 2) {
                     uint32_t b[4];
                     ldsm4t(chunk_at<DP>(sv, (((lane >> 3) & 1) << 3) + (lane & 7), f + (lane >> 4)), b);
+                    mma16(o[f], al, b[0], b[1]);
+                    mma16(o[f + 1], al, b[2], b[3]);
                     mma16(o[f], a, b[0], b[1]);
                     mma16(o[f + 1], a, b[2], b[3]);
                 }
@@ -542,9 +406,12 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                         uint32_t bh[2], bl[2];
                         split_tf32(v0, bh[0], bl[0]);
                         split_tf32(v1, bh[1], bl[1]);
-                        mma8(o[f], al, bh[0], bh[1]);
-                        mma8(o[f], ah, bl[0], bl[1]);
-                        mma8(o[f], ah, bh[0], bh[1]);
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
+                        mma8(d, al, bh[0], bh[1]);
+                        mma8(d, ah, bl[0], bl[1]);
+                        mma8(d, ah, bh[0], bh[1]);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) o[f][y] += d[y];
                     }
                 }
             }
@@ -672,14 +539,14 @@ cudaError_t launch(Ctx *c, const AttnParams &p, cudaStream_t st)
 
 size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv)
 {
-    (void)cfg; (void)kv;
-    return kKvCounterBytes + (size_t)4 * kKvMaxSm * slot_bytes();
+    const size_t few = kKvCounterBytes + (size_t)4 * kKvMaxSm * slot_bytes();
+    return kv_tc_takes(cfg, kv) && kv_tc_workspace_bytes() > few ? kv_tc_workspace_bytes() : few;
 }
 
 cudaError_t kv_attach(Ctx *c)
 {
     cudaError_t e = cudaMemset(c->kv_ws, 0, kKvCounterBytes);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || (e = kv_tc_attach(c)) != cudaSuccess) return e;
     if (c->cfg.dtype == MRP_BF16) {
         if ((e = prepare<__nv_bfloat16, 64>()) != cudaSuccess || (e = prepare<__nv_bfloat16, 128>()) != cudaSuccess) return e;
         return prepare<__nv_bfloat16, 256>();
@@ -711,6 +578,8 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
     p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
+    p.unseen = p.scale_log2 > 0.f ? -INFINITY : INFINITY;
+    if (c->kv_encode && (long long)batch.max_new * p.g > kRows) return launch_paged_attention_tc(c, p, batch.max_new, st);
     const size_t slots = (size_t)4 * kKvMaxSm;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);

@@ -56,11 +56,174 @@ __device__ __forceinline__ bool kv_sequence(const KvBatch &b, int s, int &start,
 // ---- workspace: arrival counters, then (max, sum) pairs and rows of partial results -----------------------------------
 // Slot 2 c holds CTA c's part of a unit that an earlier CTA began, slot 2 c + 1 its part of one that a later CTA goes on
 // with; a slot is `rows` rows of `width` floats and as many (max, sum) pairs.
-constexpr int kKvCounterBytes = 4096;      // int32 per CTA that begins a shared unit; zero between calls
+constexpr int kKvCounterBytes = 8192;      // int32 arrivals by the CTA that begins a shared unit (large tiles: per warp too); zero between calls
 struct KvPartials {
     int32_t *counters;
     float2 *ml;
     float *o;
 };
+
+struct AttnParams {
+    KvBatch b;
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    int64_t q_stride, out_stride;
+    int H, Hk, g, D;
+    int mask, window, sinks;
+    float scale_log2, unseen;  // unseen: the raw score that scales to -inf
+    KvPartials part;
+};
+
+// ---- the line of tiles ---------------------------------------------------------------------------------------------
+// A row tile of a sequence: its rows, what they may see, its key tiles.  Tiles 0..first-1 hold the first positions that
+// stay visible beside the window, the others start at key tile `base`.
+template <int ROWS, int TILE> struct RowTile {
+    int r0, rows;              // rows r0 .. r0 + rows - 1 of the sequence's n * g
+    int lo, hi, s1;            // some row sees positions [lo, hi), [0, s1)
+    int first, base, tiles;
+};
+template <int ROWS, int TILE>
+__device__ __forceinline__ RowTile<ROWS, TILE> row_tile(const AttnParams &p, int n, int pre, int rt)
+{
+    RowTile<ROWS, TILE> t;
+    t.r0 = rt * ROWS;
+    t.rows = min(ROWS, n * p.g - t.r0);
+    const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
+    t.hi = p.mask == MRP_ATTN_CAUSAL ? pre + i1 + 1 : p.mask == MRP_ATTN_BLOCK ? pre + n : pre;
+    t.lo = p.window > 0 ? max(0, pre + i0 + 1 - p.window) : 0;
+    t.s1 = p.window > 0 ? min(min(p.sinks, t.lo), t.hi) : 0;
+    t.base = t.lo / TILE;
+    const int end = t.hi > t.lo ? (t.hi + TILE - 1) / TILE : t.base;
+    t.first = (t.s1 + TILE - 1) / TILE;
+    if (t.first >= t.base) {               // they meet: one run from position 0
+        t.tiles = max(end > t.base ? end : 0, t.first);
+        t.first = 0;
+        t.base = 0;
+    } else {
+        t.tiles = t.first + (end - t.base);
+    }
+    t.tiles = max(t.tiles, 1);             // rows that see nothing are still written
+    return t;
+}
+template <int ROWS, int TILE>
+__device__ __forceinline__ int key_tile(const RowTile<ROWS, TILE> &t, int i) { return i < t.first ? i : t.base + i - t.first; }
+
+template <int ROWS, int TILE>
+__device__ __forceinline__ long long sequence_tiles(const AttnParams &p, int s, bool report)
+{
+    int start, n, pre;
+    if (!kv_sequence(p.b, s, start, n, pre)) {
+        if (report) kv_bad_index(p.b);
+        return 0;
+    }
+    const int nrt = (n * p.g + ROWS - 1) / ROWS;
+    long long sum = 0;
+    for (int rt = 0; rt < nrt; ++rt) sum += row_tile<ROWS, TILE>(p, n, pre, rt).tiles;
+    return sum * p.Hk;
+}
+
+// A place on the line: tile `i` of unit (sequence s, row tile rt, key head h); `at` its offset on the line, `unit` the
+// offset of the unit's first tile.
+template <int ROWS, int TILE> struct Cursor {
+    int s, rt, h, i;
+    int start, n, pre;
+    RowTile<ROWS, TILE> t;
+    long long at, unit;
+};
+template <int ROWS, int TILE>
+__device__ __forceinline__ bool open_sequence(const AttnParams &p, Cursor<ROWS, TILE> &c)
+{
+    for (; c.s < p.b.n_seqs; ++c.s)
+        if (kv_sequence(p.b, c.s, c.start, c.n, c.pre) && c.n > 0) {
+            c.rt = 0; c.h = 0; c.i = 0;
+            c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, 0);
+            return true;
+        }
+    return false;
+}
+template <int ROWS, int TILE>
+__device__ __forceinline__ void advance(const AttnParams &p, Cursor<ROWS, TILE> &c)
+{
+    ++c.at;
+    if (++c.i < c.t.tiles) return;
+    c.i = 0;
+    c.unit = c.at;
+    if (++c.h < p.Hk) return;
+    c.h = 0;
+    if (++c.rt < (c.n * p.g + ROWS - 1) / ROWS) {
+        c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, c.rt);
+        return;
+    }
+    ++c.s;
+    open_sequence(p, c);
+}
+
+// Sets `c` to the start of this CTA's piece and returns its length; `per` is the length of a full piece.
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS, TILE> &c, long long &per, long long *sh)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int WARPS = THREADS / 32;
+    long long *sh_warp = sh, *sh_found = sh + WARPS;      // [WARPS], [2]
+    long long total = 0, mine = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += THREADS) {
+        const int s = s0 + tid;
+        mine = s < p.b.n_seqs ? sequence_tiles<ROWS, TILE>(p, s, blockIdx.x == 0) : 0;
+        long long x = mine;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
+        __syncthreads();
+        if (lane == 0) sh_warp[warp] = x;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) total += sh_warp[w];
+    }
+    per = (total + gridDim.x - 1) / gridDim.x;
+    const long long begin = per * blockIdx.x, end = min(total, begin + per);
+    if (begin >= end) return 0;
+    long long done = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += THREADS) {
+        const int s = s0 + tid;
+        if (p.b.n_seqs > THREADS) mine = s < p.b.n_seqs ? sequence_tiles<ROWS, TILE>(p, s, false) : 0;
+        long long x = mine;                // inclusive sum over the lanes
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, w);
+            if (lane >= w) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) sh_warp[warp] = x;
+        __syncthreads();
+        long long before = done + x - mine;
+        for (int w = 0; w < warp; ++w) before += sh_warp[w];
+        for (int w = 0; w < WARPS; ++w) done += sh_warp[w];
+        if (mine > 0 && before <= begin && begin < before + mine) {
+            sh_found[0] = s;
+            sh_found[1] = before;
+        }
+        __syncthreads();
+        if (done > begin) break;
+    }
+    c.s = (int)sh_found[0];
+    c.at = sh_found[1];
+    open_sequence(p, c);
+    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
+        c.at += (long long)c.t.tiles * p.Hk;
+        c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, ++c.rt);
+    }
+    const int in = (int)(begin - c.at);
+    c.h = in / c.t.tiles;
+    c.i = in - c.h * c.t.tiles;
+    c.at = begin;
+    c.unit = begin - c.i;
+    return end - begin;
+}
+
+// The kernel on large tiles (kv_attention_tc.cu): the geometries it takes, its workspace, its launch.
+bool kv_tc_takes(const mrp_config &cfg, const mrp_kv_config &kv);
+size_t kv_tc_workspace_bytes();
+cudaError_t kv_tc_attach(Ctx *c);
+cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaStream_t st);
 
 }  // namespace mrp

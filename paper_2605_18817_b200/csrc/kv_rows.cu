@@ -4,19 +4,20 @@
 // with f the fraction of a turn that position p makes in pair (a, b): p * turn_j mod 2^64, turn_j = 2^64 w_j / (2 pi) on
 // the host in 64 bits, so the reduction of the angle is one exact integer product however far the position is.
 //
-// Every element is read once and written once and takes about seven operations: memory bounds it.  A head is handled by
-// the GL lanes that hold its features, 8 consecutive ones each (one or two 16-byte accesses); the sum of squares is a
-// shuffle reduction over them, and a pair's other half comes from another lane's registers by shuffle where rot_dim / 2
-// is a multiple of 8, from the same lane where pairs are adjacent, and is read again otherwise.  Sines and cosines (one
-// accurate sincospi per pair) depend on the token alone: a CTA computes them once into shared memory for its few tokens
-// and uses them for all heads.
+// Every element is read once and written once and takes about seven operations: memory bounds it, as long as the rest
+// stays short.  A warp takes one token (or, where tokens are few, one of several shares of a token's heads): it finds
+// the token's sequence and page, each lane computes the sines and cosines of its own four pairs once (sincospi), and
+// the warp goes through the token's heads, GL lanes a head, U heads' loads in flight.  A lane holds two runs of four
+// features: the two halves of its four pairs (features 4 l.. and rot_dim / 2 + 4 l.. of the rotated ones), so a
+// rotation needs no other lane's registers; adjacent pairs lie in one run anyway.  rot_dim / 2 that is no multiple of
+// four splits runs: there the other half of a pair is read again.
 #include "kv_attention.cuh"
 
 namespace mrp {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowMaxTokens = 8;           // tokens of a CTA
+constexpr int kRowWarps = kRowThreads / 32;
 
 struct RowsParams {
     KvBatch b;                 // b.n_seqs < 0: no batch, positions only
@@ -27,67 +28,36 @@ struct RowsParams {
     int heads[3];
     int to_pages;              // k and v go to the pools
     int D, rot, half, interleaved;
-    int tokens, per_cta;
+    int tokens, shares;        // warps a token
     float eps, inv_d;
     uint64_t turn[128];
 };
 
-template <typename T> struct Row8;         // 8 features of a lane
-template <> struct Row8<__nv_bfloat16> {
-    uint4 r;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { r = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void get(float f[8]) const
+template <typename T> struct Run4;         // four consecutive features
+template <> struct Run4<__nv_bfloat16> {
+    uint2 r;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { r = *reinterpret_cast<const uint2 *>(p); }
+    __device__ __forceinline__ void get(float *f) const
     {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        f[0] = __uint_as_float(r.x << 16); f[1] = __uint_as_float(r.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(r.y << 16); f[3] = __uint_as_float(r.y & 0xFFFF0000u);
     }
-    __device__ __forceinline__ void put(const float f[8])
+    __device__ __forceinline__ void put(const float *f)
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&t);
-        }
-        r = make_uint4(w[0], w[1], w[2], w[3]);
+        const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+        r = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = r; }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint2 *>(p) = r; }
 };
-template <> struct Row8<float> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const float *p)
-    {
-        a = *reinterpret_cast<const float4 *>(p);
-        b = *reinterpret_cast<const float4 *>(p + 4);
-    }
-    __device__ __forceinline__ void get(float f[8]) const
-    {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
-    __device__ __forceinline__ void put(const float f[8])
-    {
-        a = make_float4(f[0], f[1], f[2], f[3]);
-        b = make_float4(f[4], f[5], f[6], f[7]);
-    }
-    __device__ __forceinline__ void store(float *p) const
-    {
-        *reinterpret_cast<float4 *>(p) = a;
-        *reinterpret_cast<float4 *>(p + 4) = b;
-    }
+template <> struct Run4<float> {
+    float4 r;
+    __device__ __forceinline__ void load(const float *p) { r = *reinterpret_cast<const float4 *>(p); }
+    __device__ __forceinline__ void get(float *f) const { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
+    __device__ __forceinline__ void put(const float *f) { r = make_float4(f[0], f[1], f[2], f[3]); }
+    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = r; }
 };
 __device__ __forceinline__ float one_f(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float one_f(const float *p) { return *p; }
-
-// What a CTA knows of one of its tokens.
-struct TokenAt {
-    int go;                    // the token is some sequence's (or there is no batch)
-    int pos;                   // position to rotate by
-    int64_t page_off;          // element offset of its row of head 0 in a pool, or -1: not stored
-};
 
 // Sequence of row t: the number of entries of seq_start[1..n_seqs] that are <= t, found by the warp 32 probes at a time.
 __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seqs, int t, int lane)
@@ -107,154 +77,163 @@ __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seq
 template <typename T, int GL, int U>
 __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const __grid_constant__ RowsParams p)
 {
-    extern __shared__ float sh[];          // cos [per_cta][pitch], sin [per_cta][pitch]
-    __shared__ TokenAt at[kRowMaxTokens];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int pitch = (p.half + 3) & ~3;
-    float *cs = sh, *sn = sh + (size_t)p.per_cta * pitch;
-    const int t0 = blockIdx.x * p.per_cta;
-    const int nt = min(p.per_cta, p.tokens - t0);
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int gw = blockIdx.x * kRowWarps + (tid >> 5);
     pdl_wait();
     pdl_trigger();
-    for (int i = warp; i < nt; i += kRowThreads / 32) {
-        const int t = t0 + i;
-        TokenAt a;
-        a.go = 1; a.pos = 0; a.page_off = -1;
-        if (p.b.n_seqs >= 0) {
-            const int s = find_sequence(p.b.seq_start, p.b.n_seqs, t, lane);
-            int start = 0, n = 0, pre = 0;
-            const bool in = s < p.b.n_seqs && __ldg(p.b.seq_start + s) <= t;
-            const bool ok = in && kv_sequence(p.b, s, start, n, pre);
-            a.go = ok;
-            if (ok) {
-                const int place = pre + (t - start);
-                a.pos = place;
-                const int pg = fast_div(place, p.b.page);
-                const int entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
-                if ((unsigned)entry < (unsigned)p.b.n_pages)
-                    a.page_off = (int64_t)entry * p.b.page_stride + (int64_t)(place - pg * p.b.page.d) * p.D;
-                else if (lane == 0)
-                    kv_bad_index(p.b);
-            }
-        }
-        if (p.b.positions && a.go) a.pos = __ldg(p.b.positions + t);
-        if (lane == 0) at[i] = a;
-    }
     // a sequence that does not fit is reported even if no row names it
     if (blockIdx.x == 0)
         for (int s = tid; s < p.b.n_seqs; s += kRowThreads) {
             int start, n, pre;
             if (!kv_sequence(p.b, s, start, n, pre)) kv_bad_index(p.b);
         }
-    __syncthreads();
-    for (int i = tid; i < nt * p.half; i += kRowThreads) {
-        const int tk = i / p.half, j = i - tk * p.half;
-        const uint64_t f = (uint64_t)(int64_t)at[tk].pos * p.turn[j];
-        float s, c;
-        sincospif((float)(int32_t)(f >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
-        cs[tk * pitch + j] = c;
-        sn[tk * pitch + j] = s;
-    }
-    __syncthreads();
+    const int t = gw / p.shares, share = gw - t * p.shares;
+    if (t >= p.tokens) return;
 
-    constexpr int NG = kRowThreads / GL;
-    const int gl = tid & (GL - 1), e0 = gl * 8;
-    const bool mine = e0 < p.D;
-    const int per_token = p.heads[0] + p.heads[1] + p.heads[2];
-    const int total = nt * per_token;
-    const bool aligned = (p.half & 7) == 0;
-    const int hc = p.half >> 3;
-    for (int r0 = tid / GL; r0 - tid / GL < total; r0 += NG * U) {
-        Row8<T> x[U];
-        int kind[U], tok[U], head[U];
-        bool live[U];
+    // ---- the token: its sequence, position, row in the pools (element offset of head 0's, -1: not stored)
+    int pos = 0;
+    int64_t page_off = -1;
+    if (p.b.n_seqs >= 0) {
+        const int s = find_sequence(p.b.seq_start, p.b.n_seqs, t, lane);
+        int start, n, pre;
+        if (s >= p.b.n_seqs || !kv_sequence(p.b, s, start, n, pre) || t < start) return;
+        pos = pre + (t - start);
+        const int pg = fast_div(pos, p.b.page);
+        const int entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
+        if ((unsigned)entry < (unsigned)p.b.n_pages)
+            page_off = (int64_t)entry * p.b.page_stride + (int64_t)(pos - pg * p.b.page.d) * p.D;
+        else if (lane == 0)
+            kv_bad_index(p.b);
+    }
+    if (p.b.positions) pos = __ldg(p.b.positions + t);
+
+    // ---- the lane: two runs of four features, its four pairs
+    constexpr int NG = 32 / GL;
+    const int gl = lane & (GL - 1), grp = lane / GL;
+    const bool halves = !p.interleaved && (p.half & 3) == 0, again = !p.interleaved && !halves;
+    const int hl = p.half >> 2;                            // lanes whose runs are the two halves of pairs
+    const bool mine = gl * 8 < p.D;
+    int e0 = gl * 8, e1 = gl * 8 + 4;
+    if (halves) {
+        e0 = gl < hl ? gl * 4 : p.rot + (gl - hl) * 8;
+        e1 = gl < hl ? p.half + gl * 4 : e0 + 4;
+    }
+    float cs[4], sn[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = gl * 4 + i;                          // (again: computed where it is used)
+        cs[i] = 1.f;
+        sn[i] = 0.f;
+        if (!again && j < p.half) {
+            const uint64_t f = (uint64_t)(int64_t)pos * p.turn[j];
+            sincospif((float)(int32_t)(f >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);   // 2^-31: half turns
+        }
+    }
+    Run4<T> gq[2], gk[2];
+    if (mine && p.gamma[0]) {
+        gq[0].load(reinterpret_cast<const T *>(p.gamma[0]) + e0);
+        gq[1].load(reinterpret_cast<const T *>(p.gamma[0]) + e1);
+    }
+    if (mine && p.gamma[1]) {
+        gk[0].load(reinterpret_cast<const T *>(p.gamma[1]) + e0);
+        gk[1].load(reinterpret_cast<const T *>(p.gamma[1]) + e1);
+    }
+
+    // ---- the token's heads: queries, then keys, then values
+    const int nq = p.heads[0], nqk = nq + p.heads[1], total = nqk + p.heads[2];
+    const T *src0 = reinterpret_cast<const T *>(p.src[0]) + (int64_t)t * p.src_stride[0];
+    const T *src1 = reinterpret_cast<const T *>(p.src[1]) + (int64_t)t * p.src_stride[1];
+    const T *src2 = reinterpret_cast<const T *>(p.src[2]) + (int64_t)t * p.src_stride[2];
+    T *dst0 = reinterpret_cast<T *>(p.dst[0]) + (int64_t)t * p.dst_stride[0];
+    const int64_t head_out = p.to_pages ? (int64_t)p.b.page.d * p.D : p.D;
+    T *dst1 = reinterpret_cast<T *>(p.dst[1]) + (p.to_pages ? page_off : (int64_t)t * p.dst_stride[1]);
+    T *dst2 = reinterpret_cast<T *>(p.dst[2]) + page_off;
+    const bool store_kv = !p.to_pages || page_off >= 0;
+    for (int r0 = share * NG; r0 < total; r0 += p.shares * NG * U) {
+        Run4<T> x[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int r = r0 + u * NG;
-            const int rr = min(r, total - 1);
-            tok[u] = rr / per_token;
-            int h = rr - tok[u] * per_token;
-            kind[u] = 0;
-            if (h >= p.heads[0]) { h -= p.heads[0]; kind[u] = 1; }
-            if (kind[u] == 1 && h >= p.heads[1]) { h -= p.heads[1]; kind[u] = 2; }
-            head[u] = h;
-            live[u] = r < total && at[tok[u]].go;
-            x[u].load(reinterpret_cast<const T *>(p.src[kind[u]]) + (int64_t)(t0 + tok[u]) * p.src_stride[kind[u]] +
-                      (int64_t)h * p.D + (mine ? e0 : 0));
+            const int r = min(r0 + u * p.shares * NG + grp, total - 1);
+            const T *row = r < nq ? src0 + (int64_t)r * p.D : r < nqk ? src1 + (int64_t)(r - nq) * p.D : src2 + (int64_t)(r - nqk) * p.D;
+            if (mine) {
+                x[u][0].load(row + e0);
+                x[u][1].load(row + e1);
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int kd = kind[u];
-            const T *row = reinterpret_cast<const T *>(p.src[kd]) + (int64_t)(t0 + tok[u]) * p.src_stride[kd] + (int64_t)head[u] * p.D;
+            const int r = r0 + u * p.shares * NG + grp;
+            const bool is_q = r < nq, is_v = r >= nqk;
             float f[8];
-            x[u].get(f);
-            const T *gm = kd < 2 ? reinterpret_cast<const T *>(p.gamma[kd]) : nullptr;
-            // (the shuffles below are executed by all lanes: heads of one warp may be of different kinds)
-            float ss = 0.f;
+            x[u][0].get(f);
+            x[u][1].get(f + 4);
+            const bool norm = (is_q ? p.gamma[0] : p.gamma[1]) != nullptr && !is_v;
+            float rs = 1.f;
+            if (p.gamma[0] || p.gamma[1]) {
+                float ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(f[i], f[i], ss);
-            if (!mine) ss = 0.f;
+                for (int i = 0; i < 8; ++i) ss = fmaf(f[i], f[i], ss);
+                if (!mine) ss = 0.f;
 #pragma unroll
-            for (int w = GL / 2; w > 0; w >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, w);
-            const float rs = gm ? 1.f / sqrtf(fmaf(ss, p.inv_d, p.eps)) : 1.f;
-            if (gm && mine) {
-                Row8<T> g;
-                float gf[8];
-                g.load(gm + e0);
-                g.get(gf);
+                for (int w = GL / 2; w > 0; w >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, w);
+                if (norm) {
+                    rs = rsqrtf(fmaf(ss, p.inv_d, p.eps));
+                    Run4<T> g0 = is_q ? gq[0] : gk[0], g1 = is_q ? gq[1] : gk[1];
+                    float g[8];
+                    g0.get(g);
+                    g1.get(g + 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = f[i] * rs * gf[i];
+                    for (int i = 0; i < 8; ++i) f[i] *= rs * g[i];
+                }
             }
-            if (p.rot > 0) {
-                const float *c = cs + tok[u] * pitch, *s = sn + tok[u] * pitch;
-                if (p.interleaved) {
-                    if (kd < 2) {
+            if (p.rot > 0 && !is_v) {
+                if (halves) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (e0 + 2 * i < p.rot) {
-                                const float cc = c[e0 / 2 + i], sc = s[e0 / 2 + i], a = f[2 * i], b = f[2 * i + 1];
-                                f[2 * i] = a * cc - b * sc;
-                                f[2 * i + 1] = b * cc + a * sc;
-                            }
-                    }
-                } else if (aligned) {
-                    const bool first = gl < hc, turned = gl < 2 * hc;
-                    const int from = first ? gl + hc : turned ? gl - hc : gl;
-                    float o[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = __shfl_sync(0xffffffffu, f[i], from, GL);
-                    if (kd < 2 && turned) {
-                        const int j0 = first ? e0 : e0 - p.half;
-                        const float sg = first ? -1.f : 1.f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = f[i] * c[j0 + i] + sg * o[i] * s[j0 + i];
-                    }
-                } else if (kd < 2 && mine) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int e = e0 + i;
-                        if (e < p.rot) {
-                            const bool first = e < p.half;
-                            const int pe = first ? e + p.half : e - p.half, j = first ? e : pe;
-                            const float y = one_f(row + pe), o = gm ? y * rs * one_f(gm + pe) : y;
-                            f[i] = f[i] * c[j] + (first ? -o : o) * s[j];
+                    for (int i = 0; i < 4; ++i) {          // (beyond the rotated features: cosine 1, sine 0, and
+                        if (gl < hl) {                     //  whatever their partner is must not come in)
+                            const float a = f[i], b = f[4 + i];
+                            f[i] = fmaf(a, cs[i], -b * sn[i]);
+                            f[4 + i] = fmaf(b, cs[i], a * sn[i]);
                         }
                     }
+                } else if (p.interleaved) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (gl * 8 + 2 * i < p.rot) {
+                            const float a = f[2 * i], b = f[2 * i + 1];
+                            f[2 * i] = fmaf(a, cs[i], -b * sn[i]);
+                            f[2 * i + 1] = fmaf(b, cs[i], a * sn[i]);
+                        }
+                } else if (mine && r < total) {
+                    const T *row = is_q ? src0 + (int64_t)r * p.D : src1 + (int64_t)(r - nq) * p.D;
+                    const T *gm = reinterpret_cast<const T *>(is_q ? p.gamma[0] : p.gamma[1]);
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i) {
+                        const int e = gl * 8 + i;
+                        if (e >= p.rot) continue;
+                        const bool first = e < p.half;
+                        const int pe = first ? e + p.half : e - p.half;
+                        const uint64_t fr = (uint64_t)(int64_t)pos * p.turn[first ? e : pe];
+                        float s, c;
+                        sincospif((float)(int32_t)(fr >> 32) * 4.656612873077393e-10f, &s, &c);
+                        const float o = one_f(row + pe) * (norm ? rs * one_f(gm + pe) : 1.f);
+                        const float v = one_f(row + e) * (norm ? rs * one_f(gm + e) : 1.f);
+                        const float y = fmaf(v, c, (first ? -o : o) * s);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k == i) f[k] = y;
+                    }
                 }
             }
-            __syncwarp();                  // the pairs read again above lie in rows this warp alone may overwrite
-            if (live[u] && mine) {
-                T *dst = reinterpret_cast<T *>(p.dst[kd]);
-                int64_t off;
-                if (kd > 0 && p.to_pages) {
-                    off = at[tok[u]].page_off;
-                    if (off < 0) continue;
-                    off += (int64_t)head[u] * p.b.page.d * p.D;
-                } else {
-                    off = (int64_t)(t0 + tok[u]) * p.dst_stride[kd] + (int64_t)head[u] * p.D;
+            __syncwarp();                  // a head read again above is overwritten by its own lanes alone, now
+            if (mine && r < total && (is_q || store_kv)) {
+                T *dst = is_q ? dst0 + (int64_t)r * p.D : is_v ? dst2 + (int64_t)(r - nqk) * head_out : dst1 + (int64_t)(r - nq) * head_out;
+                if (!is_v) {
+                    x[u][0].put(f);
+                    x[u][1].put(f + 4);
                 }
-                if (kd < 2) x[u].put(f);
-                x[u].store(dst + off + e0);
+                x[u][0].store(dst + e0);
+                x[u][1].store(dst + e1);
             }
         }
     }
@@ -263,10 +242,9 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const __grid_const
 template <typename T, int GL>
 cudaError_t launch_rows(Ctx *c, const RowsParams &p, cudaStream_t st)
 {
-    const size_t smem = (size_t)2 * p.per_cta * ((p.half + 3) & ~3) * sizeof(float);
-    const int grid = (p.tokens + p.per_cta - 1) / p.per_cta;
-    cudaError_t e = launch_k(qk_rows_kernel<T, GL, sizeof(T) == 2 ? 4 : 2>, dim3(grid), dim3(kRowThreads), smem, st,
-                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
+    const long long warps = (long long)p.tokens * p.shares;
+    cudaError_t e = launch_k(qk_rows_kernel<T, GL, sizeof(T) == 2 ? 4 : 2>, dim3((unsigned)((warps + kRowWarps - 1) / kRowWarps)),
+                             dim3(kRowThreads), 0, st, !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
     c->launches = 1;
     return note_err(c, e, "qk_rows_kernel");
 }
@@ -309,8 +287,14 @@ cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_k
     p.half = kv.rot_dim / 2;
     p.interleaved = kv.rot_interleaved != 0;
     p.tokens = n_tokens;
-    // One token per CTA until that fills the GPU's residency; beyond it, several share the start-up and the search.
-    p.per_cta = n_tokens <= 8 * c->sm_count ? 1 : n_tokens <= 64 * c->sm_count ? 4 : kRowMaxTokens;
+    // One warp a token where there are tokens for every warp the GPU holds; with fewer, a token's heads are shared out,
+    // down to one round of loads a warp.
+    {
+        const int rows = p.heads[0] + p.heads[1] + p.heads[2], at_once = 32 / (kv.head_dim <= 64 ? 8 : kv.head_dim <= 128 ? 16 : 32);
+        const int most = (rows + at_once * 2 - 1) / (at_once * 2);
+        const long long want = (long long)c->sm_count * 24 / n_tokens;
+        p.shares = (int)(want < 1 ? 1 : want > most ? most : want);
+    }
     p.eps = kv.norm_eps;
     p.inv_d = 1.f / (float)kv.head_dim;
     for (int j = 0; j < p.half; ++j) p.turn[j] = c->kv_turn[j];
