@@ -96,6 +96,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r)
         ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
           "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+// Behind the wait: the compiler sees no other tie between the wait and the registers the loads fill, and may use them early.
+__device__ __forceinline__ void tmem_landed32(float *v)
+{
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                     "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                     "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                     "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31]) :: "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -252,7 +260,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
                     umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c * 8, v_desc(vs + c * 2048), idesc_o, !first || c > 0);
-                umma_commit(pv_done(row_tile));
+                umma_commit(pv_done(x));
             }
             __syncwarp();
         };
@@ -380,6 +388,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         uint32_t k = 0, unit = 0;
         bool ok = true;
         const float sc = p.scale_log2;
+        // P V of tile kk done.  A barrier may be one phase behind what is waited for, not two: with two S buffers the
+        // softmax can finish a tile while the product before the last still runs, so each buffer has its own.
+        auto wait_pv = [&](uint32_t kk) {
+            const bool r = NT == 2 ? mbar_wait(pv_done(x), kk & 1u, abort_flag, ws) : mbar_wait(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
+            return __all_sync(0xffffffffu, r) != 0;
+        };
         while (ok && at < piece_end) {
             const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
             const Tile t = cur.t;
@@ -425,6 +439,8 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld32(s_tm + 32 * c, s + 32 * c);
                     tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_landed32(s + 32 * c);
                     const int j0 = key_tile(t, begin + n) * kTcTile;
                     if (!(j0 >= all_lo && j0 + kTcTile <= all_hi)) {
 #pragma unroll
@@ -455,7 +471,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                         const float nm = grow ? top : m;
                         const float c = m == nm ? 1.f : ex2f(m - nm);
                         if (n > 0) {                       // the accumulator of the tiles so far
-                            ok = __all_sync(0xffffffffu, mbar_wait(pv_done(x), (k - 1) & 1u, abort_flag, ws));
+                            ok = wait_pv(k - 1);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll
@@ -463,6 +479,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                 float o[32];
                                 tmem_ld32(o_tm + 32 * f, o);
                                 tmem_wait_ld();
+                                tmem_landed32(o);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) o[i] *= c;
                                 tmem_st32(o_tm + 32 * f, o);
@@ -494,7 +511,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             }
             if (!ok) break;
             // ---- the unit's end (or this piece's)
-            ok = __all_sync(0xffffffffu, mbar_wait(pv_done(x), (k - 1) & 1u, abort_flag, ws));
+            ok = wait_pv(k - 1);
             if (!ok) break;
             tc_fence_after();
             if (warp_live) {
@@ -528,6 +545,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     float o[32];
                     tmem_ld32(o_tm + 32 * f, o);
                     tmem_wait_ld();
+                    tmem_landed32(o);
                     if (whole_unit) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) put(32 * f + i, o + i, inv);
