@@ -80,7 +80,7 @@ template <typename T, int DP> struct Geo;
 template <int DP> struct Geo<__nv_bfloat16, DP> {
     static constexpr int kChunks = DP / 8;                 // 16-byte chunks of a row
     static constexpr int kPitchK = DP * 2, kPitchV = DP * 2, kPitchQ = DP * 2;     // bytes; chunks XOR-swizzled
-    static constexpr int kStages = DP <= 128 ? 3 : 2;
+    static constexpr int kStages = DP <= 64 ? 3 : 2;
     static constexpr bool kSwizzle = true;
 };
 template <int DP> struct Geo<float, DP> {
@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long sh_find[kWarps + 2];
     __shared__ int sh_last;
+    __shared__ Cursor<kRows, kTile> sh_ld[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
     const uint32_t ring = s_addr(smem) + warp * kStages * S::kStage;
@@ -182,53 +183,89 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
     typedef RowTile<kRows, kTile> Tile;
     Cursor<kRows, kTile> cur;
     long long per;
-    const long long len = find_piece<kRows, kTile, kThreads>(p, cur, per, sh_find);
+    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
+                                            : find_piece<kRows, kTile, kThreads>(p, cur, per, sh_find);
     if (len == 0) return;
 
-    // -- loads run kStages - 1 tiles ahead of the products, through their own cursor; the page of the lane's key is
-    //    fetched another tile ahead
-    Cursor<kRows, kTile> ld = cur;
+    // -- loads run kStages - 1 tiles ahead of the products, through a cursor of their own (in shared memory: it moves
+    //    once a unit); the page of the lane's key is fetched another tile ahead
+    Cursor<kRows, kTile> &ld = sh_ld[warp];
+    if (lane == 0) ld = cur;
+    __syncwarp();
+    Tile lt = cur.t;
+    int l_i = cur.i, l_h = cur.h;
+    const int32_t *l_table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
     long long to_load = len;
     int entry = 0, row_in_page = 0;
     bool see = false;
     auto look_up = [&]() {                                 // lanes l and l + 16: key l of the warp's 16
-        const int j = key_tile(ld.t, ld.i) * kTile + warp * kWarpKeys + (lane & 15);
-        see = j < ld.t.hi && (j >= ld.t.lo || j < ld.t.s1);
+        const int j = key_tile(lt, l_i) * kTile + warp * kWarpKeys + (lane & 15);
+        see = j < lt.hi && (j >= lt.lo || j < lt.s1);
         entry = 0;
         row_in_page = 0;
         if (see) {
             const int pg = fast_div(j, p.b.page);
             row_in_page = j - pg * P;
-            entry = __ldg(p.b.page_table + (size_t)ld.s * p.b.max_pages + pg);
+            entry = __ldg(l_table + pg);
         }
     };
+    constexpr int per_row = G::kChunks;                    // lanes (16-byte chunks) a row
+    constexpr int rows_at_once = per_row >= 32 ? 1 : 32 / per_row;
+    constexpr int reps = per_row >= 32 ? per_row / 32 : 1;
+    const int l_row = per_row >= 32 ? 0 : lane / per_row, l_ch = per_row >= 32 ? lane : lane % per_row;
     auto load_tile = [&](int stage) {
         if (to_load > 0) {
             if (see && (unsigned)entry >= (unsigned)p.b.n_pages) {
                 see = false;
                 if (lane < 16) kv_bad_index(p.b);
             }
-            const long long off = see ? (long long)entry * p.b.page_stride + ((long long)ld.h * P + row_in_page) * p.D : -1;
+            const long long off = see ? (long long)entry * p.b.page_stride + ((long long)l_h * P + row_in_page) * p.D : -1;
             const uint32_t dk = ring + stage * S::kStage, dv = dk + kWarpKeys * G::kPitchK;
-            constexpr int per_row = G::kChunks;
-            constexpr int rows_at_once = per_row >= 32 ? 1 : 32 / per_row;
-            constexpr int reps = per_row >= 32 ? per_row / 32 : 1;
+            if (p.plain_rows && __all_sync(0xffffffffu, see)) {
+                // 16 rows of one page, one after the other, as wide as the stage's
+                const long long r0 = __shfl_sync(0xffffffffu, off, 0) + (long long)l_row * DP + l_ch * (16 / (int)sizeof(T));
+                const T *ks = kp + r0, *vs = vp + r0;
 #pragma unroll
-            for (int r = 0; r < kWarpKeys; r += rows_at_once) {
-                const int row = r + (per_row >= 32 ? 0 : lane / per_row);
-                const long long ro = __shfl_sync(0xffffffffu, off, row);
+                for (int r = 0; r < kWarpKeys; r += rows_at_once) {
+                    const int row = r + l_row;
 #pragma unroll
-                for (int x = 0; x < reps; ++x) {
-                    const int ch = per_row >= 32 ? lane + 32 * x : lane % per_row;
-                    const bool on = ro >= 0 && ch < chunks;
-                    const long long src = on ? ro + ch * (16 / (int)sizeof(T)) : 0;
-                    const int dc = G::kSwizzle ? ch ^ (row & 7) : ch;
-                    cp16(dk + row * G::kPitchK + dc * 16, kp + src, on);
-                    cp16(dv + row * G::kPitchV + dc * 16, vp + src, on);
+                    for (int x = 0; x < reps; ++x) {
+                        const int ch = l_ch + 32 * x, dc = G::kSwizzle ? ch ^ (row & 7) : ch;
+                        cp16(dk + row * G::kPitchK + dc * 16, ks + r * DP + x * (512 / (int)sizeof(T)), true);
+                        cp16(dv + row * G::kPitchV + dc * 16, vs + r * DP + x * (512 / (int)sizeof(T)), true);
+                    }
+                }
+            } else {
+#pragma unroll 2
+                for (int r = 0; r < kWarpKeys; r += rows_at_once) {
+                    const int row = r + l_row;
+                    const long long ro = __shfl_sync(0xffffffffu, off, row);
+#pragma unroll
+                    for (int x = 0; x < reps; ++x) {
+                        const int ch = l_ch + 32 * x;
+                        const bool on = ro >= 0 && ch < chunks;
+                        const long long src = on ? ro + ch * (16 / (int)sizeof(T)) : 0;
+                        const int dc = G::kSwizzle ? ch ^ (row & 7) : ch;
+                        cp16(dk + row * G::kPitchK + dc * 16, kp + src, on);
+                        cp16(dv + row * G::kPitchV + dc * 16, vp + src, on);
+                    }
                 }
             }
-            advance(p, ld);
-            if (--to_load > 0) look_up();
+            if (--to_load > 0) {
+                if (++l_i == lt.tiles) {
+                    __syncwarp();
+                    if (lane == 0) {
+                        ld.i = lt.tiles - 1;
+                        advance(p, ld);
+                    }
+                    __syncwarp();
+                    lt = ld.t;
+                    l_i = 0;
+                    l_h = ld.h;
+                    l_table = p.b.page_table + (size_t)ld.s * p.b.max_pages;
+                }
+                look_up();
+            }
         }
         cp_commit();
     };
@@ -344,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                 for (int y = 0; y < 4; ++y) {
                     if (!whole) {
                         const int j = j0 + x * 8 + 2 * tig + (y & 1);
-                        if (!(j < hi2[y >> 1] && (j >= lo2[y >> 1] || j < p.sinks))) s[x][y] = p.unseen;
+                        s[x][y] = sees(j, hi2[y >> 1], lo2[y >> 1], p.sinks) ? s[x][y] : p.unseen;
                     }
                     top[y >> 1] = fmaxf(top[y >> 1], s[x][y] * p.scale_log2);
                 }
@@ -478,13 +515,11 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
         }
         if (!whole_unit) {
             // ---- the pieces of a unit meet: the CTA that arrives last joins them in the order of the pieces
-            const int c0 = (int)(cur.unit / per), c1 = (int)((cur.unit + t.tiles - 1) / per);
-            __threadfence();
+            const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
             __syncthreads();
-            if (tid == 0) sh_last = atomicAdd(p.part.counters + c0, 1) == c1 - c0;
+            if (tid == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
             __syncthreads();
             if (sh_last) {
-                __threadfence();
                 for (int i = tid; i < t.rows * F4; i += kThreads) {
                     const int r = i / F4, f4 = i - r * F4;
                     float M = -INFINITY;
@@ -576,10 +611,16 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
     p.q = a.q; p.k = pages.k; p.v = pages.v; p.out = a.out; p.lse = a.lse;
     p.q_stride = a.q_stride; p.out_stride = a.out_stride;
     p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
+    p.gdiv = make_fastdiv(p.g);
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
+    {
+        // a warp's 16 keys lie one after the other in one page, in rows as wide as the kernel's stages
+        const int DP = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
+        p.plain_rows = kv.page_size % kWarpKeys == 0 && kv.head_dim == DP;
+    }
     p.unseen = p.scale_log2 > 0.f ? -INFINITY : INFINITY;
-    if (c->kv_encode && (long long)batch.max_new * p.g > kRows) return launch_paged_attention_tc(c, p, batch.max_new, st);
+    if (c->kv_encode) return launch_paged_attention_tc(c, p, batch.max_new, st);
     const size_t slots = (size_t)4 * kKvMaxSm;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);

@@ -27,6 +27,12 @@ __device__ __forceinline__ int fast_div(int n, const FastDiv &f)
     return (int)(((uint64_t)__umulhi((uint32_t)n, f.mul) + (uint32_t)n) >> f.shift);
 }
 
+// Offsets on the line of tiles pass 32 bits only for enormous batches; their division is several times as long.
+__device__ __forceinline__ long long div_line(long long a, long long b)
+{
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // The batch and the pool as the kernels see them.
 struct KvBatch {
     const int32_t *seq_start, *prefix_len, *page_table, *positions;
@@ -57,6 +63,13 @@ __device__ __forceinline__ bool kv_sequence(const KvBatch &b, int s, int &start,
 // Slot 2 c holds CTA c's part of a unit that an earlier CTA began, slot 2 c + 1 its part of one that a later CTA goes on
 // with; a slot is `rows` rows of `width` floats and as many (max, sum) pairs.
 constexpr int kKvCounterBytes = 8192;      // int32 arrivals by the CTA that begins a shared unit (large tiles: per warp too); zero between calls
+// Arrival behind a barrier of the threads that wrote: releases their stores, acquires those of the arrivals before.
+__device__ __forceinline__ int arrive_acq_rel(int32_t *counter)
+{
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+    return old;
+}
 struct KvPartials {
     int32_t *counters;
     float2 *ml;
@@ -70,10 +83,14 @@ struct AttnParams {
     float *lse;
     int64_t q_stride, out_stride;
     int H, Hk, g, D;
-    int mask, window, sinks;
+    FastDiv gdiv;              // g
+    int mask, window, sinks, plain_rows;
     float scale_log2, unseen;  // unseen: the raw score that scales to -inf
     KvPartials part;
 };
+
+// whether position j lies in [lo, hi) or among the first `sinks` (below hi); no branches
+__device__ __forceinline__ bool sees(int j, int hi, int lo, int sinks) { return (j < hi) & ((j >= lo) | (j < sinks)); }
 
 // ---- the line of tiles ---------------------------------------------------------------------------------------------
 // A row tile of a sequence: its rows, what they may see, its key tiles.  Tiles 0..first-1 hold the first positions that
@@ -89,7 +106,7 @@ __device__ __forceinline__ RowTile<ROWS, TILE> row_tile(const AttnParams &p, int
     RowTile<ROWS, TILE> t;
     t.r0 = rt * ROWS;
     t.rows = min(ROWS, n * p.g - t.r0);
-    const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
+    const int i0 = fast_div(t.r0, p.gdiv), i1 = fast_div(t.r0 + t.rows - 1, p.gdiv);
     t.hi = p.mask == MRP_ATTN_CAUSAL ? pre + i1 + 1 : p.mask == MRP_ATTN_BLOCK ? pre + n : pre;
     t.lo = p.window > 0 ? max(0, pre + i0 + 1 - p.window) : 0;
     t.s1 = p.window > 0 ? min(min(p.sinks, t.lo), t.hi) : 0;
@@ -179,7 +196,7 @@ __device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) total += sh_warp[w];
     }
-    per = (total + gridDim.x - 1) / gridDim.x;
+    per = div_line(total + gridDim.x - 1, gridDim.x);
     const long long begin = per * blockIdx.x, end = min(total, begin + per);
     if (begin >= end) return 0;
     long long done = 0;
@@ -208,6 +225,73 @@ __device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS
     c.s = (int)sh_found[0];
     c.at = sh_found[1];
     open_sequence(p, c);
+    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
+        c.at += (long long)c.t.tiles * p.Hk;
+        c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, ++c.rt);
+    }
+    const int in = (int)(begin - c.at);
+    c.h = in / c.t.tiles;
+    c.i = in - c.h * c.t.tiles;
+    c.at = begin;
+    c.unit = begin - c.i;
+    return end - begin;
+}
+
+// The same for a warp on its own, for up to 128 sequences: no barrier, and the sequence's numbers come from the lane that
+// has them.
+template <int ROWS, int TILE>
+__device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor<ROWS, TILE> &c, long long &per, bool report)
+{
+    const int lane = threadIdx.x & 31;
+    int start[4], n[4], pre[4];
+    long long tiles[4], total = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        start[i] = n[i] = pre[i] = 0;
+        tiles[i] = 0;
+        if (32 * i < p.b.n_seqs) {
+            const int s = lane + 32 * i;
+            if (s < p.b.n_seqs) {
+                if (kv_sequence(p.b, s, start[i], n[i], pre[i])) {
+                    const int nrt = (n[i] * p.g + ROWS - 1) / ROWS;
+                    for (int rt = 0; rt < nrt; ++rt) tiles[i] += row_tile<ROWS, TILE>(p, n[i], pre[i], rt).tiles;
+                    tiles[i] *= p.Hk;
+                } else if (report) {
+                    kv_bad_index(p.b);
+                }
+            }
+            total += tiles[i];
+        }
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
+    per = div_line(total + gridDim.x - 1, gridDim.x);
+    const long long begin = per * blockIdx.x, end = min(total, begin + per);
+    if (begin >= end) return 0;
+    long long done = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (32 * i < p.b.n_seqs && done <= begin) {
+            long long x = tiles[i];
+#pragma unroll
+            for (int w = 1; w < 32; w <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, w);
+                if (lane >= w) x += y;
+            }
+            const long long before = done + x - tiles[i];
+            const uint32_t hit = __ballot_sync(0xffffffffu, tiles[i] > 0 && before <= begin && begin < before + tiles[i]);
+            if (hit) {
+                const int from = __ffs(hit) - 1;
+                c.s = 32 * i + from;
+                c.at = __shfl_sync(0xffffffffu, before, from);
+                c.start = __shfl_sync(0xffffffffu, start[i], from);
+                c.n = __shfl_sync(0xffffffffu, n[i], from);
+                c.pre = __shfl_sync(0xffffffffu, pre[i], from);
+            }
+            done += __shfl_sync(0xffffffffu, x, 31);
+        }
+    c.rt = 0;
+    c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, 0);
     while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
         c.at += (long long)c.t.tiles * p.Hk;
         c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, ++c.rt);

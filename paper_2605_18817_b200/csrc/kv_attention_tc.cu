@@ -78,16 +78,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t a, float *v)
           "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(a) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t a, const float *v)
+__device__ __forceinline__ void tmem_ld16_go(uint32_t a, float *v)         // 16 columns; no wait
 {
-    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-          "r"(r[30]), "r"(r[31]) : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_landed16(float *v)
+{
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                      "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r)
 {
@@ -107,19 +109,739 @@ __device__ __forceinline__ void tmem_landed32(float *v)
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// V as the B operand of P V: [keys][64 features] rows of 128 bytes, swizzled in groups of 8 keys.  The contraction (keys)
-// runs down the rows, so the operand is MN-major: groups of 8 keys 1024 bytes apart, 64-feature blocks a tile apart.
-__device__ __forceinline__ uint64_t v_desc(uint32_t saddr)
+// ======================================================================================================================
+// Few rows (decoding, blocks): everything transposed.  S^T = K Q^T puts the 128 keys of a tile on the tensor-memory lanes
+// and the NR query rows (16, 32 or 64) on the columns, O^T += V^T P^T the features on the lanes: the work of the MMAs and of
+// the exponentials is proportional to the rows there are, and all 128 threads of a warpgroup have a key each.
+//   warp 0   K and V tiles by TMA, as below        warp 1   MMAs        warps 2, 3   queries and what rows see, a unit ahead
+//   warps 4-7, 8-11   two warpgroups that take tiles in turn, each with its own S buffer, maxima, sums and accumulator (no
+//            exchange until the unit's end): a thread turns its key's scores into probabilities and stores them as a row
+//            of the operand P [keys][rows] in shared memory, for up to 32 rows as bf16 hi and lo columns side by side
+// The maximum in use is common to a warpgroup's 128 keys, so a tile needs to know only whether some score exceeds it by
+// more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
+// rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it.
+template <int DB, int NR> struct FewGeo {
+    static constexpr bool kHiLo = NR <= 32;
+    static constexpr int kCols = kHiLo ? 2 * NR : NR;      // columns of P and of an accumulator
+    static constexpr int kTileBytes = DB * 128 * 128;
+    static constexpr int kStages = (DB == 2 ? 1 : 2) * (NR <= 32 ? 5 : 4);
+    static constexpr int kRing = kStages * kTileBytes;
+    static constexpr int kP = 128 * 128;                   // P of a warpgroup: 128 keys, rows of 128 bytes
+    static constexpr int kQ = DB * NR * 128;               // queries of a unit, two of them
+    static constexpr int kPAt = kRing, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
+    static constexpr int kSmem = kBars + 1024 + 1024;
+    static constexpr int kTmem = 2 * NR + 2 * kCols <= 128 ? 128 : 256;
+    static constexpr int kThreads = 384;
+};
+constexpr float kNone = -3.4028234e38f;    // the maximum of a row that has seen nothing
+
+template <int N> __device__ __forceinline__ void tmem_ld_n(uint32_t a, float *v);
+template <> __device__ __forceinline__ void tmem_ld_n<32>(uint32_t a, float *v)
+{
+    tmem_ld32(a, v);
+    tmem_wait_ld();
+    tmem_landed32(v);
+}
+template <> __device__ __forceinline__ void tmem_ld_n<16>(uint32_t a, float *v)
+{
+    tmem_ld16_go(a, v);
+    tmem_wait_ld();
+    tmem_landed16(v);
+}
+__device__ __forceinline__ void wg_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool any_of(int id, int threads, bool x)        // barrier of `threads` threads, true where any one's x is
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)x) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ bool wg_any(int id, bool x) { return any_of(id, 128, x); }
+// Reduces W rows (a value per lane each) over the warp; lane i returns row i (i % W).  Each step halves the rows a lane goes
+// on with: W - 1 exchanges instead of 5 W.
+template <int W, bool MAX> __device__ __forceinline__ float reduce_rows(float (&s)[W], int lane)
+{
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+#pragma unroll
+    for (int h = W / 2; h > 0; h >>= 1) {
+        const bool up = (lane & h) != 0;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float keep = up ? s[i + h] : s[i], send = up ? s[i] : s[i + h];
+            s[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, h));
+        }
+    }
+    float r = s[0];
+#pragma unroll
+    for (int h = W; h < 32; h <<= 1) r = op(r, __shfl_xor_sync(0xffffffffu, r, h));
+    return r;
+}
+
+// V^T as the A operand / P as the B operand: rows (keys) of 128 bytes, MN-major; `block` bytes to the next 64 features
+__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t block)
 {
     uint64_t d = 0;
     d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)((128 * 128) >> 4) << 16;               // next 64 features
-    d |= (uint64_t)(1024 >> 4) << 32;                      // next 8 keys
+    d |= (uint64_t)(block >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
     return d;
 }
 
+// The pages of a K or V tile's visible positions -> a ring stage; the whole warp.
+struct PageBoxes {
+    int box_rows, pages;
+};
+template <int DB, typename Tile>
+__device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const Tile &t, int n, int s,
+                                           int h, uint32_t dst, uint32_t bar, int lane)
+{
+    const int j = key_tile(t, n) * kTcTile + lane * bx.box_rows;
+    const bool need = lane < bx.pages && ((j < t.hi && j + bx.box_rows > t.lo) || j < t.s1);
+    int entry = 0, row = 0;
+    if (need) {
+        const int pg = fast_div(j, p.b.page);
+        row = j - pg * p.b.page.d;
+        entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
+        if ((unsigned)entry >= (unsigned)p.b.n_pages) {
+            kv_bad_index(p.b);
+            entry = p.b.n_pages;           // outside the map: zeros arrive
+        }
+    }
+    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
+    if (lane == 0) mbar_expect_tx(bar, boxes * bx.box_rows * 128u * DB);
+    __syncwarp();
+    if (need) {
+#pragma unroll
+        for (int x = 0; x < DB; ++x)
+            tma_load_page(dst + lane * bx.box_rows * 128 + x * (128 * 128), map, 64 * x, row, h, entry, bar);
+    }
+}
+
+// Query rows r0.. of a tile (those below `rows`; zeros beyond, and beyond the head's features) -> shared memory, as K-major
+// blocks of 64 features.  THREADS threads, all copies in flight together.
+template <int DB, int ROWS, int THREADS>
+__device__ __forceinline__ void load_queries(const AttnParams &p, int start, int h, int r0, int rows, uint32_t sq, int tid)
+{
+    constexpr int kRow = 8 * DB, kStep = THREADS / kRow;   // 16-byte chunks of a row; rows a round
+    static_assert(THREADS % kRow == 0 && ROWS % kStep == 0, "whole rounds");
+    const int ch = tid % kRow;
+    const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)start * p.q_stride + (int64_t)h * p.g * p.D;
+    const bool wide = ch * 8 < p.D;
+    int r = tid / kRow, tok = fast_div(r0 + r, p.gdiv), hg = r0 + r - tok * p.g;
+    const int dt = fast_div(kStep, p.gdiv), dh = kStep - dt * p.g;
+    uint32_t a = sq + (ch >> 3) * (ROWS * 128) + r * 128;
+#pragma unroll 4
+    for (int i = 0; i < ROWS / kStep; ++i) {
+        const bool on = wide & (r < rows);
+        const __nv_bfloat16 *q = on ? src + (int64_t)tok * p.q_stride + hg * p.D + ch * 8 : src;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(a + (((ch & 7) ^ (r & 7)) << 4)), "l"(q), "r"(on ? 16 : 0) : "memory");
+        r += kStep;
+        a += kStep * 128;
+        tok += dt;
+        hg += dh;
+        if (hg >= p.g) { hg -= p.g; ++tok; }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// What a unit's rows see together, for the V rows that must not reach a product: rows no row sees -> zeros; rows some
+// see that hold what is not finite -> zeros, remembered.  One warp, on a V tile that has landed.
+struct Seen {
+    int all_lo, all_hi;
+    bool differ;
+};
+template <typename Tile>
+__device__ __forceinline__ Seen seen_by_all(const AttnParams &p, const Tile &t, int pre)
+{
+    const int i0 = fast_div(t.r0, p.gdiv), i1 = fast_div(t.r0 + t.rows - 1, p.gdiv);
+    Seen s;
+    s.differ = i0 != i1 && (p.mask == MRP_ATTN_CAUSAL || p.window > 0);
+    s.all_hi = p.mask == MRP_ATTN_CAUSAL ? pre + i0 + 1 : t.hi;
+    s.all_lo = p.window > 0 ? max(0, pre + i1 + 1 - p.window) : 0;
+    return s;
+}
+template <int DB, typename Tile>
+__device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0, uint32_t vs, Suspects &sus, int lane)
+{
+    if ((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) {
+        if (!a.differ || (j0 >= a.all_lo && j0 + kTcTile <= a.all_hi)) return;
+    }
+    uint32_t found[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int row = w * 32 + lane, j = j0 + row;
+        const bool seen = j < t.hi && (j >= t.lo || j < t.s1);
+        bool bad = false;
+        if (seen && a.differ && !(j >= a.all_lo && j < a.all_hi)) {
+            for (int c = 0; c < 8 * DB; ++c) {
+                uint32_t u[4];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                             : "r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)) : "memory");
+#pragma unroll
+                for (int y = 0; y < 4; ++y) bad |= (u[y] & 0x7F800000u) == 0x7F800000u || (u[y] & 0x7F80u) == 0x7F80u;
+            }
+        }
+        found[w] = __ballot_sync(0xffffffffu, bad);
+        if (!seen || bad)
+            for (int c = 0; c < 8 * DB; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
+                             ::"r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
+    }
+    if (lane == 0 && (found[0] | found[1] | found[2] | found[3])) {
+        const int at_n = sus.n;
+        if (at_n < kMaxSuspects) {
+            sus.base[at_n] = j0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sus.keys[at_n][w] = found[w];
+        }
+        sus.n = at_n + 1;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ bool suspects_hit(const Suspects &sus, int hi, int lo, int sinks)
+{
+    bool hit = sus.n > kMaxSuspects;
+    for (int y = 0; y < min(sus.n, kMaxSuspects); ++y)
+        for (int w = 0; w < 4; ++w)
+            for (uint32_t bits = sus.keys[y][w]; bits; bits &= bits - 1) {
+                const int j = sus.base[y] + w * 32 + __ffs(bits) - 1;
+                hit |= sees(j, hi, lo, sinks);
+            }
+    return hit;
+}
+
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }      // (NaN goes through)
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
+
+// Joins the pieces c0..c1 of a unit in their order, with a running maximum: warp w of four takes every fourth row, RG rows
+// and U pieces of each in flight, a lane four features.
+struct JoinArgs {
+    const float2 *ml;
+    const float *o;
+    __nv_bfloat16 *out;                    // of the unit's sequence and key head
+    float *lse;
+    int64_t out_stride;
+    int H, D, g;
+    FastDiv gdiv;
+    int r0, rows, c0, c1;
+};
+__device__ __forceinline__ JoinArgs join_args(const AttnParams &p, int start, int h, int r0, int rows, int c0, int c1)
+{
+    JoinArgs a;
+    a.ml = p.part.ml;
+    a.o = p.part.o;
+    a.out = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)start * p.out_stride + (int64_t)h * p.g * p.D;
+    a.lse = p.lse ? p.lse + (int64_t)start * p.H + h * p.g : nullptr;
+    a.out_stride = p.out_stride;
+    a.H = p.H; a.D = p.D; a.g = p.g; a.gdiv = p.gdiv;
+    a.r0 = r0; a.rows = rows; a.c0 = c0; a.c1 = c1;
+    return a;
+}
+template <int NR, int RG, int U>
+__device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
+{
+    const int rows = p.rows, c0 = p.c0, c1 = p.c1;
+    const bool mine = 4 * lane < p.D;
+#pragma unroll 1
+    for (int rb = w; rb < rows; rb += 4 * RG) {
+        float M[RG], L[RG];
+        float4 a[RG];
+#pragma unroll
+        for (int y = 0; y < RG; ++y) { M[y] = kNone; L[y] = 0.f; a[y] = make_float4(0.f, 0.f, 0.f, 0.f); }
+#pragma unroll 1
+        for (int cb = c0; cb <= c1; cb += U) {
+            float2 ml[RG][U];
+            float4 o[RG][U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int c = min(cb + i, c1);
+                const size_t sl = (size_t)(2 * c + (c == c0)) * NR;
+#pragma unroll
+                for (int y = 0; y < RG; ++y) {
+                    const int r = min(rb + 4 * y, rows - 1);
+                    ml[y][i] = __ldcg(p.ml + sl + r);
+                    o[y][i] = __ldcg(reinterpret_cast<const float4 *>(p.o + (sl + r) * 128) + (mine ? lane : 0));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (cb + i <= c1) {
+#pragma unroll
+                    for (int y = 0; y < RG; ++y) {
+                        const float nm = fmaxf(M[y], ml[y][i].x);
+                        const float f = M[y] == nm ? 1.f : ex2f(M[y] - nm), e = ml[y][i].x == nm ? 1.f : ex2f(ml[y][i].x - nm);
+                        M[y] = nm;
+                        L[y] = fmaf(e, ml[y][i].y, L[y] * f);
+                        a[y].x = fmaf(e, o[y][i].x, a[y].x * f); a[y].y = fmaf(e, o[y][i].y, a[y].y * f);
+                        a[y].z = fmaf(e, o[y][i].z, a[y].z * f); a[y].w = fmaf(e, o[y][i].w, a[y].w * f);
+                    }
+                }
+        }
+#pragma unroll
+        for (int y = 0; y < RG; ++y) {
+            const int r = rb + 4 * y;
+            if (r < rows && mine) {
+                const float inv = inverse(L[y]);
+                const int rr = p.r0 + r, tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
+                __nv_bfloat16 *dst = p.out + (int64_t)tok * p.out_stride + (int64_t)hg * p.D + 4 * lane;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(a[y].x * inv, a[y].y * inv), pack_bf16(a[y].z * inv, a[y].w * inv));
+                if (lane == 0 && p.lse) p.lse[(int64_t)tok * p.H + hg] = log_sum(M[y], L[y]);
+            }
+        }
+    }
+}
+
+template <int DB, int NR>
+__global__ void __launch_bounds__(384, 1)
+kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
+                        const __grid_constant__ CUtensorMap vmap, int box_rows)
+{
+    typedef FewGeo<DB, NR> G;
+    typedef RowTile<NR, kTcTile> Tile;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ long long sh_find[G::kThreads / 32 + 2];
+    __shared__ Suspects suspects[2];
+    __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
+    __shared__ __align__(16) float sh_m[2][NR], sh_c[2][NR];       // maximum in use, factor to it, per warpgroup
+    __shared__ float sh_wm[2][4][NR], sh_wl[2][4][NR];     // row maxima and sums of the warps
+    __shared__ float sh_f[2][NR];                          // the unit's end: factors of the accumulators,
+    __shared__ int64_t sh_out[NR];                         //   where the rows go
+    __shared__ int sh_last;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t ring = base;
+    const uint32_t bars = base + G::kBars;
+    auto full_bar = [&](int s) { return bars + 8 * s; };
+    auto empty_bar = [&](int s) { return bars + 8 * (16 + s); };
+    auto s_full = [&](int x) { return bars + 8 * (32 + x); };
+    auto p_ready = [&](int x) { return bars + 8 * (34 + x); };
+    auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
+    auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
+    auto unit_end = [&](int x) { return bars + 8 * (40 + x); };    // the unit is written: everything of it may be reused
+    const uint32_t second_end = bars + 8 * 42;             // the second warpgroup's sums are there
+    unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 43);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    const WaitStatus ws = {p.b.status, p.b.user_status};
+
+    if (tid == 0) {
+        for (int s = 0; s < G::kStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(s_full(x), 1);
+            mbar_init(p_ready(x), 4);
+            mbar_init(pv_done(x), 1);
+            mbar_init(q_ready(x), 64);
+            mbar_init(unit_end(x), 4);
+        }
+        mbar_init(second_end, 4);
+        *abort_flag = 0;
+        prefetch_tmap(&kmap);
+        prefetch_tmap(&vmap);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"((uint32_t)G::kTmem) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators
+    auto s_at = [&](int x) { return tmem + x * NR; };
+    auto o_at = [&](int x) { return tmem + 2 * NR + x * G::kCols; };
+    pdl_wait();
+    pdl_trigger();
+
+    Cursor<NR, kTcTile> cur;
+    long long per;
+    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
+                                            : find_piece<NR, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    const long long piece_end = len > 0 ? cur.at + len : 0;
+    long long at = len > 0 ? cur.at : 0;
+    auto next_unit = [&](int count) {
+        at += count;
+        if (at < piece_end) {
+            cur.i = cur.t.tiles - 1;
+            cur.at = at - 1;
+            advance(p, cur);
+        }
+    };
+
+    if (warp == 0) {
+        // ================================ K and V tiles ================================
+        int stage = 0;
+        uint32_t phase = 0;
+        const PageBoxes bx = {box_rows, kTcTile / box_rows};
+        bool ok = true;
+        while (ok && at < piece_end) {
+            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+            auto fetch = [&](int n, const CUtensorMap *map) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                if (!ok) return;
+                fetch_tile<DB>(p, map, bx, cur.t, begin + n, cur.s, cur.h, ring + stage * G::kTileBytes, full_bar(stage), lane);
+                if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+            };
+            fetch(0, &kmap);
+            for (int n = 0; n < count; ++n) {
+                if (n + 1 < count) fetch(n + 1, &kmap);
+                fetch(n, &vmap);
+            }
+            next_unit(count);
+        }
+    } else if (warp == 1) {
+        // ================================ MMAs ================================
+        int stage = 0;
+        uint32_t phase = 0, k = 0, unit = 0;
+        bool ok = true;
+        const uint32_t idesc_s = make_idesc(NR), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+        auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
+        while (ok && at < piece_end) {
+            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+            const Tile t = cur.t;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const uint32_t sq = base + G::kQAt + (unit & 1u) * G::kQ;
+            wait(q_ready(unit & 1u), (unit >> 1) & 1u);
+            if (!ok) break;
+            Suspects &sus = suspects[unit & 1];            // (the unit before the last is written: see the query warps)
+            if (lane == 0) sus.n = 0;
+            __syncwarp();
+            auto scores = [&](uint32_t kk) {               // S^T of tile kk from the stage at hand
+                wait(full_bar(stage), phase);
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t ks = ring + stage * G::kTileBytes;
+                if (elect_one()) {
+#pragma unroll
+                    for (int c = 0; c < 4 * DB; ++c)
+                        umma_bf16(s_at(kk & 1u), make_smem_desc(ks + (c >> 2) * (128 * 128) + (c & 3) * 32),
+                                  make_smem_desc(sq + (c >> 2) * (NR * 128) + (c & 3) * 32), idesc_s, c > 0);
+                    umma_commit(s_full(kk & 1u));
+                    umma_commit(empty_bar(stage));
+                }
+                __syncwarp();
+                step();
+            };
+            scores(k);
+            for (int n = 0; n < count && ok; ++n, ++k) {
+                if (n + 1 < count) scores(k + 1);
+                wait(full_bar(stage), phase);
+                if (!ok) break;
+                const uint32_t vs = ring + stage * G::kTileBytes, ps = base + G::kPAt + (k & 1u) * G::kP;
+                clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
+                wait(p_ready(k & 1u), (k >> 1) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)            // (one block of features: the second 64 lanes repeat it)
+                        umma_bf16(o_at(k & 1u), mn_desc(vs + c * 2048, DB == 2 ? 128 * 128 : 0), mn_desc(ps + c * 2048, 0), idesc_o, n >= 2 || c > 0);
+                    umma_commit(pv_done(k & 1u));
+                    umma_commit(empty_bar(stage));
+                }
+                __syncwarp();
+                step();
+            }
+            ++unit;
+            next_unit(count);
+        }
+    } else if (warp < 4) {
+        // ================================ queries, a unit ahead ================================
+        uint32_t unit = 0;
+        bool ok = true;
+        while (ok && at < piece_end) {
+            const int count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+            const Tile t = cur.t;
+            const int u = unit & 1;
+            if (unit >= 2) {
+                ok = __all_sync(0xffffffffu, mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws));
+                if (!ok) break;
+            }
+            load_queries<DB, NR, 64>(p, cur.start, cur.h, t.r0, t.rows, base + G::kQAt + u * G::kQ, tid - 64);
+            for (int r = tid - 64; r < NR; r += 64) {
+                const int pos = cur.pre + fast_div(t.r0 + min(r, t.rows - 1), p.gdiv);
+                sh_hi[u][r] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
+                sh_lo[u][r] = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            }
+            mbar_arrive(q_ready(u));
+            ++unit;
+            next_unit(count);
+        }
+    } else if (warp >= 4) {
+        // ================================ softmax: a thread per key, two warpgroups in turn ================================
+        const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
+        const int bar_id = 1 + x;
+        const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+        const uint32_t s_tm = s_at(x) + lanes, o_tm = o_at(x) + lanes;
+        const uint32_t p_row = base + G::kPAt + x * G::kP + wt * 128;
+        uint32_t k0 = 0, unit = 0;
+        const float sc = p.scale_log2;
+        bool ok = true;
+        float l[NR];
+        while (at < piece_end) {
+            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+            const Tile t = cur.t;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const int u = unit & 1;
+            if (wt < NR) sh_m[x][wt] = kNone;
+            wg_sync(bar_id);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) l[r] = 0.f;
+            const int n0 = (int)((k0 & 1u) ^ (uint32_t)x); // this warpgroup's tiles: n0, n0 + 2, ..
+            for (int n = n0; n < count; n += 2) {
+                const uint32_t k = k0 + n;
+                ok = mbar_wait(s_full(x), (k >> 1) & 1u, abort_flag, ws);
+                __syncwarp();
+                tc_fence_after();
+                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + wt;
+                const bool whole = j0 >= all.all_lo && j0 + kTcTile <= all.all_hi;
+                uint64_t seen = 0;                         // by which rows, where not by all
+                if (!whole) {
+                    if (all.differ) {
+#pragma unroll 1
+                        for (int r = 0; r < NR; ++r) seen |= (uint64_t)sees(j, sh_hi[u][r], sh_lo[u][r], p.sinks) << r;
+                    } else {
+                        seen = sees(j, all.all_hi, all.all_lo, p.sinks) ? ~0ull : 0ull;
+                    }
+                }
+                constexpr int W = NR < 32 ? NR : 32;       // rows at a time; up to 32 rows stay in registers
+                float s[W];
+                auto load = [&](int r0) {                  // the key's scores of rows r0..; what a row does not see: -inf once scaled
+                    tmem_ld_n<W>(s_tm + r0, s);
+                    if (!whole) {
+                        const uint32_t mine = (uint32_t)(seen >> r0);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) s[i] = (mine >> i) & 1u ? s[i] : p.unseen;
+                    }
+                };
+                auto against_max = [&](int r0) {           // exponents
+#pragma unroll
+                    for (int i = 0; i < W; i += 4) {
+                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[x][r0 + i]);
+                        s[i] = fmaf(s[i], sc, -m.x); s[i + 1] = fmaf(s[i + 1], sc, -m.y);
+                        s[i + 2] = fmaf(s[i + 2], sc, -m.z); s[i + 3] = fmaf(s[i + 3], sc, -m.w);
+                    }
+                };
+                bool grown = true;                         // (the warpgroup's first tile of the unit sets the maxima)
+                if (n >= 2) {
+                    bool more = false;
+#pragma unroll 1
+                    for (int r0 = 0; r0 < NR; r0 += W) {
+                        load(r0);
+                        against_max(r0);
+                        float top = s[0];
+#pragma unroll
+                        for (int i = 1; i < W; ++i) top = fmaxf(top, s[i]);
+                        more |= top > 8.f;
+                    }
+                    grown = wg_any(bar_id, more || !ok);
+                }
+                if (grown) {
+                    // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
+                    if (wg_any(bar_id, !ok)) { ok = false; break; }
+#pragma unroll 1
+                    for (int r0 = 0; r0 < NR; r0 += W) {
+                        load(r0);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) s[i] *= sc;
+                        const float top = reduce_rows<W, true>(s, lane);
+                        if (lane < W) sh_wm[x][wq][r0 + lane] = top;
+                    }
+                    wg_sync(bar_id);
+                    if (wt < NR) {
+                        const float top = fmaxf(fmaxf(sh_wm[x][0][wt], sh_wm[x][1][wt]), fmaxf(sh_wm[x][2][wt], sh_wm[x][3][wt]));
+                        const float m = sh_m[x][wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
+                        sh_c[x][wt] = nm == m ? 1.f : ex2f(m - nm);
+                        sh_m[x][wt] = nm;
+                    }
+                    wg_sync(bar_id);
+                    if (n >= 2) {
+#pragma unroll
+                        for (int r = 0; r < NR; r += 4) {
+                            const float4 c = *reinterpret_cast<const float4 *>(&sh_c[x][r]);
+                            l[r] *= c.x; l[r + 1] *= c.y; l[r + 2] *= c.z; l[r + 3] *= c.w;
+                        }
+                        // (the product of this warpgroup's last tile is done: S of this one came after it)
+#pragma unroll 1
+                        for (int r0 = 0; r0 < G::kCols; r0 += 16) {
+                            float o[16];
+                            tmem_ld_n<16>(o_tm + r0, o);
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * sh_c[x][(r0 + i) & (NR - 1)]);
+                            tmem_st16(o_tm + r0, w);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                // ---- probabilities of the key -> its row of P
+#pragma unroll
+                for (int r0 = 0; r0 < NR; r0 += W) {
+                    if (NR > W || grown) {
+                        load(r0);
+                        against_max(r0);
+                    }
+#pragma unroll
+                    for (int c = r0 / 8; c < (r0 + W) / 8; ++c) {
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = 8 * c + 2 * i;
+                            const float a = ex2f(s[r - r0]), b = ex2f(s[r - r0 + 1]);
+                            l[r] += a;
+                            l[r + 1] += b;
+                            if (G::kHiLo) split_bf16(a, b, hi[i], lo[i]);
+                            else hi[i] = pack_bf16(a, b);
+                        }
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                        if (G::kHiLo)
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready(x));
+            }
+            if (!ok) break;
+            // ---- the unit's end: sums over the warp's keys
+            {
+                constexpr int W = NR < 32 ? NR : 32;
+#pragma unroll
+                for (int r0 = 0; r0 < NR; r0 += W) {
+                    float v[W];
+#pragma unroll
+                    for (int i = 0; i < W; ++i) v[i] = l[r0 + i];
+                    const float sum = reduce_rows<W, false>(v, lane);
+                    if (lane < W) sh_wl[x][wq][r0 + lane] = sum;
+                }
+            }
+            if (x == 1) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(second_end);
+                ok = mbar_wait(unit_end(u), (unit >> 1) & 1u, abort_flag, ws);
+                if (wg_any(bar_id, !ok)) break;
+            } else {
+                // the first warpgroup joins both and writes.  (The second one's sums first: it has then seen the scores of its
+                // last tile, so that the product before its last is done and pv_done(1) is at most one phase behind.)
+                ok = mbar_wait(second_end, unit & 1u, abort_flag, ws);
+                bool has[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int first = (int)((k0 & 1u) ^ (uint32_t)y);
+                    has[y] = first < count;
+                    if (has[y]) {
+                        const uint32_t last = k0 + (uint32_t)(first + ((count - 1 - first) & ~1));
+                        ok = ok && mbar_wait(pv_done(y), (last >> 1) & 1u, abort_flag, ws);
+                    }
+                }
+                if (wg_any(bar_id, !ok)) break;
+                tc_fence_after();
+                const bool whole_unit = count == t.tiles;
+                const int slot = 2 * (int)blockIdx.x + (begin == 0 ? 1 : 0);
+                const int rows = t.rows;
+                if (wt < NR) {
+                    float lw[2], mw[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        lw[y] = sh_wl[y][0][wt] + sh_wl[y][1][wt] + sh_wl[y][2][wt] + sh_wl[y][3][wt];
+                        mw[y] = sh_m[y][wt];
+                    }
+                    const float M = fmaxf(mw[0], mw[1]);
+                    const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
+                    float L = lw[0] * f0 + lw[1] * f1;
+                    if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) L = __int_as_float(0x7FC00000);
+                    const float inv = whole_unit ? inverse(L) : 1.f;
+                    sh_f[0][wt] = f0 * inv;
+                    sh_f[1][wt] = f1 * inv;
+                    if (wt < rows) {
+                        const int rr = t.r0 + wt, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
+                        if (!whole_unit) {
+                            __stcg(p.part.ml + (size_t)slot * NR + wt, make_float2(M, L));
+                        } else {
+                            sh_out[wt] = (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
+                            if (p.lse) p.lse[(int64_t)(cur.start + tok) * p.H + head] = log_sum(M, L);
+                        }
+                    }
+                }
+                wg_sync(bar_id);
+                const bool mine = wt < p.D;                // a thread per feature
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += 16) {
+                    float a[16], o[4][16];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (has[y]) {
+                            tmem_ld16_go(o_at(y) + lanes + r0, o[2 * y]);
+                            if (G::kHiLo) tmem_ld16_go(o_at(y) + lanes + NR + r0, o[2 * y + 1]);
+                        }
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) tmem_landed16(o[y]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        a[i] = 0.f;
+                        if (has[0]) a[i] = (G::kHiLo ? o[0][i] + o[1][i] : o[0][i]) * sh_f[0][r0 + i];
+                        if (has[1]) a[i] = fmaf(G::kHiLo ? o[2][i] + o[3][i] : o[2][i], sh_f[1][r0 + i], a[i]);
+                    }
+                    if (mine && whole_unit) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (r0 + i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[r0 + i] + wt] = __float2bfloat16_rn(a[i]);
+                    } else if (mine) {
+                        float *part = p.part.o + ((size_t)slot * NR + r0) * 128 + wt;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (r0 + i < rows) __stcg(part + i * 128, a[i]);
+                    }
+                }
+                tc_fence_before();
+                if (!whole_unit) {
+                    // ---- the pieces of the unit meet: the CTA that arrives last joins them in order
+                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
+                    wg_sync(bar_id);
+                    if (wt == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
+                    wg_sync(bar_id);
+                    if (sh_last) {
+                        const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
+                        if (rows <= 4) join_rows<NR, 1, 8>(ja, wq, lane);
+                        else join_rows<NR, NR == 64 ? 4 : 2, NR == 64 ? 2 : 4>(ja, wq, lane);
+                        if (wt == 0) p.part.counters[c0] = 0;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(unit_end(u));
+                wg_sync(bar_id);                           // sh_f, sh_out and sh_last are read
+            }
+            k0 += (uint32_t)count;
+            ++unit;
+            next_unit(count);
+        }
+    }
+
+    __syncthreads();
+    if (*abort_flag) {
+        // a wait gave up: give copies still in flight time to land before the CTA leaves
+        const long long t0 = clock64();
+        while (clock64() - t0 < 200000) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)G::kTmem) : "memory");
+    }
+}
+
+// ======================================================================================================================
+// Many rows: row tiles of 128 on the lanes (NT = 1: 65 to 128 rows; NT = 2: prompts).
 template <int DB, int NT>
 __global__ void __launch_bounds__(TcGeo<DB, NT>::kThreads, 1)
 kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
@@ -177,7 +899,8 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 
     Cursor<kRows, kTcTile> cur;
     long long per;
-    const long long len = find_piece<kRows, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
+                                            : find_piece<kRows, kTcTile, G::kThreads>(p, cur, per, sh_find);
     const long long piece_end = len > 0 ? cur.at + len : 0;
     long long at = len > 0 ? cur.at : 0;
     // (all roles walk the same units; a unit of the piece: tiles begin .. begin + count - 1 of cur.t)
@@ -194,38 +917,15 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         // ================================ TMA producer ================================
         int stage = 0;
         uint32_t phase = 0;
-        const int pages = kTcTile / box_rows;              // boxes of a tile
-        const int P = p.b.page.d;
+        const PageBoxes bx = {box_rows, kTcTile / box_rows};
         bool ok = true;
         while (ok && at < piece_end) {
             const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
             const Tile t = cur.t;
-            // one tile of K (which = 0) or V, the pages of its visible positions
             auto fetch = [&](int n, int which) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                 if (!ok) return;
-                ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
-                if (!ok) return;
-                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + lane * box_rows;
-                const bool need = lane < pages && ((j < t.hi && j + box_rows > t.lo) || j < t.s1);
-                int entry = 0, row = 0;
-                if (need) {
-                    const int pg = fast_div(j, p.b.page);
-                    row = j - pg * P;
-                    entry = __ldg(p.b.page_table + (size_t)cur.s * p.b.max_pages + pg);
-                    if ((unsigned)entry >= (unsigned)p.b.n_pages) {
-                        kv_bad_index(p.b);
-                        entry = p.b.n_pages;               // outside the map: zeros arrive
-                    }
-                }
-                const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
-                if (lane == 0) mbar_expect_tx(full_bar(stage), boxes * box_rows * 128u * DB);
-                __syncwarp();
-                if (need) {
-                    const uint32_t dst = ring + stage * G::kTileBytes + lane * box_rows * 128;
-#pragma unroll
-                    for (int x = 0; x < DB; ++x)
-                        tma_load_page(dst + x * (128 * 128), which ? &vmap : &kmap, 64 * x, row, cur.h, entry, full_bar(stage));
-                }
+                fetch_tile<DB>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, ring + stage * G::kTileBytes, full_bar(stage), lane);
                 if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
             };
             fetch(0, 0);
@@ -259,7 +959,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
-                    umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c * 8, v_desc(vs + c * 2048), idesc_o, !first || c > 0);
+                    umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c * 8, mn_desc(vs + c * 2048, 128 * 128), idesc_o, !first || c > 0);
                 umma_commit(pv_done(x));
             }
             __syncwarp();
@@ -271,52 +971,11 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         while (ok && at < piece_end) {
             const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
             const Tile t = cur.t;
-            const int i0 = t.r0 / p.g, i1 = (t.r0 + t.rows - 1) / p.g;
-            const bool differ = i0 != i1 && (p.mask == MRP_ATTN_CAUSAL || p.window > 0);
-            const int all_hi = p.mask == MRP_ATTN_CAUSAL ? cur.pre + i0 + 1 : t.hi;
-            const int all_lo = p.window > 0 ? max(0, cur.pre + i1 + 1 - p.window) : 0;
+            const Seen all = seen_by_all(p, t, cur.pre);
             Suspects &sus = suspects[unit & 1];
             if (lane == 0) sus.n = 0;
             __syncwarp();
-            // V rows no row sees -> zeros; rows some see that hold what is not finite -> zeros, remembered
-            auto clean = [&](int n, uint32_t vs) {
-                const int j0 = key_tile(t, begin + n) * kTcTile;
-                if ((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) {
-                    if (!differ || (j0 >= all_lo && j0 + kTcTile <= all_hi)) return;
-                }
-                uint32_t found[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int row = w * 32 + lane, j = j0 + row;
-                    const bool seen = j < t.hi && (j >= t.lo || j < t.s1);
-                    bool bad = false;
-                    if (seen && differ && !(j >= all_lo && j < all_hi)) {
-                        for (int c = 0; c < 8 * DB; ++c) {
-                            uint32_t u[4];
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                                         : "r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)) : "memory");
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) bad |= (u[y] & 0x7F800000u) == 0x7F800000u || (u[y] & 0x7F80u) == 0x7F80u;
-                        }
-                    }
-                    found[w] = __ballot_sync(0xffffffffu, bad);
-                    if (!seen || bad)
-                        for (int c = 0; c < 8 * DB; ++c)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
-                                         ::"r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
-                }
-                if (lane == 0 && (found[0] | found[1] | found[2] | found[3])) {
-                    const int at_n = sus.n;
-                    if (at_n < kMaxSuspects) {
-                        sus.base[at_n] = j0;
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) sus.keys[at_n][w] = found[w];
-                    }
-                    sus.n = at_n + 1;
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            };
+            auto clean = [&](int n, uint32_t vs) { clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
 #pragma unroll
             for (int x = 0; x < NT; ++x) wait(q_ready(x), unit & 1u);
             wait(full_bar(stage), phase);
@@ -399,18 +1058,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
-            for (int i = row; i < 128 * 8 * DB; i += 128) {
-                const int r = i / (8 * DB), ch = i - r * (8 * DB);
-                uint4 q = make_uint4(0, 0, 0, 0);
-                if (r < rows && ch * 8 < p.D) {
-                    const int rr = t.r0 + x * 128 + r, tok = rr / p.g, hg = rr - tok * p.g;
-                    q = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)(cur.start + tok) * p.q_stride +
-                                                              (int64_t)(cur.h * p.g + hg) * p.D) + ch);
-                }
-                const uint32_t a = sq + x * G::kTileBytes + (ch >> 3) * (128 * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            load_queries<DB, 128, 128>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kTileBytes, row);
             mbar_arrive(q_ready(x));
             // ---- what the row sees; what all rows of the row tile see
             const bool live = row < rows, warp_live = wq * 32 < rows;
@@ -435,37 +1083,42 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_live) {
-                    float s[128];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(s_tm + 32 * c, s + 32 * c);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_landed32(s + 32 * c);
+                    // twice through the row's scores, 32 at a time: the maximum, then the probabilities.  Reading them again
+                    // from tensor memory costs less than the 128 registers that would hold them.
                     const int j0 = key_tile(t, begin + n) * kTcTile;
-                    if (!(j0 >= all_lo && j0 + kTcTile <= all_hi)) {
+                    const bool whole = j0 >= all_lo && j0 + kTcTile <= all_hi;
+                    auto hide = [&](float *s, int i0) {    // what the row does not see
 #pragma unroll
-                        for (int i = 0; i < 128; ++i) {
-                            const int j = j0 + i;
-                            if (!(j < hi_r && (j >= lo_r || j < sink_r))) s[i] = p.unseen;
+                        for (int i = 0; i < 32; ++i) {
+                            const int j = j0 + i0 + i;
+                            s[i] = sees(j, hi_r, lo_r, sink_r) ? s[i] : p.unseen;
                         }
-                    }
-                    float t0, t1, t2, t3;
-                    if (sc > 0.f) {
-                        t0 = s[0]; t1 = s[1]; t2 = s[2]; t3 = s[3];
+                    };
+                    float sa[32], sb[32];
+                    auto largest = [&](float *s, int i0) {
+                        tmem_landed32(s);
+                        if (!whole) hide(s, i0);
+                        float t0 = s[0] * sc, t1 = s[1] * sc;
 #pragma unroll
-                        for (int i = 4; i < 128; i += 4) {
-                            t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]);
+                        for (int i = 2; i < 32; i += 2) {
+                            t0 = fmaxf(t0, s[i] * sc);
+                            t1 = fmaxf(t1, s[i + 1] * sc);
                         }
-                        t0 = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
-                    } else {
-                        t0 = s[0]; t1 = s[1]; t2 = s[2]; t3 = s[3];
-#pragma unroll
-                        for (int i = 4; i < 128; i += 4) {
-                            t0 = fminf(t0, s[i]); t1 = fminf(t1, s[i + 1]); t2 = fminf(t2, s[i + 2]); t3 = fminf(t3, s[i + 3]);
-                        }
-                        t0 = fminf(fminf(t0, t1), fminf(t2, t3));
-                    }
-                    const float top = t0 * sc;
+                        return fmaxf(t0, t1);
+                    };
+                    tmem_ld32(s_tm, sa);
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm + 32, sb);
+                    float top = largest(sa, 0);
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm + 64, sa);
+                    top = fmaxf(top, largest(sb, 32));
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm + 96, sb);
+                    top = fmaxf(top, largest(sa, 64));
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm, sa);
+                    top = fmaxf(top, largest(sb, 96));
                     const bool grow = top > m + 8.f;
                     if (__any_sync(0xffffffffu, grow)) {
                         const float nm = grow ? top : m;
@@ -474,15 +1127,14 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                             ok = wait_pv(k - 1);
                             if (!ok) break;
                             tc_fence_after();
+#pragma unroll 1
+                            for (int f = 0; f < DB * 4; ++f) {
+                                float o[16];
+                                tmem_ld_n<16>(o_tm + 16 * f, o);
+                                uint32_t w[16];
 #pragma unroll
-                            for (int f = 0; f < DB * 2; ++f) {
-                                float o[32];
-                                tmem_ld32(o_tm + 32 * f, o);
-                                tmem_wait_ld();
-                                tmem_landed32(o);
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] *= c;
-                                tmem_st32(o_tm + 32 * f, o);
+                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * c);
+                                tmem_st16(o_tm + 16 * f, w);
                             }
                         }
                         l *= c;
@@ -490,18 +1142,30 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     }
                     const float mm = m == -INFINITY ? 0.f : m;
                     float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    auto weigh = [&](float *s, int i0) {
+                        tmem_landed32(s);
+                        if (!whole) hide(s, i0);
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float a = ex2f(fmaf(s[32 * c + 2 * i], sc, -mm)), b = ex2f(fmaf(s[32 * c + 2 * i + 1], sc, -mm));
+                            const float a = ex2f(fmaf(s[2 * i], sc, -mm)), b = ex2f(fmaf(s[2 * i + 1], sc, -mm));
                             l0 += a;
                             l1 += b;
                             w[i] = pack_bf16(a, b);
                         }
-                        tmem_st16(s_tm + 16 * c, w);
-                    }
+                        tmem_st16(s_tm + i0 / 2, w);       // (columns whose scores have been read)
+                    };
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm + 32, sb);
+                    tmem_wait_ld();                        // (before the first 16 columns of P go where sb comes from)
+                    weigh(sa, 0);
+                    tmem_ld32(s_tm + 64, sa);
+                    weigh(sb, 32);
+                    tmem_wait_ld();
+                    tmem_ld32(s_tm + 96, sb);
+                    weigh(sa, 64);
+                    tmem_wait_ld();
+                    weigh(sb, 96);
                     l += l0 + l1;
                     tmem_wait_st();
                     tc_fence_before();
@@ -516,16 +1180,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             tc_fence_after();
             if (warp_live) {
                 const Suspects &sus = suspects[unit & 1];
-                if (sus.n > 0) {
-                    bool hit = sus.n > kMaxSuspects;
-                    for (int y = 0; y < min(sus.n, kMaxSuspects); ++y)
-                        for (int w = 0; w < 4; ++w)
-                            for (uint32_t bits = sus.keys[y][w]; bits; bits &= bits - 1) {
-                                const int j = sus.base[y] + w * 32 + __ffs(bits) - 1;
-                                hit |= j < hi_r && (j >= lo_r || j < sink_r);
-                            }
-                    if (hit) l = __int_as_float(0x7FC00000);
-                }
+                if (sus.n > 0 && suspects_hit(sus, hi_r, lo_r, sink_r)) l = __int_as_float(0x7FC00000);
                 const bool whole_unit = count == t.tiles;
                 const int rr = t.r0 + x * 128 + row, tok = rr / p.g, head = cur.h * p.g + rr - tok * p.g;
                 __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
@@ -559,7 +1214,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     put_lse(m, l);
                 } else {
                     if (live) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, l));
-                    const int c0 = (int)(cur.unit / per), c1 = (int)((cur.unit + t.tiles - 1) / per);
+                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
                     int *counter = p.part.counters + (c0 * NT + x) * 4 + wq;
                     __threadfence();
                     __syncwarp();
@@ -633,12 +1288,27 @@ cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const 
     return note_err(c, e, "kv_attention_tc_kernel");
 }
 
-// Rows of a TMA box: pages of 8, 16, 32 or 64 rows whole, larger ones in 128-row parts; 0: other sizes.
+template <int DB, int NR>
+cudaError_t few_prepare()
+{
+    return cudaFuncSetAttribute(kv_attention_few_kernel<DB, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<DB, NR>::kSmem);
+}
+template <int DB, int NR>
+cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
+{
+    const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
+    cudaError_t e = launch_k(kv_attention_few_kernel<DB, NR>, dim3(sms), dim3(FewGeo<DB, NR>::kThreads), FewGeo<DB, NR>::kSmem, st,
+                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
+    c->launches = 1;
+    return note_err(c, e, "kv_attention_few_kernel");
+}
+
+// Rows of a TMA box: the largest power of two, 8 to 128, that divides a page (a box is whole groups of 8 swizzled rows and
+// never crosses a page); 0: none does.
 int tc_box_rows(int page_size)
 {
-    if (page_size % kTcTile == 0) return kTcTile;
-    for (int r = 8; r < kTcTile; r *= 2)
-        if (page_size == r) return r;
+    for (int r = kTcTile; r >= 8; r /= 2)
+        if (page_size % r == 0) return r;
     return 0;
 }
 
@@ -675,7 +1345,9 @@ cudaError_t kv_tc_attach(Ctx *c)
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
     if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
-    if ((e = tc_prepare<1, 1>()) != cudaSuccess || (e = tc_prepare<1, 2>()) != cudaSuccess || (e = tc_prepare<2, 1>()) != cudaSuccess ||
+    if ((e = few_prepare<1, 16>()) != cudaSuccess || (e = few_prepare<1, 32>()) != cudaSuccess || (e = few_prepare<1, 64>()) != cudaSuccess ||
+        (e = few_prepare<2, 16>()) != cudaSuccess || (e = few_prepare<2, 32>()) != cudaSuccess || (e = few_prepare<2, 64>()) != cudaSuccess ||
+        (e = tc_prepare<1, 1>()) != cudaSuccess || (e = tc_prepare<1, 2>()) != cudaSuccess || (e = tc_prepare<2, 1>()) != cudaSuccess ||
         (e = tc_prepare<2, 2>()) != cudaSuccess)
         return e;
     c->kv_encode = fn;
@@ -691,7 +1363,11 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaSt
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
-    const bool two = (long long)max_new * p.g > 128;
+    const long long rows = (long long)max_new * p.g;
+    const bool one_block = c->kv.head_dim <= 64, two = rows > 128;
+    if (rows <= 16) return one_block ? few_launch<1, 16>(c, p, km, vm, box, st) : few_launch<2, 16>(c, p, km, vm, box, st);
+    if (rows <= 32) return one_block ? few_launch<1, 32>(c, p, km, vm, box, st) : few_launch<2, 32>(c, p, km, vm, box, st);
+    if (rows <= 64) return one_block ? few_launch<1, 64>(c, p, km, vm, box, st) : few_launch<2, 64>(c, p, km, vm, box, st);
     if (c->kv.head_dim <= 64) return two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
     return two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
 }

@@ -75,7 +75,7 @@ __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seq
 }
 
 template <typename T, int GL, int U>
-__global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const __grid_constant__ RowsParams p)
+__global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_constant__ RowsParams p)
 {
     const int tid = threadIdx.x, lane = tid & 31;
     const int gw = blockIdx.x * kRowWarps + (tid >> 5);
