@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                     }
                 }
             }
-            // what a row does not see scores -inf in units of log2 (the scale may be negative)
+            // what a row does not see scores -inf
             const bool whole = j0 >= all_lo && j0 + kWarpKeys <= all_hi;
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                 for (int y = 0; y < 4; ++y) {
                     if (!whole) {
                         const int j = j0 + x * 8 + 2 * tig + (y & 1);
-                        s[x][y] = sees(j, hi2[y >> 1], lo2[y >> 1], p.sinks) ? s[x][y] : p.unseen;
+                        s[x][y] = sees(j, hi2[y >> 1], lo2[y >> 1], p.sinks) ? s[x][y] : -INFINITY;
                     }
                     top[y >> 1] = fmaxf(top[y >> 1], s[x][y] * p.scale_log2);
                 }
@@ -619,8 +619,7 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
         const int DP = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
         p.plain_rows = kv.page_size % kWarpKeys == 0 && kv.head_dim == DP;
     }
-    p.unseen = p.scale_log2 > 0.f ? -INFINITY : INFINITY;
-    if (c->kv_encode) return launch_paged_attention_tc(c, p, batch.max_new, st);
+        if (c->kv_encode) return launch_paged_attention_tc(c, p, batch.max_new, st);
     const size_t slots = (size_t)4 * kKvMaxSm;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);

@@ -85,7 +85,7 @@ struct AttnParams {
     int H, Hk, g, D;
     FastDiv gdiv;              // g
     int mask, window, sinks, plain_rows;
-    float scale_log2, unseen;  // unseen: the raw score that scales to -inf
+    float scale_log2;          // > 0
     KvPartials part;
 };
 

@@ -40,7 +40,7 @@ template <int DB, int NT> struct TcGeo {   // DB: 64-feature blocks of a head
     static constexpr int kRing = kStages * kTileBytes;
     static constexpr int kBars = kQ + kRing;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
-    static constexpr int kThreads = 128 + NT * 128;
+    static constexpr int kThreads = 64 + NT * 128;
     static constexpr int kRows = NT * 128;
 };
 
@@ -175,6 +175,24 @@ template <int W, bool MAX> __device__ __forceinline__ float reduce_rows(float (&
 #pragma unroll
     for (int h = W; h < 32; h <<= 1) r = op(r, __shfl_xor_sync(0xffffffffu, r, h));
     return r;
+}
+
+// Two fp32 operations in one instruction: (a, b) * s + c, (a, b) + (c, d)
+__device__ __forceinline__ void fma2(float &a, float &b, float s, float c)
+{
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(s), "f"(c));
+}
+__device__ __forceinline__ void add2(float &a, float &b, float c, float d)
+{
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+// bits lo..hi-1 of 32
+__device__ __forceinline__ uint32_t bit_range(int lo, int hi)
+{
+    const uint32_t h = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u, l = lo >= 32 ? ~0u : lo <= 0 ? 0u : (1u << lo) - 1u;
+    return h & ~l;
 }
 
 // V^T as the A operand / P as the B operand: rows (keys) of 128 bytes, MN-major; `block` bytes to the next 64 features
@@ -619,7 +637,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     if (!whole) {
                         const uint32_t mine = (uint32_t)(seen >> r0);
 #pragma unroll
-                        for (int i = 0; i < W; ++i) s[i] = (mine >> i) & 1u ? s[i] : p.unseen;
+                        for (int i = 0; i < W; ++i) s[i] = (mine >> i) & 1u ? s[i] : -INFINITY;
                     }
                 };
                 auto against_max = [&](int r0) {           // exponents
@@ -1038,9 +1056,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             ++unit;
             next_unit(count);
         }
-    } else if (warp >= 4) {
+    } else {
         // ================================ softmax: a thread per row ================================
-        const int x = (warp - 4) >> 2, wq = warp & 3;      // row tile, lane quarter of tensor memory
+        const int x = (warp - 2) >> 2, wq = warp & 3;      // row tile, lane quarter of tensor memory
         const int row = wq * 32 + lane;                    // of the row tile
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
         const uint32_t o_tm = tmem + 256 + x * 128 + lanes;
@@ -1088,37 +1106,35 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     const int j0 = key_tile(t, begin + n) * kTcTile;
                     const bool whole = j0 >= all_lo && j0 + kTcTile <= all_hi;
                     auto hide = [&](float *s, int i0) {    // what the row does not see
+                        const int j = j0 + i0;
+                        const uint32_t seen = bit_range(lo_r - j, hi_r - j) | bit_range(0, min(sink_r, hi_r) - j);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const int j = j0 + i0 + i;
-                            s[i] = sees(j, hi_r, lo_r, sink_r) ? s[i] : p.unseen;
-                        }
+                        for (int i = 0; i < 32; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
                     };
-                    float sa[32], sb[32];
+                    float sa[32], sb[32], t0 = -INFINITY, t1 = -INFINITY;
                     auto largest = [&](float *s, int i0) {
                         tmem_landed32(s);
                         if (!whole) hide(s, i0);
-                        float t0 = s[0] * sc, t1 = s[1] * sc;
 #pragma unroll
-                        for (int i = 2; i < 32; i += 2) {
-                            t0 = fmaxf(t0, s[i] * sc);
-                            t1 = fmaxf(t1, s[i + 1] * sc);
+                        for (int i = 0; i < 32; i += 4) {
+                            t0 = fmaxf(fmaxf(t0, s[i]), s[i + 1]);
+                            t1 = fmaxf(fmaxf(t1, s[i + 2]), s[i + 3]);
                         }
-                        return fmaxf(t0, t1);
                     };
                     tmem_ld32(s_tm, sa);
                     tmem_wait_ld();
                     tmem_ld32(s_tm + 32, sb);
-                    float top = largest(sa, 0);
+                    largest(sa, 0);
                     tmem_wait_ld();
                     tmem_ld32(s_tm + 64, sa);
-                    top = fmaxf(top, largest(sb, 32));
+                    largest(sb, 32);
                     tmem_wait_ld();
                     tmem_ld32(s_tm + 96, sb);
-                    top = fmaxf(top, largest(sa, 64));
+                    largest(sa, 64);
                     tmem_wait_ld();
                     tmem_ld32(s_tm, sa);
-                    top = fmaxf(top, largest(sb, 96));
+                    largest(sb, 96);
+                    const float top = fmaxf(t0, t1) * sc;
                     const bool grow = top > m + 8.f;
                     if (__any_sync(0xffffffffu, grow)) {
                         const float nm = grow ? top : m;
@@ -1148,9 +1164,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float a = ex2f(fmaf(s[2 * i], sc, -mm)), b = ex2f(fmaf(s[2 * i + 1], sc, -mm));
-                            l0 += a;
-                            l1 += b;
+                            fma2(s[2 * i], s[2 * i + 1], sc, -mm);
+                            const float a = ex2f(s[2 * i]), b = ex2f(s[2 * i + 1]);
+                            add2(l0, l1, a, b);
                             w[i] = pack_bf16(a, b);
                         }
                         tmem_st16(s_tm + i0 / 2, w);       // (columns whose scores have been read)

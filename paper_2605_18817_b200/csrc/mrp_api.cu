@@ -573,7 +573,7 @@ int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_modul
     if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
     const int bad = kv_batch_status(c, batch);
     if (bad) return bad;
-    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !isfinite(args->scale))
+    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !(args->scale >= 0.f) || !isfinite(args->scale))
         return MRP_ERR_INVALID_ARG;
     c.launches = 0;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
