@@ -35,12 +35,12 @@ struct WaitStatus {
 
 template <int DB, int NT> struct TcGeo {   // DB: 64-feature blocks of a head
     static constexpr int kTileBytes = DB * 128 * 128;
-    static constexpr int kStages = DB == 2 ? (NT == 2 ? 5 : 6) : 10;
+    static constexpr int kStages = DB == 2 ? (NT == 2 ? 4 : 5) : 10;
     static constexpr int kQ = NT * kTileBytes;
     static constexpr int kRing = kStages * kTileBytes;
     static constexpr int kBars = kQ + kRing;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
-    static constexpr int kThreads = 64 + NT * 128;
+    static constexpr int kThreads = 64 + NT * 256;
     static constexpr int kRows = NT * 128;
 };
 
@@ -871,6 +871,8 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     extern __shared__ unsigned char smem_raw[];
     __shared__ long long sh_find[G::kThreads / 32 + 2];
     __shared__ Suspects suspects[2];
+    __shared__ float sh_top[2][NT][2][128], sh_sum[NT][2][128];    // what the halves of a row tell each other
+    __shared__ int sh_last[NT][4];
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -883,8 +885,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     auto p_ready = [&](int x) { return bars + 8 * (34 + x); };
     auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
     auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
+    auto p_half = [&](int x) { return bars + 8 * (40 + x); };
     unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 40);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 42);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     const WaitStatus ws = {p.b.status, p.b.user_status};
 
@@ -896,8 +899,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
             mbar_init(p_ready(x), 4);
+            mbar_init(p_half(x), 4);
             mbar_init(pv_done(x), 1);
-            mbar_init(q_ready(x), 128);
+            mbar_init(q_ready(x), 256);
         }
         *abort_flag = 0;
         prefetch_tmap(&kmap);
@@ -973,12 +977,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             }
             __syncwarp();
         };
-        auto mma_o = [&](int x, int row_tile, uint32_t vs, bool first) {   // O_row_tile += P_x V
+        auto mma_o = [&](int x, int row_tile, uint32_t vs, int c0, bool first) {     // O_row_tile += P_x V, keys 16 c0 .. 16 c0 + 63
             if (elect_one()) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c * 8, mn_desc(vs + c * 2048, 128 * 128), idesc_o, !first || c > 0);
-                umma_commit(pv_done(x));
+                for (int c = 0; c < 4; ++c)
+                    umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2048, 128 * 128), idesc_o, !first || c0 + c > 0);
+                if (c0 == 4) umma_commit(pv_done(x));
             }
             __syncwarp();
         };
@@ -1015,22 +1019,21 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     const int sk = stage;
                     const uint32_t pk = phase;
                     if (n + 1 < count) step();
+                    wait(full_bar(sv), pv);
+                    if (!ok) break;
+                    clean(n, ring + sv * G::kTileBytes);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        wait(p_ready(x), k & 1u);
-                        if (x == 0) {
-                            wait(full_bar(sv), pv);
-                            if (!ok) break;
-                            clean(n, ring + sv * G::kTileBytes);
-                        }
+                        wait(p_half(x), k & 1u);
                         if (!ok) break;
                         tc_fence_after();
-                        mma_o(x, x, ring + sv * G::kTileBytes, n == 0);
-                        if (n + 1 < count) {
-                            if (x == 0) wait(full_bar(sk), pk);
-                            if (!ok) break;
-                            mma_s(x, x, ring + sk * G::kTileBytes);
-                        }
+                        mma_o(x, x, ring + sv * G::kTileBytes, 0, n == 0);
+                        wait(p_ready(x), k & 1u);
+                        if (n + 1 < count && x == 0) wait(full_bar(sk), pk);
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_o(x, x, ring + sv * G::kTileBytes, 4, n == 0);
+                        if (n + 1 < count) mma_s(x, x, ring + sk * G::kTileBytes);
                     }
                     if (!ok) break;
                     release(sv);
@@ -1043,12 +1046,17 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                         release(stage);
                         step();
                     }
-                    wait(p_ready(k & 1u), (k >> 1) & 1u);
                     wait(full_bar(stage), phase);
                     if (!ok) break;
                     clean(n, ring + stage * G::kTileBytes);
+                    wait(p_half(k & 1u), (k >> 1) & 1u);
+                    if (!ok) break;
                     tc_fence_after();
-                    mma_o(k & 1u, 0, ring + stage * G::kTileBytes, n == 0);
+                    mma_o(k & 1u, 0, ring + stage * G::kTileBytes, 0, n == 0);
+                    wait(p_ready(k & 1u), (k >> 1) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_o(k & 1u, 0, ring + stage * G::kTileBytes, 4, n == 0);
                     release(stage);
                     step();
                 }
@@ -1057,94 +1065,90 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             next_unit(count);
         }
     } else {
-        // ================================ softmax: a thread per row ================================
-        const int x = (warp - 2) >> 2, wq = warp & 3;      // row tile, lane quarter of tensor memory
-        const int row = wq * 32 + lane;                    // of the row tile
+        // ================================ softmax: two threads per row ================================
+        const int group = (warp - 2) >> 2, x = group >> 1, half = group & 1;       // row tile, half of its keys
+        const int wq = warp & 3, row = wq * 32 + lane;     // lane quarter of tensor memory, row of the row tile
+        const int pair = 1 + x * 4 + wq;                   // barrier of the two warps that share 32 rows
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t o_tm = tmem + 256 + x * 128 + lanes;
+        const uint32_t o_tm = tmem + 256 + x * 128 + half * (DB * 32) + lanes;
         uint32_t k = 0, unit = 0;
         bool ok = true;
         const float sc = p.scale_log2;
         // P V of tile kk done.  A barrier may be one phase behind what is waited for, not two: with two S buffers the
         // softmax can finish a tile while the product before the last still runs, so each buffer has its own.
         auto wait_pv = [&](uint32_t kk) {
-            const bool r = NT == 2 ? mbar_wait(pv_done(x), kk & 1u, abort_flag, ws) : mbar_wait(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
-            return __all_sync(0xffffffffu, r) != 0;
+            return NT == 2 ? mbar_wait(pv_done(x), kk & 1u, abort_flag, ws) : mbar_wait(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
         };
-        while (ok && at < piece_end) {
+        while (at < piece_end) {
             const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
-            load_queries<DB, 128, 128>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kTileBytes, row);
+            load_queries<DB, 128, 256>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kTileBytes, half * 128 + row);
             mbar_arrive(q_ready(x));
-            // ---- what the row sees; what all rows of the row tile see
+            // ---- what the row sees; what all rows of the warp see
             const bool live = row < rows, warp_live = wq * 32 < rows;
-            int hi_r = 0, lo_r = 0, sink_r = 0;
+            int hi_r = 0, lo_r = 0;
             if (live) {
-                const int pos = cur.pre + (t.r0 + x * 128 + row) / p.g;
+                const int pos = cur.pre + fast_div(t.r0 + x * 128 + row, p.gdiv);
                 hi_r = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
                 lo_r = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
-                sink_r = p.sinks;
             }
             int all_hi = 0, all_lo = 0;
             if (warp_live) {
                 const int a = t.r0 + x * 128 + wq * 32, b = t.r0 + x * 128 + min(rows, wq * 32 + 32) - 1;
-                all_hi = p.mask == MRP_ATTN_CAUSAL ? cur.pre + a / p.g + 1 : t.hi;
-                all_lo = p.window > 0 ? max(0, cur.pre + b / p.g + 1 - p.window) : 0;
+                all_hi = p.mask == MRP_ATTN_CAUSAL ? cur.pre + fast_div(a, p.gdiv) + 1 : t.hi;
+                all_lo = p.window > 0 ? max(0, cur.pre + fast_div(b, p.gdiv) + 1 - p.window) : 0;
             }
             float m = -INFINITY, l = 0.f;
             for (int n = 0; n < count; ++n, ++k) {
                 const int buf = NT == 2 ? x : (int)(k & 1u);
-                const uint32_t s_tm = tmem + buf * 128 + lanes;
-                ok = __all_sync(0xffffffffu, mbar_wait(s_full(buf), NT == 2 ? k & 1u : (k >> 1) & 1u, abort_flag, ws));
-                if (!ok) break;
+                const uint32_t s_tm = tmem + buf * 128 + half * 64 + lanes;        // this half's scores, then its P
+                ok = mbar_wait(s_full(buf), NT == 2 ? k & 1u : (k >> 1) & 1u, abort_flag, ws);
+                __syncwarp();
                 tc_fence_after();
-                if (warp_live) {
-                    // twice through the row's scores, 32 at a time: the maximum, then the probabilities.  Reading them again
-                    // from tensor memory costs less than the 128 registers that would hold them.
-                    const int j0 = key_tile(t, begin + n) * kTcTile;
-                    const bool whole = j0 >= all_lo && j0 + kTcTile <= all_hi;
+                if (!warp_live) {
+                    if (any_of(pair, 64, !ok)) { ok = false; break; }
+                } else {
+                    // twice through the half row's scores, 32 at a time: the maximum, then the probabilities
+                    const int j0 = key_tile(t, begin + n) * kTcTile + half * 64;
+                    const bool whole = j0 >= all_lo && j0 + 64 <= all_hi;
                     auto hide = [&](float *s, int i0) {    // what the row does not see
                         const int j = j0 + i0;
-                        const uint32_t seen = bit_range(lo_r - j, hi_r - j) | bit_range(0, min(sink_r, hi_r) - j);
+                        const uint32_t seen = bit_range(lo_r - j, hi_r - j) | bit_range(0, min(p.sinks, hi_r) - j);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
                     };
-                    float sa[32], sb[32], t0 = -INFINITY, t1 = -INFINITY;
-                    auto largest = [&](float *s, int i0) {
+                    float s[32], t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_ld32(s_tm + 32 * c, s);
+                        tmem_wait_ld();
                         tmem_landed32(s);
-                        if (!whole) hide(s, i0);
+                        if (!whole) hide(s, 32 * c);
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) {
                             t0 = fmaxf(fmaxf(t0, s[i]), s[i + 1]);
                             t1 = fmaxf(fmaxf(t1, s[i + 2]), s[i + 3]);
                         }
-                    };
-                    tmem_ld32(s_tm, sa);
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm + 32, sb);
-                    largest(sa, 0);
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm + 64, sa);
-                    largest(sb, 32);
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm + 96, sb);
-                    largest(sa, 64);
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm, sa);
-                    largest(sb, 96);
-                    const float top = fmaxf(t0, t1) * sc;
+                    }
+                    t0 = fmaxf(t0, t1) * sc;
+                    sh_top[k & 1u][x][half][row] = t0;
+                    tmem_ld32(s_tm, s);                    // (on its way while the halves meet)
+                    if (any_of(pair, 64, !ok)) { ok = false; break; }
+                    const float top = fmaxf(t0, sh_top[k & 1u][x][half ^ 1][row]);
                     const bool grow = top > m + 8.f;
-                    if (__any_sync(0xffffffffu, grow)) {
+                    tmem_wait_ld();
+                    tmem_landed32(s);
+                    if (__any_sync(0xffffffffu, grow)) {   // (the same in both warps)
                         const float nm = grow ? top : m;
                         const float c = m == nm ? 1.f : ex2f(m - nm);
-                        if (n > 0) {                       // the accumulator of the tiles so far
+                        if (n > 0) {                       // the accumulator of the tiles so far, half its columns each
                             ok = wait_pv(k - 1);
-                            if (!ok) break;
+                            if (any_of(pair, 64, !ok)) { ok = false; break; }
                             tc_fence_after();
 #pragma unroll 1
-                            for (int f = 0; f < DB * 4; ++f) {
+                            for (int f = 0; f < DB * 2; ++f) {
                                 float o[16];
                                 tmem_ld_n<16>(o_tm + 16 * f, o);
                                 uint32_t w[16];
@@ -1158,9 +1162,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     }
                     const float mm = m == -INFINITY ? 0.f : m;
                     float l0 = 0.f, l1 = 0.f;
-                    auto weigh = [&](float *s, int i0) {
-                        tmem_landed32(s);
-                        if (!whole) hide(s, i0);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (!whole) hide(s, 32 * c);
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -1169,107 +1173,102 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                             add2(l0, l1, a, b);
                             w[i] = pack_bf16(a, b);
                         }
-                        tmem_st16(s_tm + i0 / 2, w);       // (columns whose scores have been read)
-                    };
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm + 32, sb);
-                    tmem_wait_ld();                        // (before the first 16 columns of P go where sb comes from)
-                    weigh(sa, 0);
-                    tmem_ld32(s_tm + 64, sa);
-                    weigh(sb, 32);
-                    tmem_wait_ld();
-                    tmem_ld32(s_tm + 96, sb);
-                    weigh(sa, 64);
-                    tmem_wait_ld();
-                    weigh(sb, 96);
+                        if (c == 0) {                      // (the second 32 scores lie above the columns P goes to)
+                            tmem_ld32(s_tm + 32, s);
+                            tmem_st16(s_tm, w);
+                            tmem_wait_ld();
+                            tmem_landed32(s);
+                        } else {
+                            tmem_st16(s_tm + 16, w);
+                        }
+                    }
                     l += l0 + l1;
                     tmem_wait_st();
                     tc_fence_before();
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready(buf));
+                if (lane == 0) mbar_arrive(half ? p_ready(buf) : p_half(buf));
             }
             if (!ok) break;
             // ---- the unit's end (or this piece's)
+            sh_sum[x][half][row] = l;
             ok = wait_pv(k - 1);
-            if (!ok) break;
+            __syncwarp();
+            if (any_of(pair, 64, !ok)) break;
             tc_fence_after();
             if (warp_live) {
+                float L = l + sh_sum[x][half ^ 1][row];
                 const Suspects &sus = suspects[unit & 1];
-                if (sus.n > 0 && suspects_hit(sus, hi_r, lo_r, sink_r)) l = __int_as_float(0x7FC00000);
+                if (sus.n > 0 && suspects_hit(sus, hi_r, lo_r, p.sinks)) L = __int_as_float(0x7FC00000);
                 const bool whole_unit = count == t.tiles;
-                const int rr = t.r0 + x * 128 + row, tok = rr / p.g, head = cur.h * p.g + rr - tok * p.g;
-                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
-                float *lse = p.lse ? p.lse + (int64_t)(cur.start + tok) * p.H + head : nullptr;
-                auto put = [&](int f0, const float *o, float inv) {        // 8 features from f0
-                    if (live && f0 < p.D)
-                        *reinterpret_cast<uint4 *>(dst + f0) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
-                                                                          pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
+                const int rr = t.r0 + x * 128 + row, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
+                const int f0 = half * (DB * 32);           // this half's features
+                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D + f0;
+                float *lse = p.lse && live && half == 0 ? p.lse + (int64_t)(cur.start + tok) * p.H + head : nullptr;
+                auto put32 = [&](int f, const float *o, float inv) {       // 32 features from f0 + f
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8)
+                        if (live && f0 + f + i < p.D)
+                            *reinterpret_cast<uint4 *>(dst + f + i) =
+                                make_uint4(pack_bf16(o[i] * inv, o[i + 1] * inv), pack_bf16(o[i + 2] * inv, o[i + 3] * inv),
+                                           pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
                 };
-                auto inverse = [](float L) { return L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L); };       // (NaN goes through)
-                auto put_lse = [&](float M, float L) { if (live && lse) *lse = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f; };
                 const int slot = (2 * (int)blockIdx.x + (begin == 0 ? 1 : 0)) * NT + x;
                 float4 *part = reinterpret_cast<float4 *>(p.part.o);       // slot: [DB * 16][128 rows] float4
-                const float inv = inverse(l);
-#pragma unroll
-                for (int f = 0; f < DB * 2; ++f) {
+                if (whole_unit && lse) *lse = log_sum(m, L);
+                if (!whole_unit && live && half == 0) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, L));
+                const float inv = inverse(L);
+#pragma unroll 1
+                for (int f = 0; f < DB; ++f) {
                     float o[32];
                     tmem_ld32(o_tm + 32 * f, o);
                     tmem_wait_ld();
                     tmem_landed32(o);
                     if (whole_unit) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) put(32 * f + i, o + i, inv);
+                        put32(32 * f, o, inv);
                     } else if (live) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(part + ((size_t)slot * (DB * 16) + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
-                    }
-                }
-                if (whole_unit) {
-                    put_lse(m, l);
-                } else {
-                    if (live) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, l));
-                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
-                    int *counter = p.part.counters + (c0 * NT + x) * 4 + wq;
-                    __threadfence();
-                    __syncwarp();
-                    int last = 0;
-                    if (lane == 0) last = atomicAdd(counter, 1) == c1 - c0;
-                    last = __shfl_sync(0xffffffffu, last, 0);
-                    if (last) {
-                        __threadfence();
-                        auto slot_of = [&](int c) { return (size_t)((2 * c + (c == c0)) * NT + x); };
-                        float M = -INFINITY, L = 0.f;
-                        if (live) {
-                            for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(p.part.ml + slot_of(c) * 128 + row).x);
-                            for (int c = c0; c <= c1; ++c) {
-                                const float2 ml = __ldcg(p.part.ml + slot_of(c) * 128 + row);
-                                if (ml.x == -INFINITY && ml.y == 0.f) continue;
-                                L = fmaf(ml.x == -INFINITY ? 0.f : ex2f(ml.x - M), ml.y, L);
-                            }
-                            const float iv = inverse(L);
-#pragma unroll 1
-                            for (int f = 0; f < DB * 8 && f * 8 < p.D; ++f) {
-                                float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-                                for (int c = c0; c <= c1; ++c) {
-                                    const float2 ml = __ldcg(p.part.ml + slot_of(c) * 128 + row);
-                                    const float4 a = __ldcg(part + (slot_of(c) * (DB * 16) + 2 * f) * 128 + row);
-                                    const float4 b = __ldcg(part + (slot_of(c) * (DB * 16) + 2 * f + 1) * 128 + row);
-                                    const float w = ml.x == -INFINITY ? 0.f : ex2f(ml.x - M);
-                                    if (ml.x == -INFINITY && ml.y == 0.f) continue;
-                                    o[0] = fmaf(w, a.x, o[0]); o[1] = fmaf(w, a.y, o[1]); o[2] = fmaf(w, a.z, o[2]); o[3] = fmaf(w, a.w, o[3]);
-                                    o[4] = fmaf(w, b.x, o[4]); o[5] = fmaf(w, b.y, o[5]); o[6] = fmaf(w, b.z, o[6]); o[7] = fmaf(w, b.w, o[7]);
-                                }
-                                put(8 * f, o, iv);
-                            }
-                            put_lse(M, L);
-                        }
-                        if (lane == 0) *counter = 0;
+                            __stcg(part + ((size_t)slot * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
                     }
                 }
                 tc_fence_before();
+                if (!whole_unit) {
+                    // ---- the pieces of these 32 rows meet: the pair that arrives last joins them in order
+                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
+                    int *counter = p.part.counters + (c0 * NT + x) * 4 + wq;
+                    any_of(pair, 64, false);
+                    if (half == 0 && lane == 0) sh_last[x][wq] = arrive_acq_rel(counter) == c1 - c0;
+                    any_of(pair, 64, false);
+                    if (sh_last[x][wq] && live) {
+                        auto slot_of = [&](int c) { return (size_t)((2 * c + (c == c0)) * NT + x); };
+#pragma unroll 1
+                        for (int f = 0; f < DB; ++f) {
+                            float M = -INFINITY, S = 0.f, o[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+#pragma unroll 1
+                            for (int c = c0; c <= c1; ++c) {
+                                const float2 ml = __ldcg(p.part.ml + slot_of(c) * 128 + row);
+                                float4 a[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) a[i] = __ldcg(part + (slot_of(c) * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
+                                const float nm = fmaxf(M, ml.x);
+                                const float e = M == nm ? 1.f : ex2f(M - nm), w = ml.x == nm ? 1.f : ex2f(ml.x - nm);
+                                M = nm;
+                                S = fmaf(w, ml.y, S * e);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    o[4 * i] = fmaf(w, a[i].x, o[4 * i] * e); o[4 * i + 1] = fmaf(w, a[i].y, o[4 * i + 1] * e);
+                                    o[4 * i + 2] = fmaf(w, a[i].z, o[4 * i + 2] * e); o[4 * i + 3] = fmaf(w, a[i].w, o[4 * i + 3] * e);
+                                }
+                            }
+                            put32(32 * f, o, inverse(S));
+                            if (f == 0 && lse) *lse = log_sum(M, S);
+                        }
+                    }
+                    if (half == 0 && lane == 0 && sh_last[x][wq]) *counter = 0;
+                }
             }
             ++unit;
             next_unit(count);
