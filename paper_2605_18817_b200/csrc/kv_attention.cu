@@ -613,6 +613,7 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
     p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
     p.gdiv = make_fastdiv(p.g);
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
+    p.min_piece = 1;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
     {
         // a warp's 16 keys lie one after the other in one page, in rows as wide as the kernel's stages

@@ -85,6 +85,7 @@ struct AttnParams {
     int H, Hk, g, D;
     FastDiv gdiv;              // g
     int mask, window, sinks, plain_rows;
+    int min_piece;             // tiles a CTA takes at least
     float scale_log2;          // > 0
     KvPartials part;
 };
@@ -196,7 +197,7 @@ __device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) total += sh_warp[w];
     }
-    per = div_line(total + gridDim.x - 1, gridDim.x);
+    per = max(div_line(total + gridDim.x - 1, gridDim.x), (long long)p.min_piece);
     const long long begin = per * blockIdx.x, end = min(total, begin + per);
     if (begin >= end) return 0;
     long long done = 0;
@@ -265,7 +266,7 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
-    per = div_line(total + gridDim.x - 1, gridDim.x);
+    per = max(div_line(total + gridDim.x - 1, gridDim.x), (long long)p.min_piece);
     const long long begin = per * blockIdx.x, end = min(total, begin + per);
     if (begin >= end) return 0;
     long long done = 0;

@@ -120,17 +120,18 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // The maximum in use is common to a warpgroup's 128 keys, so a tile needs to know only whether some score exceeds it by
 // more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
 // rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it.
-template <int DB, int NR> struct FewGeo {
-    static constexpr bool kHiLo = NR <= 32;
-    static constexpr int kCols = kHiLo ? 2 * NR : NR;      // columns of P and of an accumulator
+constexpr int kFewRows = 16;
+template <int DB> struct FewGeo {
+    static constexpr int NR = kFewRows;
+    static constexpr int kCols = 2 * NR;                   // columns of P and of an accumulator: hi, lo
     static constexpr int kTileBytes = DB * 128 * 128;
-    static constexpr int kStages = (DB == 2 ? 1 : 2) * (NR <= 32 ? 5 : 4);
+    static constexpr int kStages = DB == 2 ? 5 : 10;
     static constexpr int kRing = kStages * kTileBytes;
     static constexpr int kP = 128 * 128;                   // P of a warpgroup: 128 keys, rows of 128 bytes
     static constexpr int kQ = DB * NR * 128;               // queries of a unit, two of them
     static constexpr int kPAt = kRing, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;
-    static constexpr int kTmem = 2 * NR + 2 * kCols <= 128 ? 128 : 256;
+    static constexpr int kTmem = 128;                      // of which 2 NR + 2 kCols are used
     static constexpr int kThreads = 384;
 };
 constexpr float kNone = -3.4028234e38f;    // the maximum of a row that has seen nothing
@@ -413,12 +414,13 @@ __device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
     }
 }
 
-template <int DB, int NR>
+template <int DB>
 __global__ void __launch_bounds__(384, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, int box_rows)
 {
-    typedef FewGeo<DB, NR> G;
+    typedef FewGeo<DB> G;
+    constexpr int NR = kFewRows;
     typedef RowTile<NR, kTcTile> Tile;
     extern __shared__ unsigned char smem_raw[];
     __shared__ long long sh_find[G::kThreads / 32 + 2];
@@ -621,57 +623,49 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 tc_fence_after();
                 const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + wt;
                 const bool whole = j0 >= all.all_lo && j0 + kTcTile <= all.all_hi;
-                uint64_t seen = 0;                         // by which rows, where not by all
+                uint32_t seen = 0;                         // by which rows, where not by all
                 if (!whole) {
                     if (all.differ) {
 #pragma unroll 1
-                        for (int r = 0; r < NR; ++r) seen |= (uint64_t)sees(j, sh_hi[u][r], sh_lo[u][r], p.sinks) << r;
+                        for (int r = 0; r < NR; ++r) seen |= (uint32_t)sees(j, sh_hi[u][r], sh_lo[u][r], p.sinks) << r;
                     } else {
-                        seen = sees(j, all.all_hi, all.all_lo, p.sinks) ? ~0ull : 0ull;
+                        seen = sees(j, all.all_hi, all.all_lo, p.sinks) ? ~0u : 0u;
                     }
                 }
-                constexpr int W = NR < 32 ? NR : 32;       // rows at a time; up to 32 rows stay in registers
-                float s[W];
-                auto load = [&](int r0) {                  // the key's scores of rows r0..; what a row does not see: -inf once scaled
-                    tmem_ld_n<W>(s_tm + r0, s);
+                float s[NR];
+                auto load = [&]() {                        // the key's scores; what a row does not see: -inf
+                    tmem_ld_n<NR>(s_tm, s);
                     if (!whole) {
-                        const uint32_t mine = (uint32_t)(seen >> r0);
 #pragma unroll
-                        for (int i = 0; i < W; ++i) s[i] = (mine >> i) & 1u ? s[i] : -INFINITY;
+                        for (int i = 0; i < NR; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
                     }
                 };
-                auto against_max = [&](int r0) {           // exponents
+                auto against_max = [&]() {                 // exponents
 #pragma unroll
-                    for (int i = 0; i < W; i += 4) {
-                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[x][r0 + i]);
+                    for (int i = 0; i < NR; i += 4) {
+                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[x][i]);
                         s[i] = fmaf(s[i], sc, -m.x); s[i + 1] = fmaf(s[i + 1], sc, -m.y);
                         s[i + 2] = fmaf(s[i + 2], sc, -m.z); s[i + 3] = fmaf(s[i + 3], sc, -m.w);
                     }
                 };
                 bool grown = true;                         // (the warpgroup's first tile of the unit sets the maxima)
                 if (n >= 2) {
-                    bool more = false;
-#pragma unroll 1
-                    for (int r0 = 0; r0 < NR; r0 += W) {
-                        load(r0);
-                        against_max(r0);
-                        float top = s[0];
+                    load();
+                    against_max();
+                    float top = s[0];
 #pragma unroll
-                        for (int i = 1; i < W; ++i) top = fmaxf(top, s[i]);
-                        more |= top > 8.f;
-                    }
-                    grown = wg_any(bar_id, more || !ok);
+                    for (int i = 1; i < NR; ++i) top = fmaxf(top, s[i]);
+                    grown = wg_any(bar_id, top > 8.f || !ok);
                 }
                 if (grown) {
                     // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
                     if (wg_any(bar_id, !ok)) { ok = false; break; }
-#pragma unroll 1
-                    for (int r0 = 0; r0 < NR; r0 += W) {
-                        load(r0);
+                    load();
 #pragma unroll
-                        for (int i = 0; i < W; ++i) s[i] *= sc;
-                        const float top = reduce_rows<W, true>(s, lane);
-                        if (lane < W) sh_wm[x][wq][r0 + lane] = top;
+                    for (int i = 0; i < NR; ++i) s[i] *= sc;
+                    {
+                        const float top = reduce_rows<NR, true>(s, lane);
+                        if (lane < NR) sh_wm[x][wq][lane] = top;
                     }
                     wg_sync(bar_id);
                     if (wt < NR) {
@@ -701,28 +695,23 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     }
                 }
                 // ---- probabilities of the key -> its row of P
+                if (grown) {
+                    load();
+                    against_max();
+                }
 #pragma unroll
-                for (int r0 = 0; r0 < NR; r0 += W) {
-                    if (NR > W || grown) {
-                        load(r0);
-                        against_max(r0);
+                for (int c = 0; c < NR / 8; ++c) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 8 * c + 2 * i;
+                        const float a = ex2f(s[r]), b = ex2f(s[r + 1]);
+                        l[r] += a;
+                        l[r + 1] += b;
+                        split_bf16(a, b, hi[i], lo[i]);
                     }
-#pragma unroll
-                    for (int c = r0 / 8; c < (r0 + W) / 8; ++c) {
-                        uint32_t hi[4], lo[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = 8 * c + 2 * i;
-                            const float a = ex2f(s[r - r0]), b = ex2f(s[r - r0 + 1]);
-                            l[r] += a;
-                            l[r + 1] += b;
-                            if (G::kHiLo) split_bf16(a, b, hi[i], lo[i]);
-                            else hi[i] = pack_bf16(a, b);
-                        }
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                        if (G::kHiLo)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 tc_fence_before();
@@ -731,17 +720,8 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             }
             if (!ok) break;
             // ---- the unit's end: sums over the warp's keys
-            {
-                constexpr int W = NR < 32 ? NR : 32;
-#pragma unroll
-                for (int r0 = 0; r0 < NR; r0 += W) {
-                    float v[W];
-#pragma unroll
-                    for (int i = 0; i < W; ++i) v[i] = l[r0 + i];
-                    const float sum = reduce_rows<W, false>(v, lane);
-                    if (lane < W) sh_wl[x][wq][r0 + lane] = sum;
-                }
-            }
+            const float sum = reduce_rows<NR, false>(l, lane);
+            if (lane < NR) sh_wl[x][wq][lane] = sum;
             if (x == 1) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(second_end);
@@ -792,34 +772,31 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 }
                 wg_sync(bar_id);
                 const bool mine = wt < p.D;                // a thread per feature
-#pragma unroll 1
-                for (int r0 = 0; r0 < rows; r0 += 16) {
-                    float a[16], o[4][16];
+                float a[NR], o[4][NR];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        if (has[y]) {
-                            tmem_ld16_go(o_at(y) + lanes + r0, o[2 * y]);
-                            if (G::kHiLo) tmem_ld16_go(o_at(y) + lanes + NR + r0, o[2 * y + 1]);
-                        }
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) tmem_landed16(o[y]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        a[i] = 0.f;
-                        if (has[0]) a[i] = (G::kHiLo ? o[0][i] + o[1][i] : o[0][i]) * sh_f[0][r0 + i];
-                        if (has[1]) a[i] = fmaf(G::kHiLo ? o[2][i] + o[3][i] : o[2][i], sh_f[1][r0 + i], a[i]);
+                for (int y = 0; y < 2; ++y)
+                    if (has[y]) {
+                        tmem_ld16_go(o_at(y) + lanes, o[2 * y]);
+                        tmem_ld16_go(o_at(y) + lanes + NR, o[2 * y + 1]);
                     }
-                    if (mine && whole_unit) {
+                tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (r0 + i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[r0 + i] + wt] = __float2bfloat16_rn(a[i]);
-                    } else if (mine) {
-                        float *part = p.part.o + ((size_t)slot * NR + r0) * 128 + wt;
+                for (int y = 0; y < 4; ++y) tmem_landed16(o[y]);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (r0 + i < rows) __stcg(part + i * 128, a[i]);
-                    }
+                for (int i = 0; i < NR; ++i) {
+                    a[i] = 0.f;
+                    if (has[0]) a[i] = (o[0][i] + o[1][i]) * sh_f[0][i];
+                    if (has[1]) a[i] = fmaf(o[2][i] + o[3][i], sh_f[1][i], a[i]);
+                }
+                if (mine && whole_unit) {
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + wt] = __float2bfloat16_rn(a[i]);
+                } else if (mine) {
+                    float *part = p.part.o + (size_t)slot * NR * 128 + wt;
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) __stcg(part + i * 128, a[i]);
                 }
                 tc_fence_before();
                 if (!whole_unit) {
@@ -831,7 +808,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     if (sh_last) {
                         const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
                         if (rows <= 4) join_rows<NR, 1, 8>(ja, wq, lane);
-                        else join_rows<NR, NR == 64 ? 4 : 2, NR == 64 ? 2 : 4>(ja, wq, lane);
+                        else join_rows<NR, 2, 4>(ja, wq, lane);
                         if (wt == 0) p.part.counters[c0] = 0;
                     }
                 }
@@ -1241,6 +1218,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     if (half == 0 && lane == 0) sh_last[x][wq] = arrive_acq_rel(counter) == c1 - c0;
                     any_of(pair, 64, false);
                     if (sh_last[x][wq] && live) {
+                        constexpr int U = NT == 1 ? 2 : 1;             // pieces in flight (registers)
                         auto slot_of = [&](int c) { return (size_t)((2 * c + (c == c0)) * NT + x); };
 #pragma unroll 1
                         for (int f = 0; f < DB; ++f) {
@@ -1248,20 +1226,29 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0.f;
 #pragma unroll 1
-                            for (int c = c0; c <= c1; ++c) {
-                                const float2 ml = __ldcg(p.part.ml + slot_of(c) * 128 + row);
-                                float4 a[8];
+                            for (int cb = c0; cb <= c1; cb += U) {
+                                float2 ml[U];
+                                float4 a[U][8];
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) a[i] = __ldcg(part + (slot_of(c) * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
-                                const float nm = fmaxf(M, ml.x);
-                                const float e = M == nm ? 1.f : ex2f(M - nm), w = ml.x == nm ? 1.f : ex2f(ml.x - nm);
-                                M = nm;
-                                S = fmaf(w, ml.y, S * e);
+                                for (int y = 0; y < U; ++y) {
+                                    const size_t sl = slot_of(min(cb + y, c1));
+                                    ml[y] = __ldcg(p.part.ml + sl * 128 + row);
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    o[4 * i] = fmaf(w, a[i].x, o[4 * i] * e); o[4 * i + 1] = fmaf(w, a[i].y, o[4 * i + 1] * e);
-                                    o[4 * i + 2] = fmaf(w, a[i].z, o[4 * i + 2] * e); o[4 * i + 3] = fmaf(w, a[i].w, o[4 * i + 3] * e);
+                                    for (int i = 0; i < 8; ++i) a[y][i] = __ldcg(part + (sl * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
                                 }
+#pragma unroll
+                                for (int y = 0; y < U; ++y)
+                                    if (cb + y <= c1) {
+                                        const float nm = fmaxf(M, ml[y].x);
+                                        const float e = M == nm ? 1.f : ex2f(M - nm), w = ml[y].x == nm ? 1.f : ex2f(ml[y].x - nm);
+                                        M = nm;
+                                        S = fmaf(w, ml[y].y, S * e);
+#pragma unroll
+                                        for (int i = 0; i < 8; ++i) {
+                                            o[4 * i] = fmaf(w, a[y][i].x, o[4 * i] * e); o[4 * i + 1] = fmaf(w, a[y][i].y, o[4 * i + 1] * e);
+                                            o[4 * i + 2] = fmaf(w, a[y][i].z, o[4 * i + 2] * e); o[4 * i + 3] = fmaf(w, a[y][i].w, o[4 * i + 3] * e);
+                                        }
+                                    }
                             }
                             put32(32 * f, o, inverse(S));
                             if (f == 0 && lse) *lse = log_sum(M, S);
@@ -1303,16 +1290,16 @@ cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const 
     return note_err(c, e, "kv_attention_tc_kernel");
 }
 
-template <int DB, int NR>
+template <int DB>
 cudaError_t few_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_few_kernel<DB, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<DB, NR>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_few_kernel<DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<DB>::kSmem);
 }
-template <int DB, int NR>
+template <int DB>
 cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_few_kernel<DB, NR>, dim3(sms), dim3(FewGeo<DB, NR>::kThreads), FewGeo<DB, NR>::kSmem, st,
+    cudaError_t e = launch_k(kv_attention_few_kernel<DB>, dim3(sms), dim3(FewGeo<DB>::kThreads), FewGeo<DB>::kSmem, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
     c->launches = 1;
     return note_err(c, e, "kv_attention_few_kernel");
@@ -1360,8 +1347,7 @@ cudaError_t kv_tc_attach(Ctx *c)
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
     if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
-    if ((e = few_prepare<1, 16>()) != cudaSuccess || (e = few_prepare<1, 32>()) != cudaSuccess || (e = few_prepare<1, 64>()) != cudaSuccess ||
-        (e = few_prepare<2, 16>()) != cudaSuccess || (e = few_prepare<2, 32>()) != cudaSuccess || (e = few_prepare<2, 64>()) != cudaSuccess ||
+    if ((e = few_prepare<1>()) != cudaSuccess || (e = few_prepare<2>()) != cudaSuccess ||
         (e = tc_prepare<1, 1>()) != cudaSuccess || (e = tc_prepare<1, 2>()) != cudaSuccess || (e = tc_prepare<2, 1>()) != cudaSuccess ||
         (e = tc_prepare<2, 2>()) != cudaSuccess)
         return e;
@@ -1380,10 +1366,12 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaSt
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
     const long long rows = (long long)max_new * p.g;
     const bool one_block = c->kv.head_dim <= 64, two = rows > 128;
-    if (rows <= 16) return one_block ? few_launch<1, 16>(c, p, km, vm, box, st) : few_launch<2, 16>(c, p, km, vm, box, st);
-    if (rows <= 32) return one_block ? few_launch<1, 32>(c, p, km, vm, box, st) : few_launch<2, 32>(c, p, km, vm, box, st);
-    if (rows <= 64) return one_block ? few_launch<1, 64>(c, p, km, vm, box, st) : few_launch<2, 64>(c, p, km, vm, box, st);
-    if (c->kv.head_dim <= 64) return two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
+    // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 69 us on the
+    // transposed kernel, 76 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
+    // took 95 and 113 against 78 and 80.  Beyond 128 rows two row tiles share the stream of K and V.
+    if (rows <= kFewRows) return one_block ? few_launch<1>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
+    p.min_piece = two ? 1 : 2;
+    if (one_block) return two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
     return two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
 }
 
