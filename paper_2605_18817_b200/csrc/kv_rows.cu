@@ -4,13 +4,13 @@
 // with f the fraction of a turn that position p makes in pair (a, b): p * turn_j mod 2^64, turn_j = 2^64 w_j / (2 pi) on
 // the host in 64 bits, so the reduction of the angle is one exact integer product however far the position is.
 //
-// Every element is read once and written once and takes about seven operations: memory bounds it, as long as the rest
-// stays short.  A warp takes one token (or, where tokens are few, one of several shares of a token's heads): it finds
-// the token's sequence and page, each lane computes the sines and cosines of its own four pairs once (sincospi), and
-// the warp goes through the token's heads, GL lanes a head, U heads' loads in flight.  A lane holds two runs of four
-// features: the two halves of its four pairs (features 4 l.. and rot_dim / 2 + 4 l.. of the rotated ones), so a
-// rotation needs no other lane's registers; adjacent pairs lie in one run anyway.  rot_dim / 2 that is no multiple of
-// four splits runs: there the other half of a pair is read again.
+// Every element is read once and written once and takes about seven operations: memory bounds it as long as the
+// instructions around them stay few.  A warp takes a token (where tokens are few, one of several shares of a token): it
+// finds the token's sequence and page, each lane computes the sines and cosines of its own four pairs once (sincospi),
+// and the warp goes through the token's heads in units of one kind (queries, keys, values), GL lanes a head, U heads'
+// loads in flight.  A lane holds two runs of four features: the two halves of its four pairs (features 4 l.. and rot_dim / 2
+// + 4 l.. of the rotated ones), so a rotation needs no other lane's registers; adjacent pairs lie in one run anyway.
+// rot_dim / 2 that is no multiple of four splits runs: there the other half of a pair is read again.
 #include "kv_attention.cuh"
 
 namespace mrp {
@@ -29,6 +29,7 @@ struct RowsParams {
     int to_pages;              // k and v go to the pools
     int D, rot, half, interleaved;
     int tokens, shares;        // warps a token
+    int units[3];              // units of U * NG heads: of queries, and keys, and values
     float eps, inv_d;
     uint64_t turn[128];
 };
@@ -56,6 +57,17 @@ template <> struct Run4<float> {
     __device__ __forceinline__ void put(const float *f) { r = make_float4(f[0], f[1], f[2], f[3]); }
     __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = r; }
 };
+// two fp32 operations in one instruction
+__device__ __forceinline__ void mul2(float &a, float &b, float c, float d)
+{
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void fma2(float &a, float &b, float c, float d, float e, float f)     // (a, b) * (c, d) + (e, f)
+{
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %5};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d), "f"(e), "f"(f));
+}
 __device__ __forceinline__ float one_f(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float one_f(const float *p) { return *p; }
 
@@ -74,7 +86,9 @@ __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seq
     return lo;
 }
 
-template <typename T, int GL, int U>
+enum { kHalves = 0, kAdjacent = 1, kAgain = 2 };         // how pairs lie in a lane
+
+template <typename T, int GL, int U, int MODE>
 __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_constant__ RowsParams p)
 {
     const int tid = threadIdx.x, lane = tid & 31;
@@ -110,143 +124,164 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
     // ---- the lane: two runs of four features, its four pairs
     constexpr int NG = 32 / GL;
     const int gl = lane & (GL - 1), grp = lane / GL;
-    const bool halves = !p.interleaved && (p.half & 3) == 0, again = !p.interleaved && !halves;
     const int hl = p.half >> 2;                            // lanes whose runs are the two halves of pairs
     const bool mine = gl * 8 < p.D;
     int e0 = gl * 8, e1 = gl * 8 + 4;
-    if (halves) {
+    if (MODE == kHalves) {
         e0 = gl < hl ? gl * 4 : p.rot + (gl - hl) * 8;
         e1 = gl < hl ? p.half + gl * 4 : e0 + 4;
     }
+    if (!mine) e0 = e1 = 0;                                // (loads features that are there, stores nothing)
     float cs[4], sn[4];
+    if (MODE != kAgain) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = gl * 4 + i;                          // (again: computed where it is used)
-        cs[i] = 1.f;
-        sn[i] = 0.f;
-        if (!again && j < p.half) {
-            const uint64_t f = (uint64_t)(int64_t)pos * p.turn[j];
-            sincospif((float)(int32_t)(f >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);   // 2^-31: half turns
+        for (int i = 0; i < 4; ++i) {
+            const int j = gl * 4 + i;
+            cs[i] = 1.f;
+            sn[i] = 0.f;
+            if (j < p.half) {
+                const uint64_t f = (uint64_t)(int64_t)pos * p.turn[j];
+                sincospif((float)(int32_t)(f >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);   // 2^-31: half turns
+            }
         }
-    }
-    Run4<T> gq[2], gk[2];
-    if (mine && p.gamma[0]) {
-        gq[0].load(reinterpret_cast<const T *>(p.gamma[0]) + e0);
-        gq[1].load(reinterpret_cast<const T *>(p.gamma[0]) + e1);
-    }
-    if (mine && p.gamma[1]) {
-        gk[0].load(reinterpret_cast<const T *>(p.gamma[1]) + e0);
-        gk[1].load(reinterpret_cast<const T *>(p.gamma[1]) + e1);
     }
 
-    // ---- the token's heads: queries, then keys, then values
-    const int nq = p.heads[0], nqk = nq + p.heads[1], total = nqk + p.heads[2];
-    const T *src0 = reinterpret_cast<const T *>(p.src[0]) + (int64_t)t * p.src_stride[0];
-    const T *src1 = reinterpret_cast<const T *>(p.src[1]) + (int64_t)t * p.src_stride[1];
-    const T *src2 = reinterpret_cast<const T *>(p.src[2]) + (int64_t)t * p.src_stride[2];
-    T *dst0 = reinterpret_cast<T *>(p.dst[0]) + (int64_t)t * p.dst_stride[0];
+    // ---- the token's heads
     const int64_t head_out = p.to_pages ? (int64_t)p.b.page.d * p.D : p.D;
-    T *dst1 = reinterpret_cast<T *>(p.dst[1]) + (p.to_pages ? page_off : (int64_t)t * p.dst_stride[1]);
-    T *dst2 = reinterpret_cast<T *>(p.dst[2]) + page_off;
-    const bool store_kv = !p.to_pages || page_off >= 0;
-    for (int r0 = share * NG; r0 < total; r0 += p.shares * NG * U) {
+#pragma unroll 1
+    for (int u = share; u < p.units[2]; u += p.shares) {
+        const int kind = u < p.units[0] ? 0 : u < p.units[1] ? 1 : 2;
+        const int h0 = (u - (kind == 0 ? 0 : p.units[kind - 1])) * U * NG + grp, n = p.heads[kind] - h0;   // heads h0, h0 + NG, ..
+        const T *src = reinterpret_cast<const T *>(p.src[kind]) + (int64_t)t * p.src_stride[kind] + (int64_t)h0 * p.D;
         Run4<T> x[U][2];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int r = min(r0 + u * p.shares * NG + grp, total - 1);
-            const T *row = r < nq ? src0 + (int64_t)r * p.D : r < nqk ? src1 + (int64_t)(r - nq) * p.D : src2 + (int64_t)(r - nqk) * p.D;
-            if (mine) {
-                x[u][0].load(row + e0);
-                x[u][1].load(row + e1);
-            }
+        for (int i = 0; i < U; ++i) {
+            const T *row = i * NG < n ? src + i * NG * p.D : src - (n < 1 ? (int64_t)h0 * p.D : 0);     // (beyond the heads: one again)
+            x[i][0].load(row + e0);
+            x[i][1].load(row + e1);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int r = r0 + u * p.shares * NG + grp;
-            const bool is_q = r < nq, is_v = r >= nqk;
-            float f[8];
-            x[u][0].get(f);
-            x[u][1].get(f + 4);
-            const bool norm = (is_q ? p.gamma[0] : p.gamma[1]) != nullptr && !is_v;
-            float rs = 1.f;
-            if (p.gamma[0] || p.gamma[1]) {
-                float ss = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(f[i], f[i], ss);
-                if (!mine) ss = 0.f;
-#pragma unroll
-                for (int w = GL / 2; w > 0; w >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, w);
-                if (norm) {
-                    rs = rsqrtf(fmaf(ss, p.inv_d, p.eps));
-                    Run4<T> g0 = is_q ? gq[0] : gk[0], g1 = is_q ? gq[1] : gk[1];
-                    float g[8];
-                    g0.get(g);
-                    g1.get(g + 4);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] *= rs * g[i];
-                }
+        T *dst = reinterpret_cast<T *>(p.dst[kind]);
+        int64_t step = p.D;
+        bool store = mine;
+        if (kind > 0 && p.to_pages) {
+            step = head_out;
+            dst += page_off + (int64_t)h0 * step;
+            store = mine && page_off >= 0;
+        } else {
+            dst += (int64_t)t * p.dst_stride[kind] + (int64_t)h0 * step;
+        }
+        step *= NG;
+        if (kind < 2) {
+            const T *gm = reinterpret_cast<const T *>(p.gamma[kind]);
+            float g[8];
+            if (gm) {
+                Run4<T> g0, g1;
+                g0.load(gm + e0);
+                g1.load(gm + e1);
+                g0.get(g);
+                g1.get(g + 4);
             }
-            if (p.rot > 0 && !is_v) {
-                if (halves) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {          // (beyond the rotated features: cosine 1, sine 0, and
-                        if (gl < hl) {                     //  whatever their partner is must not come in)
-                            const float a = f[i], b = f[4 + i];
-                            f[i] = fmaf(a, cs[i], -b * sn[i]);
-                            f[4 + i] = fmaf(b, cs[i], a * sn[i]);
+            for (int i = 0; i < U; ++i) {
+                float f[8], rs = 1.f;
+                x[i][0].get(f);
+                x[i][1].get(f + 4);
+                if (gm) {
+                    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int y = 0; y < 8; y += 2) {
+                        float a = f[y], b = f[y + 1];
+                        fma2(a, b, a, b, s0, s1);
+                        s0 = a;
+                        s1 = b;
+                    }
+                    float ss = mine ? s0 + s1 : 0.f;
+#pragma unroll
+                    for (int w = GL / 2; w > 0; w >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, w);
+                    rs = rsqrtf(fmaf(ss, p.inv_d, p.eps));
+#pragma unroll
+                    for (int y = 0; y < 8; y += 2) {
+                        mul2(f[y], f[y + 1], rs, rs);
+                        mul2(f[y], f[y + 1], g[y], g[y + 1]);
+                    }
+                }
+                if (MODE == kHalves) {
+                    if (gl < hl) {                         // (other lanes: features that are not rotated)
+#pragma unroll
+                        for (int y = 0; y < 4; y += 2) {
+                            float a = f[y], b = f[y + 1], c = f[y + 4], d = f[y + 5];
+                            mul2(a, b, sn[y], sn[y + 1]);                              // x sin
+                            mul2(c, d, -sn[y], -sn[y + 1]);                            // - y sin
+                            fma2(f[y], f[y + 1], cs[y], cs[y + 1], c, d);
+                            fma2(f[y + 4], f[y + 5], cs[y], cs[y + 1], a, b);
                         }
                     }
-                } else if (p.interleaved) {
+                } else if (MODE == kAdjacent) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (gl * 8 + 2 * i < p.rot) {
-                            const float a = f[2 * i], b = f[2 * i + 1];
-                            f[2 * i] = fmaf(a, cs[i], -b * sn[i]);
-                            f[2 * i + 1] = fmaf(b, cs[i], a * sn[i]);
+                    for (int y = 0; y < 4; ++y)
+                        if (gl * 8 + 2 * y < p.rot) {
+                            const float a = f[2 * y], b = f[2 * y + 1];
+                            f[2 * y] = fmaf(a, cs[y], -b * sn[y]);
+                            f[2 * y + 1] = fmaf(b, cs[y], a * sn[y]);
                         }
-                } else if (mine && r < total) {
-                    const T *row = is_q ? src0 + (int64_t)r * p.D : src1 + (int64_t)(r - nq) * p.D;
-                    const T *gm = reinterpret_cast<const T *>(is_q ? p.gamma[0] : p.gamma[1]);
+                } else if (mine && i * NG < n) {
+                    const T *row = src + i * NG * p.D;
 #pragma unroll 1
-                    for (int i = 0; i < 8; ++i) {
-                        const int e = gl * 8 + i;
+                    for (int y = 0; y < 8; ++y) {
+                        const int e = gl * 8 + y;
                         if (e >= p.rot) continue;
                         const bool first = e < p.half;
                         const int pe = first ? e + p.half : e - p.half;
                         const uint64_t fr = (uint64_t)(int64_t)pos * p.turn[first ? e : pe];
                         float s, c;
                         sincospif((float)(int32_t)(fr >> 32) * 4.656612873077393e-10f, &s, &c);
-                        const float o = one_f(row + pe) * (norm ? rs * one_f(gm + pe) : 1.f);
-                        const float v = one_f(row + e) * (norm ? rs * one_f(gm + e) : 1.f);
-                        const float y = fmaf(v, c, (first ? -o : o) * s);
+                        const float o = one_f(row + pe) * (gm ? rs * one_f(gm + pe) : 1.f);
+                        const float v = one_f(row + e) * (gm ? rs * one_f(gm + e) : 1.f);
+                        const float z = fmaf(v, c, (first ? -o : o) * s);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (k == i) f[k] = y;
+                        for (int q = 0; q < 8; ++q)
+                            if (q == y) f[q] = z;
                     }
                 }
-            }
-            __syncwarp();                  // a head read again above is overwritten by its own lanes alone, now
-            if (mine && r < total && (is_q || store_kv)) {
-                T *dst = is_q ? dst0 + (int64_t)r * p.D : is_v ? dst2 + (int64_t)(r - nqk) * head_out : dst1 + (int64_t)(r - nq) * head_out;
-                if (!is_v) {
-                    x[u][0].put(f);
-                    x[u][1].put(f + 4);
-                }
-                x[u][0].store(dst + e0);
-                x[u][1].store(dst + e1);
+                x[i][0].put(f);
+                x[i][1].put(f + 4);
+                if (MODE == kAgain) __syncwarp();          // a head read again above is overwritten by its own lanes alone, now
             }
         }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (store && i * NG < n) {
+                x[i][0].store(dst + i * step + e0);
+                x[i][1].store(dst + i * step + e1);
+            }
     }
 }
 
-template <typename T, int GL>
-cudaError_t launch_rows(Ctx *c, const RowsParams &p, cudaStream_t st)
+template <typename T, int GL, int MODE>
+cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
 {
+    constexpr int U = sizeof(T) == 2 ? 4 : 2, kAtOnce = U * (32 / GL);
+    int n = 0;
+    for (int k = 0; k < 3; ++k) p.units[k] = n += (p.heads[k] + kAtOnce - 1) / kAtOnce;
+    // A warp a token where there are tokens for every warp the GPU holds; with fewer, a token's units are shared out.
+    const long long want = (long long)c->sm_count * 32 / p.tokens;
+    p.shares = (int)(want < 1 ? 1 : want > n ? n : want);
     const long long warps = (long long)p.tokens * p.shares;
-    cudaError_t e = launch_k(qk_rows_kernel<T, GL, sizeof(T) == 2 ? 4 : 2>, dim3((unsigned)((warps + kRowWarps - 1) / kRowWarps)),
-                             dim3(kRowThreads), 0, st, !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
+    cudaError_t e = launch_k(qk_rows_kernel<T, GL, U, MODE>, dim3((unsigned)((warps + kRowWarps - 1) / kRowWarps)), dim3(kRowThreads),
+                             0, st, !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
     c->launches = 1;
     return note_err(c, e, "qk_rows_kernel");
+}
+template <typename T, int GL>
+cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
+{
+    if (p.interleaved) return launch_rows<T, GL, kAdjacent>(c, p, st);
+    return (p.half & 3) == 0 ? launch_rows<T, GL, kHalves>(c, p, st) : launch_rows<T, GL, kAgain>(c, p, st);
+}
+template <typename T>
+cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
+{
+    return p.D <= 64 ? launch_rows<T, 8>(c, p, st) : p.D <= 128 ? launch_rows<T, 16>(c, p, st) : launch_rows<T, 32>(c, p, st);
 }
 
 }  // namespace
@@ -287,23 +322,10 @@ cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_k
     p.half = kv.rot_dim / 2;
     p.interleaved = kv.rot_interleaved != 0;
     p.tokens = n_tokens;
-    // One warp a token where there are tokens for every warp the GPU holds; with fewer, a token's heads are shared out,
-    // down to one round of loads a warp.
-    {
-        const int rows = p.heads[0] + p.heads[1] + p.heads[2], at_once = 32 / (kv.head_dim <= 64 ? 8 : kv.head_dim <= 128 ? 16 : 32);
-        const int most = (rows + at_once * 2 - 1) / (at_once * 2);
-        const long long want = (long long)c->sm_count * 24 / n_tokens;
-        p.shares = (int)(want < 1 ? 1 : want > most ? most : want);
-    }
     p.eps = kv.norm_eps;
     p.inv_d = 1.f / (float)kv.head_dim;
     for (int j = 0; j < p.half; ++j) p.turn[j] = c->kv_turn[j];
-    const int lanes = kv.head_dim / 8;
-    if (c->cfg.dtype == MRP_BF16)
-        return lanes <= 8 ? launch_rows<__nv_bfloat16, 8>(c, p, st)
-             : lanes <= 16 ? launch_rows<__nv_bfloat16, 16>(c, p, st) : launch_rows<__nv_bfloat16, 32>(c, p, st);
-    return lanes <= 8 ? launch_rows<float, 8>(c, p, st)
-         : lanes <= 16 ? launch_rows<float, 16>(c, p, st) : launch_rows<float, 32>(c, p, st);
+    return c->cfg.dtype == MRP_BF16 ? launch_rows<__nv_bfloat16>(c, p, st) : launch_rows<float>(c, p, st);
 }
 
 }  // namespace mrp
