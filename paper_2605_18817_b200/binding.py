@@ -501,36 +501,35 @@ class KvBatch:
 
 
 def _kv_shape(ctx):
-    kv = getattr(ctx, "kv", None)
-    if kv is None:
+    if ctx.kv is None:
         raise MrpError("paged cache", 2, "mrp_kv_attach first")
-    return kv
+    return ctx.kv
 
 
 def _rows(kv, t, row, n_tokens, what):
     """(address, token stride) of rows [>= n_tokens, heads, head_dim]: the heads of a token side by side."""
-    if t.dtype != kv.dtype or t.get_device() != kv.device:
+    if t.dtype is not kv.dtype or t.get_device() != kv.device:
         raise TypeError("%s must be a CUDA tensor of %s on the context's device" % (what, kv.dtype))
-    st = t.stride()
-    if tuple(t.shape[1:]) != row or t.shape[0] < n_tokens or (n_tokens > 0 and (st[2] != 1 or (st[1] != row[1] and row[0] > 1))):
+    n, heads, dim = t.shape if t.dim() == 3 else (-1, 0, 0)
+    s0, s1, s2 = t.stride() if n >= 0 else (0, 0, 0)
+    if n < n_tokens or heads != row[0] or dim != row[1] or (n_tokens > 0 and (s2 != 1 or (s1 != dim and heads > 1))):
         raise ValueError("%s is [tokens, %d, %d] with the heads of a token side by side" % (what, row[0], row[1]))
-    # the stride of a single row means nothing
-    return t.data_ptr(), st[0] if t.shape[0] > 1 else row[0] * row[1]
+    return t.data_ptr(), s0 if n > 1 else heads * dim           # (the stride of a single row means nothing)
 
 
 def _gamma(kv, t, what):
     if t is None:
         return None
-    if t.dtype != kv.dtype or t.get_device() != kv.device or t.numel() != kv.k_row[1] or not t.is_contiguous():
+    if t.dtype is not kv.dtype or t.get_device() != kv.device or t.numel() != kv.k_row[1] or not t.is_contiguous():
         raise TypeError("%s is a contiguous CUDA tensor [head_dim] of %s" % (what, kv.dtype))
     return t.data_ptr()
 
 
 def _pools(kv, batch, k_pages, v_pages):
     for t in (k_pages, v_pages):
-        if t.dtype != kv.dtype or t.get_device() != kv.device:
+        if t.dtype is not kv.dtype or t.get_device() != kv.device:
             raise TypeError("pools are CUDA tensors of %s on the context's device" % kv.dtype)
-        if tuple(t.shape) != kv.pool or t.stride() != kv.pool_stride:
+        if t.shape != kv.pool or t.stride() != kv.pool_stride:
             raise ValueError("pools are [n_pages, n_kv_heads, page_size, head_dim] with the strides attached")
     if batch.max_pages != kv.max_pages or batch.device != kv.device:
         raise ValueError("the batch's page table is [B, max_pages] on the context's device")
@@ -541,27 +540,29 @@ def _raw_stream(kv, stream):
     return torch._C._cuda_getCurrentRawStream(kv.device) if stream is None else stream.cuda_stream
 
 
+def _kv_error(ctx, where, rc):
+    raise MrpError(where, rc, lib.mrp_last_error(ctx.handle).decode())
+
+
 def mrp_qk_norm_rotate(ctx: Context, positions, q, k, q_out, k_out, gamma_q=None, gamma_k=None, stream=None) -> None:
     """Per-head RMSNorm (with gamma) and rotation by ``positions`` [tokens] int32 of query rows q [tokens, n_heads, head_dim]
     and key rows k [tokens, n_kv_heads, head_dim], either None; rows may be strided (a packed projection), outputs the inputs."""
     kv = _kv_shape(ctx)
-    n = (q if q is not None else k).shape[0]
-    r = mrp_qkv_rows()
-    if q is not None:
-        r.q, r.q_stride = _rows(kv, q, kv.q_row, n, "q")
-        r.q_out, r.q_out_stride = _rows(kv, q_out, kv.q_row, n, "q_out")
-    if k is not None:
-        r.k, r.k_stride = _rows(kv, k, kv.k_row, n, "k")
-        r.k_out, r.k_out_stride = _rows(kv, k_out, kv.k_row, n, "k_out")
-    r.gamma_q, r.gamma_k = _gamma(kv, gamma_q, "gamma_q"), _gamma(kv, gamma_k, "gamma_k")
+    if q is None and k is None:
+        raise ValueError("neither q nor k")
+    n = (k if q is None else q).shape[0]
+    qp, qs = (None, 0) if q is None else _rows(kv, q, kv.q_row, n, "q")
+    qo, qos = (None, 0) if q is None else _rows(kv, q_out, kv.q_row, n, "q_out")
+    kp, ks = (None, 0) if k is None else _rows(kv, k, kv.k_row, n, "k")
+    ko, kos = (None, 0) if k is None else _rows(kv, k_out, kv.k_row, n, "k_out")
     if positions is not None:
-        _check(positions, torch.int32, "positions")
-        if positions.numel() < n or positions.get_device() != kv.device:
-            raise ValueError("positions [tokens] on the context's device")
+        if positions.dtype is not torch.int32 or positions.get_device() != kv.device or positions.numel() < n or not positions.is_contiguous():
+            raise TypeError("positions is a contiguous CUDA tensor [tokens] of torch.int32 on the context's device")
         positions = positions.data_ptr()
-    rc = lib.mrp_qk_norm_rotate(ctx.handle, positions, n, ctypes.byref(r), _raw_stream(kv, stream))
+    r = mrp_qkv_rows(qp, kp, None, qs, ks, 0, _gamma(kv, gamma_q, "gamma_q"), _gamma(kv, gamma_k, "gamma_k"), qo, ko, qos, kos)
+    rc = _rotate_c(ctx.handle, positions, n, _byref(r), _raw_stream(kv, stream))
     if rc != 0:
-        raise MrpError("mrp_qk_norm_rotate", rc, lib.mrp_last_error(ctx.handle).decode())
+        _kv_error(ctx, "mrp_qk_norm_rotate", rc)
 
 
 def mrp_kv_append(ctx: Context, batch: KvBatch, k_pages, v_pages, k, v, gamma_k=None, q=None, q_out=None, gamma_q=None,
@@ -571,17 +572,14 @@ def mrp_kv_append(ctx: Context, batch: KvBatch, k_pages, v_pages, k, v, gamma_k=
     kv = _kv_shape(ctx)
     n = batch.n_tokens
     pools = _pools(kv, batch, k_pages, v_pages)
-    r = mrp_qkv_rows()
-    r.k, r.k_stride = _rows(kv, k, kv.k_row, n, "k")
-    r.v, r.v_stride = _rows(kv, v, kv.k_row, n, "v")
-    r.gamma_k = _gamma(kv, gamma_k, "gamma_k")
-    if q is not None:
-        r.q, r.q_stride = _rows(kv, q, kv.q_row, n, "q")
-        r.q_out, r.q_out_stride = _rows(kv, q_out, kv.q_row, n, "q_out")
-        r.gamma_q = _gamma(kv, gamma_q, "gamma_q")
-    rc = lib.mrp_kv_append(ctx.handle, batch.ref, ctypes.byref(pools), ctypes.byref(r), _raw_stream(kv, stream))
+    kp, ks = _rows(kv, k, kv.k_row, n, "k")
+    vp, vs = _rows(kv, v, kv.k_row, n, "v")
+    qp, qs = (None, 0) if q is None else _rows(kv, q, kv.q_row, n, "q")
+    qo, qos = (None, 0) if q is None else _rows(kv, q_out, kv.q_row, n, "q_out")
+    r = mrp_qkv_rows(qp, kp, vp, qs, ks, vs, _gamma(kv, gamma_q, "gamma_q"), _gamma(kv, gamma_k, "gamma_k"), qo, None, qos, 0)
+    rc = _append_c(ctx.handle, batch.ref, _byref(pools), _byref(r), _raw_stream(kv, stream))
     if rc != 0:
-        raise MrpError("mrp_kv_append", rc, lib.mrp_last_error(ctx.handle).decode())
+        _kv_error(ctx, "mrp_kv_append", rc)
 
 
 def mrp_paged_attention(ctx: Context, batch: KvBatch, k_pages, v_pages, q, out, lse=None, mask=MRP_ATTN_CAUSAL, window=0,
@@ -591,17 +589,20 @@ def mrp_paged_attention(ctx: Context, batch: KvBatch, k_pages, v_pages, q, out, 
     kv = _kv_shape(ctx)
     n = batch.n_tokens
     pools = _pools(kv, batch, k_pages, v_pages)
-    a = mrp_attention_args()
-    a.q, a.q_stride = _rows(kv, q, kv.q_row, n, "q")
-    a.out, a.out_stride = _rows(kv, out, kv.q_row, n, "out")
+    qp, qs = _rows(kv, q, kv.q_row, n, "q")
+    op, os_ = _rows(kv, out, kv.q_row, n, "out")
     if lse is not None:
-        if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != kv.device or lse.numel() < n * kv.q_row[0]:
+        if lse.dtype is not torch.float32 or lse.get_device() != kv.device or not lse.is_contiguous() or lse.numel() < n * kv.q_row[0]:
             raise TypeError("lse is a contiguous CUDA tensor [tokens, n_heads] of float32 on the context's device")
-        a.lse = lse.data_ptr()
-    a.mask, a.window, a.sinks, a.scale = mask, window, sinks, scale
-    rc = lib.mrp_paged_attention(ctx.handle, batch.ref, ctypes.byref(pools), ctypes.byref(a), _raw_stream(kv, stream))
+        lse = lse.data_ptr()
+    a = mrp_attention_args(qp, op, qs, os_, lse, mask, window, sinks, scale)
+    rc = _attention_c(ctx.handle, batch.ref, _byref(pools), _byref(a), _raw_stream(kv, stream))
     if rc != 0:
-        raise MrpError("mrp_paged_attention", rc, lib.mrp_last_error(ctx.handle).decode())
+        _kv_error(ctx, "mrp_paged_attention", rc)
+
+
+# the calls of every layer of every step: looked up once
+_byref, _rotate_c, _append_c, _attention_c = ctypes.byref, lib.mrp_qk_norm_rotate, lib.mrp_kv_append, lib.mrp_paged_attention
 
 
 def mrp_set_input_rows(ctx: Context, n_rows: int) -> None:
