@@ -86,7 +86,7 @@ template <int DP> struct Geo<__nv_bfloat16, DP> {
 template <int DP> struct Geo<float, DP> {
     static constexpr int kChunks = DP / 4;
     static constexpr int kPitchK = DP * 4 + 32, kPitchV = DP * 4 + 16, kPitchQ = DP * 4 + 32;
-    static constexpr int kStages = DP <= 64 ? 3 : DP <= 128 ? 2 : 1;
+    static constexpr int kStages = DP <= 128 ? 2 : 1;
     static constexpr bool kSwizzle = false;
 };
 template <typename T, int DP> struct Smem {
@@ -515,7 +515,8 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
         }
         if (!whole_unit) {
             // ---- the pieces of a unit meet: the CTA that arrives last joins them in the order of the pieces
-            const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
+            int c0, c1;
+            unit_pieces(p, cur, per, c0, c1);
             __syncthreads();
             if (tid == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
             __syncthreads();
@@ -613,14 +614,17 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
     p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
     p.gdiv = make_fastdiv(p.g);
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
+    p.rows_above = 0;
+    p.rows_upto = 0x7fffffff;
     p.min_piece = 1;
+    p.lead = 0;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
     {
         // a warp's 16 keys lie one after the other in one page, in rows as wide as the kernel's stages
         const int DP = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
         p.plain_rows = kv.page_size % kWarpKeys == 0 && kv.head_dim == DP;
     }
-        if (c->kv_encode) return launch_paged_attention_tc(c, p, batch.max_new, st);
+        if (c->kv_encode) return launch_paged_attention_tc(c, p, batch, st);
     const size_t slots = (size_t)4 * kKvMaxSm;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);

@@ -85,7 +85,9 @@ struct AttnParams {
     int H, Hk, g, D;
     FastDiv gdiv;              // g
     int mask, window, sinks, plain_rows;
+    int rows_above, rows_upto; // sequences with more than rows_above and at most rows_upto query rows a key head are this launch's
     int min_piece;             // tiles a CTA takes at least
+    int lead;                  // what a unit costs besides its tiles, in tiles: so much of the line lies ahead of each unit
     float scale_log2;          // > 0
     KvPartials part;
 };
@@ -127,6 +129,12 @@ __device__ __forceinline__ RowTile<ROWS, TILE> row_tile(const AttnParams &p, int
 template <int ROWS, int TILE>
 __device__ __forceinline__ int key_tile(const RowTile<ROWS, TILE> &t, int i) { return i < t.first ? i : t.base + i - t.first; }
 
+__device__ __forceinline__ bool takes(const AttnParams &p, int n)
+{
+    const long long rows = (long long)n * p.g;
+    return rows > p.rows_above && rows <= p.rows_upto;
+}
+
 template <int ROWS, int TILE>
 __device__ __forceinline__ long long sequence_tiles(const AttnParams &p, int s, bool report)
 {
@@ -135,14 +143,15 @@ __device__ __forceinline__ long long sequence_tiles(const AttnParams &p, int s, 
         if (report) kv_bad_index(p.b);
         return 0;
     }
+    if (!takes(p, n)) return 0;
     const int nrt = (n * p.g + ROWS - 1) / ROWS;
     long long sum = 0;
-    for (int rt = 0; rt < nrt; ++rt) sum += row_tile<ROWS, TILE>(p, n, pre, rt).tiles;
+    for (int rt = 0; rt < nrt; ++rt) sum += row_tile<ROWS, TILE>(p, n, pre, rt).tiles + p.lead;
     return sum * p.Hk;
 }
 
-// A place on the line: tile `i` of unit (sequence s, row tile rt, key head h); `at` its offset on the line, `unit` the
-// offset of the unit's first tile.
+// A place on the line: place `i` of unit (sequence s, row tile rt, key head h), tile i - lead of it from i = lead on; `at` its
+// offset on the line, `unit` the offset of the unit's first place.
 template <int ROWS, int TILE> struct Cursor {
     int s, rt, h, i;
     int start, n, pre;
@@ -153,7 +162,7 @@ template <int ROWS, int TILE>
 __device__ __forceinline__ bool open_sequence(const AttnParams &p, Cursor<ROWS, TILE> &c)
 {
     for (; c.s < p.b.n_seqs; ++c.s)
-        if (kv_sequence(p.b, c.s, c.start, c.n, c.pre) && c.n > 0) {
+        if (kv_sequence(p.b, c.s, c.start, c.n, c.pre) && takes(p, c.n)) {
             c.rt = 0; c.h = 0; c.i = 0;
             c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, 0);
             return true;
@@ -164,7 +173,7 @@ template <int ROWS, int TILE>
 __device__ __forceinline__ void advance(const AttnParams &p, Cursor<ROWS, TILE> &c)
 {
     ++c.at;
-    if (++c.i < c.t.tiles) return;
+    if (++c.i < c.t.tiles + p.lead) return;
     c.i = 0;
     c.unit = c.at;
     if (++c.h < p.Hk) return;
@@ -175,6 +184,38 @@ __device__ __forceinline__ void advance(const AttnParams &p, Cursor<ROWS, TILE> 
     }
     ++c.s;
     open_sequence(p, c);
+}
+
+// The unit at `c`, as far as it lies in a piece that ends at piece_end: places, of which tiles begin .. begin + count - 1.
+struct UnitPart {
+    int places, begin, count;
+};
+template <int ROWS, int TILE>
+__device__ __forceinline__ UnitPart unit_part(const AttnParams &p, const Cursor<ROWS, TILE> &c, long long piece_end)
+{
+    UnitPart u;
+    u.places = (int)min((long long)(c.t.tiles + p.lead - c.i), piece_end - c.at);
+    u.begin = max(0, c.i - p.lead);
+    u.count = max(0, c.i + u.places - p.lead) - u.begin;
+    return u;
+}
+// On to the next unit, behind the `places` of this one.
+template <int ROWS, int TILE>
+__device__ __forceinline__ void leave_unit(const AttnParams &p, Cursor<ROWS, TILE> &c, int places, long long piece_end)
+{
+    c.at += places;
+    if (c.at < piece_end) {
+        c.i = c.t.tiles + p.lead - 1;
+        --c.at;
+        advance(p, c);
+    }
+}
+// The CTAs that hold tiles of the unit at `c`, by the length `per` of their pieces.
+template <int ROWS, int TILE>
+__device__ __forceinline__ void unit_pieces(const AttnParams &p, const Cursor<ROWS, TILE> &c, long long per, int &c0, int &c1)
+{
+    c0 = (int)div_line(c.unit + p.lead, per);
+    c1 = (int)div_line(c.unit + p.lead + c.t.tiles - 1, per);
 }
 
 // Sets `c` to the start of this CTA's piece and returns its length; `per` is the length of a full piece.
@@ -226,13 +267,13 @@ __device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS
     c.s = (int)sh_found[0];
     c.at = sh_found[1];
     open_sequence(p, c);
-    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
-        c.at += (long long)c.t.tiles * p.Hk;
+    while (c.at + (long long)(c.t.tiles + p.lead) * p.Hk <= begin) {
+        c.at += (long long)(c.t.tiles + p.lead) * p.Hk;
         c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, ++c.rt);
     }
     const int in = (int)(begin - c.at);
-    c.h = in / c.t.tiles;
-    c.i = in - c.h * c.t.tiles;
+    c.h = in / (c.t.tiles + p.lead);
+    c.i = in - c.h * (c.t.tiles + p.lead);
     c.at = begin;
     c.unit = begin - c.i;
     return end - begin;
@@ -254,8 +295,8 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
             const int s = lane + 32 * i;
             if (s < p.b.n_seqs) {
                 if (kv_sequence(p.b, s, start[i], n[i], pre[i])) {
-                    const int nrt = (n[i] * p.g + ROWS - 1) / ROWS;
-                    for (int rt = 0; rt < nrt; ++rt) tiles[i] += row_tile<ROWS, TILE>(p, n[i], pre[i], rt).tiles;
+                    const int nrt = takes(p, n[i]) ? (n[i] * p.g + ROWS - 1) / ROWS : 0;
+                    for (int rt = 0; rt < nrt; ++rt) tiles[i] += row_tile<ROWS, TILE>(p, n[i], pre[i], rt).tiles + p.lead;
                     tiles[i] *= p.Hk;
                 } else if (report) {
                     kv_bad_index(p.b);
@@ -293,13 +334,13 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
         }
     c.rt = 0;
     c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, 0);
-    while (c.at + (long long)c.t.tiles * p.Hk <= begin) {
-        c.at += (long long)c.t.tiles * p.Hk;
+    while (c.at + (long long)(c.t.tiles + p.lead) * p.Hk <= begin) {
+        c.at += (long long)(c.t.tiles + p.lead) * p.Hk;
         c.t = row_tile<ROWS, TILE>(p, c.n, c.pre, ++c.rt);
     }
     const int in = (int)(begin - c.at);
-    c.h = in / c.t.tiles;
-    c.i = in - c.h * c.t.tiles;
+    c.h = in / (c.t.tiles + p.lead);
+    c.i = in - c.h * (c.t.tiles + p.lead);
     c.at = begin;
     c.unit = begin - c.i;
     return end - begin;
@@ -309,6 +350,6 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
 bool kv_tc_takes(const mrp_config &cfg, const mrp_kv_config &kv);
 size_t kv_tc_workspace_bytes();
 cudaError_t kv_tc_attach(Ctx *c);
-cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaStream_t st);
+cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);
 
 }  // namespace mrp

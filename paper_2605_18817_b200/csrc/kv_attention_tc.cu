@@ -484,16 +484,8 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
     long long per;
     const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
                                             : find_piece<NR, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    if (len == 0) cur.at = 0;
     const long long piece_end = len > 0 ? cur.at + len : 0;
-    long long at = len > 0 ? cur.at : 0;
-    auto next_unit = [&](int count) {
-        at += count;
-        if (at < piece_end) {
-            cur.i = cur.t.tiles - 1;
-            cur.at = at - 1;
-            advance(p, cur);
-        }
-    };
 
     if (warp == 0) {
         // ================================ K and V tiles ================================
@@ -501,8 +493,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         uint32_t phase = 0;
         const PageBoxes bx = {box_rows, kTcTile / box_rows};
         bool ok = true;
-        while (ok && at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             auto fetch = [&](int n, const CUtensorMap *map) {
                 ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                 if (!ok) return;
@@ -514,7 +508,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 if (n + 1 < count) fetch(n + 1, &kmap);
                 fetch(n, &vmap);
             }
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     } else if (warp == 1) {
         // ================================ MMAs ================================
@@ -524,8 +518,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         const uint32_t idesc_s = make_idesc(NR), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
-        while (ok && at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const uint32_t sq = base + G::kQAt + (unit & 1u) * G::kQ;
@@ -571,14 +567,15 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 step();
             }
             ++unit;
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     } else if (warp < 4) {
         // ================================ queries, a unit ahead ================================
         uint32_t unit = 0;
         bool ok = true;
-        while (ok && at < piece_end) {
-            const int count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            if (part.count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const int u = unit & 1;
             if (unit >= 2) {
@@ -593,7 +590,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             }
             mbar_arrive(q_ready(u));
             ++unit;
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     } else if (warp >= 4) {
         // ================================ softmax: a thread per key, two warpgroups in turn ================================
@@ -606,8 +603,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         const float sc = p.scale_log2;
         bool ok = true;
         float l[NR];
-        while (at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const int u = unit & 1;
@@ -793,15 +792,16 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     for (int i = 0; i < NR; ++i)
                         if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + wt] = __float2bfloat16_rn(a[i]);
                 } else if (mine) {
-                    float *part = p.part.o + (size_t)slot * NR * 128 + wt;
+                    float *to = p.part.o + (size_t)slot * NR * 128 + wt;
 #pragma unroll
                     for (int i = 0; i < NR; ++i)
-                        if (i < rows) __stcg(part + i * 128, a[i]);
+                        if (i < rows) __stcg(to + i * 128, a[i]);
                 }
                 tc_fence_before();
                 if (!whole_unit) {
                     // ---- the pieces of the unit meet: the CTA that arrives last joins them in order
-                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
+                    int c0, c1;
+                    unit_pieces(p, cur, per, c0, c1);
                     wg_sync(bar_id);
                     if (wt == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
                     wg_sync(bar_id);
@@ -818,7 +818,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             }
             k0 += (uint32_t)count;
             ++unit;
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     }
 
@@ -900,17 +900,8 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     long long per;
     const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
                                             : find_piece<kRows, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    if (len == 0) cur.at = 0;
     const long long piece_end = len > 0 ? cur.at + len : 0;
-    long long at = len > 0 ? cur.at : 0;
-    // (all roles walk the same units; a unit of the piece: tiles begin .. begin + count - 1 of cur.t)
-    auto next_unit = [&](int count) {
-        at += count;
-        if (at < piece_end) {
-            cur.i = cur.t.tiles - 1;
-            cur.at = at - 1;
-            advance(p, cur);
-        }
-    };
 
     if (warp == 0) {
         // ================================ TMA producer ================================
@@ -918,8 +909,10 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         uint32_t phase = 0;
         const PageBoxes bx = {box_rows, kTcTile / box_rows};
         bool ok = true;
-        while (ok && at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             auto fetch = [&](int n, int which) {
                 ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
@@ -933,7 +926,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 if (n + 1 < count) fetch(n + 1, 0);
                 if (NT == 1) fetch(n, 1);
             }
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     } else if (warp == 1) {
         // ================================ MMA issuer ================================
@@ -967,8 +960,10 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (elect_one()) umma_commit(empty_bar(s));
             __syncwarp();
         };
-        while (ok && at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             Suspects &sus = suspects[unit & 1];
@@ -1039,7 +1034,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 }
             }
             ++unit;
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     } else {
         // ================================ softmax: two threads per row ================================
@@ -1056,8 +1051,10 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         auto wait_pv = [&](uint32_t kk) {
             return NT == 2 ? mbar_wait(pv_done(x), kk & 1u, abort_flag, ws) : mbar_wait(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
         };
-        while (at < piece_end) {
-            const int begin = cur.i, count = (int)min((long long)(cur.t.tiles - cur.i), piece_end - at);
+        while (cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
@@ -1191,7 +1188,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                            pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
                 };
                 const int slot = (2 * (int)blockIdx.x + (begin == 0 ? 1 : 0)) * NT + x;
-                float4 *part = reinterpret_cast<float4 *>(p.part.o);       // slot: [DB * 16][128 rows] float4
+                float4 *parts = reinterpret_cast<float4 *>(p.part.o);       // slot: [DB * 16][128 rows] float4
                 if (whole_unit && lse) *lse = log_sum(m, L);
                 if (!whole_unit && live && half == 0) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, L));
                 const float inv = inverse(L);
@@ -1206,13 +1203,14 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     } else if (live) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(part + ((size_t)slot * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+                            __stcg(parts + ((size_t)slot * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
                     }
                 }
                 tc_fence_before();
                 if (!whole_unit) {
                     // ---- the pieces of these 32 rows meet: the pair that arrives last joins them in order
-                    const int c0 = (int)div_line(cur.unit, per), c1 = (int)div_line(cur.unit + t.tiles - 1, per);
+                    int c0, c1;
+                    unit_pieces(p, cur, per, c0, c1);
                     int *counter = p.part.counters + (c0 * NT + x) * 4 + wq;
                     any_of(pair, 64, false);
                     if (half == 0 && lane == 0) sh_last[x][wq] = arrive_acq_rel(counter) == c1 - c0;
@@ -1234,7 +1232,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                     const size_t sl = slot_of(min(cb + y, c1));
                                     ml[y] = __ldcg(p.part.ml + sl * 128 + row);
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) a[y][i] = __ldcg(part + (sl * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
+                                    for (int i = 0; i < 8; ++i) a[y][i] = __ldcg(parts + (sl * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
                                 }
 #pragma unroll
                                 for (int y = 0; y < U; ++y)
@@ -1258,7 +1256,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 }
             }
             ++unit;
-            next_unit(count);
+            leave_unit(p, cur, part.places, piece_end);
         }
     }
 
@@ -1355,7 +1353,7 @@ cudaError_t kv_tc_attach(Ctx *c)
     return cudaSuccess;
 }
 
-cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaStream_t st)
+cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
 {
     const int box = tc_box_rows(c->kv.page_size);
     CUtensorMap km, vm;
@@ -1364,15 +1362,37 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, int max_new, cudaSt
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
-    const long long rows = (long long)max_new * p.g;
-    const bool one_block = c->kv.head_dim <= 64, two = rows > 128;
-    // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 69 us on the
-    // transposed kernel, 76 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
+    const long long rows = (long long)batch.max_new * p.g;
+    const bool narrow = c->kv.head_dim <= 64;
+    auto few = [&]() {
+        p.min_piece = 1;
+        p.lead = 2;
+        return narrow ? few_launch<1>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
+    };
+    // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 65 us on the
+    // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
     // took 95 and 113 against 78 and 80.  Beyond 128 rows two row tiles share the stream of K and V.
-    if (rows <= kFewRows) return one_block ? few_launch<1>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
+    if (rows <= kFewRows) return few();
+    // A step of single tokens beside a prompt: where most sequences must be far shorter than the longest, those of up to 16
+    // rows go to the transposed kernel in a launch of their own.
+    int launches = 0;
+    if ((long long)batch.n_tokens * 4 < (long long)batch.n_seqs * batch.max_new) {
+        p.rows_upto = kFewRows;
+        const cudaError_t e = few();
+        if (e != cudaSuccess) return e;
+        launches = c->launches;
+        p.rows_above = kFewRows;
+        p.rows_upto = INT_MAX;
+    }
+    // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
+    const bool two = rows > 128;
     p.min_piece = two ? 1 : 2;
-    if (one_block) return two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
-    return two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
+    p.lead = two ? 4 : 3;
+    cudaError_t e;
+    if (narrow) e = two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
+    else e = two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
+    c->launches += launches;
+    return e;
 }
 
 }  // namespace mrp
