@@ -1385,7 +1385,9 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
         p.rows_upto = INT_MAX;
     }
     // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
-    const bool two = rows > 128;
+    // Two row tiles share the stream of K and V where there are units for all SMs; with fewer the smaller units end sooner (512
+    // tokens alone 28 against 27 us, 1024 44 against 36, 2048 74 against 78; 24 blocks of 33 behind 3000 102 against 120).
+    const bool two = rows > 128 && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
     p.min_piece = two ? 1 : 2;
     p.lead = two ? 4 : 3;
     cudaError_t e;
