@@ -33,15 +33,22 @@ struct WaitStatus {
     int32_t *status, *user_status;
 };
 
-template <int DB, int NT> struct TcGeo {   // DB: 64-feature blocks of a head
-    static constexpr int kTileBytes = DB * 128 * 128;
-    static constexpr int kStages = DB == 2 ? (NT == 2 ? 4 : 5) : 10;
-    static constexpr int kQ = NT * kTileBytes;
-    static constexpr int kRing = kStages * kTileBytes;
+// A head is NB blocks of 64 features (1, 2 or 4); a ring stage holds DB of them (1 or 2) of a K or V tile, HB stages a tile.
+template <int NB> struct Blocks {
+    static constexpr int DB = NB >= 2 ? 2 : 1, HB = NB / DB;
+    static constexpr int kStageBytes = DB * 128 * 128;
+};
+template <int NB, int NT> struct TcGeo {
+    typedef Blocks<NB> B;
+    static constexpr int kStages = B::DB == 1 ? 10 : B::HB == 2 || NT == 2 ? 4 : 5;
+    static constexpr int kQTile = NB * 128 * 128;          // queries of a row tile
+    static constexpr int kQ = NT * kQTile;
+    static constexpr int kRing = kStages * B::kStageBytes;
     static constexpr int kBars = kQ + kRing;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
     static constexpr int kThreads = 64 + NT * 256;
     static constexpr int kRows = NT * 128;
+    static_assert(NT == 1 || NB <= 2, "tensor memory: two row tiles of accumulators of at most 128 features");
 };
 
 struct Suspects {                          // boundary tiles with V rows that were zeroed for what they held
@@ -121,18 +128,19 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
 // rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it.
 constexpr int kFewRows = 16;
-template <int DB> struct FewGeo {
+template <int NB> struct FewGeo {
+    typedef Blocks<NB> B;
     static constexpr int NR = kFewRows;
-    static constexpr int kCols = 2 * NR;                   // columns of P and of an accumulator: hi, lo
-    static constexpr int kTileBytes = DB * 128 * 128;
-    static constexpr int kStages = DB == 2 ? 5 : 10;
-    static constexpr int kRing = kStages * kTileBytes;
+    static constexpr int kCols = 2 * NR;                   // columns of P and of an accumulator of 128 features: hi, lo
+    static constexpr int kStages = B::DB == 2 ? 5 : 10;
+    static constexpr int kRing = kStages * B::kStageBytes;
     static constexpr int kP = 128 * 128;                   // P of a warpgroup: 128 keys, rows of 128 bytes
-    static constexpr int kQ = DB * NR * 128;               // queries of a unit, two of them
+    static constexpr int kQ = NB * NR * 128;               // queries of a unit, two of them
     static constexpr int kPAt = kRing, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;
-    static constexpr int kTmem = 128;                      // of which 2 NR + 2 kCols are used
+    static constexpr int kTmem = B::HB == 2 ? 256 : 128;   // of which 2 NR + 2 HB kCols are used
     static constexpr int kThreads = 384;
+    static constexpr int kWide = B::HB * 128;              // features of a row of partial results
 };
 constexpr float kNone = -3.4028234e38f;    // the maximum of a row that has seen nothing
 
@@ -208,13 +216,13 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t block)
     return d;
 }
 
-// The pages of a K or V tile's visible positions -> a ring stage; the whole warp.
+// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
 struct PageBoxes {
     int box_rows, pages;
 };
 template <int DB, typename Tile>
 __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const Tile &t, int n, int s,
-                                           int h, uint32_t dst, uint32_t bar, int lane)
+                                           int h, int feature, uint32_t dst, uint32_t bar, int lane)
 {
     const int j = key_tile(t, n) * kTcTile + lane * bx.box_rows;
     const bool need = lane < bx.pages && ((j < t.hi && j + bx.box_rows > t.lo) || j < t.s1);
@@ -234,16 +242,16 @@ __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMa
     if (need) {
 #pragma unroll
         for (int x = 0; x < DB; ++x)
-            tma_load_page(dst + lane * bx.box_rows * 128 + x * (128 * 128), map, 64 * x, row, h, entry, bar);
+            tma_load_page(dst + lane * bx.box_rows * 128 + x * (128 * 128), map, feature + 64 * x, row, h, entry, bar);
     }
 }
 
 // Query rows r0.. of a tile (those below `rows`; zeros beyond, and beyond the head's features) -> shared memory, as K-major
 // blocks of 64 features.  THREADS threads, all copies in flight together.
-template <int DB, int ROWS, int THREADS>
+template <int NB, int ROWS, int THREADS>
 __device__ __forceinline__ void load_queries(const AttnParams &p, int start, int h, int r0, int rows, uint32_t sq, int tid)
 {
-    constexpr int kRow = 8 * DB, kStep = THREADS / kRow;   // 16-byte chunks of a row; rows a round
+    constexpr int kRow = 8 * NB, kStep = THREADS / kRow;   // 16-byte chunks of a row; rows a round
     static_assert(THREADS % kRow == 0 && ROWS % kStep == 0, "whole rounds");
     const int ch = tid % kRow;
     const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)start * p.q_stride + (int64_t)h * p.g * p.D;
@@ -360,66 +368,70 @@ __device__ __forceinline__ JoinArgs join_args(const AttnParams &p, int start, in
     a.r0 = r0; a.rows = rows; a.c0 = c0; a.c1 = c1;
     return a;
 }
-template <int NR, int RG, int U>
+template <int NR, int WIDE, int RG, int U>
 __device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
 {
     const int rows = p.rows, c0 = p.c0, c1 = p.c1;
-    const bool mine = 4 * lane < p.D;
 #pragma unroll 1
-    for (int rb = w; rb < rows; rb += 4 * RG) {
-        float M[RG], L[RG];
-        float4 a[RG];
-#pragma unroll
-        for (int y = 0; y < RG; ++y) { M[y] = kNone; L[y] = 0.f; a[y] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    for (int f0 = 0; f0 < WIDE; f0 += 128) {
+        const bool mine = f0 + 4 * lane < p.D;
 #pragma unroll 1
-        for (int cb = c0; cb <= c1; cb += U) {
-            float2 ml[RG][U];
-            float4 o[RG][U];
+        for (int rb = w; rb < rows; rb += 4 * RG) {
+            float M[RG], L[RG];
+            float4 a[RG];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int c = min(cb + i, c1);
-                const size_t sl = (size_t)(2 * c + (c == c0)) * NR;
+            for (int y = 0; y < RG; ++y) { M[y] = kNone; L[y] = 0.f; a[y] = make_float4(0.f, 0.f, 0.f, 0.f); }
+#pragma unroll 1
+            for (int cb = c0; cb <= c1; cb += U) {
+                float2 ml[RG][U];
+                float4 o[RG][U];
 #pragma unroll
-                for (int y = 0; y < RG; ++y) {
-                    const int r = min(rb + 4 * y, rows - 1);
-                    ml[y][i] = __ldcg(p.ml + sl + r);
-                    o[y][i] = __ldcg(reinterpret_cast<const float4 *>(p.o + (sl + r) * 128) + (mine ? lane : 0));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (cb + i <= c1) {
+                for (int i = 0; i < U; ++i) {
+                    const int c = min(cb + i, c1);
+                    const size_t sl = (size_t)(2 * c + (c == c0)) * NR;
 #pragma unroll
                     for (int y = 0; y < RG; ++y) {
-                        const float nm = fmaxf(M[y], ml[y][i].x);
-                        const float f = M[y] == nm ? 1.f : ex2f(M[y] - nm), e = ml[y][i].x == nm ? 1.f : ex2f(ml[y][i].x - nm);
-                        M[y] = nm;
-                        L[y] = fmaf(e, ml[y][i].y, L[y] * f);
-                        a[y].x = fmaf(e, o[y][i].x, a[y].x * f); a[y].y = fmaf(e, o[y][i].y, a[y].y * f);
-                        a[y].z = fmaf(e, o[y][i].z, a[y].z * f); a[y].w = fmaf(e, o[y][i].w, a[y].w * f);
+                        const int r = min(rb + 4 * y, rows - 1);
+                        ml[y][i] = __ldcg(p.ml + sl + r);
+                        o[y][i] = __ldcg(reinterpret_cast<const float4 *>(p.o + (sl + r) * WIDE) + (mine ? f0 / 4 + lane : 0));
                     }
                 }
-        }
 #pragma unroll
-        for (int y = 0; y < RG; ++y) {
-            const int r = rb + 4 * y;
-            if (r < rows && mine) {
-                const float inv = inverse(L[y]);
-                const int rr = p.r0 + r, tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
-                __nv_bfloat16 *dst = p.out + (int64_t)tok * p.out_stride + (int64_t)hg * p.D + 4 * lane;
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(a[y].x * inv, a[y].y * inv), pack_bf16(a[y].z * inv, a[y].w * inv));
-                if (lane == 0 && p.lse) p.lse[(int64_t)tok * p.H + hg] = log_sum(M[y], L[y]);
+                for (int i = 0; i < U; ++i)
+                    if (cb + i <= c1) {
+#pragma unroll
+                        for (int y = 0; y < RG; ++y) {
+                            const float nm = fmaxf(M[y], ml[y][i].x);
+                            const float f = M[y] == nm ? 1.f : ex2f(M[y] - nm), e = ml[y][i].x == nm ? 1.f : ex2f(ml[y][i].x - nm);
+                            M[y] = nm;
+                            L[y] = fmaf(e, ml[y][i].y, L[y] * f);
+                            a[y].x = fmaf(e, o[y][i].x, a[y].x * f); a[y].y = fmaf(e, o[y][i].y, a[y].y * f);
+                            a[y].z = fmaf(e, o[y][i].z, a[y].z * f); a[y].w = fmaf(e, o[y][i].w, a[y].w * f);
+                        }
+                    }
             }
-        }
+#pragma unroll
+            for (int y = 0; y < RG; ++y) {
+                const int r = rb + 4 * y;
+                if (r < rows && mine) {
+                    const float inv = inverse(L[y]);
+                    const int rr = p.r0 + r, tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
+                    __nv_bfloat16 *dst = p.out + (int64_t)tok * p.out_stride + (int64_t)hg * p.D + f0 + 4 * lane;
+                    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(a[y].x * inv, a[y].y * inv), pack_bf16(a[y].z * inv, a[y].w * inv));
+                    if (f0 + lane == 0 && p.lse) p.lse[(int64_t)tok * p.H + hg] = log_sum(M[y], L[y]);
+                }
+            }
+    }
     }
 }
 
-template <int DB>
+template <int NB>
 __global__ void __launch_bounds__(384, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, int box_rows)
 {
-    typedef FewGeo<DB> G;
+    typedef FewGeo<NB> G;
+    constexpr int DB = G::B::DB, HB = G::B::HB;
     constexpr int NR = kFewRows;
     typedef RowTile<NR, kTcTile> Tile;
     extern __shared__ unsigned char smem_raw[];
@@ -476,7 +488,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
     tc_fence_after();
     const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators
     auto s_at = [&](int x) { return tmem + x * NR; };
-    auto o_at = [&](int x) { return tmem + 2 * NR + x * G::kCols; };
+    auto o_at = [&](int x) { return tmem + 2 * NR + x * HB * G::kCols; };         // (HB accumulators of 128 features)
     pdl_wait();
     pdl_trigger();
 
@@ -498,10 +510,13 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             const int begin = part.begin, count = part.count;
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             auto fetch = [&](int n, const CUtensorMap *map) {
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
-                if (!ok) return;
-                fetch_tile<DB>(p, map, bx, cur.t, begin + n, cur.s, cur.h, ring + stage * G::kTileBytes, full_bar(stage), lane);
-                if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    if (!ok) return;
+                    fetch_tile<DB>(p, map, bx, cur.t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+                }
             };
             fetch(0, &kmap);
             for (int n = 0; n < count; ++n) {
@@ -530,41 +545,48 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             Suspects &sus = suspects[unit & 1];            // (the unit before the last is written: see the query warps)
             if (lane == 0) sus.n = 0;
             __syncwarp();
-            auto scores = [&](uint32_t kk) {               // S^T of tile kk from the stage at hand
-                wait(full_bar(stage), phase);
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t ks = ring + stage * G::kTileBytes;
-                if (elect_one()) {
+            auto scores = [&](uint32_t kk) {               // S^T of tile kk from the stages at hand
 #pragma unroll
-                    for (int c = 0; c < 4 * DB; ++c)
-                        umma_bf16(s_at(kk & 1u), make_smem_desc(ks + (c >> 2) * (128 * 128) + (c & 3) * 32),
-                                  make_smem_desc(sq + (c >> 2) * (NR * 128) + (c & 3) * 32), idesc_s, c > 0);
-                    umma_commit(s_full(kk & 1u));
-                    umma_commit(empty_bar(stage));
+                for (int y = 0; y < HB; ++y) {
+                    wait(full_bar(stage), phase);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint32_t ks = ring + stage * G::B::kStageBytes, qs = sq + y * DB * (NR * 128);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int c = 0; c < 4 * DB; ++c)
+                            umma_bf16(s_at(kk & 1u), make_smem_desc(ks + (c >> 2) * (128 * 128) + (c & 3) * 32),
+                                      make_smem_desc(qs + (c >> 2) * (NR * 128) + (c & 3) * 32), idesc_s, y + c > 0);
+                        if (y + 1 == HB) umma_commit(s_full(kk & 1u));
+                        umma_commit(empty_bar(stage));
+                    }
+                    __syncwarp();
+                    step();
                 }
-                __syncwarp();
-                step();
             };
             scores(k);
             for (int n = 0; n < count && ok; ++n, ++k) {
                 if (n + 1 < count) scores(k + 1);
-                wait(full_bar(stage), phase);
-                if (!ok) break;
-                const uint32_t vs = ring + stage * G::kTileBytes, ps = base + G::kPAt + (k & 1u) * G::kP;
-                clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
-                wait(p_ready(k & 1u), (k >> 1) & 1u);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
+                const uint32_t ps = base + G::kPAt + (k & 1u) * G::kP;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)            // (one block of features: the second 64 lanes repeat it)
-                        umma_bf16(o_at(k & 1u), mn_desc(vs + c * 2048, DB == 2 ? 128 * 128 : 0), mn_desc(ps + c * 2048, 0), idesc_o, n >= 2 || c > 0);
-                    umma_commit(pv_done(k & 1u));
-                    umma_commit(empty_bar(stage));
+                for (int y = 0; y < HB; ++y) {
+                    wait(full_bar(stage), phase);
+                    if (!ok) break;
+                    const uint32_t vs = ring + stage * G::B::kStageBytes;
+                    clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
+                    if (y == 0) wait(p_ready(k & 1u), (k >> 1) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)        // (one block of features: the second 64 lanes repeat it)
+                            umma_bf16(o_at(k & 1u) + y * G::kCols, mn_desc(vs + c * 2048, DB == 2 ? 128 * 128 : 0), mn_desc(ps + c * 2048, 0), idesc_o, n >= 2 || c > 0);
+                        if (y + 1 == HB) umma_commit(pv_done(k & 1u));
+                        umma_commit(empty_bar(stage));
+                    }
+                    __syncwarp();
+                    step();
                 }
-                __syncwarp();
-                step();
             }
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
@@ -582,7 +604,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 ok = __all_sync(0xffffffffu, mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws));
                 if (!ok) break;
             }
-            load_queries<DB, NR, 64>(p, cur.start, cur.h, t.r0, t.rows, base + G::kQAt + u * G::kQ, tid - 64);
+            load_queries<NB, NR, 64>(p, cur.start, cur.h, t.r0, t.rows, base + G::kQAt + u * G::kQ, tid - 64);
             for (int r = tid - 64; r < NR; r += 64) {
                 const int pos = cur.pre + fast_div(t.r0 + min(r, t.rows - 1), p.gdiv);
                 sh_hi[u][r] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
@@ -682,7 +704,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                         }
                         // (the product of this warpgroup's last tile is done: S of this one came after it)
 #pragma unroll 1
-                        for (int r0 = 0; r0 < G::kCols; r0 += 16) {
+                        for (int r0 = 0; r0 < HB * G::kCols; r0 += 16) {
                             float o[16];
                             tmem_ld_n<16>(o_tm + r0, o);
                             uint32_t w[16];
@@ -770,32 +792,35 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     }
                 }
                 wg_sync(bar_id);
-                const bool mine = wt < p.D;                // a thread per feature
-                float a[NR], o[4][NR];
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    if (has[y]) {
-                        tmem_ld16_go(o_at(y) + lanes, o[2 * y]);
-                        tmem_ld16_go(o_at(y) + lanes + NR, o[2 * y + 1]);
+                for (int y = 0; y < HB; ++y) {             // a thread per feature, of each 128
+                    const int f = y * 128 + wt;
+                    float a[NR], o[4][NR];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z)
+                        if (has[z]) {
+                            tmem_ld16_go(o_at(z) + y * G::kCols + lanes, o[2 * z]);
+                            tmem_ld16_go(o_at(z) + y * G::kCols + lanes + NR, o[2 * z + 1]);
+                        }
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) tmem_landed16(o[z]);
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) {
+                        a[i] = 0.f;
+                        if (has[0]) a[i] = (o[0][i] + o[1][i]) * sh_f[0][i];
+                        if (has[1]) a[i] = fmaf(o[2][i] + o[3][i], sh_f[1][i], a[i]);
                     }
-                tmem_wait_ld();
+                    if (f < p.D && whole_unit) {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) tmem_landed16(o[y]);
+                        for (int i = 0; i < NR; ++i)
+                            if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + f] = __float2bfloat16_rn(a[i]);
+                    } else if (f < p.D) {
+                        float *to = p.part.o + (size_t)slot * NR * G::kWide + f;
 #pragma unroll
-                for (int i = 0; i < NR; ++i) {
-                    a[i] = 0.f;
-                    if (has[0]) a[i] = (o[0][i] + o[1][i]) * sh_f[0][i];
-                    if (has[1]) a[i] = fmaf(o[2][i] + o[3][i], sh_f[1][i], a[i]);
-                }
-                if (mine && whole_unit) {
-#pragma unroll
-                    for (int i = 0; i < NR; ++i)
-                        if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + wt] = __float2bfloat16_rn(a[i]);
-                } else if (mine) {
-                    float *to = p.part.o + (size_t)slot * NR * 128 + wt;
-#pragma unroll
-                    for (int i = 0; i < NR; ++i)
-                        if (i < rows) __stcg(to + i * 128, a[i]);
+                        for (int i = 0; i < NR; ++i)
+                            if (i < rows) __stcg(to + i * G::kWide, a[i]);
+                    }
                 }
                 tc_fence_before();
                 if (!whole_unit) {
@@ -807,8 +832,8 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     wg_sync(bar_id);
                     if (sh_last) {
                         const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
-                        if (rows <= 4) join_rows<NR, 1, 8>(ja, wq, lane);
-                        else join_rows<NR, 2, 4>(ja, wq, lane);
+                        if (rows <= 4) join_rows<NR, G::kWide, 1, 8>(ja, wq, lane);
+                        else join_rows<NR, G::kWide, 2, 4>(ja, wq, lane);
                         if (wt == 0) p.part.counters[c0] = 0;
                     }
                 }
@@ -837,12 +862,13 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
 
 // ======================================================================================================================
 // Many rows: row tiles of 128 on the lanes (NT = 1: 65 to 128 rows; NT = 2: prompts).
-template <int DB, int NT>
-__global__ void __launch_bounds__(TcGeo<DB, NT>::kThreads, 1)
+template <int NB, int NT>
+__global__ void __launch_bounds__(TcGeo<NB, NT>::kThreads, 1)
 kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                        const __grid_constant__ CUtensorMap vmap, int box_rows)
 {
-    typedef TcGeo<DB, NT> G;
+    typedef TcGeo<NB, NT> G;
+    constexpr int DB = G::B::DB, HB = G::B::HB;
     constexpr int kRows = G::kRows;
     typedef RowTile<kRows, kTcTile> Tile;
     extern __shared__ unsigned char smem_raw[];
@@ -915,10 +941,13 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             auto fetch = [&](int n, int which) {
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
-                if (!ok) return;
-                fetch_tile<DB>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, ring + stage * G::kTileBytes, full_bar(stage), lane);
-                if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    if (!ok) return;
+                    fetch_tile<DB>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+                }
             };
             fetch(0, 0);
             for (int n = 0; n < count; ++n) {              // the order in which the MMA warp takes them
@@ -936,23 +965,24 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         const uint32_t idesc_s = make_idesc(128), idesc_o = make_idesc(DB * 64) | (1u << 16);
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
-        auto mma_s = [&](int x, int row_tile, uint32_t ks) {       // S buffer x = Q_row_tile K^T
+        auto mma_s = [&](int x, int row_tile, uint32_t ks, int y) {        // S buffer x (+)= Q_row_tile K^T, features 128 y ..
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4 * DB; ++c) {
                     const uint32_t off = (c >> 2) * (128 * 128) + (c & 3) * 32;
-                    umma_bf16(tmem + x * 128, make_smem_desc(sq + row_tile * G::kTileBytes + off), make_smem_desc(ks + off), idesc_s, c > 0);
+                    umma_bf16(tmem + x * 128, make_smem_desc(sq + row_tile * G::kQTile + y * G::B::kStageBytes + off), make_smem_desc(ks + off), idesc_s, y + c > 0);
                 }
-                umma_commit(s_full(x));
+                if (y + 1 == HB) umma_commit(s_full(x));
             }
             __syncwarp();
         };
-        auto mma_o = [&](int x, int row_tile, uint32_t vs, int c0, bool first) {     // O_row_tile += P_x V, keys 16 c0 .. 16 c0 + 63
+        // O_row_tile += P_x V, keys 16 c0 .. 16 c0 + 63, features 128 y ..
+        auto mma_o = [&](int x, int row_tile, uint32_t vs, int y, int c0, bool first) {
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    umma_ts(tmem + 256 + row_tile * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2048, 128 * 128), idesc_o, !first || c0 + c > 0);
-                if (c0 == 4) umma_commit(pv_done(x));
+                    umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2048, 128 * 128), idesc_o, !first || c0 + c > 0);
+                if (c0 == 4 && y + 1 == HB) umma_commit(pv_done(x));
             }
             __syncwarp();
         };
@@ -970,19 +1000,22 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (lane == 0) sus.n = 0;
             __syncwarp();
             auto clean = [&](int n, uint32_t vs) { clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
+            auto at_stage = [&](int s) { return ring + s * G::B::kStageBytes; };
 #pragma unroll
             for (int x = 0; x < NT; ++x) wait(q_ready(x), unit & 1u);
-            wait(full_bar(stage), phase);
-            if (!ok) break;
-            tc_fence_after();
-            if constexpr (NT == 2) {
-                mma_s(0, 0, ring + stage * G::kTileBytes);
-                mma_s(1, 1, ring + stage * G::kTileBytes);
-            } else {
-                mma_s(k & 1u, 0, ring + stage * G::kTileBytes);
-            }
-            release(stage);
-            step();
+            auto first_scores = [&](int x0) {              // S of the tile whose K is next in the ring, for all row tiles
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(full_bar(stage), phase);
+                    if (!ok) return;
+                    tc_fence_after();
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) mma_s(NT == 2 ? x : x0, x, at_stage(stage), y);
+                    release(stage);
+                    step();
+                }
+            };
+            first_scores(k & 1u);
             for (int n = 0; n < count && ok; ++n, ++k) {
                 if constexpr (NT == 2) {
                     const int sv = stage;
@@ -993,44 +1026,46 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     if (n + 1 < count) step();
                     wait(full_bar(sv), pv);
                     if (!ok) break;
-                    clean(n, ring + sv * G::kTileBytes);
+                    clean(n, at_stage(sv));
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         wait(p_half(x), k & 1u);
                         if (!ok) break;
                         tc_fence_after();
-                        mma_o(x, x, ring + sv * G::kTileBytes, 0, n == 0);
+                        mma_o(x, x, at_stage(sv), 0, 0, n == 0);
                         wait(p_ready(x), k & 1u);
                         if (n + 1 < count && x == 0) wait(full_bar(sk), pk);
                         if (!ok) break;
                         tc_fence_after();
-                        mma_o(x, x, ring + sv * G::kTileBytes, 4, n == 0);
-                        if (n + 1 < count) mma_s(x, x, ring + sk * G::kTileBytes);
+                        mma_o(x, x, at_stage(sv), 0, 4, n == 0);
+                        if (n + 1 < count) mma_s(x, x, at_stage(sk), 0);
                     }
                     if (!ok) break;
                     release(sv);
                     if (n + 1 < count) release(sk);
                 } else {
-                    if (n + 1 < count) {
+                    if (n + 1 < count) first_scores((k + 1) & 1u);
+                    int sv[HB];
+#pragma unroll
+                    for (int y = 0; y < HB; ++y) {
                         wait(full_bar(stage), phase);
                         if (!ok) break;
-                        mma_s((k + 1) & 1u, 0, ring + stage * G::kTileBytes);
-                        release(stage);
+                        clean(n, at_stage(stage));
+                        if (y == 0) wait(p_half(k & 1u), (k >> 1) & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        sv[y] = stage;
+                        mma_o(k & 1u, 0, at_stage(stage), y, 0, n == 0);
                         step();
                     }
-                    wait(full_bar(stage), phase);
-                    if (!ok) break;
-                    clean(n, ring + stage * G::kTileBytes);
-                    wait(p_half(k & 1u), (k >> 1) & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    mma_o(k & 1u, 0, ring + stage * G::kTileBytes, 0, n == 0);
                     wait(p_ready(k & 1u), (k >> 1) & 1u);
                     if (!ok) break;
                     tc_fence_after();
-                    mma_o(k & 1u, 0, ring + stage * G::kTileBytes, 4, n == 0);
-                    release(stage);
-                    step();
+#pragma unroll
+                    for (int y = 0; y < HB; ++y) {
+                        mma_o(k & 1u, 0, at_stage(sv[y]), y, 4, n == 0);
+                        release(sv[y]);
+                    }
                 }
             }
             ++unit;
@@ -1042,7 +1077,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         const int wq = warp & 3, row = wq * 32 + lane;     // lane quarter of tensor memory, row of the row tile
         const int pair = 1 + x * 4 + wq;                   // barrier of the two warps that share 32 rows
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t o_tm = tmem + 256 + x * 128 + half * (DB * 32) + lanes;
+        const uint32_t o_tm = tmem + 256 + x * 128 + half * (NB * 32) + lanes;
         uint32_t k = 0, unit = 0;
         bool ok = true;
         const float sc = p.scale_log2;
@@ -1058,7 +1093,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
-            load_queries<DB, 128, 256>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kTileBytes, half * 128 + row);
+            load_queries<NB, 128, 256>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kQTile, half * 128 + row);
             mbar_arrive(q_ready(x));
             // ---- what the row sees; what all rows of the warp see
             const bool live = row < rows, warp_live = wq * 32 < rows;
@@ -1122,7 +1157,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                             if (any_of(pair, 64, !ok)) { ok = false; break; }
                             tc_fence_after();
 #pragma unroll 1
-                            for (int f = 0; f < DB * 2; ++f) {
+                            for (int f = 0; f < NB * 2; ++f) {
                                 float o[16];
                                 tmem_ld_n<16>(o_tm + 16 * f, o);
                                 uint32_t w[16];
@@ -1176,7 +1211,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 if (sus.n > 0 && suspects_hit(sus, hi_r, lo_r, p.sinks)) L = __int_as_float(0x7FC00000);
                 const bool whole_unit = count == t.tiles;
                 const int rr = t.r0 + x * 128 + row, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
-                const int f0 = half * (DB * 32);           // this half's features
+                const int f0 = half * (NB * 32);           // this half's features
                 __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D + f0;
                 float *lse = p.lse && live && half == 0 ? p.lse + (int64_t)(cur.start + tok) * p.H + head : nullptr;
                 auto put32 = [&](int f, const float *o, float inv) {       // 32 features from f0 + f
@@ -1188,12 +1223,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                            pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
                 };
                 const int slot = (2 * (int)blockIdx.x + (begin == 0 ? 1 : 0)) * NT + x;
-                float4 *parts = reinterpret_cast<float4 *>(p.part.o);       // slot: [DB * 16][128 rows] float4
+                float4 *parts = reinterpret_cast<float4 *>(p.part.o);       // slot: [NB * 16][128 rows] float4
                 if (whole_unit && lse) *lse = log_sum(m, L);
                 if (!whole_unit && live && half == 0) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, L));
                 const float inv = inverse(L);
 #pragma unroll 1
-                for (int f = 0; f < DB; ++f) {
+                for (int f = 0; f < NB; ++f) {
                     float o[32];
                     tmem_ld32(o_tm + 32 * f, o);
                     tmem_wait_ld();
@@ -1203,7 +1238,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     } else if (live) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(parts + ((size_t)slot * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+                            __stcg(parts + ((size_t)slot * (NB * 16) + f0 / 4 + f * 8 + i) * 128 + row, make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
                     }
                 }
                 tc_fence_before();
@@ -1219,7 +1254,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                         constexpr int U = NT == 1 ? 2 : 1;             // pieces in flight (registers)
                         auto slot_of = [&](int c) { return (size_t)((2 * c + (c == c0)) * NT + x); };
 #pragma unroll 1
-                        for (int f = 0; f < DB; ++f) {
+                        for (int f = 0; f < NB; ++f) {
                             float M = -INFINITY, S = 0.f, o[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0.f;
@@ -1232,7 +1267,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                     const size_t sl = slot_of(min(cb + y, c1));
                                     ml[y] = __ldcg(p.part.ml + sl * 128 + row);
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) a[y][i] = __ldcg(parts + (sl * (DB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
+                                    for (int i = 0; i < 8; ++i) a[y][i] = __ldcg(parts + (sl * (NB * 16) + f0 / 4 + f * 8 + i) * 128 + row);
                                 }
 #pragma unroll
                                 for (int y = 0; y < U; ++y)
@@ -1273,31 +1308,31 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     }
 }
 
-template <int DB, int NT>
+template <int NB, int NT>
 cudaError_t tc_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_tc_kernel<DB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<DB, NT>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_tc_kernel<NB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<NB, NT>::kSmem);
 }
-template <int DB, int NT>
+template <int NB, int NT>
 cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_tc_kernel<DB, NT>, dim3(sms), dim3(TcGeo<DB, NT>::kThreads), TcGeo<DB, NT>::kSmem, st,
+    cudaError_t e = launch_k(kv_attention_tc_kernel<NB, NT>, dim3(sms), dim3(TcGeo<NB, NT>::kThreads), TcGeo<NB, NT>::kSmem, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
     c->launches = 1;
     return note_err(c, e, "kv_attention_tc_kernel");
 }
 
-template <int DB>
+template <int NB>
 cudaError_t few_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_few_kernel<DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<DB>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_few_kernel<NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<NB>::kSmem);
 }
-template <int DB>
+template <int NB>
 cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_few_kernel<DB>, dim3(sms), dim3(FewGeo<DB>::kThreads), FewGeo<DB>::kSmem, st,
+    cudaError_t e = launch_k(kv_attention_few_kernel<NB>, dim3(sms), dim3(FewGeo<NB>::kThreads), FewGeo<NB>::kSmem, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
     c->launches = 1;
     return note_err(c, e, "kv_attention_few_kernel");
@@ -1327,14 +1362,14 @@ bool page_map(Ctx *c, CUtensorMap *map, const void *pool, int box)
 
 bool kv_tc_takes(const mrp_config &cfg, const mrp_kv_config &kv)
 {
-    // (strides of a tensor map: multiples of 16 bytes below 2^40; heads narrower than 64 would be mostly padding)
-    return cfg.dtype == MRP_BF16 && kv.n_pages > 0 && kv.head_dim >= 64 && kv.head_dim <= 128 && tc_box_rows(kv.page_size) > 0 &&
+    // (strides of a tensor map: multiples of 16 bytes below 2^40; features beyond the head's read as zeros)
+    return cfg.dtype == MRP_BF16 && kv.n_pages > 0 && tc_box_rows(kv.page_size) > 0 &&
            kv.page_stride < (1ll << 39) && (long long)kv.page_size * kv.head_dim < (1ll << 39) && !(cfg.flags & MRP_FLAG_FORCE_SIMT);
 }
 
 size_t kv_tc_workspace_bytes()
 {
-    return kKvCounterBytes + (size_t)2 * kKvMaxSm * 2 * 128 * (128 * 4 + 8);
+    return kKvCounterBytes + (size_t)2 * kKvMaxSm * 2 * 128 * (128 * 4 + 8);      // (or one row tile of 256 features)
 }
 
 cudaError_t kv_tc_attach(Ctx *c)
@@ -1345,7 +1380,8 @@ cudaError_t kv_tc_attach(Ctx *c)
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
     if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
-    if ((e = few_prepare<1>()) != cudaSuccess || (e = few_prepare<2>()) != cudaSuccess ||
+    if ((e = few_prepare<1>()) != cudaSuccess || (e = few_prepare<2>()) != cudaSuccess || (e = few_prepare<4>()) != cudaSuccess ||
+        (e = tc_prepare<4, 1>()) != cudaSuccess ||
         (e = tc_prepare<1, 1>()) != cudaSuccess || (e = tc_prepare<1, 2>()) != cudaSuccess || (e = tc_prepare<2, 1>()) != cudaSuccess ||
         (e = tc_prepare<2, 2>()) != cudaSuccess)
         return e;
@@ -1363,11 +1399,11 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
     const long long rows = (long long)batch.max_new * p.g;
-    const bool narrow = c->kv.head_dim <= 64;
+    const bool narrow = c->kv.head_dim <= 64, wide = c->kv.head_dim > 128;
     auto few = [&]() {
         p.min_piece = 1;
         p.lead = 2;
-        return narrow ? few_launch<1>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
+        return narrow ? few_launch<1>(c, p, km, vm, box, st) : wide ? few_launch<4>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
     };
     // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 65 us on the
     // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
@@ -1387,11 +1423,12 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
     // Two row tiles share the stream of K and V where there are units for all SMs; with fewer the smaller units end sooner (512
     // tokens alone 28 against 27 us, 1024 44 against 36, 2048 74 against 78; 24 blocks of 33 behind 3000 102 against 120).
-    const bool two = rows > 128 && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
+    const bool two = rows > 128 && !wide && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
     p.min_piece = two ? 1 : 2;
     p.lead = two ? 4 : 3;
     cudaError_t e;
     if (narrow) e = two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
+    else if (wide) e = tc_launch<4, 1>(c, p, km, vm, box, st);
     else e = two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
     c->launches += launches;
     return e;

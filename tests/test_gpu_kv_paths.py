@@ -71,6 +71,12 @@ BIG = [
     ("bf16", 4, 2, 128, 32, [(130 + i, 1) for i in range(300)], 0, 0, 0),
     ("bf16", 4, 2, 72, 100, [(1000, 30), (77, 1)], 0, 0, 0),                                 # pages that TMA boxes do not tile
     ("bf16", 8, 1, 256, 32, [(1500, 2), (300, 70)], 0, 0, 0),
+    ("bf16", 16, 4, 256, 16, [(37 * i % 1500, 1) for i in range(40)], 0, 0, 0),
+    ("bf16", 8, 2, 200, 16, [(1000, 4), (333, 1), (0, 4)], 1, 0, 0),
+    ("bf16", 8, 2, 136, 64, [(700, 150), (129, 33), (0, 260)], 0, 100, 7),
+    ("bf16", 12, 4, 40, 16, [(900, 1), (131, 5), (0, 3)], 0, 0, 0),
+    ("bf16", 12, 4, 24, 32, [(700, 40), (0, 130)], 0, 0, 0),
+    ("bf16", 6, 1, 8, 8, [(500, 2), (77, 30)], 0, 0, 0),
     ("f32", 8, 2, 128, 16, [(1200, 1), (700, 30), (0, 90)], 0, 0, 0),
 ]
 
