@@ -86,7 +86,7 @@ template <int DP> struct Geo<__nv_bfloat16, DP> {
 template <int DP> struct Geo<float, DP> {
     static constexpr int kChunks = DP / 4;
     static constexpr int kPitchK = DP * 4 + 32, kPitchV = DP * 4 + 16, kPitchQ = DP * 4 + 32;
-    static constexpr int kStages = DP <= 128 ? 2 : 1;
+    static constexpr int kStages = DP <= 64 ? 2 : 1;
     static constexpr bool kSwizzle = false;
 };
 template <typename T, int DP> struct Smem {
@@ -345,31 +345,41 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                     mma16(s[1], a, b[2], b[3]);
                 }
             } else {
-#pragma unroll 4
-                for (int ks = 0; ks < DP / 8; ++ks) {      // features 2 tig, 2 tig + 1 stand for k = tig, tig + 4
-                    float2 qa, qb;
-                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qa.x), "=f"(qa.y) : "r"(sq + gid * G::kPitchQ + (ks * 8 + 2 * tig) * 4) : "memory");
-                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qb.x), "=f"(qb.y) : "r"(sq + (gid + 8) * G::kPitchQ + (ks * 8 + 2 * tig) * 4) : "memory");
-                    uint32_t ah[4], al[4];
-                    split_tf32(qa.x, ah[0], al[0]);
-                    split_tf32(qb.x, ah[1], al[1]);
-                    split_tf32(qa.y, ah[2], al[2]);
-                    split_tf32(qb.y, ah[3], al[3]);
+                // the tensor pipe cuts its sums off instead of rounding them: 32 products at a time, added here
+#pragma unroll 1
+                for (int k4 = 0; k4 < DP / 32; ++k4) {
+                    float d[2][4];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        float2 kb;
-                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(kb.x), "=f"(kb.y) : "r"(sk + (x * 8 + gid) * G::kPitchK + (ks * 8 + 2 * tig) * 4) : "memory");
-                        uint32_t bh[2], bl[2];
-                        split_tf32(kb.x, bh[0], bl[0]);
-                        split_tf32(kb.y, bh[1], bl[1]);
-                        // the tensor pipe cuts its sums off instead of rounding them: eight products at a time, added here
-                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma8(d, al, bh[0], bh[1]);
-                        mma8(d, ah, bl[0], bl[1]);
-                        mma8(d, ah, bh[0], bh[1]);
+                    for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) s[x][y] += d[y];
+                        for (int y = 0; y < 4; ++y) d[x][y] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {          // features 2 tig, 2 tig + 1 stand for k = tig, tig + 4
+                        const int at = ((k4 * 4 + i) * 8 + 2 * tig) * 4;
+                        float2 qa, qb;
+                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qa.x), "=f"(qa.y) : "r"(sq + gid * G::kPitchQ + at) : "memory");
+                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(qb.x), "=f"(qb.y) : "r"(sq + (gid + 8) * G::kPitchQ + at) : "memory");
+                        uint32_t ah[4], al[4];
+                        split_tf32(qa.x, ah[0], al[0]);
+                        split_tf32(qb.x, ah[1], al[1]);
+                        split_tf32(qa.y, ah[2], al[2]);
+                        split_tf32(qb.y, ah[3], al[3]);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            float2 kb;
+                            asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(kb.x), "=f"(kb.y) : "r"(sk + (x * 8 + gid) * G::kPitchK + at) : "memory");
+                            uint32_t bh[2], bl[2];
+                            split_tf32(kb.x, bh[0], bl[0]);
+                            split_tf32(kb.y, bh[1], bl[1]);
+                            mma8(d[x], al, bh[0], bh[1]);
+                            mma8(d[x], ah, bl[0], bl[1]);
+                            mma8(d[x], ah, bh[0], bh[1]);
+                        }
                     }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) s[x][y] += d[x][y];
                 }
             }
             // what a row does not see scores -inf
@@ -427,15 +437,19 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                     mma16(o[f + 1], a, b[2], b[3]);
                 }
             } else {
+                uint32_t ah[2][4], al[2][4];               // keys 2 tig, 2 tig + 1 stand for k = tig, tig + 4
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {              // keys 2 tig, 2 tig + 1 stand for k = tig, tig + 4
-                    uint32_t ah[4], al[4];
-                    split_tf32(s[x][0], ah[0], al[0]);
-                    split_tf32(s[x][2], ah[1], al[1]);
-                    split_tf32(s[x][1], ah[2], al[2]);
-                    split_tf32(s[x][3], ah[3], al[3]);
+                for (int x = 0; x < 2; ++x) {
+                    split_tf32(s[x][0], ah[x][0], al[x][0]);
+                    split_tf32(s[x][2], ah[x][1], al[x][1]);
+                    split_tf32(s[x][1], ah[x][2], al[x][2]);
+                    split_tf32(s[x][3], ah[x][3], al[x][3]);
+                }
 #pragma unroll
-                    for (int f = 0; f < NF; ++f) {
+                for (int f = 0; f < NF; ++f) {
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
                         float v0, v1;
                         const uint32_t a0 = sv + (x * 8 + 2 * tig) * G::kPitchV + (f * 8 + gid) * 4;
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v0) : "r"(a0) : "memory");
@@ -443,13 +457,12 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                         uint32_t bh[2], bl[2];
                         split_tf32(v0, bh[0], bl[0]);
                         split_tf32(v1, bh[1], bl[1]);
-                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma8(d, al, bh[0], bh[1]);
-                        mma8(d, ah, bl[0], bl[1]);
-                        mma8(d, ah, bh[0], bh[1]);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) o[f][y] += d[y];
+                        mma8(d, al[x], bh[0], bh[1]);
+                        mma8(d, ah[x], bl[0], bl[1]);
+                        mma8(d, ah[x], bh[0], bh[1]);
                     }
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) o[f][y] += d[y];
                 }
             }
             __syncwarp();
