@@ -204,45 +204,72 @@ __device__ __forceinline__ uint32_t bit_range(int lo, int hi)
     return h & ~l;
 }
 
-// V^T as the A operand / P as the B operand: rows (keys) of 128 bytes, MN-major; `block` bytes to the next 64 features
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t block)
+// K as an operand whose contraction runs along its rows (features), groups of 8 rows `group` bytes apart
+__device__ __forceinline__ uint64_t k_desc(uint32_t saddr, uint32_t group)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)(group >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// V^T as the A operand, V or P as the B operand: rows (keys) of 128 bytes, MN-major; `block` bytes to the next 64 features,
+// `group` to the next 8 keys
+__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t block, uint32_t group)
 {
     uint64_t d = 0;
     d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
     d |= (uint64_t)(block >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)(group >> 4) << 32;
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
     return d;
 }
 
-// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
+// How pages become tiles.  A box is `rows` rows of one page and key head: 64 features wide, a box per 64-feature block, the
+// blocks of a tile 16 KB apart; or JOINED, where a page holds whole blocks of 128 features: 128 features wide (the pool seen
+// as [groups of 8 rows][64-feature block][row of the group][64 features]), the two blocks of a group of 8 rows side by side.
+// Half as many boxes of twice the size: with small pages their number is what bounds the stream.
 struct PageBoxes {
-    int box_rows, pages;
+    int rows;
+    int page_groups, head_groups, groups;  // joined (else 0): groups of 8 rows from page to page, head to head, in all
 };
-template <int DB, typename Tile>
+template <int DB, bool JOINED> struct TileAt {             // of a tile: bytes to the next 64-feature block, the next group of 8 keys
+    static constexpr uint32_t block = JOINED ? 1024 : 128 * 128, group = JOINED ? DB * 1024 : 1024;
+};
+
+// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
+template <int DB, bool JOINED, typename Tile>
 __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const Tile &t, int n, int s,
                                            int h, int feature, uint32_t dst, uint32_t bar, int lane)
 {
-    const int j = key_tile(t, n) * kTcTile + lane * bx.box_rows;
-    const bool need = lane < bx.pages && ((j < t.hi && j + bx.box_rows > t.lo) || j < t.s1);
+    const int j = key_tile(t, n) * kTcTile + lane * bx.rows;
+    const bool need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
     int entry = 0, row = 0;
+    bool bad = false;
     if (need) {
         const int pg = fast_div(j, p.b.page);
         row = j - pg * p.b.page.d;
         entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
-        if ((unsigned)entry >= (unsigned)p.b.n_pages) {
-            kv_bad_index(p.b);
-            entry = p.b.n_pages;           // outside the map: zeros arrive
-        }
+        bad = (unsigned)entry >= (unsigned)p.b.n_pages;
+        if (bad) kv_bad_index(p.b);
     }
     const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
-    if (lane == 0) mbar_expect_tx(bar, boxes * bx.box_rows * 128u * DB);
+    if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * 128u * DB);
     __syncwarp();
     if (need) {
+        dst += lane * (bx.rows >> 3) * TileAt<DB, JOINED>::group;
+        // (a page that is not one: outside the map, zeros arrive)
+        if (JOINED) {
+            const int g = bad ? bx.groups : entry * bx.page_groups + h * bx.head_groups + (row >> 3);
+            tma_load_page(dst, map, 0, 0, feature >> 6, g, bar);
+        } else {
 #pragma unroll
-        for (int x = 0; x < DB; ++x)
-            tma_load_page(dst + lane * bx.box_rows * 128 + x * (128 * 128), map, feature + 64 * x, row, h, entry, bar);
+            for (int x = 0; x < DB; ++x)
+                tma_load_page(dst + x * (128 * 128), map, feature + 64 * x, row, h, bad ? p.b.n_pages : entry, bar);
+        }
     }
 }
 
@@ -290,9 +317,10 @@ __device__ __forceinline__ Seen seen_by_all(const AttnParams &p, const Tile &t, 
     s.all_lo = p.window > 0 ? max(0, pre + i1 + 1 - p.window) : 0;
     return s;
 }
-template <int DB, typename Tile>
+template <int DB, bool JOINED, typename Tile>
 __device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0, uint32_t vs, Suspects &sus, int lane)
 {
+    typedef TileAt<DB, JOINED> lay;
     if ((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) {
         if (!a.differ || (j0 >= a.all_lo && j0 + kTcTile <= a.all_hi)) return;
     }
@@ -300,13 +328,14 @@ __device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0,
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const int row = w * 32 + lane, j = j0 + row;
+        const uint32_t at = vs + (row >> 3) * lay::group + (row & 7) * 128;
         const bool seen = j < t.hi && (j >= t.lo || j < t.s1);
         bool bad = false;
         if (seen && a.differ && !(j >= a.all_lo && j < a.all_hi)) {
             for (int c = 0; c < 8 * DB; ++c) {
                 uint32_t u[4];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                             : "r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)) : "memory");
+                             : "r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)) : "memory");
 #pragma unroll
                 for (int y = 0; y < 4; ++y) bad |= (u[y] & 0x7F800000u) == 0x7F800000u || (u[y] & 0x7F80u) == 0x7F80u;
             }
@@ -315,7 +344,7 @@ __device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0,
         if (!seen || bad)
             for (int c = 0; c < 8 * DB; ++c)
                 asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
-                             ::"r"(vs + (c >> 3) * (128 * 128) + row * 128 + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
+                             ::"r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
     }
     if (lane == 0 && (found[0] | found[1] | found[2] | found[3])) {
         const int at_n = sus.n;
@@ -425,10 +454,10 @@ __device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
     }
 }
 
-template <int NB>
+template <int NB, bool JOINED>
 __global__ void __launch_bounds__(384, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
-                        const __grid_constant__ CUtensorMap vmap, int box_rows)
+                        const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
 {
     typedef FewGeo<NB> G;
     constexpr int DB = G::B::DB, HB = G::B::HB;
@@ -503,7 +532,6 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         // ================================ K and V tiles ================================
         int stage = 0;
         uint32_t phase = 0;
-        const PageBoxes bx = {box_rows, kTcTile / box_rows};
         bool ok = true;
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
@@ -514,7 +542,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB>(p, map, bx, cur.t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    fetch_tile<DB, JOINED>(p, map, bx, cur.t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
                     if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
                 }
             };
@@ -531,6 +559,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         uint32_t phase = 0, k = 0, unit = 0;
         bool ok = true;
         const uint32_t idesc_s = make_idesc(NR), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
+        typedef TileAt<DB, JOINED> lay;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         while (ok && cur.at < piece_end) {
@@ -555,7 +584,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     if (elect_one()) {
 #pragma unroll
                         for (int c = 0; c < 4 * DB; ++c)
-                            umma_bf16(s_at(kk & 1u), make_smem_desc(ks + (c >> 2) * (128 * 128) + (c & 3) * 32),
+                            umma_bf16(s_at(kk & 1u), k_desc(ks + (c >> 2) * lay::block + (c & 3) * 32, lay::group),
                                       make_smem_desc(qs + (c >> 2) * (NR * 128) + (c & 3) * 32), idesc_s, y + c > 0);
                         if (y + 1 == HB) umma_commit(s_full(kk & 1u));
                         umma_commit(empty_bar(stage));
@@ -573,14 +602,15 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     wait(full_bar(stage), phase);
                     if (!ok) break;
                     const uint32_t vs = ring + stage * G::B::kStageBytes;
-                    clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
+                    clean_tile<DB, JOINED>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
                     if (y == 0) wait(p_ready(k & 1u), (k >> 1) & 1u);
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c)        // (one block of features: the second 64 lanes repeat it)
-                            umma_bf16(o_at(k & 1u) + y * G::kCols, mn_desc(vs + c * 2048, DB == 2 ? 128 * 128 : 0), mn_desc(ps + c * 2048, 0), idesc_o, n >= 2 || c > 0);
+                            umma_bf16(o_at(k & 1u) + y * G::kCols, mn_desc(vs + c * 2 * lay::group, DB == 2 ? lay::block : 0, lay::group), mn_desc(ps + c * 2048, 0, 1024), idesc_o,
+                                      n >= 2 || c > 0);
                         if (y + 1 == HB) umma_commit(pv_done(k & 1u));
                         umma_commit(empty_bar(stage));
                     }
@@ -862,10 +892,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
 
 // ======================================================================================================================
 // Many rows: row tiles of 128 on the lanes (NT = 1: 65 to 128 rows; NT = 2: prompts).
-template <int NB, int NT>
+template <int NB, int NT, bool JOINED>
 __global__ void __launch_bounds__(TcGeo<NB, NT>::kThreads, 1)
 kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
-                       const __grid_constant__ CUtensorMap vmap, int box_rows)
+                       const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
 {
     typedef TcGeo<NB, NT> G;
     constexpr int DB = G::B::DB, HB = G::B::HB;
@@ -933,7 +963,6 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         // ================================ TMA producer ================================
         int stage = 0;
         uint32_t phase = 0;
-        const PageBoxes bx = {box_rows, kTcTile / box_rows};
         bool ok = true;
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
@@ -945,7 +974,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    fetch_tile<DB, JOINED>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
                     if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
                 }
             };
@@ -963,14 +992,15 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         uint32_t phase = 0, k = 0, unit = 0;               // k: tiles done
         bool ok = true;
         const uint32_t idesc_s = make_idesc(128), idesc_o = make_idesc(DB * 64) | (1u << 16);
+        typedef TileAt<DB, JOINED> lay;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         auto mma_s = [&](int x, int row_tile, uint32_t ks, int y) {        // S buffer x (+)= Q_row_tile K^T, features 128 y ..
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4 * DB; ++c) {
-                    const uint32_t off = (c >> 2) * (128 * 128) + (c & 3) * 32;
-                    umma_bf16(tmem + x * 128, make_smem_desc(sq + row_tile * G::kQTile + y * G::B::kStageBytes + off), make_smem_desc(ks + off), idesc_s, y + c > 0);
+                    umma_bf16(tmem + x * 128, make_smem_desc(sq + row_tile * G::kQTile + y * G::B::kStageBytes + (c >> 2) * (128 * 128) + (c & 3) * 32),
+                              k_desc(ks + (c >> 2) * lay::block + (c & 3) * 32, lay::group), idesc_s, y + c > 0);
                 }
                 if (y + 1 == HB) umma_commit(s_full(x));
             }
@@ -981,7 +1011,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2048, 128 * 128), idesc_o, !first || c0 + c > 0);
+                    umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2 * lay::group, lay::block, lay::group), idesc_o, !first || c0 + c > 0);
                 if (c0 == 4 && y + 1 == HB) umma_commit(pv_done(x));
             }
             __syncwarp();
@@ -999,7 +1029,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             Suspects &sus = suspects[unit & 1];
             if (lane == 0) sus.n = 0;
             __syncwarp();
-            auto clean = [&](int n, uint32_t vs) { clean_tile<DB>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
+            auto clean = [&](int n, uint32_t vs) { clean_tile<DB, JOINED>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
             auto at_stage = [&](int s) { return ring + s * G::B::kStageBytes; };
 #pragma unroll
             for (int x = 0; x < NT; ++x) wait(q_ready(x), unit & 1u);
@@ -1308,32 +1338,32 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     }
 }
 
-template <int NB, int NT>
+template <int NB, int NT, bool JOINED>
 cudaError_t tc_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_tc_kernel<NB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<NB, NT>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_tc_kernel<NB, NT, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<NB, NT>::kSmem);
 }
-template <int NB, int NT>
-cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
+template <int NB, int NT, bool JOINED>
+cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, const PageBoxes &bx, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_tc_kernel<NB, NT>, dim3(sms), dim3(TcGeo<NB, NT>::kThreads), TcGeo<NB, NT>::kSmem, st,
-                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
+    cudaError_t e = launch_k(kv_attention_tc_kernel<NB, NT, JOINED>, dim3(sms), dim3(TcGeo<NB, NT>::kThreads), TcGeo<NB, NT>::kSmem, st,
+                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, bx);
     c->launches = 1;
     return note_err(c, e, "kv_attention_tc_kernel");
 }
 
-template <int NB>
+template <int NB, bool JOINED>
 cudaError_t few_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_few_kernel<NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<NB>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_few_kernel<NB, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<NB>::kSmem);
 }
-template <int NB>
-cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, int box, cudaStream_t st)
+template <int NB, bool JOINED>
+cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, const PageBoxes &bx, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_few_kernel<NB>, dim3(sms), dim3(FewGeo<NB>::kThreads), FewGeo<NB>::kSmem, st,
-                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, box);
+    cudaError_t e = launch_k(kv_attention_few_kernel<NB, JOINED>, dim3(sms), dim3(FewGeo<NB>::kThreads), FewGeo<NB>::kSmem, st,
+                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, bx);
     c->launches = 1;
     return note_err(c, e, "kv_attention_few_kernel");
 }
@@ -1347,13 +1377,32 @@ int tc_box_rows(int page_size)
     return 0;
 }
 
-bool page_map(Ctx *c, CUtensorMap *map, const void *pool, int box)
+PageBoxes page_boxes(const mrp_kv_config &kv, bool join)
+{
+    PageBoxes bx = {};
+    bx.rows = tc_box_rows(kv.page_size);
+    if (!join) return bx;
+    const int64_t group = 8ll * kv.head_dim, in_all = (int64_t)kv.n_pages * (kv.page_stride / group);
+    if (kv.head_dim % 128 == 0 && kv.page_stride % group == 0 && in_all < INT_MAX) {
+        bx.page_groups = (int)(kv.page_stride / group);
+        bx.head_groups = kv.page_size / 8;
+        bx.groups = (int)in_all;
+    }
+    return bx;
+}
+
+bool page_map(Ctx *c, CUtensorMap *map, const void *pool, const PageBoxes &bx)
 {
     const mrp_kv_config &kv = c->kv;
-    const cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)kv.head_dim * 2, (cuuint64_t)kv.page_size * kv.head_dim * 2, (cuuint64_t)kv.page_stride * 2};
-    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, es[4] = {1, 1, 1, 1};
-    return ((EncodeTiledFn)c->kv_encode)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(pool), dims, strides, boxes, es,
+    const cuuint64_t D = (cuuint64_t)kv.head_dim;
+    const cuuint64_t dims_apart[4] = {D, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
+    const cuuint64_t strides_apart[3] = {D * 2, (cuuint64_t)kv.page_size * D * 2, (cuuint64_t)kv.page_stride * 2};
+    const cuuint32_t box_apart[4] = {64, (cuuint32_t)bx.rows, 1, 1}, es[4] = {1, 1, 1, 1};
+    const cuuint64_t dims_joined[4] = {64, 8, D / 64, (cuuint64_t)bx.groups};
+    const cuuint64_t strides_joined[3] = {D * 2, 128, D * 16};
+    const cuuint32_t box_joined[4] = {64, 8, 2, (cuuint32_t)bx.rows / 8};
+    return ((EncodeTiledFn)c->kv_encode)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(pool), bx.groups ? dims_joined : dims_apart,
+                                         bx.groups ? strides_joined : strides_apart, bx.groups ? box_joined : box_apart, es,
                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -1380,56 +1429,66 @@ cudaError_t kv_tc_attach(Ctx *c)
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
     if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
-    if ((e = few_prepare<1>()) != cudaSuccess || (e = few_prepare<2>()) != cudaSuccess || (e = few_prepare<4>()) != cudaSuccess ||
-        (e = tc_prepare<4, 1>()) != cudaSuccess ||
-        (e = tc_prepare<1, 1>()) != cudaSuccess || (e = tc_prepare<1, 2>()) != cudaSuccess || (e = tc_prepare<2, 1>()) != cudaSuccess ||
-        (e = tc_prepare<2, 2>()) != cudaSuccess)
-        return e;
+    cudaError_t all[] = {few_prepare<1, false>(), few_prepare<2, false>(), few_prepare<4, false>(), few_prepare<2, true>(), few_prepare<4, true>(),
+                         tc_prepare<1, 1, false>(), tc_prepare<2, 1, false>(), tc_prepare<4, 1, false>(), tc_prepare<2, 1, true>(),
+                         tc_prepare<4, 1, true>(), tc_prepare<1, 2, false>(), tc_prepare<2, 2, false>()};
+    for (cudaError_t one : all)
+        if (one != cudaSuccess) return one;
     c->kv_encode = fn;
     return cudaSuccess;
 }
 
 cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
 {
-    const int box = tc_box_rows(c->kv.page_size);
-    CUtensorMap km, vm;
-    if (!page_map(c, &km, p.k, box) || !page_map(c, &vm, p.v, box)) return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const size_t slots = (size_t)2 * kKvMaxSm * 2;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
     const long long rows = (long long)batch.max_new * p.g;
     const bool narrow = c->kv.head_dim <= 64, wide = c->kv.head_dim > 128;
+    // Two row tiles share the stream of K and V where there are units for all SMs; with fewer the smaller units end sooner (512
+    // tokens alone 28 against 27 us, 1024 44 against 36, 2048 74 against 78; 24 blocks of 33 behind 3000 102 against 120).
+    const bool two = rows > 128 && !wide && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
+    CUtensorMap km, vm;
+    PageBoxes bx;
+    auto maps = [&](bool join) {
+        bx = page_boxes(c->kv, join);
+        return page_map(c, &km, p.k, bx) && page_map(c, &vm, p.v, bx) ? cudaSuccess : note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    };
+    // Pages of up to 32 rows joined: one token each of 24 sequences 76 against 66 us at 16 rows, 64 against 63 at 64; prompts are
+    // bound by their products.
+    const bool join = tc_box_rows(c->kv.page_size) <= 32;
+    cudaError_t e = maps(join);
+    if (e != cudaSuccess) return e;
     auto few = [&]() {
         p.min_piece = 1;
         p.lead = 2;
-        return narrow ? few_launch<1>(c, p, km, vm, box, st) : wide ? few_launch<4>(c, p, km, vm, box, st) : few_launch<2>(c, p, km, vm, box, st);
+        if (narrow) return few_launch<1, false>(c, p, km, vm, bx, st);
+        if (bx.groups) return wide ? few_launch<4, true>(c, p, km, vm, bx, st) : few_launch<2, true>(c, p, km, vm, bx, st);
+        return wide ? few_launch<4, false>(c, p, km, vm, bx, st) : few_launch<2, false>(c, p, km, vm, bx, st);
     };
     // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 65 us on the
     // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
-    // took 95 and 113 against 78 and 80.  Beyond 128 rows two row tiles share the stream of K and V.
+    // took 95 and 113 against 78 and 80.
     if (rows <= kFewRows) return few();
     // A step of single tokens beside a prompt: where most sequences must be far shorter than the longest, those of up to 16
-    // rows go to the transposed kernel in a launch of their own.
+    // rows go to the transposed kernel in a launch of their own (48 single tokens and a prompt of 512: 172 against 146 us).
     int launches = 0;
     if ((long long)batch.n_tokens * 4 < (long long)batch.n_seqs * batch.max_new) {
         p.rows_upto = kFewRows;
-        const cudaError_t e = few();
-        if (e != cudaSuccess) return e;
+        if ((e = few()) != cudaSuccess) return e;
         launches = c->launches;
         p.rows_above = kFewRows;
         p.rows_upto = INT_MAX;
     }
+    if (two && bx.groups && (e = maps(false)) != cudaSuccess) return e;
     // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
-    // Two row tiles share the stream of K and V where there are units for all SMs; with fewer the smaller units end sooner (512
-    // tokens alone 28 against 27 us, 1024 44 against 36, 2048 74 against 78; 24 blocks of 33 behind 3000 102 against 120).
-    const bool two = rows > 128 && !wide && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
     p.min_piece = two ? 1 : 2;
     p.lead = two ? 4 : 3;
-    cudaError_t e;
-    if (narrow) e = two ? tc_launch<1, 2>(c, p, km, vm, box, st) : tc_launch<1, 1>(c, p, km, vm, box, st);
-    else if (wide) e = tc_launch<4, 1>(c, p, km, vm, box, st);
-    else e = two ? tc_launch<2, 2>(c, p, km, vm, box, st) : tc_launch<2, 1>(c, p, km, vm, box, st);
+    if (two) e = narrow ? tc_launch<1, 2, false>(c, p, km, vm, bx, st) : tc_launch<2, 2, false>(c, p, km, vm, bx, st);
+    else if (narrow) e = tc_launch<1, 1, false>(c, p, km, vm, bx, st);
+    else if (bx.groups) e = wide ? tc_launch<4, 1, true>(c, p, km, vm, bx, st) : tc_launch<2, 1, true>(c, p, km, vm, bx, st);
+    else e = wide ? tc_launch<4, 1, false>(c, p, km, vm, bx, st) : tc_launch<2, 1, false>(c, p, km, vm, bx, st);
     c->launches += launches;
     return e;
 }
