@@ -28,7 +28,6 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kWarpKeys = kTile / kWarps;  // 16
 constexpr float kLazy = 8.f;               // log2 of the growth a running maximum may lag behind
 
-
 __device__ __forceinline__ uint32_t s_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool read)
 {
@@ -594,8 +593,9 @@ size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv)
 
 cudaError_t kv_attach(Ctx *c)
 {
+    // (done before the call returns: the caller's stream need not wait for the legacy one)
     cudaError_t e = cudaMemset(c->kv_ws, 0, kKvCounterBytes);
-    if (e != cudaSuccess || (e = kv_tc_attach(c)) != cudaSuccess) return e;
+    if (e != cudaSuccess || (e = cudaStreamSynchronize(cudaStreamLegacy)) != cudaSuccess || (e = kv_tc_attach(c)) != cudaSuccess) return e;
     if (c->cfg.dtype == MRP_BF16) {
         if ((e = prepare<__nv_bfloat16, 64>()) != cudaSuccess || (e = prepare<__nv_bfloat16, 128>()) != cudaSuccess) return e;
         return prepare<__nv_bfloat16, 256>();
@@ -637,7 +637,7 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
         const int DP = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
         p.plain_rows = kv.page_size % kWarpKeys == 0 && kv.head_dim == DP;
     }
-        if (c->kv_encode) return launch_paged_attention_tc(c, p, batch, st);
+    if (c->kv_encode) return launch_paged_attention_tc(c, p, batch, st);
     const size_t slots = (size_t)4 * kKvMaxSm;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);

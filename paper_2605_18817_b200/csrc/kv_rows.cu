@@ -71,7 +71,8 @@ __device__ __forceinline__ void fma2(float &a, float &b, float c, float d, float
 __device__ __forceinline__ float one_f(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float one_f(const float *p) { return *p; }
 
-// Sequence of row t: the number of entries of seq_start[1..n_seqs] that are <= t, found by the warp 32 probes at a time.
+// Sequence of row t: the number of entries of seq_start[1..n_seqs] that are <= t, found by the warp 32 probes at a time
+// (in 0..n_seqs whatever the list holds).
 __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seqs, int t, int lane)
 {
     int lo = 0, n = n_seqs;                // the answer lies in [lo, lo + n]
@@ -84,6 +85,19 @@ __device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seq
         n = min(step - 1, n - k * step);
     }
     return lo;
+}
+
+// The same where that list is not ascending (a sequence in it does not fit) or no sequence has the row: all of them; -1: none.
+__device__ __noinline__ int scan_sequences(const KvBatch &b, int t, int lane)
+{
+    for (int s0 = 0; s0 < b.n_seqs; s0 += 32) {
+        const int s = s0 + lane;
+        int start, n, pre;
+        const bool has = s < b.n_seqs && kv_sequence(b, s, start, n, pre) && t >= start && t - start < n;
+        const uint32_t hit = __ballot_sync(0xffffffffu, has);
+        if (hit) return s0 + __ffs(hit) - 1;
+    }
+    return -1;
 }
 
 enum { kHalves = 0, kAdjacent = 1, kAgain = 2 };         // how pairs lie in a lane
@@ -108,9 +122,13 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
     int pos = 0;
     int64_t page_off = -1;
     if (p.b.n_seqs >= 0) {
-        const int s = find_sequence(p.b.seq_start, p.b.n_seqs, t, lane);
+        int s = find_sequence(p.b.seq_start, p.b.n_seqs, t, lane);
         int start, n, pre;
-        if (s >= p.b.n_seqs || !kv_sequence(p.b, s, start, n, pre) || t < start) return;
+        if (s >= p.b.n_seqs || !kv_sequence(p.b, s, start, n, pre) || t < start || t - start >= n) {
+            s = scan_sequences(p.b, t, lane);
+            if (s < 0) return;
+            kv_sequence(p.b, s, start, n, pre);
+        }
         pos = pre + (t - start);
         const int pg = fast_div(pos, p.b.page);
         const int entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);

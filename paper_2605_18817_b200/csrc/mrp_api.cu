@@ -579,6 +579,7 @@ int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_modul
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
     if (!pools_ok(pages) || !rows_ok(c, args->q, args->q_stride, c.kv.n_heads) || !rows_ok(c, args->out, args->out_stride, c.kv.n_heads))
         return MRP_ERR_INVALID_ARG;
+    if (args->q == args->out && args->q_stride != args->out_stride) return MRP_ERR_INVALID_ARG;
     DeviceGuard guard(c.cfg.device);
     if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
     c.err[0] = 0;

@@ -178,6 +178,52 @@ def test_sequences_and_pages_that_are_not_valid(dtype, D, P, new):
 
 
 @gpu
+@pytest.mark.parametrize("start", [[0, 99, 4, 8, 12], [0, 99, 1, 2, 5], [0, 8, 4, 8, 12], [99, 0, 4, 7, 7], [0, 4, 99, -1, 6], [0, 2, 100, 1, 9]])
+@pytest.mark.parametrize("new", [1, 5])
+def test_lists_of_rows_that_do_not_ascend(start, new):
+    """Sequences that do not fit make the list of starts rise and fall: the others keep their rows, no row goes elsewhere."""
+    c = Cache("bf16", 4, 2, 64, 16, [(15, 4), (40, 4), (31, 4), (30, 4)], seed=9, extra_rows=3, rot=64)
+    c.batch.c.max_new = new
+    rows = c.rand(c.T, 8, 64)
+    c.start_np = np.array(start, np.int32)
+    c.seq_start.copy_(torch.from_numpy(c.start_np))
+    taken = [s + i for _, s, n, _ in ref.sequences(c.start_np, c.pre_np, c.T, c.max_pages * 16) for i in range(n)]
+    before = f64(c.v_pages)
+    qo = torch.full((c.T, 4, 64), 7.0, device=DEV, dtype=torch.bfloat16)
+    c.b.mrp_kv_append(c.ctx, c.batch, c.k_pages, c.v_pages, rows[:, 4:6], rows[:, 6:8], None, rows[:, :4], qo)
+    _, vp = ref.append(before, before, np.zeros((c.T, 2, 64)), f64(rows[:, 6:8]), c.start_np, c.pre_np, c.table_np, 16)
+    if len(set(taken)) == len(taken):                      # (else two sequences claim a row)
+        assert np.array_equal(f64(c.v_pages), vp, equal_nan=True)
+        out, lse = c.attend(qo)
+        c.check(qo, out, lse)
+    wrote = (f64(qo) != 7.0).any((1, 2))
+    assert np.array_equal(np.flatnonzero(wrote), np.unique(taken))
+    assert int(c.status.item()) == c.b.MRP_DEV_BAD_INDEX
+
+
+@gpu
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 20), ("bf16", 150), ("f32", 3)])
+def test_attention_in_place(dtype, new):
+    c = Cache(dtype, 8, 2, 128, 16, [(3000, new), (70, new), (0, new)], seed=5)
+    q = c.rand(c.T, 8, 128)
+    out, lse = c.attend(q)
+    c.check(q, out, lse)
+    same = q.clone()
+    again, lse2 = c.attend(same, same)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@gpu
+@pytest.mark.parametrize("gap", [8, 1024, 4096 + 1024])
+@pytest.mark.parametrize("D,P,new", [(128, 16, 1), (128, 24, 9), (128, 32, 40), (256, 8, 2), (256, 96, 40), (128, 16, 200)])
+def test_small_pages_with_gaps(D, P, new, gap):
+    c = Cache("bf16", 4, 2, D, P, [(500, new), (P - 1, new), (1, new)], seed=7, page_gap=gap)
+    q = c.rand(c.T, 4, D)
+    out, lse = c.attend(q)
+    c.check(q, out, lse)
+
+
+@gpu
 @pytest.mark.parametrize("dtype,D,new", [("bf16", 128, 1), ("bf16", 128, 24), ("bf16", 64, 150), ("f32", 64, 3)])
 def test_a_captured_step_serves_other_lengths(dtype, D, new):
     c = Cache(dtype, 4, 2, D, 16, [(700, new), (64, new), (300, new)], seed=8, rot=D)
@@ -458,6 +504,9 @@ def test_refusals():
     wide = torch.zeros((3, 5, 128), device=DEV, dtype=torch.bfloat16)
     r = b.mrp_qkv_rows(wide.data_ptr(), None, None, 640, 0, 0, None, None, wide.data_ptr(), None, 512, 0)
     assert b.lib.mrp_qk_norm_rotate(c.ctx.handle, pos.data_ptr(), 3, ctypes.byref(r), None) == 1
+    a = b.mrp_attention_args(wide.data_ptr(), wide.data_ptr(), 640, 512, None, 0, 0, 0, 0.0)
+    pools = b.mrp_module_kv(c.k_pages.data_ptr(), c.v_pages.data_ptr())
+    assert b.lib.mrp_paged_attention(c.ctx.handle, c.batch.ref, ctypes.byref(pools), ctypes.byref(a), None) == 1
     for kw in (dict(n_heads=3), dict(head_dim=12), dict(head_dim=264), dict(page_size=0), dict(n_pages=-1), dict(max_pages=0), dict(page_stride=100),
                dict(page_stride=4100), dict(rot_dim=3), dict(rot_dim=130), dict(rot_theta=0.0), dict(norm_eps=-1.0), dict(inv_freq=[float("inf")] * 64)):
         a = dict(n_heads=4, n_kv_heads=2, head_dim=128, page_size=16, n_pages=4, max_pages=4, rot_dim=128, rot_theta=1e4)
