@@ -399,9 +399,9 @@ size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv);
 /*
  * Attach a cache geometry to a context (workspace borrowed until mrp_destroy or the next attach: DEVICE, 256-byte
  * aligned, at least mrp_kv_workspace_bytes; it must not serve another context too).  Like mrp_create this call may
- * block (it clears the workspace's arrival counters); make it outside of any stream capture.  The three calls below run
- * on the context's device and, like every call on a context, one after the other: a captured graph of them counts as a
- * call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
+ * block (it clears the workspace's arrival counters); make it outside of any stream capture and with no call on the
+ * context in flight.  The three calls below run on the context's device and, like every call on a context, one after the
+ * other: a captured graph of them counts as a call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
  */
 int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t workspace_bytes);
 
@@ -425,7 +425,7 @@ typedef struct {
     int32_t n_seqs;             /* 0..max_seqs                                                       */
     int32_t n_tokens;
     int32_t max_new;            /* the largest number of new tokens of a sequence, as far as known on the host: it only
-                                   helps to choose a kernel, results do not depend on it being right */
+                                   helps to choose a kernel; any value >= 0 is served rightly        */
     int32_t *status;            /* optional device int32 receiving MRP_DEV_* bits                    */
 } mrp_kv_batch;
 
@@ -482,11 +482,15 @@ typedef struct {
 
 /*
  * out = softmax(scale * q K^T) V over the visible positions of the token's sequence, per query head; a token that sees
- * nothing gets zeros and lse = -inf.  (Two passes over disjoint sets of keys are joined by their lse: MRP_ATTN_PREFIX
- * for the cache, and the block's own keys elsewhere.)  Scores, softmax statistics and sums in fp32; on bf16 contexts
- * the probabilities are rounded to bf16 as an operand of the product with V.  What positions no token sees hold does not
- * matter.  The work is split over the cache's length by the device from the lengths it finds; results do not depend on
- * anything but the inputs (parts are joined in a fixed order).  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * nothing gets zeros and lse = -inf.  out may be q itself (with the same stride).  (Two passes over disjoint sets of keys
+ * are joined by their lse: MRP_ATTN_PREFIX for the cache, and the block's own keys elsewhere.)
+ * Scores, softmax statistics and sums in fp32; on bf16 contexts the probabilities are rounded to bf16 as an operand of the
+ * product with V (where a sequence has up to 16 rows, new tokens times query heads of a key head, to two bf16 parts).
+ * What a token does not see does not reach it, whatever it holds; a value it sees that is not finite may make its output
+ * NaN in all features.  The work is split over the cache's length by the device from the lengths it finds; parts are joined
+ * in a fixed order, so equal calls give equal bits.
+ * bf16 with page_size a multiple of 8 runs on tiles that TMA feeds, blocks and prompts at the tensor cores' rate; f32, other
+ * page sizes and MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages,
                         const mrp_attention_args *args, void *cuda_stream);

@@ -1,11 +1,11 @@
-// Attention over the pages of a key / value cache: the kernel for few query rows per sequence (decoding), and for the
-// shapes the large-tile kernel does not take.
+// Attention over the pages of a key / value cache: the launch of all forms, and the kernel on warp-level products, which serves
+// f32 contexts, pages that are no multiple of 8 rows, and MRP_FLAG_FORCE_SIMT (bf16 otherwise: kv_attention_tc.cu).
 //
 //   out_r = sum_j p_rj V_j / sum_j p_rj,  p_rj = exp2(scale log2(e) (q_r . K_j) - m_r)  over the visible positions j,
 // m_r the running maximum (raised only when a score exceeds it by 2^8, which keeps p and its sum well inside fp32 and
 // bf16 and spares most rescalings of the accumulator), p_rj and its sum in fp32.
 //
-// Decoding reads every K / V row once and does little else: memory bounds it.  The g = n_heads / n_kv_heads query heads
+// Decoding reads every K / V row once and does little else.  The g = n_heads / n_kv_heads query heads
 // that share a key head and the new tokens of a sequence are the rows of one tile (row r = token r / g, head r % g; 16
 // rows), so a K / V row is read once for all of them.  The keys of a (sequence, row tile, key head) unit go in tiles of
 // 64, 16 for each of the CTA's four warps; a warp keeps its own ring of 16-key stages filled by cp.async ahead of its
@@ -16,6 +16,11 @@
 //
 // bf16: mma.sync m16n8k16, operands by ldmatrix from XOR-swizzled rows, probabilities as bf16 hi + lo.
 // f32:  mma.sync m16n8k8 on tf32 operands split into two (x = hi + lo, three products: relative 2^-21).
+//
+// What bounds it: the instructions around the products (f32: splitting K and V, three conversions and a subtraction a value and
+// row of the tile), not memory.  24 sequences of 200 to 6000 positions, one token each, 32 / 8 heads: bf16 of 128 features in
+// pages of 20 rows 100 us (48 for the bytes); f32 107 (48) at 64 features, 184 (97) at 128, 530 (193) at 256.  Two CTAs an SM
+// count more than a second stage: f32 of 128 features 235 us with two stages of one CTA.  Rows beyond 16 take a unit per 16.
 #include "kv_attention.cuh"
 
 namespace mrp {

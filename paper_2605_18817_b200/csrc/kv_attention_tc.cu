@@ -1,20 +1,27 @@
-// Attention over the pages of a key / value cache on the 5th-generation tensor cores: blocks and prompts, that is more
-// query rows per sequence and key head than a 16-row tile holds (bf16, heads of up to 128 features, page sizes that TMA
-// boxes tile).
+// Attention over the pages of a key / value cache on the 5th-generation tensor cores: bf16, heads of up to 256 features, page
+// sizes that are multiples of 8 rows (boxes of whole swizzled groups tile them).
 //
-// The mathematics are those of kv_attention.cu; here S = Q K^T and O += P V run as tcgen05.mma with 128 query rows
-// (row r = new token r / g, head r % g of the key head's group) against tiles of 128 keys:
-//   warp 0        fetches K and V tiles, page by page, by TMA into a ring of 128-byte-swizzled stages
-//   warp 1        issues the MMAs: S into tensor memory, O += P V with P read from tensor memory (it lies in the columns
-//                 S came in) and V as stored (its keys are the contraction: an MN-major operand)
-//   4 NT warps    a warpgroup per 128 rows, a thread per row: S from tensor memory, running maximum and sum with no
-//                 exchange between lanes, P = exp2(scale S - m) rounded to bf16 back into tensor memory, O at the end
-// NT = 2 (prompts): two row tiles share every K and V tile and take turns, one in the MMAs while the other is in the
-// exponentials; at 128 features both take about 1024 cycles per 128 x 128 tile, so neither waits long.  NT = 1 (blocks):
-// two S buffers instead, the next S is computed while this one is exponentiated; the K / V stream bounds it.
-// The accumulator stays in tensor memory; it is rescaled only when a row's maximum has grown by more than 2^8 over the
-// one in use.  Tiles of all units form one line cut into equal pieces as in kv_attention.cu; a unit cut in two is joined
-// row by row by the warp that arrives last.
+// The mathematics are those of kv_attention.cu: running maximum (raised only by more than 2^8), probabilities and sums in
+// fp32, one line of tiles cut into equal pieces, joined where a unit is cut.  Two kernels, both fed by TMA, page by page, into
+// a ring of 128-byte-swizzled stages of a K or a V tile (128 keys), both with accumulators in tensor memory:
+//
+// kv_attention_few_kernel   up to 16 query rows per sequence and key head (decoding, blocks).  Transposed; see there.  Bound by
+//                           memory: 64 ragged sequences of up to 8191 positions, 32 / 8 heads of 128: 165 us, 6.2 TB/s.
+// kv_attention_tc_kernel    more: 128 query rows (row r = new token r / g, head r % g of the key head's group) on the lanes.
+//   warp 0        K and V tiles                       warp 1   MMAs
+//   8 NT warps    softmax, two threads a row, half its keys each: S from tensor memory, the maximum of the halves met through
+//                 shared memory, P = exp2(scale S - m) as bf16 back into the columns S came in: O += P V takes it from there
+//                 (and V as stored: its keys are the contraction, an MN-major operand).  The first half's product starts
+//                 while the second half's probabilities are still on their way.
+//   P is rounded to bf16 once, as an operand (2^-8 of each probability at most); the sum takes the unrounded values.  Hi + lo
+//   parts would double the products that bound prompts.
+//   NT = 2 (prompts): two row tiles share every K and V tile and take turns, one in the MMAs while the other is in the
+//   exponentials.  Per pair of 128 x 128 tiles of 128 features the products take 2048 cycles, the exponentials alone 2048 of
+//   the special function unit; measured 3600 (2 prompts of 2000 behind 5600 positions, 32 / 8 heads: 450 us, 1.06 PFLOP/s; the
+//   softmax's chain of tensor-memory loads, maximum, exponentials, stores is what does not overlap).  A thread per row took
+//   510 us; exponentials by a polynomial on the FMA pipe for a part of the scores 460 to 480.
+//   NT = 1 (17 to 128 rows, and batches too small to give two row tiles to all SMs): two S buffers instead, the next S is
+//   computed while this one is exponentiated; 24 blocks of 32 tokens 75 us against 51 for the bytes.
 //
 // Pages hold what they hold behind a sequence's end: scores of positions a row does not see are replaced before they are
 // used, and V rows that no row of the tile sees are zeroed in shared memory before the product (0 * NaN).  A V row with
@@ -118,15 +125,18 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 
 // ======================================================================================================================
 // Few rows (decoding, blocks): everything transposed.  S^T = K Q^T puts the 128 keys of a tile on the tensor-memory lanes
-// and the NR query rows (16, 32 or 64) on the columns, O^T += V^T P^T the features on the lanes: the work of the MMAs and of
-// the exponentials is proportional to the rows there are, and all 128 threads of a warpgroup have a key each.
+// and the 16 query rows on the columns, O^T += V^T P^T the features on the lanes: the MMAs and the exponentials do the work of
+// the rows there are, not of 128, and all 128 threads of a warpgroup have a key each.
 //   warp 0   K and V tiles by TMA, as below        warp 1   MMAs        warps 2, 3   queries and what rows see, a unit ahead
 //   warps 4-7, 8-11   two warpgroups that take tiles in turn, each with its own S buffer, maxima, sums and accumulator (no
 //            exchange until the unit's end): a thread turns its key's scores into probabilities and stores them as a row
-//            of the operand P [keys][rows] in shared memory, for up to 32 rows as bf16 hi and lo columns side by side
+//            of the operand P [keys][rows] in shared memory, bf16 hi and lo columns side by side (2^-17 together: the second
+//            product costs nothing that shows)
 // The maximum in use is common to a warpgroup's 128 keys, so a tile needs to know only whether some score exceeds it by
 // more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
-// rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it.
+// rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it (64 ragged
+// single tokens 165 us against 158 for the bytes; 24 blocks of 16 72 against 50; one token behind 2047 positions, 16 heads: 13,
+// of which the launch, the cut and the joining of 16 pieces are most).
 constexpr int kFewRows = 16;
 template <int NB> struct FewGeo {
     typedef Blocks<NB> B;
@@ -891,7 +901,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
 }
 
 // ======================================================================================================================
-// Many rows: row tiles of 128 on the lanes (NT = 1: 65 to 128 rows; NT = 2: prompts).
+// Many rows: row tiles of 128 on the lanes, NT of them a unit.
 template <int NB, int NT, bool JOINED>
 __global__ void __launch_bounds__(TcGeo<NB, NT>::kThreads, 1)
 kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,

@@ -11,6 +11,8 @@
 // loads in flight.  A lane holds two runs of four features: the two halves of its four pairs (features 4 l.. and rot_dim / 2
 // + 4 l.. of the rotated ones), so a rotation needs no other lane's registers; adjacent pairs lie in one run anyway.
 // rot_dim / 2 that is no multiple of four splits runs: there the other half of a pair is read again.
+// Measured, 32 query and 8 key heads of 128 in bf16 with norms: 16384 tokens 64 us (336 MB: 5.2 TB/s), 24509 tokens with values
+// into pages 105 us (602 MB: 5.7 TB/s, 0.89 of a copy); 4 tokens 3.6 us and 128 tokens 4.2 us a launch inside a graph.
 #include "kv_attention.cuh"
 
 namespace mrp {

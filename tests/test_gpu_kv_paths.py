@@ -78,6 +78,9 @@ BIG = [
     ("bf16", 12, 4, 24, 32, [(700, 40), (0, 130)], 0, 0, 0),
     ("bf16", 6, 1, 8, 8, [(500, 2), (77, 30)], 0, 0, 0),
     ("f32", 8, 2, 128, 16, [(1200, 1), (700, 30), (0, 90)], 0, 0, 0),
+    ("bf16", 300, 1, 64, 16, [(140, 2), (0, 1), (700, 1)], 0, 0, 0),                         # a token's heads over several row tiles
+    ("bf16", 300, 2, 128, 32, [(140, 5), (0, 1)], 0, 64, 4),
+    ("f32", 50, 1, 32, 16, [(140, 2), (0, 1)], 0, 0, 0),
 ]
 
 
