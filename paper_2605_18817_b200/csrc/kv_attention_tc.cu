@@ -250,35 +250,46 @@ template <int DB, bool JOINED> struct TileAt {             // of a tile: bytes t
     static constexpr uint32_t block = JOINED ? 1024 : 128 * 128, group = JOINED ? DB * 1024 : 1024;
 };
 
-// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
-template <int DB, bool JOINED, typename Tile>
-__device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const Tile &t, int n, int s,
-                                           int h, int feature, uint32_t dst, uint32_t bar, int lane)
+// The box of a tile's keys that is the lane's: where it lies in the pool.  Looked up a tile ahead of its use.
+struct PageRef {
+    bool need;                 // holds visible positions
+    int entry, row;            // page, row in it
+};
+template <typename Tile>
+__device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes &bx, const Tile &t, int n, int s, int lane)
 {
     const int j = key_tile(t, n) * kTcTile + lane * bx.rows;
-    const bool need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
-    int entry = 0, row = 0;
-    bool bad = false;
-    if (need) {
+    PageRef r;
+    r.need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
+    r.entry = r.row = 0;
+    if (r.need) {
         const int pg = fast_div(j, p.b.page);
-        row = j - pg * p.b.page.d;
-        entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
-        bad = (unsigned)entry >= (unsigned)p.b.n_pages;
-        if (bad) kv_bad_index(p.b);
+        r.row = j - pg * p.b.page.d;
+        r.entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
     }
-    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, need));
+    return r;
+}
+
+// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
+template <int DB, bool JOINED>
+__device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
+                                           uint32_t dst, uint32_t bar, int lane)
+{
+    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, r.need));
     if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * 128u * DB);
     __syncwarp();
-    if (need) {
+    if (r.need) {
+        const bool bad = (unsigned)r.entry >= (unsigned)p.b.n_pages;
+        if (bad) kv_bad_index(p.b);
         dst += lane * (bx.rows >> 3) * TileAt<DB, JOINED>::group;
         // (a page that is not one: outside the map, zeros arrive)
         if (JOINED) {
-            const int g = bad ? bx.groups : entry * bx.page_groups + h * bx.head_groups + (row >> 3);
+            const int g = bad ? bx.groups : r.entry * bx.page_groups + h * bx.head_groups + (r.row >> 3);
             tma_load_page(dst, map, 0, 0, feature >> 6, g, bar);
         } else {
 #pragma unroll
             for (int x = 0; x < DB; ++x)
-                tma_load_page(dst + x * (128 * 128), map, feature + 64 * x, row, h, bad ? p.b.n_pages : entry, bar);
+                tma_load_page(dst + x * (128 * 128), map, feature + 64 * x, r.row, h, bad ? p.b.n_pages : r.entry, bar);
         }
     }
 }
@@ -547,19 +558,24 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
-            auto fetch = [&](int n, const CUtensorMap *map) {
+            auto fetch = [&](const PageRef &r, const CUtensorMap *map) {
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB, JOINED>(p, map, bx, cur.t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    fetch_tile<DB, JOINED>(p, map, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
                     if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
                 }
             };
-            fetch(0, &kmap);
+            PageRef now = look_up(p, bx, cur.t, begin, cur.s, lane), next = now, then = now;
+            if (count > 1) next = look_up(p, bx, cur.t, begin + 1, cur.s, lane);
+            fetch(now, &kmap);
             for (int n = 0; n < count; ++n) {
-                if (n + 1 < count) fetch(n + 1, &kmap);
-                fetch(n, &vmap);
+                if (n + 2 < count) then = look_up(p, bx, cur.t, begin + n + 2, cur.s, lane);
+                if (n + 1 < count) fetch(next, &kmap);
+                fetch(now, &vmap);
+                now = next;
+                next = then;
             }
             leave_unit(p, cur, part.places, piece_end);
         }
@@ -979,20 +995,25 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             const int begin = part.begin, count = part.count;
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
-            auto fetch = [&](int n, int which) {
+            auto fetch = [&](const PageRef &r, int which) {
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB, JOINED>(p, which ? &vmap : &kmap, bx, t, begin + n, cur.s, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    fetch_tile<DB, JOINED>(p, which ? &vmap : &kmap, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
                     if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
                 }
             };
-            fetch(0, 0);
+            PageRef now = look_up(p, bx, t, begin, cur.s, lane), next = now, then = now;
+            if (count > 1) next = look_up(p, bx, t, begin + 1, cur.s, lane);
+            fetch(now, 0);
             for (int n = 0; n < count; ++n) {              // the order in which the MMA warp takes them
-                if (NT == 2) fetch(n, 1);
-                if (n + 1 < count) fetch(n + 1, 0);
-                if (NT == 1) fetch(n, 1);
+                if (n + 2 < count) then = look_up(p, bx, t, begin + n + 2, cur.s, lane);
+                if (NT == 2) fetch(now, 1);
+                if (n + 1 < count) fetch(next, 0);
+                if (NT == 1) fetch(now, 1);
+                now = next;
+                next = then;
             }
             leave_unit(p, cur, part.places, piece_end);
         }
