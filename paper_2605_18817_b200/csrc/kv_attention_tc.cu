@@ -129,9 +129,12 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // the rows there are, not of 128, and all 128 threads of a warpgroup have a key each.
 //   warp 0   K and V tiles by TMA, as below        warp 1   MMAs        warps 2, 3   queries and what rows see, a unit ahead
 //   warps 4-7, 8-11   two warpgroups that take tiles in turn, each with its own S buffer, maxima, sums and accumulator (no
-//            exchange until the unit's end): a thread turns its key's scores into probabilities and stores them as a row
-//            of the operand P [keys][rows] in shared memory, bf16 hi and lo columns side by side (2^-17 together: the second
+//            exchange between them): a thread turns its key's scores into probabilities and stores them as a row of the
+//            operand P [keys][rows] in shared memory, bf16 hi and lo columns side by side (2^-17 together: the second
 //            product costs nothing that shows)
+//   warps 12-15   the units' ends: both accumulators joined, rows or partial results written, pieces joined, while the others
+//            are in the next unit (accumulators, sums and maxima of two units).  The first warpgroup did it before: 24 single
+//            tokens 65 against 61 us, at 64 features 54 against 44
 // The maximum in use is common to a warpgroup's 128 keys, so a tile needs to know only whether some score exceeds it by
 // more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
 // rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it (64 ragged
@@ -148,8 +151,8 @@ template <int NB> struct FewGeo {
     static constexpr int kQ = NB * NR * 128;               // queries of a unit, two of them
     static constexpr int kPAt = kRing, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;
-    static constexpr int kTmem = B::HB == 2 ? 256 : 128;   // of which 2 NR + 2 HB kCols are used
-    static constexpr int kThreads = 384;
+    static constexpr int kTmem = B::HB == 2 ? 512 : 256;   // of which 2 NR + 4 HB kCols are used
+    static constexpr int kThreads = 512;
     static constexpr int kWide = B::HB * 128;              // features of a row of partial results
 };
 constexpr float kNone = -3.4028234e38f;    // the maximum of a row that has seen nothing
@@ -476,7 +479,7 @@ __device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
 }
 
 template <int NB, bool JOINED>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(512, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
 {
@@ -488,8 +491,8 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
     __shared__ long long sh_find[G::kThreads / 32 + 2];
     __shared__ Suspects suspects[2];
     __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
-    __shared__ __align__(16) float sh_m[2][NR], sh_c[2][NR];       // maximum in use, factor to it, per warpgroup
-    __shared__ float sh_wm[2][4][NR], sh_wl[2][4][NR];     // row maxima and sums of the warps
+    __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR];   // maximum in use (unit, warpgroup), factor to it
+    __shared__ float sh_wm[2][4][NR], sh_wl[2][2][4][NR];  // row maxima and (of a unit) sums of the warps
     __shared__ float sh_f[2][NR];                          // the unit's end: factors of the accumulators,
     __shared__ int64_t sh_out[NR];                         //   where the rows go
     __shared__ int sh_last;
@@ -505,9 +508,9 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
     auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
     auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
     auto unit_end = [&](int x) { return bars + 8 * (40 + x); };    // the unit is written: everything of it may be reused
-    const uint32_t second_end = bars + 8 * 42;             // the second warpgroup's sums are there
+    auto acc_full = [&](int x) { return bars + 8 * (42 + x); };    // the unit's sums, maxima and accumulators are there
     unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 43);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 44);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     const WaitStatus ws = {p.b.status, p.b.user_status};
 
@@ -522,8 +525,8 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             mbar_init(pv_done(x), 1);
             mbar_init(q_ready(x), 64);
             mbar_init(unit_end(x), 4);
+            mbar_init(acc_full(x), 8);
         }
-        mbar_init(second_end, 4);
         *abort_flag = 0;
         prefetch_tmap(&kmap);
         prefetch_tmap(&vmap);
@@ -536,9 +539,9 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators
+    const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators of two units
     auto s_at = [&](int x) { return tmem + x * NR; };
-    auto o_at = [&](int x) { return tmem + 2 * NR + x * HB * G::kCols; };         // (HB accumulators of 128 features)
+    auto o_at = [&](int u, int x) { return tmem + 2 * NR + (2 * u + x) * HB * G::kCols; };       // (HB accumulators of 128 features)
     pdl_wait();
     pdl_trigger();
 
@@ -635,7 +638,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     if (elect_one()) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c)        // (one block of features: the second 64 lanes repeat it)
-                            umma_bf16(o_at(k & 1u) + y * G::kCols, mn_desc(vs + c * 2 * lay::group, DB == 2 ? lay::block : 0, lay::group), mn_desc(ps + c * 2048, 0, 1024), idesc_o,
+                            umma_bf16(o_at(unit & 1u, k & 1u) + y * G::kCols, mn_desc(vs + c * 2 * lay::group, DB == 2 ? lay::block : 0, lay::group), mn_desc(ps + c * 2048, 0, 1024), idesc_o,
                                       n >= 2 || c > 0);
                         if (y + 1 == HB) umma_commit(pv_done(k & 1u));
                         umma_commit(empty_bar(stage));
@@ -670,12 +673,12 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
         }
-    } else if (warp >= 4) {
+    } else if (warp < 12) {
         // ================================ softmax: a thread per key, two warpgroups in turn ================================
         const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
         const int bar_id = 1 + x;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t s_tm = s_at(x) + lanes, o_tm = o_at(x) + lanes;
+        const uint32_t s_tm = s_at(x) + lanes;
         const uint32_t p_row = base + G::kPAt + x * G::kP + wt * 128;
         uint32_t k0 = 0, unit = 0;
         const float sc = p.scale_log2;
@@ -688,7 +691,11 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const int u = unit & 1;
-            if (wt < NR) sh_m[x][wt] = kNone;
+            const uint32_t o_tm = o_at(u, x) + lanes;
+            float *sh_m = sh_ms[u][x];
+            if (unit >= 2) ok = mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws);
+            if (wg_any(bar_id, !ok)) break;
+            if (wt < NR) sh_m[wt] = kNone;
             wg_sync(bar_id);
 #pragma unroll
             for (int r = 0; r < NR; ++r) l[r] = 0.f;
@@ -720,7 +727,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 auto against_max = [&]() {                 // exponents
 #pragma unroll
                     for (int i = 0; i < NR; i += 4) {
-                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[x][i]);
+                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[i]);
                         s[i] = fmaf(s[i], sc, -m.x); s[i + 1] = fmaf(s[i + 1], sc, -m.y);
                         s[i + 2] = fmaf(s[i + 2], sc, -m.z); s[i + 3] = fmaf(s[i + 3], sc, -m.w);
                     }
@@ -747,9 +754,9 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     wg_sync(bar_id);
                     if (wt < NR) {
                         const float top = fmaxf(fmaxf(sh_wm[x][0][wt], sh_wm[x][1][wt]), fmaxf(sh_wm[x][2][wt], sh_wm[x][3][wt]));
-                        const float m = sh_m[x][wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
+                        const float m = sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
                         sh_c[x][wt] = nm == m ? 1.f : ex2f(m - nm);
-                        sh_m[x][wt] = nm;
+                        sh_m[wt] = nm;
                     }
                     wg_sync(bar_id);
                     if (n >= 2) {
@@ -796,107 +803,114 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 if (lane == 0) mbar_arrive(p_ready(x));
             }
             if (!ok) break;
-            // ---- the unit's end: sums over the warp's keys
+            // ---- the unit's end: sums over the warp's keys, the last product
             const float sum = reduce_rows<NR, false>(l, lane);
-            if (lane < NR) sh_wl[x][wq][lane] = sum;
-            if (x == 1) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(second_end);
-                ok = mbar_wait(unit_end(u), (unit >> 1) & 1u, abort_flag, ws);
-                if (wg_any(bar_id, !ok)) break;
-            } else {
-                // the first warpgroup joins both and writes.  (The second one's sums first: it has then seen the scores of its
-                // last tile, so that the product before its last is done and pv_done(1) is at most one phase behind.)
-                ok = mbar_wait(second_end, unit & 1u, abort_flag, ws);
-                bool has[2];
+            if (lane < NR) sh_wl[u][x][wq][lane] = sum;
+            if (n0 < count) {
+                const uint32_t last = k0 + (uint32_t)(n0 + ((count - 1 - n0) & ~1));
+                ok = mbar_wait(pv_done(x), (last >> 1) & 1u, abort_flag, ws);
+            }
+            if (wg_any(bar_id, !ok)) break;
+            tc_fence_before();
+            if (lane == 0) mbar_arrive(acc_full(u));
+            k0 += (uint32_t)count;
+            ++unit;
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else {
+        // ================================ units' ends: both accumulators joined, written, pieces joined ================================
+        const int wq = warp & 3, wt = wq * 32 + lane;
+        const int bar_id = 3;
+        const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+        uint32_t k0 = 0, unit = 0;
+        bool ok = true;
+        while (cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const int u = unit & 1;
+            ok = mbar_wait(acc_full(u), (unit >> 1) & 1u, abort_flag, ws);
+            if (wg_any(bar_id, !ok)) break;
+            bool has[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) has[y] = (int)((k0 & 1u) ^ (uint32_t)y) < count;
+            tc_fence_after();
+            const bool whole_unit = count == t.tiles;
+            const int slot = 2 * (int)blockIdx.x + (begin == 0 ? 1 : 0);
+            const int rows = t.rows;
+            if (wt < NR) {
+                float lw[2], mw[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const int first = (int)((k0 & 1u) ^ (uint32_t)y);
-                    has[y] = first < count;
-                    if (has[y]) {
-                        const uint32_t last = k0 + (uint32_t)(first + ((count - 1 - first) & ~1));
-                        ok = ok && mbar_wait(pv_done(y), (last >> 1) & 1u, abort_flag, ws);
+                    lw[y] = sh_wl[u][y][0][wt] + sh_wl[u][y][1][wt] + sh_wl[u][y][2][wt] + sh_wl[u][y][3][wt];
+                    mw[y] = sh_ms[u][y][wt];
+                }
+                const float M = fmaxf(mw[0], mw[1]);
+                const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
+                float L = lw[0] * f0 + lw[1] * f1;
+                if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) L = __int_as_float(0x7FC00000);
+                const float inv = whole_unit ? inverse(L) : 1.f;
+                sh_f[0][wt] = f0 * inv;
+                sh_f[1][wt] = f1 * inv;
+                if (wt < rows) {
+                    const int rr = t.r0 + wt, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
+                    if (!whole_unit) {
+                        __stcg(p.part.ml + (size_t)slot * NR + wt, make_float2(M, L));
+                    } else {
+                        sh_out[wt] = (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
+                        if (p.lse) p.lse[(int64_t)(cur.start + tok) * p.H + head] = log_sum(M, L);
                     }
                 }
-                if (wg_any(bar_id, !ok)) break;
-                tc_fence_after();
-                const bool whole_unit = count == t.tiles;
-                const int slot = 2 * (int)blockIdx.x + (begin == 0 ? 1 : 0);
-                const int rows = t.rows;
-                if (wt < NR) {
-                    float lw[2], mw[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        lw[y] = sh_wl[y][0][wt] + sh_wl[y][1][wt] + sh_wl[y][2][wt] + sh_wl[y][3][wt];
-                        mw[y] = sh_m[y][wt];
-                    }
-                    const float M = fmaxf(mw[0], mw[1]);
-                    const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
-                    float L = lw[0] * f0 + lw[1] * f1;
-                    if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) L = __int_as_float(0x7FC00000);
-                    const float inv = whole_unit ? inverse(L) : 1.f;
-                    sh_f[0][wt] = f0 * inv;
-                    sh_f[1][wt] = f1 * inv;
-                    if (wt < rows) {
-                        const int rr = t.r0 + wt, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
-                        if (!whole_unit) {
-                            __stcg(p.part.ml + (size_t)slot * NR + wt, make_float2(M, L));
-                        } else {
-                            sh_out[wt] = (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
-                            if (p.lse) p.lse[(int64_t)(cur.start + tok) * p.H + head] = log_sum(M, L);
-                        }
-                    }
-                }
-                wg_sync(bar_id);
-#pragma unroll
-                for (int y = 0; y < HB; ++y) {             // a thread per feature, of each 128
-                    const int f = y * 128 + wt;
-                    float a[NR], o[4][NR];
-#pragma unroll
-                    for (int z = 0; z < 2; ++z)
-                        if (has[z]) {
-                            tmem_ld16_go(o_at(z) + y * G::kCols + lanes, o[2 * z]);
-                            tmem_ld16_go(o_at(z) + y * G::kCols + lanes + NR, o[2 * z + 1]);
-                        }
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) tmem_landed16(o[z]);
-#pragma unroll
-                    for (int i = 0; i < NR; ++i) {
-                        a[i] = 0.f;
-                        if (has[0]) a[i] = (o[0][i] + o[1][i]) * sh_f[0][i];
-                        if (has[1]) a[i] = fmaf(o[2][i] + o[3][i], sh_f[1][i], a[i]);
-                    }
-                    if (f < p.D && whole_unit) {
-#pragma unroll
-                        for (int i = 0; i < NR; ++i)
-                            if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + f] = __float2bfloat16_rn(a[i]);
-                    } else if (f < p.D) {
-                        float *to = p.part.o + (size_t)slot * NR * G::kWide + f;
-#pragma unroll
-                        for (int i = 0; i < NR; ++i)
-                            if (i < rows) __stcg(to + i * G::kWide, a[i]);
-                    }
-                }
-                tc_fence_before();
-                if (!whole_unit) {
-                    // ---- the pieces of the unit meet: the CTA that arrives last joins them in order
-                    int c0, c1;
-                    unit_pieces(p, cur, per, c0, c1);
-                    wg_sync(bar_id);
-                    if (wt == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
-                    wg_sync(bar_id);
-                    if (sh_last) {
-                        const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
-                        if (rows <= 4) join_rows<NR, G::kWide, 1, 8>(ja, wq, lane);
-                        else join_rows<NR, G::kWide, 2, 4>(ja, wq, lane);
-                        if (wt == 0) p.part.counters[c0] = 0;
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(unit_end(u));
-                wg_sync(bar_id);                           // sh_f, sh_out and sh_last are read
             }
+            wg_sync(bar_id);
+#pragma unroll
+            for (int y = 0; y < HB; ++y) {             // a thread per feature, of each 128
+                const int f = y * 128 + wt;
+                float a[NR];
+#pragma unroll
+                for (int i = 0; i < NR; ++i) a[i] = 0.f;
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    if (has[z]) {
+                        float o[2][NR];
+                        tmem_ld16_go(o_at(u, z) + y * G::kCols + lanes, o[0]);
+                        tmem_ld16_go(o_at(u, z) + y * G::kCols + lanes + NR, o[1]);
+                        tmem_wait_ld();
+                        tmem_landed16(o[0]);
+                        tmem_landed16(o[1]);
+#pragma unroll
+                        for (int i = 0; i < NR; ++i) a[i] = fmaf(o[0][i] + o[1][i], sh_f[z][i], a[i]);
+                    }
+                if (f < p.D && whole_unit) {
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + f] = __float2bfloat16_rn(a[i]);
+                } else if (f < p.D) {
+                    float *to = p.part.o + (size_t)slot * NR * G::kWide + f;
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) __stcg(to + i * G::kWide, a[i]);
+                }
+            }
+            tc_fence_before();
+            if (!whole_unit) {
+                // ---- the pieces of the unit meet: the CTA that arrives last joins them in order
+                int c0, c1;
+                unit_pieces(p, cur, per, c0, c1);
+                wg_sync(bar_id);
+                if (wt == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
+                wg_sync(bar_id);
+                if (sh_last) {
+                    const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
+                    if (rows <= 4) join_rows<NR, G::kWide, 1, 8>(ja, wq, lane);
+                    else join_rows<NR, G::kWide, 2, 4>(ja, wq, lane);
+                    if (wt == 0) p.part.counters[c0] = 0;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(unit_end(u));
+            wg_sync(bar_id);                           // sh_f, sh_out and sh_last are read
             k0 += (uint32_t)count;
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
