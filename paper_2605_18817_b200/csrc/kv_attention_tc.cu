@@ -138,8 +138,9 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // The maximum in use is common to a warpgroup's 128 keys, so a tile needs to know only whether some score exceeds it by
 // more than 2^8: one barrier with a vote.  Only then are the row maxima reduced (lanes, then warps) and the accumulator
 // rescaled.  Sums stay per thread until the unit's end.  K and V are the only streams that count: memory bounds it (64 ragged
-// single tokens 165 us against 158 for the bytes; 24 blocks of 16 72 against 50; one token behind 2047 positions, 16 heads: 13,
-// of which the launch, the cut and the joining of 16 pieces are most).
+// single tokens 165 us against 158 for the bytes; 24 sequences of 200 to 6000 positions, one token 61 and four 64 against 48;
+// one token behind 2047 positions, 16 heads: 13, of which the launch, the cut and the joining of 16 pieces are most).  Caches of
+// one or two tiles are bound by a unit's chain instead, about 6 us an SM: 256 sequences of 20 to 300 positions 118 against 27.
 constexpr int kFewRows = 16;
 template <int NB> struct FewGeo {
     typedef Blocks<NB> B;
@@ -1512,7 +1513,7 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
         if (bx.groups) return wide ? few_launch<4, true>(c, p, km, vm, bx, st) : few_launch<2, true>(c, p, km, vm, bx, st);
         return wide ? few_launch<4, false>(c, p, km, vm, bx, st) : few_launch<2, false>(c, p, km, vm, bx, st);
     };
-    // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 65 us on the
+    // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 61 us on the
     // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
     // took 95 and 113 against 78 and 80.
     if (rows <= kFewRows) return few();
