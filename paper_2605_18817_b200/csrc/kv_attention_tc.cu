@@ -1241,6 +1241,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * c);
                                 tmem_st16(o_tm + 16 * f, w);
                             }
+                            // The first half's product adds to ALL columns and waits for the first half's warps alone: both halves'
+                            // columns are stored before either goes on.
+                            tmem_wait_st();
+                            tc_fence_before();
+                            any_of(pair, 64, false);
+                            tc_fence_after();
                         }
                         l *= c;
                         m = nm;
