@@ -62,7 +62,8 @@ __device__ __forceinline__ bool kv_sequence(const KvBatch &b, int s, int &start,
 // ---- workspace: arrival counters, then (max, sum) pairs and rows of partial results -----------------------------------
 // Slot 2 c holds CTA c's part of a unit that an earlier CTA began, slot 2 c + 1 its part of one that a later CTA goes on
 // with; a slot is `rows` rows of `width` floats and as many (max, sum) pairs.
-constexpr int kKvCounterBytes = 8192;      // int32 arrivals by the CTA that begins a shared unit (large tiles: per warp too); zero between calls
+constexpr int kKvCounterBytes = 8192;      // int32 arrivals by the CTA that begins a shared unit (large tiles: per warp too); zero between
+                                           // calls, also behind one whose wait gave up (settle_arrivals)
 // Arrival behind a barrier of the threads that wrote: releases their stores, acquires those of the arrivals before.
 __device__ __forceinline__ int arrive_acq_rel(int32_t *counter)
 {
@@ -216,6 +217,23 @@ __device__ __forceinline__ void unit_pieces(const AttnParams &p, const Cursor<RO
 {
     c0 = (int)div_line(c.unit + p.lead, per);
     c1 = (int)div_line(c.unit + p.lead + c.t.tiles - 1, per);
+}
+
+// What a CTA that leaves early (a wait gave up) still owes: an arrival at each cut unit it holds tiles of, from the unit at `c`
+// to the end of its piece, so that the counters come back to zero and the next call's pieces are not joined early.
+// `arrive(c, c0, c1)` counts one of the c1 - c0 + 1 arrivals and clears the counter at the last; nothing is joined.
+template <int ROWS, int TILE, typename F>
+__device__ __forceinline__ void settle_arrivals(const AttnParams &p, Cursor<ROWS, TILE> &c, long long per, long long piece_end, F arrive)
+{
+    while (c.at < piece_end) {
+        const UnitPart u = unit_part(p, c, piece_end);
+        if (u.count > 0 && u.count < c.t.tiles) {
+            int c0, c1;
+            unit_pieces(p, c, per, c0, c1);
+            arrive(c, c0, c1);
+        }
+        leave_unit(p, c, u.places, piece_end);
+    }
 }
 
 // Sets `c` to the start of this CTA's piece and returns its length; `per` is the length of a full piece.

@@ -916,6 +916,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
         }
+        if (wt == 0)                                   // (units are left over only where a wait gave up)
+            settle_arrivals(p, cur, per, piece_end, [&](const Cursor<NR, kTcTile> &, int c0, int c1) {
+                if (arrive_acq_rel(p.part.counters + c0) == c1 - c0) p.part.counters[c0] = 0;
+            });
     }
 
     __syncthreads();
@@ -1375,6 +1379,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
         }
+        if (half == 0 && lane == 0)                    // (units are left over only where a wait gave up)
+            settle_arrivals(p, cur, per, piece_end, [&](const Cursor<kRows, kTcTile> &c, int c0, int c1) {
+                if (x * 128 + wq * 32 >= c.t.rows) return;             // no row of these 32: nobody counts them
+                int *counter = p.part.counters + (c0 * NT + x) * 4 + wq;
+                if (arrive_acq_rel(counter) == c1 - c0) *counter = 0;
+            });
     }
 
     __syncthreads();
