@@ -254,6 +254,7 @@ class Context:
     keep: tuple           # weights + workspace kept alive for the context's lifetime
     guards: tuple = ()    # (buffer, workspace offset, workspace bytes, guard bytes) for workspace_guards_intact
     kv: object = None     # geometry of the paged cache (mrp_kv_attach)
+    kv_ws: object = None  # and its workspace: one for all geometries that fit in it
 
     @property
     def family(self) -> str:
@@ -441,7 +442,8 @@ def mrp_module_set_prefix(ctx: Context, caches, prefix_len, append=False) -> Non
 def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_pages=0, max_pages=0, page_stride=0, rot_dim=0,
                   rot_theta=10000.0, rot_interleaved=False, inv_freq=None, norm_eps=1e-6) -> None:
     """Attach the geometry of a paged key / value cache (mrp_kv_config); allocates its workspace (a torch tensor kept with
-    the context).  ``inv_freq``: rot_dim / 2 numbers instead of the powers of ``rot_theta``."""
+    the context; another attach, say for a pool that has grown, takes the one that is there).
+    ``inv_freq``: rot_dim / 2 numbers instead of the powers of ``rot_theta``."""
     freq = None
     if inv_freq is not None:
         vals = [float(x) for x in inv_freq]
@@ -453,7 +455,12 @@ def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_page
     nbytes = int(lib.mrp_kv_workspace_bytes(ctypes.byref(ctx.cfg), ctypes.byref(kv)))
     if nbytes == 0:
         raise MrpError("mrp_kv_workspace_bytes", 1)
-    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda:%d" % ctx.cfg.device)
+    ws = ctx.kv_ws
+    if ws is None or ws.numel() < nbytes + 256:
+        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda:%d" % ctx.cfg.device)
+        ctx.keep, ctx.kv_ws = tuple(ctx.keep) + (ws,), ws
+    else:
+        torch.cuda.synchronize(ctx.cfg.device)             # calls that still use it
     off = (-ws.data_ptr()) % 256
     rc = lib.mrp_kv_attach(ctx.handle, ctypes.byref(kv), ctypes.c_void_p(ws.data_ptr() + off), ctypes.c_size_t(nbytes))
     if rc != 0:
@@ -463,7 +470,6 @@ def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_page
     ctx.kv = _KvShape(dtype, ctx.cfg.device, (kv.n_heads, kv.head_dim), (kv.n_kv_heads, kv.head_dim),
                       (kv.n_pages, kv.n_kv_heads, kv.page_size, kv.head_dim),
                       (kv.page_stride or page, kv.page_size * kv.head_dim, kv.head_dim, 1), kv.max_pages)
-    ctx.keep = tuple(ctx.keep) + (ws,)
 
 
 @dataclass
