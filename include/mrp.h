@@ -399,8 +399,8 @@ size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv);
 /*
  * Attach a cache geometry to a context (workspace borrowed until mrp_destroy or the next attach: DEVICE, 256-byte
  * aligned, at least mrp_kv_workspace_bytes; it must not serve another context too).  Like mrp_create this call may
- * block (it clears the workspace's arrival counters); make it outside of any stream capture and with no call on the
- * context in flight.  The three calls below run on the context's device and, like every call on a context, one after the
+ * block (it clears the workspace's arrival counters, on the legacy stream); make it outside of any stream capture, with no
+ * call on the context in flight and nothing pending on any stream that writes the workspace.  The three calls below run on the context's device and, like every call on a context, one after the
  * other: a captured graph of them counts as a call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
  */
 int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t workspace_bytes);

@@ -442,7 +442,7 @@ def mrp_module_set_prefix(ctx: Context, caches, prefix_len, append=False) -> Non
 def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_pages=0, max_pages=0, page_stride=0, rot_dim=0,
                   rot_theta=10000.0, rot_interleaved=False, inv_freq=None, norm_eps=1e-6) -> None:
     """Attach the geometry of a paged key / value cache (mrp_kv_config); allocates its workspace (a torch tensor kept with
-    the context; another attach, say for a pool that has grown, takes the one that is there).
+    the context; another attach, say for a pool that has grown, takes the one that is there) and waits for the device.
     ``inv_freq``: rot_dim / 2 numbers instead of the powers of ``rot_theta``."""
     freq = None
     if inv_freq is not None:
@@ -459,8 +459,9 @@ def mrp_kv_attach(ctx: Context, n_heads, n_kv_heads, head_dim, page_size, n_page
     if ws is None or ws.numel() < nbytes + 256:
         ws = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda:%d" % ctx.cfg.device)
         ctx.keep, ctx.kv_ws = tuple(ctx.keep) + (ws,), ws
-    else:
-        torch.cuda.synchronize(ctx.cfg.device)             # calls that still use it
+    # the workspace is cleared on a stream of its own: calls that still use it, and what is pending on memory that the
+    # allocator hands out again, end first
+    torch.cuda.synchronize(ctx.cfg.device)
     off = (-ws.data_ptr()) % 256
     rc = lib.mrp_kv_attach(ctx.handle, ctypes.byref(kv), ctypes.c_void_p(ws.data_ptr() + off), ctypes.c_size_t(nbytes))
     if rc != 0:

@@ -1,4 +1,4 @@
-"""Attaching a cache geometry again."""
+"""Attaching a cache geometry again, and a workspace from memory that is still in use."""
 import pytest
 import torch
 
@@ -45,3 +45,27 @@ def test_attaching_behind_a_call_that_still_runs():
             c.b.mrp_paged_attention(c.ctx, c.batch, c.k_pages, c.v_pages, q, out, lse)
             side.synchronize()
             assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+@gpu
+def test_a_workspace_from_memory_with_work_pending():
+    """The allocator hands a block out again on its stream while a kernel there has yet to write it."""
+    c = Cache("bf16", 8, 2, 128, 16, [(3000, 1)], seed=5)
+    q = c.rand(c.T, 8, 128)
+    size = int(c.ctx.kv_ws.numel()) if getattr(c.ctx, "kv_ws", None) is not None else c.ctx.keep[-1].numel()
+    w_lm = torch.zeros((32, 64), device=DEV, dtype=torch.bfloat16)
+    fresh = c.b.mrp_create(64, 64, 32, [], w_lm, max_rows=1, max_seqs=1, block_len=1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        x = torch.empty(size, dtype=torch.uint8, device=DEV)
+        torch.cuda._sleep(400000000)
+        x.fill_(1)
+        at = x.data_ptr()
+        del x
+        c.b.mrp_kv_attach(fresh, 8, 2, 128, 16, c.k_pages.shape[0], c.max_pages)
+        assert any(t.data_ptr() == at for t in fresh.keep)
+    torch.cuda.synchronize()
+    out, lse = torch.full((1, 8, 128), 7.0, device=DEV, dtype=torch.bfloat16), torch.full((1, 8), 7.0, device=DEV)
+    c.b.mrp_paged_attention(fresh, c.batch, c.k_pages, c.v_pages, q, out, lse)
+    close(c, q, out, lse)
