@@ -487,7 +487,7 @@ typedef struct {
  * Scores, softmax statistics and sums in fp32; on bf16 contexts the probabilities are rounded to bf16 as an operand of the
  * product with V (where a sequence has up to 16 rows, new tokens times query heads of a key head, to two bf16 parts).
  * What a token does not see does not reach it, whatever it holds; a value it sees that is not finite may make its output
- * NaN in all features.  The work is split over the cache's length by the device from the lengths it finds; parts are joined
+ * NaN in all features (its lse does not depend on values).  The work is split over the cache's length by the device from the lengths it finds; parts are joined
  * in a fixed order, so equal calls give equal bits.
  * bf16 with page_size a multiple of 8 runs on tiles that TMA feeds, blocks and prompts at the tensor cores' rate; f32, other
  * page sizes and MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.

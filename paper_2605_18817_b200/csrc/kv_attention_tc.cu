@@ -849,9 +849,10 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 }
                 const float M = fmaxf(mw[0], mw[1]);
                 const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
-                float L = lw[0] * f0 + lw[1] * f1;
-                if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) L = __int_as_float(0x7FC00000);
-                const float inv = whole_unit ? inverse(L) : 1.f;
+                const float L = lw[0] * f0 + lw[1] * f1;
+                float inv = whole_unit ? inverse(L) : 1.f;
+                // (the row's features, in a part of them too; its log-sum-exp knows nothing of values)
+                if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) inv = __int_as_float(0x7FC00000);
                 sh_f[0][wt] = f0 * inv;
                 sh_f[1][wt] = f1 * inv;
                 if (wt < rows) {
@@ -1292,9 +1293,9 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (any_of(pair, 64, !ok)) break;
             tc_fence_after();
             if (warp_live) {
-                float L = l + sh_sum[x][half ^ 1][row];
+                const float L = l + sh_sum[x][half ^ 1][row];
                 const Suspects &sus = suspects[unit & 1];
-                if (sus.n > 0 && suspects_hit(sus, hi_r, lo_r, p.sinks)) L = __int_as_float(0x7FC00000);
+                const bool hit = sus.n > 0 && suspects_hit(sus, hi_r, lo_r, p.sinks);      // NaN features; the log-sum-exp knows nothing of values
                 const bool whole_unit = count == t.tiles;
                 const int rr = t.r0 + x * 128 + row, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
                 const int f0 = half * (NB * 32);           // this half's features
@@ -1319,6 +1320,10 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     tmem_ld32(o_tm + 32 * f, o);
                     tmem_wait_ld();
                     tmem_landed32(o);
+                    if (hit) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __int_as_float(0x7FC00000);
+                    }
                     if (whole_unit) {
                         put32(32 * f, o, inv);
                     } else if (live) {
