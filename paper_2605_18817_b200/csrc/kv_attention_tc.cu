@@ -14,7 +14,9 @@
 //                 (and V as stored: its keys are the contraction, an MN-major operand).  The first half's product starts
 //                 while the second half's probabilities are still on their way.
 //   P is rounded to bf16 once, as an operand (2^-8 of each probability at most); the sum takes the unrounded values.  Hi + lo
-//   parts would double the products that bound prompts.
+//   parts would double the products that bound prompts.  Units of up to 16 rows, which the transposed kernel computes with both
+//   parts, get both here too (NT = 1), so a sequence's precision does not depend on the others of its batch: lo takes the
+//   columns of scores that have been read, and a second product.  24 blocks of 16, which have none: 67 -> 68 us.
 //   NT = 2 (prompts): two row tiles share every K and V tile and take turns, one in the MMAs while the other is in the
 //   exponentials.  Per pair of 128 x 128 tiles of 128 features the products take 2048 cycles, the exponentials alone 2048 of
 //   the special function unit; measured 3600 (2 prompts of 2000 behind 5600 positions, 32 / 8 heads: 450 us, 1.06 PFLOP/s; the
@@ -1041,7 +1043,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         // ================================ MMA issuer ================================
         int stage = 0;
         uint32_t phase = 0, k = 0, unit = 0;               // k: tiles done
-        bool ok = true;
+        bool ok = true, two_parts = false;
         const uint32_t idesc_s = make_idesc(128), idesc_o = make_idesc(DB * 64) | (1u << 16);
         typedef TileAt<DB, JOINED> lay;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
@@ -1063,6 +1065,11 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2 * lay::group, lay::block, lay::group), idesc_o, !first || c0 + c > 0);
+                if (two_parts) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + 32 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2 * lay::group, lay::block, lay::group), idesc_o, 1);
+                }
                 if (c0 == 4 && y + 1 == HB) umma_commit(pv_done(x));
             }
             __syncwarp();
@@ -1077,6 +1084,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
+            two_parts = NT == 1 && t.rows <= kFewRows;
             Suspects &sus = suspects[unit & 1];
             if (lane == 0) sus.n = 0;
             __syncwarp();
@@ -1173,6 +1181,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
+            const bool two_parts = NT == 1 && t.rows <= kFewRows;
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
             load_queries<NB, 128, 256>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kQTile, half * 128 + row);
             mbar_arrive(q_ready(x));
@@ -1258,24 +1267,48 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     }
                     const float mm = m == -INFINITY ? 0.f : m;
                     float l0 = 0.f, l1 = 0.f;
+                    auto exponentials = [&](int i, uint32_t &w, float &a, float &b) {
+                        fma2(s[2 * i], s[2 * i + 1], sc, -mm);
+                        a = ex2f(s[2 * i]);
+                        b = ex2f(s[2 * i + 1]);
+                        add2(l0, l1, a, b);
+                        w = pack_bf16(a, b);
+                    };
+                    if (!two_parts) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (!whole) hide(s, 32 * c);
-                        uint32_t w[16];
+                        for (int c = 0; c < 2; ++c) {
+                            if (!whole) hide(s, 32 * c);
+                            uint32_t w[16];
+                            float a, b;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            fma2(s[2 * i], s[2 * i + 1], sc, -mm);
-                            const float a = ex2f(s[2 * i]), b = ex2f(s[2 * i + 1]);
-                            add2(l0, l1, a, b);
-                            w[i] = pack_bf16(a, b);
+                            for (int i = 0; i < 16; ++i) exponentials(i, w[i], a, b);
+                            if (c == 0) {                  // (the second 32 scores lie above the columns P goes to)
+                                tmem_ld32(s_tm + 32, s);
+                                tmem_st16(s_tm, w);
+                                tmem_wait_ld();
+                                tmem_landed32(s);
+                            } else {
+                                tmem_st16(s_tm + 16, w);
+                            }
                         }
-                        if (c == 0) {                      // (the second 32 scores lie above the columns P goes to)
-                            tmem_ld32(s_tm + 32, s);
-                            tmem_st16(s_tm, w);
-                            tmem_wait_ld();
-                            tmem_landed32(s);
-                        } else {
-                            tmem_st16(s_tm + 16, w);
+                    } else {
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {      // what the rounding leaves out goes where the second 32 scores were
+                            if (!whole) hide(s, 32 * c);
+                            uint32_t w[16], lo[16];
+                            float a, b;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                exponentials(i, w[i], a, b);
+                                lo[i] = pack_bf16(a - __uint_as_float(w[i] << 16), b - __uint_as_float(w[i] & 0xFFFF0000u));
+                            }
+                            tmem_st16(s_tm + 16 * c, w);
+                            if (c == 0) {
+                                tmem_ld32(s_tm + 32, s);
+                                tmem_wait_ld();
+                                tmem_landed32(s);
+                            }
+                            tmem_st16(s_tm + 32 + 16 * c, lo);
                         }
                     }
                     l += l0 + l1;
@@ -1540,8 +1573,10 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     if (rows <= kFewRows) return few();
     // A step of single tokens beside a prompt: where most sequences must be far shorter than the longest, those of up to 16
     // rows go to the transposed kernel in a launch of their own (48 single tokens and a prompt of 512: 172 against 146 us).
+    // Two row tiles have no registers for both parts of P (prompts 470 -> 494 us with them): there they always do, which costs 5 us
+    // where there is no such sequence (three prompts of 1000: 94 -> 98; longer ones 470 -> 478, under the power cap nothing).
     int launches = 0;
-    if ((long long)batch.n_tokens * 4 < (long long)batch.n_seqs * batch.max_new) {
+    if (two || (long long)batch.n_tokens * 4 < (long long)batch.n_seqs * batch.max_new) {
         p.rows_upto = kFewRows;
         if ((e = few()) != cudaSuccess) return e;
         launches = c->launches;
