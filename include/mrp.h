@@ -486,9 +486,10 @@ typedef struct {
  * are joined by their lse: MRP_ATTN_PREFIX for the cache, and the block's own keys elsewhere.)
  * Scores, softmax statistics and sums in fp32; on bf16 contexts the probabilities are rounded to bf16 as an operand of the
  * product with V (where a sequence has up to 16 rows, new tokens times query heads of a key head, to two bf16 parts).
- * What a token does not see does not reach it, whatever it holds; a value it sees that is not finite may make its output
- * NaN in all features (its lse does not depend on values).  The work is split over the cache's length by the device from the lengths it finds; parts are joined
- * in a fixed order, so equal calls give equal bits.
+ * What a token does not see does not reach it, whatever it holds; a value it sees that is not finite (f32: or not below
+ * 2^128 - 2^116) may make its output NaN in all features (its lse does not depend on values).  The work is split over the
+ * cache's length by the device from the lengths it finds; parts are joined in a fixed order, so equal calls give equal bits.
+ * A call whose status shows MRP_DEV_TIMEOUT has written rows that mean nothing; later calls are not affected.
  * bf16 with page_size a multiple of 8 runs on tiles that TMA feeds, blocks and prompts at the tensor cores' rate; f32, other
  * page sizes and MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */

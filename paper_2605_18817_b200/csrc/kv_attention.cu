@@ -112,7 +112,8 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int row, int chunk) 
 }
 
 // Zeroes values that are not finite in rows that some but not all query rows see, after adding them to the rows that
-// do: 0 * inf must not reach the others.  p[nt][4]: the warp's probabilities; v: the warp's 16 value rows.
+// do: 0 * inf must not reach the others.  p[nt][4]: the warp's probabilities; v: the warp's 16 value rows.  f32: the numbers that
+// round to infinity as tf32 too (from 2^128 - 2^116 on).
 template <typename T, int DP, int NF>
 __device__ __noinline__ void patch_nonfinite(uint32_t v, const float (&pr)[2][4], float (&o)[NF][4], int lane)
 {
@@ -124,7 +125,7 @@ __device__ __noinline__ void patch_nonfinite(uint32_t v, const float (&pr)[2][4]
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + key * pitch + c * 16) : "memory");
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            bad |= sizeof(T) == 4 ? (w[i] & 0x7F800000u) == 0x7F800000u
+            bad |= sizeof(T) == 4 ? (w[i] & 0x7FFFFFFFu) >= 0x7F7FF000u
                                   : (w[i] & 0x7F800000u) == 0x7F800000u || (w[i] & 0x7F80u) == 0x7F80u;
     }
     uint32_t rows = __ballot_sync(0xffffffffu, bad);

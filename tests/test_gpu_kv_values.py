@@ -55,3 +55,27 @@ def test_the_log_sum_exp_does_not_depend_on_values(case, where):
         check_lse(c, q, lse)
         c.v_pages[page, :, row] = kept
         close(c, q, out, lse, rows=clean)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,D,P,new", [("f32", 64, 16, 9), ("f32", 128, 24, 30), ("f32", 256, 16, 12), ("bf16", 64, 20, 9), ("bf16", 128, 16, 3),
+                                           ("bf16", 128, 16, 40), ("bf16", 64, 32, 40)])
+def test_the_types_extreme_values_reach_only_the_rows_that_see_them(dtype, D, P, new):
+    """Finite, but at the end of the type's range: rows that do not see them are as they would be."""
+    c = Cache(dtype, 4, 2, D, P, [(150, new), (40, new)], seed=D)
+    q = c.rand(c.T, 4, D)
+    page, row = c.table_np[0, (150 + new // 2) // P], (150 + new // 2) % P
+    limits = torch.finfo(q.dtype)
+    clean = torch.ones(c.T, dtype=torch.bool, device=DEV)
+    clean[new // 2:new] = False
+    kept = c.v_pages[page, :, row].clone(), c.k_pages[page, :, row].clone()
+    for what in (limits.max, limits.min):
+        c.v_pages[page, :, row] = what
+        out, lse = c.attend(q)
+        check_lse(c, q, lse)
+        c.v_pages[page, :, row] = kept[0]
+        close(c, q, out, lse, rows=clean)
+        c.k_pages[page, :, row] = what
+        out, lse = c.attend(q)
+        c.k_pages[page, :, row] = kept[1]
+        close(c, q, out, lse, rows=clean)
