@@ -445,6 +445,11 @@ int mrp_module_step_kl(mrp_ctx *ctx, const int32_t *tokens, const void *hidden0,
 }
 
 // ---- the paged key / value cache ------------------------------------------------------------------------------------
+static double pair_frequency(const mrp_kv_config &kv, int j)
+{
+    return kv.inv_freq ? kv.inv_freq[j] : pow(kv.rot_theta, -2.0 * j / kv.rot_dim);
+}
+
 static bool kv_ok(const mrp_kv_config *kv)
 {
     if (!kv || kv->n_heads < 1 || kv->n_kv_heads < 1 || kv->n_heads % kv->n_kv_heads || kv->n_heads > 65536) return false;
@@ -456,10 +461,9 @@ static bool kv_ok(const mrp_kv_config *kv)
     if (kv->n_pages > 0 && (kv->page_stride ? kv->page_stride : page) > (1ll << 60) / kv->n_pages) return false;
     if (kv->rot_dim < 0 || kv->rot_dim > kv->head_dim || kv->rot_dim % 2) return false;
     if (kv->rot_dim > 0 && !kv->inv_freq && !(kv->rot_theta > 0 && isfinite(kv->rot_theta))) return false;
-    if (kv->rot_dim > 0 && kv->inv_freq)
-        for (int j = 0; j < kv->rot_dim / 2; ++j)
-            if (!isfinite(kv->inv_freq[j])) return false;
-    return kv->norm_eps >= 0.f;
+    for (int j = 0; j < kv->rot_dim / 2; ++j)
+        if (!isfinite(pair_frequency(*kv, j))) return false;
+    return kv->norm_eps >= 0.f && isfinite(kv->norm_eps);
 }
 
 size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv)
@@ -481,8 +485,7 @@ int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t
     c.kv.inv_freq = nullptr;
     if (c.kv.page_stride == 0) c.kv.page_stride = (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim;
     for (int j = 0; j < kv->rot_dim / 2; ++j) {
-        const double w = kv->inv_freq ? kv->inv_freq[j] : pow(kv->rot_theta, -2.0 * j / kv->rot_dim);
-        double turns = w / 6.283185307179586476925;       // of a turn per position; whole turns are dropped
+        double turns = pair_frequency(*kv, j) / 6.283185307179586476925;       // of a turn per position; whole turns are dropped
         turns -= floor(turns);
         c.kv_turn[j] = turns >= 1.0 ? 0 : (uint64_t)(turns * 18446744073709551616.0);
     }

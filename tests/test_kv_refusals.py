@@ -1,0 +1,20 @@
+"""Arguments of the paged-cache calls that the host refuses beside those of test_gpu_kv_paths.py."""
+import ctypes
+
+import pytest
+
+
+def workspace_bytes(**kw):
+    from paper_2605_18817_b200 import binding as b
+    cfg = b.mrp_config(64, 64, 32, 0, 1, 4, 1, b.MRP_BF16, 1e-6, 0, 0)
+    a = dict(n_heads=8, n_kv_heads=2, head_dim=128, page_size=16, n_pages=10, max_pages=4, page_stride=0, rot_dim=128, rot_interleaved=0,
+             rot_theta=1e4, inv_freq=None, norm_eps=1e-6)
+    a.update(kw)
+    return int(b.lib.mrp_kv_workspace_bytes(ctypes.byref(cfg), ctypes.byref(b.mrp_kv_config(*a.values()))))
+
+
+def test_numbers_of_a_geometry_that_are_not_finite():
+    assert workspace_bytes() > 0 and workspace_bytes(rot_theta=1e-300) > 0 and workspace_bytes(norm_eps=0.0) > 0
+    for kw in (dict(rot_theta=5e-324), dict(norm_eps=float("inf")), dict(rot_theta=float("nan")),
+               dict(inv_freq=(ctypes.c_double * 64)(*([0.5] * 63 + [float("nan")])))):
+        assert workspace_bytes(**kw) == 0, kw
