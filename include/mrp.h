@@ -477,7 +477,7 @@ typedef struct {
     int32_t mask;               /* mrp_attention_mask                                                 */
     int32_t window;             /* > 0: of those only positions > p - window, and                     */
     int32_t sinks;              /* the first `sinks` positions, which stay visible (read with a window only) */
-    float scale;                /* of the scores, >= 0; 0 = 1 / sqrt(head_dim)                        */
+    float scale;                /* of the scores, >= 0, log2(e) times it finite; 0 = 1 / sqrt(head_dim) */
 } mrp_attention_args;
 
 /*

@@ -576,7 +576,8 @@ int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_modul
     if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
     const int bad = kv_batch_status(c, batch);
     if (bad) return bad;
-    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !(args->scale >= 0.f) || !isfinite(args->scale))
+    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !(args->scale >= 0.f) ||
+        !isfinite(args->scale * 1.4426950408889634f))             // (in base 2)
         return MRP_ERR_INVALID_ARG;
     c.launches = 0;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;

@@ -18,3 +18,16 @@ def test_numbers_of_a_geometry_that_are_not_finite():
     for kw in (dict(rot_theta=5e-324), dict(norm_eps=float("inf")), dict(rot_theta=float("nan")),
                dict(inv_freq=(ctypes.c_double * 64)(*([0.5] * 63 + [float("nan")])))):
         assert workspace_bytes(**kw) == 0, kw
+
+
+@pytest.mark.gpu
+def test_a_scale_beyond_fp32_in_base_2():
+    from test_gpu_kv import Cache
+    c = Cache("bf16", 4, 2, 128, 16, [(20, 3)], seed=1)
+    q = c.rand(3, 4, 128)
+    with pytest.raises(c.b.MrpError) as e:
+        c.attend(q, scale=3e38)
+    assert e.value.status == 1
+    c.attend(q, scale=2e38)
+    out, lse = c.attend(q)
+    c.check(q, out, lse)
