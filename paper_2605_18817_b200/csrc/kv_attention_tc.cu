@@ -1571,12 +1571,14 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
     // took 95 and 113 against 78 and 80.
     if (rows <= kFewRows) return few();
-    // A step of single tokens beside a prompt: where most sequences must be far shorter than the longest, those of up to 16
-    // rows go to the transposed kernel in a launch of their own (48 single tokens and a prompt of 512: 172 against 146 us).
-    // Two row tiles have no registers for both parts of P (prompts 470 -> 494 us with them): there they always do, which costs 5 us
-    // where there is no such sequence (three prompts of 1000: 94 -> 98; longer ones 470 -> 478, under the power cap nothing).
+    // Two row tiles leave sequences of up to 16 rows to the transposed kernel, in a launch of their own: they would fill a unit of
+    // 256 rows each (48 single tokens and a prompt of 512: 132 against 108 us), and two row tiles have no registers for both
+    // parts of P (prompts 470 -> 494 us with them).  Where there is no such sequence it costs 5 us (three prompts of 1000: 94 ->
+    // 98; longer ones 470 -> 478, under the power cap nothing).  One row tile takes all sequences: a second launch costs more
+    // than it saves (30 single tokens and two blocks of 32: 69 against 90 us; 12 and a prompt of 512 at 256 features: 85 against
+    // 115; only beyond about 200 sequences it gains, 200 and ten blocks of 32: 277 against 249).
     int launches = 0;
-    if (two || (long long)batch.n_tokens * 4 < (long long)batch.n_seqs * batch.max_new) {
+    if (two) {
         p.rows_upto = kFewRows;
         if ((e = few()) != cudaSuccess) return e;
         launches = c->launches;
