@@ -635,7 +635,6 @@ cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
     p.rows_above = 0;
     p.rows_upto = 0x7fffffff;
-    p.min_piece = 1;
     p.lead = 0;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
     {

@@ -87,7 +87,6 @@ struct AttnParams {
     FastDiv gdiv;              // g
     int mask, window, sinks, plain_rows;
     int rows_above, rows_upto; // sequences with more than rows_above and at most rows_upto query rows a key head are this launch's
-    int min_piece;             // tiles a CTA takes at least
     int lead;                  // what a unit costs besides its tiles, in tiles: so much of the line lies ahead of each unit
     float scale_log2;          // > 0
     KvPartials part;
@@ -256,7 +255,7 @@ __device__ __forceinline__ long long find_piece(const AttnParams &p, Cursor<ROWS
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) total += sh_warp[w];
     }
-    per = max(div_line(total + gridDim.x - 1, gridDim.x), (long long)p.min_piece);
+    per = div_line(total + gridDim.x - 1, gridDim.x);
     const long long begin = per * blockIdx.x, end = min(total, begin + per);
     if (begin >= end) return 0;
     long long done = 0;
@@ -325,7 +324,7 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
-    per = max(div_line(total + gridDim.x - 1, gridDim.x), (long long)p.min_piece);
+    per = div_line(total + gridDim.x - 1, gridDim.x);
     const long long begin = per * blockIdx.x, end = min(total, begin + per);
     if (begin >= end) return 0;
     long long done = 0;

@@ -1561,7 +1561,6 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     cudaError_t e = maps(join);
     if (e != cudaSuccess) return e;
     auto few = [&]() {
-        p.min_piece = 1;
         p.lead = 2;                        // (24 single tokens 63, 61, 61 us at 1, 2, 3; 128 short caches 89, 86, 85)
         if (narrow) return few_launch<1, false>(c, p, km, vm, bx, st);
         if (bx.groups) return wide ? few_launch<4, true>(c, p, km, vm, bx, st) : few_launch<2, true>(c, p, km, vm, bx, st);
@@ -1587,7 +1586,6 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     }
     if (two && bx.groups && (e = maps(false)) != cudaSuccess) return e;
     // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
-    p.min_piece = two ? 1 : 2;
     p.lead = two ? 4 : 3;
     if (two) e = narrow ? tc_launch<1, 2, false>(c, p, km, vm, bx, st) : tc_launch<2, 2, false>(c, p, km, vm, bx, st);
     else if (narrow) e = tc_launch<1, 1, false>(c, p, km, vm, bx, st);

@@ -1,6 +1,6 @@
 // The cut of the line of tiles (kv_attention.cuh), run on the host: which CTA arrives where, when some of them give up part way.
 //
-// Reads batches from stdin, a line each: rows tile heads g mask window sinks lead min_piece ctas seed n (prefix new) * n
+// Reads batches from stdin, a line each: rows tile heads g mask window sinks lead ctas seed n (prefix new) * n
 // Every CTA's piece is walked as the kernels walk it: arrivals of the units up to a random one (where a wait gives up), the
 // others by settle_arrivals.  Prints "cut <units> left <arrivals missing or too many> dirty <counters that are not zero>".
 #include <algorithm>
@@ -43,7 +43,7 @@ template <int ROWS, int TILE> static void run(AttnParams p, int ctas, std::mt199
     typedef Cursor<ROWS, TILE> C;
     long long total = 0;
     for (int s = 0; s < p.b.n_seqs; ++s) total += sequence_tiles<ROWS, TILE>(p, s, false);
-    const long long per = max(div_line(total + ctas - 1, ctas), (long long)p.min_piece);
+    const long long per = div_line(total + ctas - 1, ctas);
     std::vector<int> counters(ctas + 1, 0), seen(ctas + 1, 0), due(ctas + 1, 0);
     std::vector<C> at(ctas);
     std::vector<long long> end(ctas, 0);
@@ -91,9 +91,9 @@ template <int ROWS, int TILE> static void run(AttnParams p, int ctas, std::mt199
 
 int main()
 {
-    int rows, tile, heads, g, mask, window, sinks, lead, min_piece, ctas, n;
+    int rows, tile, heads, g, mask, window, sinks, lead, ctas, n;
     unsigned seed;
-    while (scanf("%d %d %d %d %d %d %d %d %d %d %u %d", &rows, &tile, &heads, &g, &mask, &window, &sinks, &lead, &min_piece, &ctas, &seed, &n) == 12) {
+    while (scanf("%d %d %d %d %d %d %d %d %d %u %d", &rows, &tile, &heads, &g, &mask, &window, &sinks, &lead, &ctas, &seed, &n) == 11) {
         std::vector<int32_t> pre(n), start(1, 0);
         for (int i = 0, m; i < n; ++i) {
             if (scanf("%d %d", &pre[i], &m) != 2) return 1;
@@ -110,7 +110,7 @@ int main()
         p.gdiv = make_fastdiv(g);
         p.mask = mask; p.window = window; p.sinks = window > 0 ? sinks : 0;
         p.rows_upto = 0x7fffffff;
-        p.lead = lead; p.min_piece = min_piece;
+        p.lead = lead;
         std::mt19937 rng(seed);
         if (rows == 16 && tile == 128) run<16, 128>(p, ctas, rng);
         else if (rows == 16) run<16, 64>(p, ctas, rng);
