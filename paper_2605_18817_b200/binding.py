@@ -536,7 +536,8 @@ def _pools(kv, batch, k_pages, v_pages):
     for t in (k_pages, v_pages):
         if t.dtype is not kv.dtype or t.get_device() != kv.device:
             raise TypeError("pools are CUDA tensors of %s on the context's device" % kv.dtype)
-        if t.shape != kv.pool or t.stride() != kv.pool_stride:
+        # (the stride of a dimension of one entry means nothing)
+        if t.shape != kv.pool or (t.stride() != kv.pool_stride and any(n > 1 and a != b for n, a, b in zip(kv.pool, t.stride(), kv.pool_stride))):
             raise ValueError("pools are [n_pages, n_kv_heads, page_size, head_dim] with the strides attached")
     if batch.max_pages != kv.max_pages or batch.device != kv.device:
         raise ValueError("the batch's page table is [B, max_pages] on the context's device")

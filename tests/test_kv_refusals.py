@@ -31,3 +31,22 @@ def test_a_scale_beyond_fp32_in_base_2():
     c.attend(q, scale=2e38)
     out, lse = c.attend(q)
     c.check(q, out, lse)
+
+
+def test_pools_whose_dimensions_of_one_entry_have_other_strides():
+    """One key head stored [pages, rows, 1, features], one row a page, one page: the same memory, other strides by name."""
+    import torch
+    from types import SimpleNamespace
+    from paper_2605_18817_b200 import binding as b
+
+    def shape(n, hk, p, d):
+        return b._KvShape(torch.float32, -1, (2 * hk, d), (hk, d), (n, hk, p, d), (hk * p * d, p * d, d, 1), 4)
+    batch = SimpleNamespace(max_pages=4, device=-1)
+    for n, hk, p, pool in ((6, 1, 16, torch.zeros(6, 16, 1, 8).transpose(1, 2)), (6, 3, 1, torch.zeros(6, 1, 3, 8).transpose(1, 2)),
+                           (1, 3, 16, torch.zeros(3, 1, 16, 8).transpose(0, 1)), (6, 3, 16, torch.zeros(6, 3, 16, 8))):
+        got = b._pools(shape(n, hk, p, 8), batch, pool, pool)
+        assert got.k == got.v == pool.data_ptr()
+    for n, hk, p, pool in ((6, 2, 16, torch.zeros(6, 16, 2, 8).transpose(1, 2)), (6, 1, 16, torch.zeros(6, 1, 16, 16)[..., :8]),
+                           (6, 1, 16, torch.zeros(12, 1, 16, 8)[::2])):
+        with pytest.raises(ValueError):
+            b._pools(shape(n, hk, p, 8), batch, pool, pool)
