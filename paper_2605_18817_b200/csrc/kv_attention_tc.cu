@@ -19,11 +19,14 @@
 //   columns of scores that have been read, and a second product.  24 blocks of 16, which have none: 67 -> 68 us.
 //   NT = 2 (prompts): two row tiles share every K and V tile and take turns, one in the MMAs while the other is in the
 //   exponentials.  Per pair of 128 x 128 tiles of 128 features the products take 2048 cycles, the exponentials alone 2048 of
-//   the special function unit; measured 3600 (2 prompts of 2000 behind 5600 positions, 32 / 8 heads: 450 us, 1.06 PFLOP/s; the
-//   softmax's chain of tensor-memory loads, maximum, exponentials, stores is what does not overlap).  A thread per row took
-//   510 us; exponentials by a polynomial on the FMA pipe for a part of the scores 460 to 480.
+//   the special function unit; measured 3600 (the softmax's chain of tensor-memory loads, maximum, exponentials, stores is what
+//   does not overlap).  2 prompts of 2000 behind 5600 positions, 32 / 8 heads: 478 us, 1.0 PFLOP/s in a run of a few
+//   milliseconds; 533 to 543 us, 0.88 PFLOP/s in one of seconds, under the power cap.  In short runs a thread per row took 40 us
+//   more, exponentials by a polynomial on the FMA pipe for a part of the scores 10 to 30.
 //   NT = 1 (17 to 128 rows, and batches too small to give two row tiles to all SMs): two S buffers instead, the next S is
-//   computed while this one is exponentiated; 24 blocks of 32 tokens 75 us against 51 for the bytes.
+//   computed while this one is exponentiated; 24 blocks of 32 tokens 78 us against 51 for the bytes.
+//   Where a maximum grows, each warp of a pair rescales half of the accumulator's columns, and the pair meets before the first
+//   product of the tile may start: that product adds to all columns.
 //
 // Pages hold what they hold behind a sequence's end: scores of positions a row does not see are replaced before they are
 // used, and V rows that no row of the tile sees are zeroed in shared memory before the product (0 * NaN).  A V row with

@@ -2,7 +2,9 @@
 //
 //   y = x * rsqrt(mean(x^2) + eps) * gamma;   (y_a, y_b) <- (y_a c - y_b s, y_b c + y_a s),  c + i s = exp(2 pi i f)
 // with f the fraction of a turn that position p makes in pair (a, b): p * turn_j mod 2^64, turn_j = 2^64 w_j / (2 pi) on
-// the host in 64 bits, so the reduction of the angle is one exact integer product however far the position is.
+// the host in 64 bits, so the reduction of the angle is one exact integer product however far the position is.  What is left,
+// within half a turn either way, is rounded to fp32 for sincospif (2^-25 half turns at most, an angle of 9e-8: about the
+// rounding of the sines themselves).
 //
 // Every element is read once and written once and takes about seven operations: memory bounds it as long as the
 // instructions around them stay few.  A warp takes a token (where tokens are few, one of several shares of a token): it
