@@ -496,6 +496,77 @@ typedef struct {
 int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages,
                         const mrp_attention_args *args, void *cuda_stream);
 
+/*
+ * The same cache held in 8 bits: of a layer, beside each other,
+ *     k, v               DEVICE [n_pages, n_kv_heads, page_size, head_dim] e4m3 codes, 16-byte aligned, pages page_stride
+ *                        bytes apart (the geometry attached, a byte an element)
+ *     k_scale, v_scale   DEVICE [n_pages, n_kv_heads, page_size] one byte s a row, 16-byte aligned, pages one after the
+ *                        other: the row is its codes times 2^(s - 127); 255: NaN in all features
+ * Half the bytes of a bf16 cache to hold and to read (head_dim + 1 a row).  A power of two as the scale costs no precision
+ * that a finer one would keep, codes being floating point themselves, and makes every row exact in bf16.  Codes 0x7F and
+ * 0xFF (NaN) are never written; in a row that is seen, mrp_paged_attention_q8 may read them as any value.
+ */
+typedef struct {
+    uint8_t *k, *v;
+    uint8_t *k_scale, *v_scale;
+} mrp_kv_pool_q8;
+
+/*
+ * mrp_kv_append into such a cache: k normalised and rotated on the way, then k and v row by row to codes.  E = s - 127 is the
+ * smallest integer with max |row| <= 448 * 2^E (at least -127; 0 for a row of zeros), codes are rounded to nearest, ties to
+ * even: once, from the fp32 result (k) or from the values themselves (v).  A row with a value that is not finite becomes a
+ * row of NaN.  Everything else as in mrp_kv_append.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int mrp_kv_append_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_qkv_rows *rows,
+                     void *cuda_stream);
+
+/*
+ * Read rows of such a cache back in the context dtype, for a cache that moves to another layout, another model or the host:
+ * row t of the batch becomes the key and the value [n_kv_heads, head_dim] at the position mrp_kv_append_q8 would store it
+ * at, so the same batch reads what it has appended; prefix_len[b] = 0 and as many rows as the sequence has reads all of it.
+ * Exact (bf16 below 2^-133: rounded).  k or v may be NULL (not both); rows 16-byte aligned, strides multiples of 16 bytes.
+ * A page entry outside the pool reads as zeros.  batch->positions is not read.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+typedef struct {
+    void *k, *v;                /* [n_tokens, n_kv_heads, head_dim] rows, *_stride elements apart     */
+    int64_t k_stride, v_stride;
+} mrp_kv_rows;
+
+int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_kv_rows *rows,
+                   void *cuda_stream);
+
+/*
+ * mrp_paged_attention over such a cache: the same masks, outputs and work split, on the values the rows stand for.  Queries
+ * stay as they are.  A visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does
+ * not depend on values).  bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA
+ * feeds; others, f32 and MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool,
+                           const mrp_attention_args *args, void *cuda_stream);
+
+/*
+ * Attention of rows over each other, without a cache: the tokens of sequence b are rows seq_start[b] .. seq_start[b + 1] - 1
+ * of queries, keys and values alike (already normalised and rotated), and token i of them sees tokens 0 .. i of its sequence
+ * (MRP_ATTN_CAUSAL: whole prompts, one after the other) or all of them (MRP_ATTN_BLOCK: the blocks of block diffusion);
+ * with a window > 0 only tokens > i - window and the sequence's first `sinks`.  MRP_ATTN_PREFIX is refused.
+ * join != 0: out and lse hold the result of a pass over OTHER keys for the same queries (a block's cached prefix:
+ * mrp_paged_attention or _q8 with MRP_ATTN_PREFIX) and become the result over both sets, so a block that is decoded again
+ * and again attends to its own keys as they are and stores them only once it is committed.  Where lse holds -inf, out is
+ * not read.  out is a result rounded to the context dtype, so a joined row carries that rounding beside its own.
+ * Of the batch, prefix_len, page_table and positions are not read and may be NULL; needs a geometry (mrp_kv_attach; n_pages
+ * may be 0), whose workspace it uses.  A token that sees nothing, scores, sums, values that are not finite, streams and
+ * repeats as in mrp_paged_attention; probabilities are rounded to bf16 once on the tiles that TMA feeds (all bf16 contexts
+ * without MRP_FLAG_FORCE_SIMT).  k and v must not overlap out.  Errors: INVALID_ARG, UNSUPPORTED (nothing attached), CUDA.
+ */
+typedef struct {
+    const void *k, *v;          /* [n_tokens, n_kv_heads, head_dim] rows, *_stride elements apart, 16-byte aligned, */
+    int64_t k_stride, v_stride; /* strides multiples of 16 bytes                                                   */
+    int32_t join;               /* args->out and args->lse (needed then; out is not q) go into the result          */
+} mrp_packed_kv;
+
+int mrp_packed_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_packed_kv *kv, const mrp_attention_args *args,
+                         void *cuda_stream);
+
 typedef enum { MRP_SELECT_STATIC = 0, MRP_SELECT_DYNAMIC_REMASK = 1 } mrp_select_mode;
 
 typedef struct {

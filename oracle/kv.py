@@ -91,3 +91,47 @@ def attention(q, k_pages, v_pages, seq_start, prefix_len, page_table, page_size,
                 reach[s + i, h] = e @ np.abs(vv) / e.sum()
                 size[s + i, h] = (np.abs(kk) @ np.abs(x)).max() * abs(scale)
     return o, lse, reach, size
+
+
+# ---- the cache in 8 bits (codes: oracle/fp8.py) ------------------------------------------------------------------------
+
+def q8_rows(x):
+    """Rows x [.., D] -> (e4m3 codes uint8 [.., D], scale bytes uint8 [..]): row = codes * 2^(byte - 127), the exponent the
+    smallest one >= -127 with max |row| <= 448 * 2^E, 0 for a row of zeros; byte 255 (codes 0) where a value is not finite."""
+    from oracle import fp8
+    x = np.asarray(x, np.float64)
+    flat = x.reshape(-1, x.shape[-1])
+    bad = ~np.isfinite(flat).all(-1)
+    flat = np.where(bad[:, None], 0.0, flat)
+    scale = np.maximum(fp8.row_scales(flat), 2.0 ** -127)
+    codes = fp8.encode(flat / scale[:, None])
+    byte = np.where(bad, 255, np.frexp(scale)[1] - 1 + 127).astype(np.uint8)
+    return codes.reshape(x.shape), byte.reshape(x.shape[:-1])
+
+
+def q8_values(codes, byte):
+    """What codes and scale bytes stand for, float64: NaN codes and rows of byte 255 are NaN."""
+    from oracle import fp8
+    codes, byte = np.asarray(codes, np.uint8), np.asarray(byte, np.uint8)
+    v = np.where((codes & 0x7F) == 0x7F, np.nan, fp8.decode(codes)) * 2.0 ** (byte.astype(np.float64) - 127)[..., None]
+    return np.where((byte == 255)[..., None], np.nan, v)
+
+
+def join(o1, l1, o2, l2):
+    """Two passes over disjoint sets of keys, as one: (out, lse)."""
+    l = np.logaddexp(l1, l2)
+    with np.errstate(invalid="ignore"):
+        w1, w2 = (np.where(np.isneginf(x), 0.0, np.exp(x - l)) for x in (l1, l2))
+    return np.where(w1[..., None] > 0, w1[..., None] * o1, 0.0) + np.where(w2[..., None] > 0, w2[..., None] * o2, 0.0), l
+
+
+def packed(q, k, v, seq_start, mask=CAUSAL, window=0, sinks=0, scale=0.0):
+    """Attention of rows over each other: every sequence is a cache of its own rows, all of them new."""
+    n_seqs = len(seq_start) - 1
+    longest = max([1] + [int(seq_start[b + 1]) - int(seq_start[b]) for b in range(n_seqs)])
+    kp, vp = (np.zeros((n_seqs, k.shape[1], longest, k.shape[2])) for _ in range(2))
+    for b in range(n_seqs):
+        s, e = int(seq_start[b]), int(seq_start[b + 1])
+        if 0 <= s <= e <= q.shape[0]:
+            kp[b, :, :e - s], vp[b, :, :e - s] = np.swapaxes(k[s:e], 0, 1), np.swapaxes(v[s:e], 0, 1)
+    return attention(q, kp, vp, seq_start, np.zeros(n_seqs, np.int32), np.arange(n_seqs)[:, None], longest, mask, window, sinks, scale)

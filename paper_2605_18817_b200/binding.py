@@ -39,7 +39,8 @@ EXPORTS = ("mrp_workspace_bytes", "mrp_create", "mrp_destroy", "mrp_draft", "mrp
            "mrp_reveal_remask_noalloc", "mrp_selftest_wait_timeout", "mrp_draft_from_hidden", "mrp_commit",
            "mrp_set_logits0_event", "mrp_set_input_rows", "mrp_fetch_status", "mrp_draft_kl", "mrp_draft_bf16_logits", "mrp_quantised_lm_head",
            "mrp_module_workspace_bytes", "mrp_module_attach", "mrp_module_step", "mrp_module_set_prefix", "mrp_module_step_kl",
-           "mrp_kv_workspace_bytes", "mrp_kv_attach", "mrp_qk_norm_rotate", "mrp_kv_append", "mrp_paged_attention")
+           "mrp_kv_workspace_bytes", "mrp_kv_attach", "mrp_qk_norm_rotate", "mrp_kv_append", "mrp_paged_attention",
+           "mrp_kv_append_q8", "mrp_kv_read_q8", "mrp_paged_attention_q8", "mrp_packed_attention")
 MRP_NOALLOC_MAX_POSITIONS = 65536
 MRP_ERR_CAPACITY = 7
 
@@ -116,6 +117,19 @@ class mrp_attention_args(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
                 ("lse", ctypes.c_void_p), ("mask", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class mrp_kv_pool_q8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class mrp_kv_rows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class mrp_packed_kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("join", ctypes.c_int32)]
 
 
 class mrp_block_state(ctypes.Structure):
@@ -205,6 +219,12 @@ def _load():
     lib.mrp_paged_attention.restype = ctypes.c_int
     lib.mrp_paged_attention.argtypes = [ctypes.c_void_p, ctypes.POINTER(mrp_kv_batch), ctypes.POINTER(mrp_module_kv),
                                         ctypes.POINTER(mrp_attention_args), ctypes.c_void_p]
+    for name, third, fourth in (("mrp_kv_append_q8", mrp_kv_pool_q8, mrp_qkv_rows), ("mrp_kv_read_q8", mrp_kv_pool_q8, mrp_kv_rows),
+                                ("mrp_paged_attention_q8", mrp_kv_pool_q8, mrp_attention_args),
+                                ("mrp_packed_attention", mrp_packed_kv, mrp_attention_args)):
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = [ctypes.c_void_p, ctypes.POINTER(mrp_kv_batch), ctypes.POINTER(third), ctypes.POINTER(fourth), ctypes.c_void_p]
     lib.mrp_profile_enable.restype = ctypes.c_int
     lib.mrp_profile_enable.argtypes = [ctypes.c_void_p, ctypes.c_int32]
     lib.mrp_profile_read.restype = ctypes.c_int
@@ -486,7 +506,8 @@ class _KvShape:
 
 class KvBatch:
     """A step's tokens (mrp_kv_batch): ``seq_start`` [B + 1], ``prefix_len`` [B], ``page_table`` [B, max_pages], optionally
-    ``positions`` [n_tokens], ``status`` [1], all int32 on the device; made once per step, used by the calls of all layers."""
+    ``positions`` [n_tokens], ``status`` [1], all int32 on the device; made once per step, used by the calls of all layers.
+    ``prefix_len`` and ``page_table`` None: sequences without a cache, for mrp_packed_attention alone."""
 
     def __init__(self, seq_start, prefix_len, page_table, n_tokens, max_new, positions=None, status=None):
         for t, nm in ((seq_start, "seq_start"), (prefix_len, "prefix_len"), (page_table, "page_table"), (positions, "positions"),
@@ -494,17 +515,52 @@ class KvBatch:
             _check(t, torch.int32, nm)
             if t is not None and t.device != seq_start.device:
                 raise TypeError("%s is on another device than seq_start" % nm)
-        n_seqs = prefix_len.numel()
-        if seq_start.numel() != n_seqs + 1 or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+        n_seqs = seq_start.numel() - 1
+        if n_seqs < 0 or (prefix_len is None) != (page_table is None) or (
+                prefix_len is not None and (prefix_len.numel() != n_seqs or page_table.dim() != 2 or page_table.shape[0] != n_seqs)):
             raise ValueError("seq_start [B + 1], prefix_len [B], page_table [B, max_pages]")
         if positions is not None and positions.numel() < int(n_tokens):
             raise ValueError("positions [n_tokens]")
-        self.max_pages, self.n_tokens, self.device = int(page_table.shape[1]), int(n_tokens), seq_start.device.index
+        self.max_pages = None if page_table is None else int(page_table.shape[1])
+        self.n_tokens, self.device = int(n_tokens), seq_start.device.index
         self.keep = (seq_start, prefix_len, page_table, positions, status)
-        self.c = mrp_kv_batch(seq_start.data_ptr(), prefix_len.data_ptr(), page_table.data_ptr(),
-                              None if positions is None else positions.data_ptr(), n_seqs, int(n_tokens), int(max_new),
-                              None if status is None else status.data_ptr())
+        ptr = lambda t: None if t is None else t.data_ptr()                    # noqa: E731
+        self.c = mrp_kv_batch(seq_start.data_ptr(), ptr(prefix_len), ptr(page_table), ptr(positions), n_seqs, int(n_tokens),
+                              int(max_new), ptr(status))
         self.ref = ctypes.byref(self.c)
+
+
+class KvPoolQ8:
+    """A layer's cache in 8 bits (mrp_kv_pool_q8), made once per layer: ``k``, ``v`` [n_pages, n_kv_heads, page_size, head_dim]
+    torch.float8_e4m3fn (or uint8) codes and ``k_scale``, ``v_scale`` [n_pages, n_kv_heads, page_size] torch.float8_e8m0fnu (or
+    uint8: exponent + 127), scales contiguous."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        for t, nm in ((k, "k"), (v, "v")):
+            if not t.is_cuda or t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.dim() != 4 or t.device != k.device:
+                raise TypeError("%s holds e4m3 codes [n_pages, n_kv_heads, page_size, head_dim] on one CUDA device" % nm)
+        for t, nm in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype not in (torch.float8_e8m0fnu, torch.uint8) or t.device != k.device or not t.is_contiguous():
+                raise TypeError("%s holds e8m0 scales, contiguous, on the codes' device" % nm)
+            if t.shape != k.shape[:3]:
+                raise ValueError("%s is [n_pages, n_kv_heads, page_size]" % nm)
+        if v.shape != k.shape:
+            raise ValueError("k and v have the same shape")
+        self.keep, self.device, self.fits = (k, v, k_scale, v_scale), k.get_device(), None
+        self.c = mrp_kv_pool_q8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+    def check(self, kv, batch):
+        if self.fits is not kv:
+            for t in self.keep[:2]:
+                if t.shape != kv.pool or any(n > 1 and a != b for n, a, b in zip(kv.pool, t.stride(), kv.pool_stride)):
+                    raise ValueError("pools are [n_pages, n_kv_heads, page_size, head_dim] with the strides attached")
+            if self.device != kv.device:
+                raise TypeError("pools are on the context's device")
+            self.fits = kv
+        if batch.max_pages != kv.max_pages or batch.device != kv.device:
+            raise ValueError("the batch's page table is [B, max_pages] on the context's device")
+        return self.ref
 
 
 def _kv_shape(ctx):
@@ -590,6 +646,14 @@ def mrp_kv_append(ctx: Context, batch: KvBatch, k_pages, v_pages, k, v, gamma_k=
         _kv_error(ctx, "mrp_kv_append", rc)
 
 
+def _lse(kv, t, n):
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.get_device() != kv.device or not t.is_contiguous() or t.numel() < n * kv.q_row[0]:
+        raise TypeError("lse is a contiguous CUDA tensor [tokens, n_heads] of float32 on the context's device")
+    return t.data_ptr()
+
+
 def mrp_paged_attention(ctx: Context, batch: KvBatch, k_pages, v_pages, q, out, lse=None, mask=MRP_ATTN_CAUSAL, window=0,
                         sinks=0, scale=0.0, stream=None) -> None:
     """Attention of the batch's queries q [tokens, n_heads, head_dim] over their sequences' pages into ``out``; ``lse``
@@ -599,18 +663,78 @@ def mrp_paged_attention(ctx: Context, batch: KvBatch, k_pages, v_pages, q, out, 
     pools = _pools(kv, batch, k_pages, v_pages)
     qp, qs = _rows(kv, q, kv.q_row, n, "q")
     op, os_ = _rows(kv, out, kv.q_row, n, "out")
-    if lse is not None:
-        if lse.dtype is not torch.float32 or lse.get_device() != kv.device or not lse.is_contiguous() or lse.numel() < n * kv.q_row[0]:
-            raise TypeError("lse is a contiguous CUDA tensor [tokens, n_heads] of float32 on the context's device")
-        lse = lse.data_ptr()
-    a = mrp_attention_args(qp, op, qs, os_, lse, mask, window, sinks, scale)
+    a = mrp_attention_args(qp, op, qs, os_, _lse(kv, lse, n), mask, window, sinks, scale)
     rc = _attention_c(ctx.handle, batch.ref, _byref(pools), _byref(a), _raw_stream(kv, stream))
     if rc != 0:
         _kv_error(ctx, "mrp_paged_attention", rc)
 
 
+def mrp_kv_append_q8(ctx: Context, batch: KvBatch, pool: KvPoolQ8, k, v, gamma_k=None, q=None, q_out=None, gamma_q=None,
+                     stream=None) -> None:
+    """mrp_kv_append into a cache in 8 bits: keys (normalised with gamma_k, rotated) and values as e4m3 codes with a power of
+    two per row; with ``q`` also q -> q_out, normalised with gamma_q and rotated."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    pages = pool.check(kv, batch)
+    kp, ks = _rows(kv, k, kv.k_row, n, "k")
+    vp, vs = _rows(kv, v, kv.k_row, n, "v")
+    qp, qs = (None, 0) if q is None else _rows(kv, q, kv.q_row, n, "q")
+    qo, qos = (None, 0) if q is None else _rows(kv, q_out, kv.q_row, n, "q_out")
+    r = mrp_qkv_rows(qp, kp, vp, qs, ks, vs, _gamma(kv, gamma_q, "gamma_q"), _gamma(kv, gamma_k, "gamma_k"), qo, None, qos, 0)
+    rc = _append_q8_c(ctx.handle, batch.ref, pages, _byref(r), _raw_stream(kv, stream))
+    if rc != 0:
+        _kv_error(ctx, "mrp_kv_append_q8", rc)
+
+
+def mrp_kv_read_q8(ctx: Context, batch: KvBatch, pool: KvPoolQ8, k_out, v_out, stream=None) -> None:
+    """The keys and values (either None) of the batch's rows, [tokens, n_kv_heads, head_dim], as the cache holds them: what
+    mrp_kv_append_q8 with the same batch has stored."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    pages = pool.check(kv, batch)
+    kp, ks = (None, 0) if k_out is None else _rows(kv, k_out, kv.k_row, n, "k_out")
+    vp, vs = (None, 0) if v_out is None else _rows(kv, v_out, kv.k_row, n, "v_out")
+    rc = _read_q8_c(ctx.handle, batch.ref, pages, _byref(mrp_kv_rows(kp, vp, ks, vs)), _raw_stream(kv, stream))
+    if rc != 0:
+        _kv_error(ctx, "mrp_kv_read_q8", rc)
+
+
+def mrp_paged_attention_q8(ctx: Context, batch: KvBatch, pool: KvPoolQ8, q, out, lse=None, mask=MRP_ATTN_CAUSAL, window=0,
+                           sinks=0, scale=0.0, stream=None) -> None:
+    """mrp_paged_attention over a cache in 8 bits."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    pages = pool.check(kv, batch)
+    qp, qs = _rows(kv, q, kv.q_row, n, "q")
+    op, os_ = _rows(kv, out, kv.q_row, n, "out")
+    a = mrp_attention_args(qp, op, qs, os_, _lse(kv, lse, n), mask, window, sinks, scale)
+    rc = _attention_q8_c(ctx.handle, batch.ref, pages, _byref(a), _raw_stream(kv, stream))
+    if rc != 0:
+        _kv_error(ctx, "mrp_paged_attention_q8", rc)
+
+
+def mrp_packed_attention(ctx: Context, batch: KvBatch, k, v, q, out, lse=None, mask=MRP_ATTN_CAUSAL, window=0, sinks=0, scale=0.0,
+                         join=False, stream=None) -> None:
+    """Attention of the batch's rows over each other, sequence by sequence: q [tokens, n_heads, head_dim], k and v [tokens,
+    n_kv_heads, head_dim] into ``out``; ``join``: with what ``out`` and ``lse`` hold from a pass over other keys."""
+    kv = _kv_shape(ctx)
+    n = batch.n_tokens
+    if batch.device != kv.device:
+        raise ValueError("the batch is on the context's device")
+    kp, ks = _rows(kv, k, kv.k_row, n, "k")
+    vp, vs = _rows(kv, v, kv.k_row, n, "v")
+    qp, qs = _rows(kv, q, kv.q_row, n, "q")
+    op, os_ = _rows(kv, out, kv.q_row, n, "out")
+    a = mrp_attention_args(qp, op, qs, os_, _lse(kv, lse, n), mask, window, sinks, scale)
+    rc = _packed_c(ctx.handle, batch.ref, _byref(mrp_packed_kv(kp, vp, ks, vs, join)), _byref(a), _raw_stream(kv, stream))
+    if rc != 0:
+        _kv_error(ctx, "mrp_packed_attention", rc)
+
+
 # the calls of every layer of every step: looked up once
 _byref, _rotate_c, _append_c, _attention_c = ctypes.byref, lib.mrp_qk_norm_rotate, lib.mrp_kv_append, lib.mrp_paged_attention
+_append_q8_c, _read_q8_c = lib.mrp_kv_append_q8, lib.mrp_kv_read_q8
+_attention_q8_c, _packed_c = lib.mrp_paged_attention_q8, lib.mrp_packed_attention
 
 
 def mrp_set_input_rows(ctx: Context, n_rows: int) -> None:

@@ -21,7 +21,10 @@
 // row of the tile), not memory.  24 sequences of 200 to 6000 positions, one token each, 32 / 8 heads: bf16 of 128 features in
 // pages of 20 rows 100 us (48 for the bytes); f32 107 (48) at 64 features, 184 (97) at 128, 530 (193) at 256.  Two CTAs an SM
 // count more than a second stage: f32 of 128 features 235 us with two stages of one CTA.  Rows beyond 16 take a unit per 16.
+#include <cuda_fp16.h>
+
 #include "kv_attention.cuh"
+#include "kv_q8.cuh"
 
 namespace mrp {
 namespace {
@@ -37,6 +40,10 @@ __device__ __forceinline__ uint32_t s_addr(const void *p) { return (uint32_t)__c
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool read)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
+}
+template <int BYTES> __device__ __forceinline__ void cp_some(uint32_t dst, const void *src, int n)     // 4 or 8, of which n are read
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -93,16 +100,24 @@ template <int DP> struct Geo<float, DP> {
     static constexpr int kStages = DP <= 64 ? 2 : 1;
     static constexpr bool kSwizzle = false;
 };
-template <typename T, int DP> struct Smem {
+template <typename T, int DP, int SRC> struct Smem {
     typedef Geo<T, DP> G;
     static constexpr int kStage = kWarpKeys * (G::kPitchK + G::kPitchV);
-    static constexpr int kRing = kWarps * G::kStages * kStage;
-    static constexpr int kQ = kRows * G::kPitchQ;
     static constexpr int kRedPitch = DP + 4;               // floats
-    static constexpr int kRed = kWarps * kRows * kRedPitch * 4;
+    // 8 bits: a ring of raw stages (codes of K and V, the 4-byte words their scales lie in, the bytes in those), and one
+    // stage of values, which at the end of a unit takes the warp's parts
+    static constexpr int kLoads = SRC != kFromQ8 ? G::kStages : DP <= 128 ? 3 : 2;
+    static constexpr int kRaw = 2 * kWarpKeys * DP + 2 * kWarpKeys * 4 + 2 * kWarpKeys;
+    static constexpr int kParts = kRows * kRedPitch * 4;
+    static constexpr int kValues = kStage > kParts ? kStage : kParts;
+    static constexpr int kWarp = SRC == kFromQ8 ? kLoads * kRaw + kValues : kLoads * kStage;
+    static constexpr int kRing = kWarps * kWarp;
+    static constexpr int kQ = kRows * G::kPitchQ;
+    static constexpr int kRed = SRC == kFromQ8 ? 0 : kWarps * kParts;
     static constexpr int kMl = 2 * kWarps * kRows * 4;
     static constexpr int kTotal = kRing + kQ + kRed + kMl;
     static constexpr int kCtas = kTotal <= 113 * 1024 ? 2 : 1;
+    static_assert(kStage % 32 == 0 && kRaw % 32 == 0 && kValues % 32 == 0, "aligned stages");
 };
 
 template <int DP>
@@ -161,24 +176,27 @@ __device__ __noinline__ void patch_nonfinite(uint32_t v, const float (&pr)[2][4]
     }
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_kernel(const __grid_constant__ AttnParams p)
+template <typename T, int DP, int SRC>
+__global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attention_kernel(const __grid_constant__ AttnParams p)
 {
     typedef Geo<T, DP> G;
-    typedef Smem<T, DP> S;
+    typedef Smem<T, DP, SRC> S;
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int kStages = G::kStages;
+    constexpr int kStages = S::kLoads;
     constexpr int NF = DP / 8;                             // 8-feature blocks of the accumulator
     constexpr bool kQRegs = kBf16 && DP <= 128;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long sh_find[kWarps + 2];
     __shared__ int sh_last;
     __shared__ Cursor<kRows, kTile> sh_ld[kWarps];
+    __shared__ float sh_prior[kRows];                      // log-sum-exps to join with
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
-    const uint32_t ring = s_addr(smem) + warp * kStages * S::kStage;
+    const uint32_t ring = s_addr(smem) + warp * S::kWarp;
     const uint32_t sq = s_addr(smem) + S::kRing;
-    float *red = reinterpret_cast<float *>(smem + S::kRing + S::kQ);
+    auto red = [&](int w) {                                // warp w's parts
+        return reinterpret_cast<float *>(smem + (SRC == kFromQ8 ? w * S::kWarp + kStages * S::kRaw : S::kRing + S::kQ + w * S::kParts));
+    };
     float *red_m = reinterpret_cast<float *>(smem + S::kRing + S::kQ + S::kRed), *red_l = red_m + kWarps * kRows;
     const T *kp = reinterpret_cast<const T *>(p.k), *vp = reinterpret_cast<const T *>(p.v);
     const int P = p.b.page.d, chunks = kBf16 ? p.D / 8 : p.D / 4;
@@ -198,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
     if (lane == 0) ld = cur;
     __syncwarp();
     Tile lt = cur.t;
-    int l_i = cur.i, l_h = cur.h;
+    int l_i = cur.i, l_h = cur.h, l_start = cur.start;
     const int32_t *l_table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
     long long to_load = len;
     int entry = 0, row_in_page = 0;
@@ -208,7 +226,9 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
         see = j < lt.hi && (j >= lt.lo || j < lt.s1);
         entry = 0;
         row_in_page = 0;
-        if (see) {
+        if (SRC == kFromRows) {
+            entry = l_start + j;
+        } else if (see) {
             const int pg = fast_div(j, p.b.page);
             row_in_page = j - pg * P;
             entry = __ldg(l_table + pg);
@@ -220,10 +240,44 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
     const int l_row = per_row >= 32 ? 0 : lane / per_row, l_ch = per_row >= 32 ? lane : lane % per_row;
     auto load_tile = [&](int stage) {
         if (to_load > 0) {
-            if (see && (unsigned)entry >= (unsigned)p.b.n_pages) {
+            if (SRC != kFromRows && see && (unsigned)entry >= (unsigned)p.b.n_pages) {
                 see = false;
                 if (lane < 16) kv_bad_index(p.b);
             }
+            if constexpr (SRC == kFromRows) {
+                const uint32_t dk = ring + stage * S::kStage, dv = dk + kWarpKeys * G::kPitchK;
+                const long long ko = see ? (long long)entry * p.k_stride + l_h * p.D : -1, vo = see ? (long long)entry * p.v_stride + l_h * p.D : -1;
+#pragma unroll 2
+                for (int r = 0; r < kWarpKeys; r += rows_at_once) {
+                    const int row = r + l_row;
+                    const long long rk = __shfl_sync(0xffffffffu, ko, row), rv = __shfl_sync(0xffffffffu, vo, row);
+#pragma unroll
+                    for (int x = 0; x < reps; ++x) {
+                        const int ch = l_ch + 32 * x, dc = G::kSwizzle ? ch ^ (row & 7) : ch;
+                        const bool on = rk >= 0 && ch < chunks;
+                        cp16(dk + row * G::kPitchK + dc * 16, kp + (on ? rk + ch * (16 / (int)sizeof(T)) : 0), on);
+                        cp16(dv + row * G::kPitchV + dc * 16, vp + (on ? rv + ch * (16 / (int)sizeof(T)) : 0), on);
+                    }
+                }
+            } else if constexpr (SRC == kFromQ8) {
+                const uint32_t raw = ring + stage * S::kRaw, words = raw + 2 * kWarpKeys * DP;
+                const uint8_t *kc = reinterpret_cast<const uint8_t *>(p.k), *vc = reinterpret_cast<const uint8_t *>(p.v);
+                const long long off = see ? (long long)entry * p.b.page_stride + ((long long)l_h * P + row_in_page) * p.D : -1;
+                constexpr int lanes = DP / 8;              // lanes (8 codes) a row
+                const int c_row = lane / lanes, c_ch = lane % lanes;
+#pragma unroll 2
+                for (int r = 0; r < kWarpKeys; r += 32 / lanes) {
+                    const int row = r + c_row;
+                    const long long ro = __shfl_sync(0xffffffffu, off, row);
+                    const bool on = ro >= 0 && c_ch * 8 < p.D;
+                    cp_some<8>(raw + row * DP + c_ch * 8, kc + (on ? ro + c_ch * 8 : 0), on ? 8 : 0);
+                    cp_some<8>(raw + (kWarpKeys + row) * DP + c_ch * 8, vc + (on ? ro + c_ch * 8 : 0), on ? 8 : 0);
+                }
+                // lane l: the key's scale of K (l < 16) or V, in the aligned word it lies in (no byte beyond the scales is read)
+                const long long so = see ? ((long long)entry * p.Hk + l_h) * P + row_in_page : 0, word = so & ~3ll;
+                cp_some<4>(words + lane * 4, (lane < 16 ? p.k_scale : p.v_scale) + word, see ? (int)min(4ll, (long long)p.scale_bytes - word) : 0);
+                asm volatile("st.shared.u8 [%0], %1;" ::"r"(words + 2 * kWarpKeys * 4 + lane), "r"((uint32_t)(so & 3)) : "memory");
+            } else {
             const long long off = see ? (long long)entry * p.b.page_stride + ((long long)l_h * P + row_in_page) * p.D : -1;
             const uint32_t dk = ring + stage * S::kStage, dv = dk + kWarpKeys * G::kPitchK;
             if (p.plain_rows && __all_sync(0xffffffffu, see)) {
@@ -256,6 +310,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                     }
                 }
             }
+            }
             if (--to_load > 0) {
                 if (++l_i == lt.tiles) {
                     __syncwarp();
@@ -267,12 +322,40 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                     lt = ld.t;
                     l_i = 0;
                     l_h = ld.h;
+                    l_start = ld.start;
                     l_table = p.b.page_table + (size_t)ld.s * p.b.max_pages;
                 }
                 look_up();
             }
         }
         cp_commit();
+    };
+    // 8 bits: a landed raw stage -> values, as a stage of the other kinds holds them
+    auto to_values = [&](uint32_t raw, uint32_t sk) {
+        const uint32_t sv = sk + kWarpKeys * G::kPitchK, words = raw + 2 * kWarpKeys * DP;
+        constexpr int lanes = DP / 8;
+#pragma unroll 2
+        for (int i = lane; i < 2 * kWarpKeys * lanes; i += 32) {
+            const int row = i / lanes, ch = i % lanes, key = row & 15;         // rows 0 .. 15: keys, then values
+            uint32_t c0, c1, at, sc;
+            asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c0), "=r"(c1) : "r"(raw + row * DP + ch * 8) : "memory");
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(at) : "r"(words + 2 * kWarpKeys * 4 + row) : "memory");
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(words + row * 4 + at) : "memory");
+            const float f = q8_factor(sc);
+            const float2 a = q8_values(c0 & 0xFFFFu, f), b = q8_values(c0 >> 16, f), c = q8_values(c1 & 0xFFFFu, f), d = q8_values(c1 >> 16, f);
+            const uint32_t to = row < kWarpKeys ? sk + key * G::kPitchK : sv + key * G::kPitchV;
+            if constexpr (kBf16) {                         // (exact: four significant bits)
+                const __nv_bfloat162 w0 = __floats2bfloat162_rn(a.x, a.y), w1 = __floats2bfloat162_rn(b.x, b.y),
+                                     w2 = __floats2bfloat162_rn(c.x, c.y), w3 = __floats2bfloat162_rn(d.x, d.y);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + ((ch ^ (key & 7)) << 4)), "r"(*reinterpret_cast<const uint32_t *>(&w0)),
+                             "r"(*reinterpret_cast<const uint32_t *>(&w1)), "r"(*reinterpret_cast<const uint32_t *>(&w2)),
+                             "r"(*reinterpret_cast<const uint32_t *>(&w3)) : "memory");
+            } else {
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + ch * 32), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y) : "memory");
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + ch * 32 + 16), "f"(c.x), "f"(c.y), "f"(d.x), "f"(d.y) : "memory");
+            }
+        }
+        __syncwarp();
     };
     look_up();
 #pragma unroll
@@ -297,6 +380,10 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
             }
             const uint32_t a = sq + r * G::kPitchQ + ((G::kSwizzle ? ch ^ (r & 7) : ch) << 4);
             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        }
+        if (SRC == kFromRows && p.join && tid < t.rows) {
+            const int row = t.r0 + tid, tok = row / p.g;
+            sh_prior[tid] = p.lse[(int64_t)(cur.start + tok) * p.H + cur.h * p.g + row - tok * p.g];
         }
         __syncthreads();
         uint32_t qf[kQRegs ? DP / 16 : 1][4];
@@ -328,7 +415,8 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
             load_tile((stage + kStages - 1) % kStages);
             cp_wait<kStages - 1>();
             __syncwarp();
-            const uint32_t sk = ring + stage * S::kStage, sv = sk + kWarpKeys * G::kPitchK;
+            const uint32_t sk = SRC == kFromQ8 ? ring + kStages * S::kRaw : ring + stage * S::kStage, sv = sk + kWarpKeys * G::kPitchK;
+            if constexpr (SRC == kFromQ8) to_values(ring + stage * S::kRaw, sk);
             const int j0 = key_tile(t, begin_tile + n) * kTile + warp * kWarpKeys;
             float s[2][4];
 #pragma unroll
@@ -485,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
             }
 #pragma unroll
             for (int f = 0; f < NF; ++f)
-                *reinterpret_cast<float2 *>(red + (size_t)(warp * kRows + gid + 8 * x) * S::kRedPitch + f * 8 + 2 * tig) =
+                *reinterpret_cast<float2 *>(red(warp) + (gid + 8 * x) * S::kRedPitch + f * 8 + 2 * tig) =
                     make_float2(o[f][2 * x], o[f][2 * x + 1]);
         }
         __syncthreads();
@@ -494,9 +582,24 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
         constexpr int F4 = DP / 4;
         auto put = [&](int r, int f4, float4 a, float M, float L) {       // final values of a row's four features
             const int row = t.r0 + r, tok = row / p.g, head = cur.h * p.g + row - tok * p.g;
-            const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);   // (NaN goes through)
-            a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+            float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);         // (NaN goes through)
             T *dst = reinterpret_cast<T *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D + f4 * 4;
+            JoinWith with = {0.f, 0.f, L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f};
+            float4 prior = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (SRC == kFromRows && p.join) {
+                with = join_with(M, L, sh_prior[r]);
+                inv = with.a;
+                if (with.b != 0.f && f4 * 4 < p.D) {
+                    if constexpr (kBf16) {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(dst);
+                        prior = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+                    } else {
+                        prior = *reinterpret_cast<const float4 *>(dst);
+                    }
+                    prior.x *= with.b; prior.y *= with.b; prior.z *= with.b; prior.w *= with.b;
+                }
+            }
+            a.x = fmaf(a.x, inv, prior.x); a.y = fmaf(a.y, inv, prior.y); a.z = fmaf(a.z, inv, prior.z); a.w = fmaf(a.w, inv, prior.w);
             if (f4 * 4 < p.D) {
                 if constexpr (kBf16) {
                     const __nv_bfloat162 x0 = __floats2bfloat162_rn(a.x, a.y), x1 = __floats2bfloat162_rn(a.z, a.w);
@@ -506,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                 }
             }
             if (f4 == 0 && p.lse)
-                p.lse[(int64_t)(cur.start + tok) * p.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+                p.lse[(int64_t)(cur.start + tok) * p.H + head] = with.lse;
         };
         for (int i = tid; i < t.rows * F4; i += kThreads) {
             const int r = i / F4, f4 = i - r * F4;
@@ -520,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
                 const float mw = red_m[w * kRows + r];
                 const float c = mw == -INFINITY ? 0.f : exp2_fast(mw - M);
                 if (mw == -INFINITY && red_l[w * kRows + r] == 0.f) continue;        // saw nothing
-                const float4 x = *reinterpret_cast<const float4 *>(red + (size_t)(w * kRows + r) * S::kRedPitch + f4 * 4);
+                const float4 x = *reinterpret_cast<const float4 *>(red(w) + r * S::kRedPitch + f4 * 4);
                 L = fmaf(c, red_l[w * kRows + r], L);
                 a.x = fmaf(c, x.x, a.x); a.y = fmaf(c, x.y, a.y); a.z = fmaf(c, x.z, a.z); a.w = fmaf(c, x.w, a.w);
             }
@@ -574,19 +677,58 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP>::kCtas) kv_attention_ker
 
 size_t slot_bytes() { return (size_t)kRows * (256 * 4 + 8); }
 
-template <typename T, int DP>
+template <typename T, int DP, int SRC>
 cudaError_t prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<T, DP>::kTotal);
+    return cudaFuncSetAttribute(kv_attention_kernel<T, DP, SRC>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<T, DP, SRC>::kTotal);
 }
-template <typename T, int DP>
+template <typename T>
+cudaError_t prepare()
+{
+    cudaError_t all[] = {prepare<T, 64, kFromPages>(), prepare<T, 128, kFromPages>(), prepare<T, 256, kFromPages>(),
+                         prepare<T, 64, kFromRows>(), prepare<T, 128, kFromRows>(), prepare<T, 256, kFromRows>(),
+                         prepare<T, 64, kFromQ8>(), prepare<T, 128, kFromQ8>(), prepare<T, 256, kFromQ8>()};
+    for (cudaError_t one : all)
+        if (one != cudaSuccess) return one;
+    return cudaSuccess;
+}
+template <typename T, int DP, int SRC>
 cudaError_t launch(Ctx *c, const AttnParams &p, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_kernel<T, DP>, dim3(sms * Smem<T, DP>::kCtas), dim3(kThreads), Smem<T, DP>::kTotal, st,
+    cudaError_t e = launch_k(kv_attention_kernel<T, DP, SRC>, dim3(sms * Smem<T, DP, SRC>::kCtas), dim3(kThreads), Smem<T, DP, SRC>::kTotal, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
     c->launches = 1;
     return note_err(c, e, "kv_attention_kernel");
+}
+template <int SRC>
+cudaError_t launch(Ctx *c, AttnParams &p, cudaStream_t st)
+{
+    const size_t slots = (size_t)4 * kKvMaxSm;
+    p.part.counters = (int32_t *)c->kv_ws;
+    p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
+    p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * kRows * 8);
+    if (c->cfg.dtype == MRP_BF16)
+        return p.D <= 64 ? launch<__nv_bfloat16, 64, SRC>(c, p, st)
+             : p.D <= 128 ? launch<__nv_bfloat16, 128, SRC>(c, p, st) : launch<__nv_bfloat16, 256, SRC>(c, p, st);
+    return p.D <= 64 ? launch<float, 64, SRC>(c, p, st)
+         : p.D <= 128 ? launch<float, 128, SRC>(c, p, st) : launch<float, 256, SRC>(c, p, st);
+}
+
+// what does not depend on where keys and values lie
+AttnParams attn_params(Ctx *c, const mrp_kv_batch &batch, const mrp_attention_args &a)
+{
+    const mrp_kv_config &kv = c->kv;
+    AttnParams p = {};
+    p.b = kv_batch_of(c, batch);
+    p.q = a.q; p.out = a.out; p.lse = a.lse;
+    p.q_stride = a.q_stride; p.out_stride = a.out_stride;
+    p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
+    p.gdiv = make_fastdiv(p.g);
+    p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
+    p.rows_upto = 0x7fffffff;
+    p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
+    return p;
 }
 
 }  // namespace
@@ -594,7 +736,7 @@ cudaError_t launch(Ctx *c, const AttnParams &p, cudaStream_t st)
 size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv)
 {
     const size_t few = kKvCounterBytes + (size_t)4 * kKvMaxSm * slot_bytes();
-    return kv_tc_takes(cfg, kv) && kv_tc_workspace_bytes() > few ? kv_tc_workspace_bytes() : few;
+    return kv_tc_any(cfg, kv) && kv_tc_workspace_bytes() > few ? kv_tc_workspace_bytes() : few;
 }
 
 cudaError_t kv_attach(Ctx *c)
@@ -602,56 +744,42 @@ cudaError_t kv_attach(Ctx *c)
     // (done before the call returns: the caller's stream need not wait for the legacy one)
     cudaError_t e = cudaMemset(c->kv_ws, 0, kKvCounterBytes);
     if (e != cudaSuccess || (e = cudaStreamSynchronize(cudaStreamLegacy)) != cudaSuccess || (e = kv_tc_attach(c)) != cudaSuccess) return e;
-    if (c->cfg.dtype == MRP_BF16) {
-        if ((e = prepare<__nv_bfloat16, 64>()) != cudaSuccess || (e = prepare<__nv_bfloat16, 128>()) != cudaSuccess) return e;
-        return prepare<__nv_bfloat16, 256>();
-    }
-    if ((e = prepare<float, 64>()) != cudaSuccess || (e = prepare<float, 128>()) != cudaSuccess) return e;
-    return prepare<float, 256>();
+    return c->cfg.dtype == MRP_BF16 ? prepare<__nv_bfloat16>() : prepare<float>();
 }
 
 cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_module_kv &pages,
                                    const mrp_attention_args &a, cudaStream_t st)
 {
     const mrp_kv_config &kv = c->kv;
-    AttnParams p;
-    p.b.seq_start = batch.seq_start;
-    p.b.prefix_len = batch.prefix_len;
-    p.b.page_table = batch.page_table;
-    p.b.positions = nullptr;
-    p.b.n_seqs = batch.n_seqs;
-    p.b.n_tokens = batch.n_tokens;
-    p.b.n_pages = kv.n_pages;
-    p.b.max_pages = kv.max_pages;
-    p.b.cap = kv.max_pages * kv.page_size;
-    p.b.page = make_fastdiv(kv.page_size);
-    p.b.page_stride = kv.page_stride;
-    p.b.status = (int32_t *)(c->ws + c->lay.status);
-    p.b.user_status = batch.status;
-    p.q = a.q; p.k = pages.k; p.v = pages.v; p.out = a.out; p.lse = a.lse;
-    p.q_stride = a.q_stride; p.out_stride = a.out_stride;
-    p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
-    p.gdiv = make_fastdiv(p.g);
-    p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
-    p.rows_above = 0;
-    p.rows_upto = 0x7fffffff;
-    p.lead = 0;
-    p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
+    AttnParams p = attn_params(c, batch, a);
+    p.k = pages.k; p.v = pages.v;
     {
         // a warp's 16 keys lie one after the other in one page, in rows as wide as the kernel's stages
         const int DP = kv.head_dim <= 64 ? 64 : kv.head_dim <= 128 ? 128 : 256;
         p.plain_rows = kv.page_size % kWarpKeys == 0 && kv.head_dim == DP;
     }
-    if (c->kv_encode) return launch_paged_attention_tc(c, p, batch, st);
-    const size_t slots = (size_t)4 * kKvMaxSm;
-    p.part.counters = (int32_t *)c->kv_ws;
-    p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
-    p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * kRows * 8);
-    if (c->cfg.dtype == MRP_BF16)
-        return kv.head_dim <= 64 ? launch<__nv_bfloat16, 64>(c, p, st)
-             : kv.head_dim <= 128 ? launch<__nv_bfloat16, 128>(c, p, st) : launch<__nv_bfloat16, 256>(c, p, st);
-    return kv.head_dim <= 64 ? launch<float, 64>(c, p, st)
-         : kv.head_dim <= 128 ? launch<float, 128>(c, p, st) : launch<float, 256>(c, p, st);
+    return kv_tc_takes(c->cfg, kv) ? launch_paged_attention_tc(c, p, batch, st) : launch<kFromPages>(c, p, st);
+}
+
+cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const mrp_kv_pool_q8 &pool,
+                                      const mrp_attention_args &a, cudaStream_t st)
+{
+    AttnParams p = attn_params(c, batch, a);
+    p.k = pool.k; p.v = pool.v;
+    p.k_scale = pool.k_scale; p.v_scale = pool.v_scale;
+    p.scale_bytes = (int64_t)c->kv.n_pages * c->kv.n_kv_heads * c->kv.page_size;
+    return launch<kFromQ8>(c, p, st);
+}
+
+cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_packed_kv &kv, const mrp_attention_args &a, cudaStream_t st)
+{
+    AttnParams p = attn_params(c, batch, a);
+    p.b.prefix_len = nullptr;
+    p.b.cap = 0x7fffffff;
+    p.k = kv.k; p.v = kv.v;
+    p.k_stride = kv.k_stride; p.v_stride = kv.v_stride;
+    p.join = kv.join != 0;
+    return launch<kFromRows>(c, p, st);
 }
 
 }  // namespace mrp

@@ -43,6 +43,25 @@ struct KvBatch {
     int32_t *status, *user_status;
 };
 
+inline KvBatch kv_batch_of(const Ctx *c, const mrp_kv_batch &batch)
+{
+    KvBatch b;
+    b.seq_start = batch.seq_start;
+    b.prefix_len = batch.prefix_len;
+    b.page_table = batch.page_table;
+    b.positions = nullptr;
+    b.n_seqs = batch.n_seqs;
+    b.n_tokens = batch.n_tokens;
+    b.n_pages = c->kv.n_pages;
+    b.max_pages = c->kv.max_pages;
+    b.cap = c->kv.max_pages * c->kv.page_size;
+    b.page = make_fastdiv(c->kv.page_size);
+    b.page_stride = c->kv.page_stride;
+    b.status = (int32_t *)(c->ws + c->lay.status);
+    b.user_status = batch.status;
+    return b;
+}
+
 __device__ __forceinline__ void kv_bad_index(const KvBatch &b)
 {
     atomicOr(b.status, MRP_DEV_BAD_INDEX);
@@ -54,7 +73,7 @@ __device__ __forceinline__ bool kv_sequence(const KvBatch &b, int s, int &start,
 {
     start = __ldg(b.seq_start + s);
     const int end = __ldg(b.seq_start + s + 1);
-    pre = __ldg(b.prefix_len + s);
+    pre = b.prefix_len ? __ldg(b.prefix_len + s) : 0;     // (no cache: nothing lies in front of the rows)
     n = end - start;
     return start >= 0 && end >= start && end <= b.n_tokens && pre >= 0 && pre <= b.cap && n <= b.cap - pre;
 }
@@ -77,6 +96,9 @@ struct KvPartials {
     float *o;
 };
 
+// Where a kernel's keys and values lie: in pages of the context type, in rows beside the queries, in pages of 8 bits.
+enum { kFromPages = 0, kFromRows = 1, kFromQ8 = 2 };
+
 struct AttnParams {
     KvBatch b;
     const void *q, *k, *v;
@@ -90,7 +112,28 @@ struct AttnParams {
     int lead;                  // what a unit costs besides its tiles, in tiles: so much of the line lies ahead of each unit
     float scale_log2;          // > 0
     KvPartials part;
+    int64_t k_stride, v_stride;                            // rows: elements from token to token
+    int join;                  // rows: out and lse hold the result of a pass over other keys
+    const uint8_t *k_scale, *v_scale;                      // 8 bits: scale bytes, of which there are scale_bytes
+    int64_t scale_bytes;
 };
+
+// A row's sum over new keys (sum of p V with sum of p L at maximum m, base 2) beside the result of another pass (lse): out =
+// a (sum of p V) + b (that pass's row).  b = 0 where that pass saw nothing: its row is not read then.
+struct JoinWith {
+    float a, b, lse;
+};
+__device__ __forceinline__ JoinWith join_with(float m, float L, float lse)
+{
+    const float l = L == 0.f ? -INFINITY : m + log2f(L), q = lse * 1.4426950408889634f;
+    JoinWith j = {0.f, 0.f, -INFINITY};
+    if (l == -INFINITY && q == -INFINITY) return j;
+    const float top = fmaxf(l, q), x = exp2f(l - top), y = exp2f(q - top), s = x + y;      // (NaN goes through)
+    j.a = L == 0.f ? 0.f : x / (s * L);
+    j.b = y / s;
+    j.lse = (top + log2f(s)) * 0.6931471805599453f;
+    return j;
+}
 
 // whether position j lies in [lo, hi) or among the first `sinks` (below hi); no branches
 __device__ __forceinline__ bool sees(int j, int hi, int lo, int sinks) { return (j < hi) & ((j >= lo) | (j < sinks)); }
@@ -365,6 +408,7 @@ __device__ __forceinline__ long long find_piece_warp(const AttnParams &p, Cursor
 
 // The kernel on large tiles (kv_attention_tc.cu): the geometries it takes, its workspace, its launch.
 bool kv_tc_takes(const mrp_config &cfg, const mrp_kv_config &kv);
+bool kv_tc_any(const mrp_config &cfg, const mrp_kv_config &kv);
 size_t kv_tc_workspace_bytes();
 cudaError_t kv_tc_attach(Ctx *c);
 cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);

@@ -1519,6 +1519,12 @@ bool kv_tc_takes(const mrp_config &cfg, const mrp_kv_config &kv)
            kv.page_stride < (1ll << 39) && (long long)kv.page_size * kv.head_dim < (1ll << 39) && !(cfg.flags & MRP_FLAG_FORCE_SIMT);
 }
 
+// some call on the geometry runs on large tiles (rows over each other need no pages)
+bool kv_tc_any(const mrp_config &cfg, const mrp_kv_config &)
+{
+    return cfg.dtype == MRP_BF16 && !(cfg.flags & MRP_FLAG_FORCE_SIMT);
+}
+
 size_t kv_tc_workspace_bytes()
 {
     return kKvCounterBytes + (size_t)2 * kKvMaxSm * 2 * 128 * (128 * 4 + 8);      // (or one row tile of 256 features)
@@ -1527,7 +1533,7 @@ size_t kv_tc_workspace_bytes()
 cudaError_t kv_tc_attach(Ctx *c)
 {
     c->kv_encode = nullptr;
-    if (!kv_tc_takes(c->cfg, c->kv)) return cudaSuccess;
+    if (!kv_tc_any(c->cfg, c->kv)) return cudaSuccess;
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);

@@ -15,7 +15,11 @@
 // rot_dim / 2 that is no multiple of four splits runs: there the other half of a pair is read again.
 // Measured, 32 query and 8 key heads of 128 in bf16 with norms: 16384 tokens 64 us (336 MB: 5.2 TB/s), 24509 tokens with values
 // into pages 105 us (602 MB: 5.7 TB/s, 0.89 of a copy); 4 tokens 3.6 us and 128 tokens 4.2 us a launch inside a graph.
+#include <cuda_fp16.h>
+
 #include "kv_attention.cuh"
+#include "kv_find.cuh"
+#include "kv_q8.cuh"
 
 namespace mrp {
 namespace {
@@ -31,6 +35,7 @@ struct RowsParams {
     const void *gamma[2];
     int heads[3];
     int to_pages;              // k and v go to the pools
+    uint8_t *scale[2];         // of keys and values, where the pools hold 8 bits
     int D, rot, half, interleaved;
     int tokens, shares;        // warps a token
     int units[3];              // units of U * NG heads: of queries, and keys, and values
@@ -75,71 +80,30 @@ __device__ __forceinline__ void fma2(float &a, float &b, float c, float d, float
 __device__ __forceinline__ float one_f(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float one_f(const float *p) { return *p; }
 
-// Sequence of row t: the number of entries of seq_start[1..n_seqs] that are <= t, found by the warp 32 probes at a time
-// (in 0..n_seqs whatever the list holds).
-__device__ __forceinline__ int find_sequence(const int32_t *seq_start, int n_seqs, int t, int lane)
-{
-    int lo = 0, n = n_seqs;                // the answer lies in [lo, lo + n]
-    while (n > 0) {
-        const int step = (n + 31) / 32;
-        const int at = lo + (lane + 1) * step - 1;
-        const bool le = (lane + 1) * step - 1 < n && __ldg(seq_start + 1 + at) <= t;
-        const int k = __popc(__ballot_sync(0xffffffffu, le));
-        lo += k * step;
-        n = min(step - 1, n - k * step);
-    }
-    return lo;
-}
-
-// The same where that list is not ascending (a sequence in it does not fit) or no sequence has the row: all of them; -1: none.
-__device__ __noinline__ int scan_sequences(const KvBatch &b, int t, int lane)
-{
-    for (int s0 = 0; s0 < b.n_seqs; s0 += 32) {
-        const int s = s0 + lane;
-        int start, n, pre;
-        const bool has = s < b.n_seqs && kv_sequence(b, s, start, n, pre) && t >= start && t - start < n;
-        const uint32_t hit = __ballot_sync(0xffffffffu, has);
-        if (hit) return s0 + __ffs(hit) - 1;
-    }
-    return -1;
-}
-
 enum { kHalves = 0, kAdjacent = 1, kAgain = 2 };         // how pairs lie in a lane
 
-template <typename T, int GL, int U, int MODE>
+template <typename T, int GL, int U, int MODE, bool Q8>
 __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_constant__ RowsParams p)
 {
     const int tid = threadIdx.x, lane = tid & 31;
     const int gw = blockIdx.x * kRowWarps + (tid >> 5);
     pdl_wait();
     pdl_trigger();
-    // a sequence that does not fit is reported even if no row names it
-    if (blockIdx.x == 0)
-        for (int s = tid; s < p.b.n_seqs; s += kRowThreads) {
-            int start, n, pre;
-            if (!kv_sequence(p.b, s, start, n, pre)) kv_bad_index(p.b);
-        }
+    if (blockIdx.x == 0) report_sequences(p.b, tid, kRowThreads);
     const int t = gw / p.shares, share = gw - t * p.shares;
     if (t >= p.tokens) return;
 
     // ---- the token: its sequence, position, row in the pools (element offset of head 0's, -1: not stored)
     int pos = 0;
-    int64_t page_off = -1;
+    int64_t page_off = -1, scale_off = 0;                  // (8 bits: head 0's scale byte)
     if (p.b.n_seqs >= 0) {
-        int s = find_sequence(p.b.seq_start, p.b.n_seqs, t, lane);
-        int start, n, pre;
-        if (s >= p.b.n_seqs || !kv_sequence(p.b, s, start, n, pre) || t < start || t - start >= n) {
-            s = scan_sequences(p.b, t, lane);
-            if (s < 0) return;
-            kv_sequence(p.b, s, start, n, pre);
+        TokenPlace at;
+        if (!find_token(p.b, t, lane, at)) return;
+        pos = at.pos;
+        if (at.page >= 0) {
+            page_off = (int64_t)at.page * p.b.page_stride + (int64_t)at.row * p.D;
+            if (Q8) scale_off = (int64_t)at.page * p.heads[1] * p.b.page.d + at.row;
         }
-        pos = pre + (t - start);
-        const int pg = fast_div(pos, p.b.page);
-        const int entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
-        if ((unsigned)entry < (unsigned)p.b.n_pages)
-            page_off = (int64_t)entry * p.b.page_stride + (int64_t)(pos - pg * p.b.page.d) * p.D;
-        else if (lane == 0)
-            kv_bad_index(p.b);
     }
     if (p.b.positions) pos = __ldg(p.b.positions + t);
 
@@ -193,6 +157,25 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
             dst += (int64_t)t * p.dst_stride[kind] + (int64_t)h0 * step;
         }
         step *= NG;
+        const bool codes = Q8 && kind > 0;
+        // 8 bits: the row's scale from its largest magnitude, then the lane's codes and the row's byte
+        auto put_codes = [&](const float *f, int i) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) top = max(top, __float_as_uint(f[y]) & 0x7FFFFFFFu);
+            if (!mine) top = 0;
+#pragma unroll
+            for (int w = GL / 2; w > 0; w >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+            const uint32_t sc = q8_scale(top);
+            const bool fine = sc != kQ8NaN;
+            const float inv = q8_inverse(fine ? sc : 127u);
+            if (store && i * NG < n) {
+                uint8_t *to = reinterpret_cast<uint8_t *>(p.dst[kind]) + page_off + (int64_t)(h0 + i * NG) * head_out;
+                *reinterpret_cast<uint32_t *>(to + e0) = fine ? q8_codes(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv) : 0u;
+                *reinterpret_cast<uint32_t *>(to + e1) = fine ? q8_codes(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv) : 0u;
+                if (gl == 0) p.scale[kind - 1][scale_off + (int64_t)(h0 + i * NG) * p.b.page.d] = (uint8_t)sc;
+            }
+        };
         if (kind < 2) {
             const T *gm = reinterpret_cast<const T *>(p.gamma[kind]);
             float g[8];
@@ -265,10 +248,26 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
                             if (q == y) f[q] = z;
                     }
                 }
-                x[i][0].put(f);
-                x[i][1].put(f + 4);
+                if (codes) {
+                    put_codes(f, i);
+                } else {
+                    x[i][0].put(f);
+                    x[i][1].put(f + 4);
+                }
                 if (MODE == kAgain) __syncwarp();          // a head read again above is overwritten by its own lanes alone, now
             }
+        }
+        if (codes) {
+            if (kind == 2) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    float f[8];
+                    x[i][0].get(f);
+                    x[i][1].get(f + 4);
+                    put_codes(f, i);
+                }
+            }
+            continue;
         }
 #pragma unroll
         for (int i = 0; i < U; ++i)
@@ -279,7 +278,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
     }
 }
 
-template <typename T, int GL, int MODE>
+template <typename T, int GL, int MODE, bool Q8>
 cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
 {
     constexpr int U = sizeof(T) == 2 ? 4 : 2, kAtOnce = U * (32 / GL);
@@ -289,50 +288,29 @@ cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
     const long long want = (long long)c->sm_count * 32 / p.tokens;
     p.shares = (int)(want < 1 ? 1 : want > n ? n : want);
     const long long warps = (long long)p.tokens * p.shares;
-    cudaError_t e = launch_k(qk_rows_kernel<T, GL, U, MODE>, dim3((unsigned)((warps + kRowWarps - 1) / kRowWarps)), dim3(kRowThreads),
+    cudaError_t e = launch_k(qk_rows_kernel<T, GL, U, MODE, Q8>, dim3((unsigned)((warps + kRowWarps - 1) / kRowWarps)), dim3(kRowThreads),
                              0, st, !(c->cfg.flags & MRP_FLAG_NO_PDL), p);
     c->launches = 1;
     return note_err(c, e, "qk_rows_kernel");
 }
-template <typename T, int GL>
+template <typename T, int GL, bool Q8>
 cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
 {
-    if (p.interleaved) return launch_rows<T, GL, kAdjacent>(c, p, st);
-    return (p.half & 3) == 0 ? launch_rows<T, GL, kHalves>(c, p, st) : launch_rows<T, GL, kAgain>(c, p, st);
+    if (p.interleaved) return launch_rows<T, GL, kAdjacent, Q8>(c, p, st);
+    return (p.half & 3) == 0 ? launch_rows<T, GL, kHalves, Q8>(c, p, st) : launch_rows<T, GL, kAgain, Q8>(c, p, st);
 }
-template <typename T>
+template <typename T, bool Q8>
 cudaError_t launch_rows(Ctx *c, RowsParams &p, cudaStream_t st)
 {
-    return p.D <= 64 ? launch_rows<T, 8>(c, p, st) : p.D <= 128 ? launch_rows<T, 16>(c, p, st) : launch_rows<T, 32>(c, p, st);
+    return p.D <= 64 ? launch_rows<T, 8, Q8>(c, p, st) : p.D <= 128 ? launch_rows<T, 16, Q8>(c, p, st) : launch_rows<T, 32, Q8>(c, p, st);
 }
 
-}  // namespace
-
-cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_kv *pages, const int32_t *positions,
-                           int n_tokens, const mrp_qkv_rows &rows, cudaStream_t st)
+// what does not depend on where keys and values go
+void fill_rows(Ctx *c, RowsParams &p, int n_tokens, const mrp_qkv_rows &rows)
 {
     const mrp_kv_config &kv = c->kv;
-    RowsParams p;
-    p.b = KvBatch{};
-    p.b.n_seqs = -1;
-    p.b.positions = positions;
-    if (batch) {
-        p.b.seq_start = batch->seq_start;
-        p.b.prefix_len = batch->prefix_len;
-        p.b.page_table = batch->page_table;
-        p.b.n_seqs = batch->n_seqs;
-        p.b.user_status = batch->status;
-    }
-    p.b.n_tokens = n_tokens;
-    p.b.n_pages = kv.n_pages;
-    p.b.max_pages = kv.max_pages;
-    p.b.cap = kv.max_pages * kv.page_size;
-    p.b.page = make_fastdiv(kv.page_size);
-    p.b.page_stride = kv.page_stride;
-    p.b.status = (int32_t *)(c->ws + c->lay.status);
-    p.to_pages = pages != nullptr;
-    p.src[0] = rows.q; p.src[1] = rows.k; p.src[2] = pages ? rows.v : nullptr;
-    p.dst[0] = rows.q_out; p.dst[1] = pages ? pages->k : rows.k_out; p.dst[2] = pages ? pages->v : nullptr;
+    p.src[0] = rows.q; p.src[1] = rows.k; p.src[2] = p.to_pages ? rows.v : nullptr;
+    p.dst[0] = rows.q_out;
     p.src_stride[0] = rows.q_stride; p.src_stride[1] = rows.k_stride; p.src_stride[2] = rows.v_stride;
     p.dst_stride[0] = rows.q_out_stride; p.dst_stride[1] = rows.k_out_stride; p.dst_stride[2] = 0;
     p.gamma[0] = rows.gamma_q; p.gamma[1] = rows.gamma_k;
@@ -347,7 +325,42 @@ cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_k
     p.eps = kv.norm_eps;
     p.inv_d = 1.f / (float)kv.head_dim;
     for (int j = 0; j < p.half; ++j) p.turn[j] = c->kv_turn[j];
-    return c->cfg.dtype == MRP_BF16 ? launch_rows<__nv_bfloat16>(c, p, st) : launch_rows<float>(c, p, st);
+}
+
+}  // namespace
+
+cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_kv *pages, const int32_t *positions,
+                           int n_tokens, const mrp_qkv_rows &rows, cudaStream_t st)
+{
+    RowsParams p;
+    if (batch) {
+        p.b = kv_batch_of(c, *batch);
+    } else {
+        p.b = KvBatch{};
+        p.b.n_seqs = -1;
+        p.b.n_tokens = n_tokens;
+        p.b.page = make_fastdiv(c->kv.page_size);
+        p.b.status = (int32_t *)(c->ws + c->lay.status);
+    }
+    p.b.positions = positions;
+    p.to_pages = pages != nullptr;
+    p.scale[0] = p.scale[1] = nullptr;
+    fill_rows(c, p, n_tokens, rows);
+    p.dst[1] = pages ? pages->k : rows.k_out;
+    p.dst[2] = pages ? pages->v : nullptr;
+    return c->cfg.dtype == MRP_BF16 ? launch_rows<__nv_bfloat16, false>(c, p, st) : launch_rows<float, false>(c, p, st);
+}
+
+cudaError_t launch_qk_rows_q8(Ctx *c, const mrp_kv_batch &batch, const mrp_kv_pool_q8 &pool, const mrp_qkv_rows &rows, cudaStream_t st)
+{
+    RowsParams p;
+    p.b = kv_batch_of(c, batch);
+    p.b.positions = batch.positions;
+    p.to_pages = 1;
+    fill_rows(c, p, batch.n_tokens, rows);
+    p.dst[1] = pool.k; p.dst[2] = pool.v;
+    p.scale[0] = pool.k_scale; p.scale[1] = pool.v_scale;
+    return c->cfg.dtype == MRP_BF16 ? launch_rows<__nv_bfloat16, true>(c, p, st) : launch_rows<float, true>(c, p, st);
 }
 
 }  // namespace mrp

@@ -506,11 +506,11 @@ static bool rows_ok(const Ctx &c, const void *ptr, int64_t stride, int heads)
     return ptr && !((uintptr_t)ptr & 15u) && stride >= (int64_t)heads * c.kv.head_dim && stride <= (1ll << 40) && (stride * size) % 16 == 0;
 }
 
-static int kv_batch_status(const Ctx &c, const mrp_kv_batch *b)
+static int kv_batch_status(const Ctx &c, const mrp_kv_batch *b, bool cached = true)
 {
     if (!b || b->n_seqs < 0 || b->n_seqs > c.cfg.max_seqs || b->n_tokens < 0 || b->max_new < 0) return MRP_ERR_INVALID_ARG;
     if ((long long)b->n_tokens * c.kv.n_heads > (1ll << 30)) return MRP_ERR_INVALID_ARG;
-    if (b->n_seqs > 0 && b->n_tokens > 0 && (!b->seq_start || !b->prefix_len || !b->page_table)) return MRP_ERR_INVALID_ARG;
+    if (b->n_seqs > 0 && b->n_tokens > 0 && (!b->seq_start || (cached && (!b->prefix_len || !b->page_table)))) return MRP_ERR_INVALID_ARG;
     return MRP_OK;
 }
 
@@ -568,26 +568,113 @@ int mrp_kv_append(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *
     return launch_qk_rows(&c, batch, pages, batch->positions, batch->n_tokens, *rows, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
 }
 
+// what all attention calls check of their arguments
+static int attention_status(const mrp_attention_args *a)
+{
+    if (a->mask < MRP_ATTN_CAUSAL || a->mask > MRP_ATTN_PREFIX || a->window < 0 || a->sinks < 0 || !(a->scale >= 0.f) ||
+        !isfinite(a->scale * 1.4426950408889634f))             // (in base 2)
+        return MRP_ERR_INVALID_ARG;
+    return MRP_OK;
+}
+static int attention_rows_status(const Ctx &c, const mrp_attention_args *a)
+{
+    if (!rows_ok(c, a->q, a->q_stride, c.kv.n_heads) || !rows_ok(c, a->out, a->out_stride, c.kv.n_heads)) return MRP_ERR_INVALID_ARG;
+    return a->q == a->out && a->q_stride != a->out_stride ? MRP_ERR_INVALID_ARG : MRP_OK;
+}
+
 int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *pages, const mrp_attention_args *args,
                         void *cuda_stream)
 {
     if (!ctx || !args) return MRP_ERR_INVALID_ARG;
     Ctx &c = ctx->c;
     if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
-    const int bad = kv_batch_status(c, batch);
-    if (bad) return bad;
-    if (args->mask < MRP_ATTN_CAUSAL || args->mask > MRP_ATTN_PREFIX || args->window < 0 || args->sinks < 0 || !(args->scale >= 0.f) ||
-        !isfinite(args->scale * 1.4426950408889634f))             // (in base 2)
-        return MRP_ERR_INVALID_ARG;
+    int bad = kv_batch_status(c, batch);
+    if (bad || (bad = attention_status(args)) != MRP_OK) return bad;
     c.launches = 0;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
-    if (!pools_ok(pages) || !rows_ok(c, args->q, args->q_stride, c.kv.n_heads) || !rows_ok(c, args->out, args->out_stride, c.kv.n_heads))
-        return MRP_ERR_INVALID_ARG;
-    if (args->q == args->out && args->q_stride != args->out_stride) return MRP_ERR_INVALID_ARG;
+    if (!pools_ok(pages) || (bad = attention_rows_status(c, args)) != MRP_OK) return MRP_ERR_INVALID_ARG;
     DeviceGuard guard(c.cfg.device);
     if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
     c.err[0] = 0;
     return launch_paged_attention(&c, *batch, *pages, *args, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+// ---- the cache in 8 bits, rows over each other ----------------------------------------------------------------------
+static bool pool_q8_ok(const mrp_kv_pool_q8 *p)
+{
+    return p && p->k && p->v && p->k_scale && p->v_scale &&
+           !(((uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->k_scale | (uintptr_t)p->v_scale) & 15u);
+}
+
+int mrp_kv_append_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_qkv_rows *rows, void *cuda_stream)
+{
+    if (!ctx || !rows) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
+    int bad = kv_batch_status(c, batch);
+    if (bad) return bad;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!pool_q8_ok(pool) || !rows->k || !rows_ok(c, rows->v, rows->v_stride, c.kv.n_kv_heads)) return MRP_ERR_INVALID_ARG;
+    if ((bad = qk_rows_status(c, rows, false)) != MRP_OK) return bad;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_qk_rows_q8(&c, *batch, *pool, *rows, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_kv_rows *rows, void *cuda_stream)
+{
+    if (!ctx || !rows) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
+    const int bad = kv_batch_status(c, batch);
+    if (bad) return bad;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!pool_q8_ok(pool) || (!rows->k && !rows->v)) return MRP_ERR_INVALID_ARG;
+    if ((rows->k && !rows_ok(c, rows->k, rows->k_stride, c.kv.n_kv_heads)) || (rows->v && !rows_ok(c, rows->v, rows->v_stride, c.kv.n_kv_heads)))
+        return MRP_ERR_INVALID_ARG;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_kv_read_q8(&c, *batch, *pool, *rows, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_attention_args *args,
+                           void *cuda_stream)
+{
+    if (!ctx || !args) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv || c.kv.n_pages == 0) return MRP_ERR_UNSUPPORTED;
+    int bad = kv_batch_status(c, batch);
+    if (bad || (bad = attention_status(args)) != MRP_OK) return bad;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!pool_q8_ok(pool) || (bad = attention_rows_status(c, args)) != MRP_OK) return MRP_ERR_INVALID_ARG;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_paged_attention_q8(&c, *batch, *pool, *args, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
+}
+
+int mrp_packed_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_packed_kv *kv, const mrp_attention_args *args, void *cuda_stream)
+{
+    if (!ctx || !args || !kv) return MRP_ERR_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (!c.has_kv) return MRP_ERR_UNSUPPORTED;
+    int bad = kv_batch_status(c, batch, false);
+    if (bad || (bad = attention_status(args)) != MRP_OK) return bad;
+    if (args->mask == MRP_ATTN_PREFIX) return MRP_ERR_INVALID_ARG;
+    c.launches = 0;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return MRP_OK;
+    if (!rows_ok(c, kv->k, kv->k_stride, c.kv.n_kv_heads) || !rows_ok(c, kv->v, kv->v_stride, c.kv.n_kv_heads)) return MRP_ERR_INVALID_ARG;
+    if ((bad = attention_rows_status(c, args)) != MRP_OK) return bad;
+    if (kv->k == args->out || kv->v == args->out || (kv->join && (!args->lse || args->q == args->out))) return MRP_ERR_INVALID_ARG;
+    DeviceGuard guard(c.cfg.device);
+    if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
+    c.err[0] = 0;
+    return launch_packed_attention(&c, *batch, *kv, *args, (cudaStream_t)cuda_stream) == cudaSuccess ? MRP_OK : MRP_ERR_CUDA;
 }
 
 int mrp_quantised_lm_head(mrp_ctx *ctx, const uint8_t **codes, const float **scales)

@@ -287,13 +287,19 @@ cudaError_t module_step(Ctx *c, const int32_t *tokens, const void *hidden0, floa
 size_t module_workspace_bytes(const mrp_config &cfg, int n_layers);
 size_t module_att_offset(const mrp_config &cfg);   // the clean-prefix attention's area of the module workspace
 
-// ---- the paged key / value cache (kv_rows.cu, kv_attention.cu, kv_attention_tc.cu) ------
+// ---- the paged key / value cache (kv_rows.cu, kv_read.cu, kv_attention.cu, kv_attention_tc.cu) ------
 size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv);
 cudaError_t kv_attach(Ctx *c);               // after the kv fields are set: clears the counters, sets kernel attributes
 cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_kv *pages, const int32_t *positions,
                            int n_tokens, const mrp_qkv_rows &rows, cudaStream_t st);
 cudaError_t launch_paged_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_module_kv &pages,
                                    const mrp_attention_args &a, cudaStream_t st);
+// the cache in 8 bits; rows over each other
+cudaError_t launch_qk_rows_q8(Ctx *c, const mrp_kv_batch &batch, const mrp_kv_pool_q8 &pool, const mrp_qkv_rows &rows, cudaStream_t st);
+cudaError_t launch_kv_read_q8(Ctx *c, const mrp_kv_batch &batch, const mrp_kv_pool_q8 &pool, const mrp_kv_rows &rows, cudaStream_t st);
+cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const mrp_kv_pool_q8 &pool,
+                                      const mrp_attention_args &a, cudaStream_t st);
+cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_packed_kv &kv, const mrp_attention_args &a, cudaStream_t st);
 
 // Few-row variants (tc_skinny.cu): weight rows on the MMA M axis; rows <= 32.
 bool sk_rows_ok(int rows);          // LM head: row-steps incl. step 0
