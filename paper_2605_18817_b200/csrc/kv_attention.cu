@@ -768,7 +768,7 @@ cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const m
     p.k = pool.k; p.v = pool.v;
     p.k_scale = pool.k_scale; p.v_scale = pool.v_scale;
     p.scale_bytes = (int64_t)c->kv.n_pages * c->kv.n_kv_heads * c->kv.page_size;
-    return launch<kFromQ8>(c, p, st);
+    return kv_tc_takes_q8(c->cfg, c->kv) ? launch_paged_attention_q8_tc(c, p, batch, st) : launch<kFromQ8>(c, p, st);
 }
 
 cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_packed_kv &kv, const mrp_attention_args &a, cudaStream_t st)
@@ -779,7 +779,7 @@ cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp
     p.k = kv.k; p.v = kv.v;
     p.k_stride = kv.k_stride; p.v_stride = kv.v_stride;
     p.join = kv.join != 0;
-    return launch<kFromRows>(c, p, st);
+    return kv_tc_takes_rows(c->cfg, c->kv, kv) ? launch_packed_attention_tc(c, p, batch, st) : launch<kFromRows>(c, p, st);
 }
 
 }  // namespace mrp

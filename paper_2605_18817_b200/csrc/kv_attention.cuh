@@ -412,5 +412,9 @@ bool kv_tc_any(const mrp_config &cfg, const mrp_kv_config &kv);
 size_t kv_tc_workspace_bytes();
 cudaError_t kv_tc_attach(Ctx *c);
 cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);
+bool kv_tc_takes_q8(const mrp_config &cfg, const mrp_kv_config &kv);
+cudaError_t launch_paged_attention_q8_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);
+bool kv_tc_takes_rows(const mrp_config &cfg, const mrp_kv_config &kv, const mrp_packed_kv &rows);
+cudaError_t launch_packed_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);
 
 }  // namespace mrp

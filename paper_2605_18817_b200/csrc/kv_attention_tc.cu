@@ -32,7 +32,10 @@
 // used, and V rows that no row of the tile sees are zeroed in shared memory before the product (0 * NaN).  A V row with
 // an infinity or NaN that only some rows of a tile see (later tokens of a prompt) is zeroed too and makes the output of
 // the rows that do see it NaN, all features, instead of that of the rows that do not.
+#include <cuda_fp16.h>
+
 #include "kv_attention.cuh"
+#include "kv_q8.cuh"
 #include "tc_common.cuh"
 
 namespace mrp {
@@ -50,15 +53,25 @@ template <int NB> struct Blocks {
     static constexpr int DB = NB >= 2 ? 2 : 1, HB = NB / DB;
     static constexpr int kStageBytes = DB * 128 * 128;
 };
-template <int NB, int NT> struct TcGeo {
+// How the keys and values lie (see TileAt, PageBoxes): pages, a box a 64-feature block (kApart) or two (kJoined); rows beside the
+// queries (kPacked); pages of 8 bits (kCodes).
+enum { kApart = 0, kJoined = 1, kPacked = 2, kCodes = 3 };
+
+template <int NB, int NT, int LAY> struct TcGeo {
     typedef Blocks<NB> B;
-    static constexpr int kStages = B::DB == 1 ? 10 : B::HB == 2 || NT == 2 ? 4 : 5;
+    // 8 bits: raw stages (128 rows of up to 128 codes) beside the ring, and warps that turn them into stages of it
+    static constexpr int kRawStage = LAY == kCodes ? B::kStageBytes / 2 : 0;
+    static constexpr int kRawStages = LAY != kCodes ? 0 : B::DB == 1 ? 4 : NT == 1 && B::HB == 1 ? 3 : 2;
+    static constexpr int kTurners = LAY != kCodes ? 0 : NT == 1 ? 4 : 2;
+    static constexpr int kStages = LAY == kCodes ? (B::DB == 1 ? 8 : B::HB == 2 || NT == 2 ? 3 : 4)
+                                                 : B::DB == 1 ? 10 : B::HB == 2 || NT == 2 ? 4 : 5;
     static constexpr int kQTile = NB * 128 * 128;          // queries of a row tile
     static constexpr int kQ = NT * kQTile;
     static constexpr int kRing = kStages * B::kStageBytes;
-    static constexpr int kBars = kQ + kRing;
+    static constexpr int kRaw = kQ + kRing;
+    static constexpr int kBars = kRaw + kRawStages * kRawStage;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
-    static constexpr int kThreads = 64 + NT * 256;
+    static constexpr int kThreads = 64 + NT * 256 + kTurners * 32;
     static constexpr int kRows = NT * 128;
     static_assert(NT == 1 || NB <= 2, "tensor memory: two row tiles of accumulators of at most 128 features");
 };
@@ -255,8 +268,8 @@ struct PageBoxes {
     int rows;
     int page_groups, head_groups, groups;  // joined (else 0): groups of 8 rows from page to page, head to head, in all
 };
-template <int DB, bool JOINED> struct TileAt {             // of a tile: bytes to the next 64-feature block, the next group of 8 keys
-    static constexpr uint32_t block = JOINED ? 1024 : 128 * 128, group = JOINED ? DB * 1024 : 1024;
+template <int DB, int LAY> struct TileAt {                 // of a tile: bytes to the next 64-feature block, the next group of 8 keys
+    static constexpr uint32_t block = LAY == kJoined ? 1024 : 128 * 128, group = LAY == kJoined ? DB * 1024 : 1024;
 };
 
 // The box of a tile's keys that is the lane's: where it lies in the pool.  Looked up a tile ahead of its use.
@@ -264,14 +277,16 @@ struct PageRef {
     bool need;                 // holds visible positions
     int entry, row;            // page, row in it
 };
-template <typename Tile>
-__device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes &bx, const Tile &t, int n, int s, int lane)
+template <int LAY, typename Tile>
+__device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes &bx, const Tile &t, int n, int s, int start, int lane)
 {
     const int j = key_tile(t, n) * kTcTile + lane * bx.rows;
     PageRef r;
     r.need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
     r.entry = r.row = 0;
-    if (r.need) {
+    if (LAY == kPacked) {
+        r.row = start + j;                                 // (rows behind the sequence's: not seen, whatever they are)
+    } else if (r.need) {
         const int pg = fast_div(j, p.b.page);
         r.row = j - pg * p.b.page.d;
         r.entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
@@ -280,7 +295,7 @@ __device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes 
 }
 
 // The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
-template <int DB, bool JOINED>
+template <int DB, int LAY>
 __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
                                            uint32_t dst, uint32_t bar, int lane)
 {
@@ -288,11 +303,11 @@ __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMa
     if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * 128u * DB);
     __syncwarp();
     if (r.need) {
-        const bool bad = (unsigned)r.entry >= (unsigned)p.b.n_pages;
+        const bool bad = LAY != kPacked && (unsigned)r.entry >= (unsigned)p.b.n_pages;
         if (bad) kv_bad_index(p.b);
-        dst += lane * (bx.rows >> 3) * TileAt<DB, JOINED>::group;
+        dst += lane * (bx.rows >> 3) * TileAt<DB, LAY>::group;
         // (a page that is not one: outside the map, zeros arrive)
-        if (JOINED) {
+        if (LAY == kJoined) {
             const int g = bad ? bx.groups : r.entry * bx.page_groups + h * bx.head_groups + (r.row >> 3);
             tma_load_page(dst, map, 0, 0, feature >> 6, g, bar);
         } else {
@@ -301,6 +316,39 @@ __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMa
                 tma_load_page(dst + x * (128 * 128), map, feature + 64 * x, r.row, h, bad ? p.b.n_pages : r.entry, bar);
         }
     }
+}
+
+// 8 bits: the same, 128 keys of `pitch` codes from `feature` on, one row after the other, -> a raw stage.
+__device__ __forceinline__ void fetch_codes(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
+                                            int pitch, uint32_t dst, uint32_t bar, int lane)
+{
+    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, r.need));
+    if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * (uint32_t)pitch);
+    __syncwarp();
+    if (r.need) {
+        const bool bad = (unsigned)r.entry >= (unsigned)p.b.n_pages;
+        if (bad) kv_bad_index(p.b);
+        tma_load_page(dst + lane * bx.rows * pitch, map, feature, r.row, h, bad ? p.b.n_pages : r.entry, bar);
+    }
+}
+
+// 16 codes times the scale with byte s -> 16 bf16.  A code's bits, moved to a bf16's sign, lower exponent and upper mantissa bits, are
+// its value times 2^-120 (subnormal codes: subnormal bf16), so one exact product with 2^(s - 7) is all; scales above 2^7 take two.
+struct Turn {
+    __nv_bfloat162 f, g;
+};
+__device__ __forceinline__ Turn turn_of(uint32_t s, bool seen)             // a key's factors; 0 where no row sees it
+{
+    const uint32_t a = !seen ? 0u : s == kQ8NaN ? 0x7FC0u : (min(s, 134u) + 120u) << 7, b = s > 134u && s != kQ8NaN ? (s - 7u) << 7 : 0x3F80u;
+    const uint32_t f = a | a << 16, g = b | b << 16;
+    return Turn{*reinterpret_cast<const __nv_bfloat162 *>(&f), *reinterpret_cast<const __nv_bfloat162 *>(&g)};
+}
+__device__ __forceinline__ uint32_t turn_two(uint32_t bytes, const Turn &t, bool large)    // [0, code, 0, code]
+{
+    const uint32_t h = (bytes & 0x80008000u) | ((bytes >> 4) & 0x07F007F0u);
+    __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&h), t.f);
+    if (large) x = __hmul2(x, t.g);
+    return *reinterpret_cast<const uint32_t *>(&x);
 }
 
 // Query rows r0.. of a tile (those below `rows`; zeros beyond, and beyond the head's features) -> shared memory, as K-major
@@ -347,10 +395,10 @@ __device__ __forceinline__ Seen seen_by_all(const AttnParams &p, const Tile &t, 
     s.all_lo = p.window > 0 ? max(0, pre + i1 + 1 - p.window) : 0;
     return s;
 }
-template <int DB, bool JOINED, typename Tile>
+template <int DB, int LAY, typename Tile>
 __device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0, uint32_t vs, Suspects &sus, int lane)
 {
-    typedef TileAt<DB, JOINED> lay;
+    typedef TileAt<DB, LAY> lay;
     if ((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) {
         if (!a.differ || (j0 >= a.all_lo && j0 + kTcTile <= a.all_hi)) return;
     }
@@ -484,7 +532,7 @@ __device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
     }
 }
 
-template <int NB, bool JOINED>
+template <int NB, int LAY>
 __global__ void __launch_bounds__(512, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
@@ -572,15 +620,15 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB, JOINED>(p, map, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    fetch_tile<DB, LAY>(p, map, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
                     if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
                 }
             };
-            PageRef now = look_up(p, bx, cur.t, begin, cur.s, lane), next = now, then = now;
-            if (count > 1) next = look_up(p, bx, cur.t, begin + 1, cur.s, lane);
+            PageRef now = look_up<LAY>(p, bx, cur.t, begin, cur.s, cur.start, lane), next = now, then = now;
+            if (count > 1) next = look_up<LAY>(p, bx, cur.t, begin + 1, cur.s, cur.start, lane);
             fetch(now, &kmap);
             for (int n = 0; n < count; ++n) {
-                if (n + 2 < count) then = look_up(p, bx, cur.t, begin + n + 2, cur.s, lane);
+                if (n + 2 < count) then = look_up<LAY>(p, bx, cur.t, begin + n + 2, cur.s, cur.start, lane);
                 if (n + 1 < count) fetch(next, &kmap);
                 fetch(now, &vmap);
                 now = next;
@@ -594,7 +642,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
         uint32_t phase = 0, k = 0, unit = 0;
         bool ok = true;
         const uint32_t idesc_s = make_idesc(NR), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
-        typedef TileAt<DB, JOINED> lay;
+        typedef TileAt<DB, LAY> lay;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         while (ok && cur.at < piece_end) {
@@ -637,7 +685,7 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
                     wait(full_bar(stage), phase);
                     if (!ok) break;
                     const uint32_t vs = ring + stage * G::B::kStageBytes;
-                    clean_tile<DB, JOINED>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
+                    clean_tile<DB, LAY>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane);
                     if (y == 0) wait(p_ready(k & 1u), (k >> 1) & 1u);
                     if (!ok) break;
                     tc_fence_after();
@@ -943,12 +991,12 @@ kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_const
 
 // ======================================================================================================================
 // Many rows: row tiles of 128 on the lanes, NT of them a unit.
-template <int NB, int NT, bool JOINED>
-__global__ void __launch_bounds__(TcGeo<NB, NT>::kThreads, 1)
+template <int NB, int NT, int LAY>
+__global__ void __launch_bounds__(TcGeo<NB, NT, LAY>::kThreads, 1)
 kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                        const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
 {
-    typedef TcGeo<NB, NT> G;
+    typedef TcGeo<NB, NT, LAY> G;
     constexpr int DB = G::B::DB, HB = G::B::HB;
     constexpr int kRows = G::kRows;
     typedef RowTile<kRows, kTcTile> Tile;
@@ -970,6 +1018,8 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
     auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
     auto p_half = [&](int x) { return bars + 8 * (40 + x); };
+    auto raw_full = [&](int s) { return bars + 8 * (48 + s); };    // 8 bits
+    auto raw_empty = [&](int s) { return bars + 8 * (56 + s); };
     unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 42);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
@@ -977,8 +1027,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 
     if (tid == 0) {
         for (int s = 0; s < G::kStages; ++s) {
-            mbar_init(full_bar(s), 1);
+            mbar_init(full_bar(s), LAY == kCodes ? G::kTurners : 1);
             mbar_init(empty_bar(s), 1);
+        }
+        for (int s = 0; s < G::kRawStages; ++s) {
+            mbar_init(raw_full(s), 1);
+            mbar_init(raw_empty(s), G::kTurners);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
@@ -1023,17 +1077,20 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             auto fetch = [&](const PageRef &r, int which) {
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(LAY == kCodes ? raw_empty(stage) : empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    fetch_tile<DB, JOINED>(p, which ? &vmap : &kmap, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
-                    if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+                    if constexpr (LAY == kCodes)
+                        fetch_codes(p, which ? &vmap : &kmap, bx, r, cur.h, 128 * y, min(p.D, 128), base + G::kRaw + stage * G::kRawStage, raw_full(stage), lane);
+                    else
+                        fetch_tile<DB, LAY>(p, which ? &vmap : &kmap, bx, r, cur.h, 128 * y, ring + stage * G::B::kStageBytes, full_bar(stage), lane);
+                    if (++stage == (LAY == kCodes ? G::kRawStages : G::kStages)) { stage = 0; phase ^= 1u; }
                 }
             };
-            PageRef now = look_up(p, bx, t, begin, cur.s, lane), next = now, then = now;
-            if (count > 1) next = look_up(p, bx, t, begin + 1, cur.s, lane);
+            PageRef now = look_up<LAY>(p, bx, t, begin, cur.s, cur.start, lane), next = now, then = now;
+            if (count > 1) next = look_up<LAY>(p, bx, t, begin + 1, cur.s, cur.start, lane);
             fetch(now, 0);
             for (int n = 0; n < count; ++n) {              // the order in which the MMA warp takes them
-                if (n + 2 < count) then = look_up(p, bx, t, begin + n + 2, cur.s, lane);
+                if (n + 2 < count) then = look_up<LAY>(p, bx, t, begin + n + 2, cur.s, cur.start, lane);
                 if (NT == 2) fetch(now, 1);
                 if (n + 1 < count) fetch(next, 0);
                 if (NT == 1) fetch(now, 1);
@@ -1048,7 +1105,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         uint32_t phase = 0, k = 0, unit = 0;               // k: tiles done
         bool ok = true, two_parts = false;
         const uint32_t idesc_s = make_idesc(128), idesc_o = make_idesc(DB * 64) | (1u << 16);
-        typedef TileAt<DB, JOINED> lay;
+        typedef TileAt<DB, LAY> lay;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         auto mma_s = [&](int x, int row_tile, uint32_t ks, int y) {        // S buffer x (+)= Q_row_tile K^T, features 128 y ..
@@ -1087,11 +1144,11 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
-            two_parts = NT == 1 && t.rows <= kFewRows;
+            two_parts = NT == 1 && LAY != kPacked && t.rows <= kFewRows;
             Suspects &sus = suspects[unit & 1];
             if (lane == 0) sus.n = 0;
             __syncwarp();
-            auto clean = [&](int n, uint32_t vs) { clean_tile<DB, JOINED>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
+            auto clean = [&](int n, uint32_t vs) { clean_tile<DB, LAY>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
             auto at_stage = [&](int s) { return ring + s * G::B::kStageBytes; };
 #pragma unroll
             for (int x = 0; x < NT; ++x) wait(q_ready(x), unit & 1u);
@@ -1163,6 +1220,138 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             ++unit;
             leave_unit(p, cur, part.places, piece_end);
         }
+    } else if (LAY == kCodes && warp >= 2 + 8 * NT) {
+        // ================================ 8 bits: raw stages -> stages of the ring ================================
+        // A warp has KW keys of every tile and a lane 16 codes at a time: four lanes a key, 64 features, and of two features blocks
+        // neighbouring keys take different ones, so that loads and (swizzled) stores touch all banks once.
+        constexpr int KW = G::kTurners ? 128 / (G::kTurners ? G::kTurners : 1) : 128, KR = KW / 32;
+        const int w = warp - (2 + 8 * NT), kk = lane >> 2, q = lane & 3;
+        const int pitch = min(p.D, 128);
+        int stage = 0, raw = 0;
+        uint32_t phase = 0, raw_phase = 0;
+        bool ok = true;
+        struct Place {                                     // a lane's keys in the scales (-1: not seen, or no page)
+            int entry[KR], row[KR];
+        };
+        struct Bytes {
+            uint32_t k[KR], v[KR];
+            bool seen[KR];
+        };
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
+            auto peek = [&](int n, Place &a) {
+#pragma unroll
+                for (int i = 0; i < KR; ++i) {
+                    a.entry[i] = -1;
+                    a.row[i] = 0;
+                    if (n < count) {
+                        const int j = key_tile(t, begin + n) * kTcTile + w * KW + i * 32 + lane;
+                        if (j < t.hi && (j >= t.lo || j < t.s1)) {
+                            const int pg = fast_div(j, p.b.page);
+                            a.row[i] = j - pg * p.b.page.d;
+                            a.entry[i] = __ldg(table + pg);
+                        }
+                    }
+                }
+            };
+            auto fetch = [&](const Place &a, Bytes &b) {
+#pragma unroll
+                for (int i = 0; i < KR; ++i) {
+                    b.seen[i] = (unsigned)a.entry[i] < (unsigned)p.b.n_pages;
+                    const int64_t at = b.seen[i] ? ((int64_t)a.entry[i] * p.Hk + cur.h) * p.b.page.d + a.row[i] : 0;
+                    b.k[i] = __ldg(p.k_scale + at);
+                    b.v[i] = __ldg(p.v_scale + at);
+                }
+            };
+            auto turn = [&](const uint32_t (&bytes)[KR], const bool (&seen)[KR]) {
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < KR; ++i) any |= seen[i] && bytes[i] > 134u && bytes[i] != kQ8NaN;
+                const bool large = __any_sync(0xffffffffu, any);
+#pragma unroll 1
+                for (int y = 0; y < HB; ++y) {
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(raw_full(raw), raw_phase, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    if (!ok) return;
+                    const uint32_t from = base + G::kRaw + raw * G::kRawStage, to = ring + stage * G::B::kStageBytes;
+                    const int wide = p.D - 128 * y;        // features of this stage, less than 64 DB at a head's end
+#pragma unroll
+                    for (int i = 0; i < KR; ++i)
+#pragma unroll 1
+                        for (int e = 0; e < 4; ++e) {      // 8 keys
+                            const Turn f = turn_of(__shfl_sync(0xffffffffu, bytes[i], e * 8 + kk), __shfl_sync(0xffffffffu, (int)seen[i], e * 8 + kk));
+                            const int key = w * KW + i * 32 + e * 8 + kk;
+                            const uint32_t row = to + (key >> 3) * 1024 + (key & 7) * 128;
+                            uint4 c[DB];
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) {
+                                const int ch = q + (DB == 2 ? 4 * (d ^ (kk & 1)) : 0);
+                                c[d] = make_uint4(0, 0, 0, 0);
+                                if (ch * 16 < wide)
+                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[d].x), "=r"(c[d].y), "=r"(c[d].z), "=r"(c[d].w)
+                                                 : "r"(from + key * pitch + ch * 16) : "memory");
+                            }
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) {
+                                const int ch = q + (DB == 2 ? 4 * (d ^ (kk & 1)) : 0);
+                                const uint32_t x[4] = {c[d].x, c[d].y, c[d].z, c[d].w};
+                                uint32_t o[8];
+                                if (!large) {
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) {
+                                        o[2 * z] = turn_two(__byte_perm(x[z], 0, 0x1404), f, false);
+                                        o[2 * z + 1] = turn_two(__byte_perm(x[z], 0, 0x3424), f, false);
+                                    }
+                                } else {
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) {
+                                        o[2 * z] = turn_two(__byte_perm(x[z], 0, 0x1404), f, true);
+                                        o[2 * z + 1] = turn_two(__byte_perm(x[z], 0, 0x3424), f, true);
+                                    }
+                                }
+                                // (beyond the head's features: zeros, also in a row of NaN)
+                                if (ch * 16 >= wide)
+#pragma unroll
+                                    for (int z = 0; z < 8; ++z) o[z] = 0u;
+                                const uint32_t at = row + (ch >> 2) * TileAt<DB, LAY>::block, sw = key & 7;
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * q) ^ sw) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * q + 1) ^ sw) << 4)), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+                            }
+                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(full_bar(stage));
+                        mbar_arrive(raw_empty(raw));
+                    }
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1u; }
+                    if (++raw == G::kRawStages) { raw = 0; raw_phase ^= 1u; }
+                }
+            };
+            // scales a tile ahead of their use, their pages another tile
+            Place at;
+            Bytes now, next, then;
+            peek(0, at);
+            fetch(at, now);
+            peek(1, at);
+            fetch(at, next);
+            peek(2, at);
+            turn(now.k, now.seen);
+            for (int n = 0; n < count && ok; ++n) {        // the order in which the MMA warp takes them
+                fetch(at, then);
+                peek(n + 3, at);
+                if (NT == 2) turn(now.v, now.seen);
+                if (n + 1 < count) turn(next.k, next.seen);
+                if (NT == 1) turn(now.v, now.seen);
+                now = next;
+                next = then;
+            }
+            leave_unit(p, cur, part.places, piece_end);
+        }
     } else {
         // ================================ softmax: two threads per row ================================
         const int group = (warp - 2) >> 2, x = group >> 1, half = group & 1;       // row tile, half of its keys
@@ -1184,10 +1373,11 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
-            const bool two_parts = NT == 1 && t.rows <= kFewRows;
+            const bool two_parts = NT == 1 && LAY != kPacked && t.rows <= kFewRows;
             // ---- queries -> shared memory (the S products of the unit before are done: its last S has been read)
             load_queries<NB, 128, 256>(p, cur.start, cur.h, t.r0 + x * 128, rows, sq + x * G::kQTile, half * 128 + row);
             mbar_arrive(q_ready(x));
+            float prior = 0.f;                             // log-sum-exp to join with (both threads of the row, before either writes)
             // ---- what the row sees; what all rows of the warp see
             const bool live = row < rows, warp_live = wq * 32 < rows;
             int hi_r = 0, lo_r = 0;
@@ -1195,6 +1385,10 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 const int pos = cur.pre + fast_div(t.r0 + x * 128 + row, p.gdiv);
                 hi_r = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
                 lo_r = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+                if (LAY == kPacked && p.join) {
+                    const int rr = t.r0 + x * 128 + row, tok = fast_div(rr, p.gdiv);
+                    prior = p.lse[(int64_t)(cur.start + tok) * p.H + cur.h * p.g + rr - tok * p.g];
+                }
             }
             int all_hi = 0, all_lo = 0;
             if (warp_live) {
@@ -1337,7 +1531,23 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 const int f0 = half * (NB * 32);           // this half's features
                 __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D + f0;
                 float *lse = p.lse && live && half == 0 ? p.lse + (int64_t)(cur.start + tok) * p.H + head : nullptr;
-                auto put32 = [&](int f, const float *o, float inv) {       // 32 features from f0 + f
+                auto put32 = [&](int f, float *o, float inv, float was) {  // 32 features from f0 + f; `was`: weight of the other pass's row
+                    if (LAY == kPacked && p.join) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] *= inv;
+                        inv = 1.f;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            if (live && was != 0.f && f0 + f + i < p.D) {
+                                const uint4 w = *reinterpret_cast<const uint4 *>(dst + f + i);
+                                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) {
+                                    o[i + 2 * y] = fmaf(__uint_as_float(u[y] << 16), was, o[i + 2 * y]);
+                                    o[i + 2 * y + 1] = fmaf(__uint_as_float(u[y] & 0xFFFF0000u), was, o[i + 2 * y + 1]);
+                                }
+                            }
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; i += 8)
                         if (live && f0 + f + i < p.D)
@@ -1347,9 +1557,15 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 };
                 const int slot = (2 * (int)blockIdx.x + (begin == 0 ? 1 : 0)) * NT + x;
                 float4 *parts = reinterpret_cast<float4 *>(p.part.o);       // slot: [NB * 16][128 rows] float4
-                if (whole_unit && lse) *lse = log_sum(m, L);
+                float inv = inverse(L), was = 0.f, total = log_sum(m, L);
+                if (LAY == kPacked && p.join) {
+                    const JoinWith with = join_with(m, L, prior);
+                    inv = with.a;
+                    was = with.b;
+                    total = with.lse;
+                }
+                if (whole_unit && lse) *lse = total;
                 if (!whole_unit && live && half == 0) __stcg(p.part.ml + (size_t)slot * 128 + row, make_float2(m, L));
-                const float inv = inverse(L);
 #pragma unroll 1
                 for (int f = 0; f < NB; ++f) {
                     float o[32];
@@ -1361,7 +1577,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                         for (int i = 0; i < 32; ++i) o[i] = __int_as_float(0x7FC00000);
                     }
                     if (whole_unit) {
-                        put32(32 * f, o, inv);
+                        put32(32 * f, o, inv, was);
                     } else if (live) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
@@ -1410,8 +1626,14 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                                         }
                                     }
                             }
-                            put32(32 * f, o, inverse(S));
-                            if (f == 0 && lse) *lse = log_sum(M, S);
+                            if (LAY == kPacked && p.join) {
+                                const JoinWith with = join_with(M, S, prior);
+                                put32(32 * f, o, with.a, with.b);
+                                if (f == 0 && lse) *lse = with.lse;
+                            } else {
+                                put32(32 * f, o, inverse(S), 0.f);
+                                if (f == 0 && lse) *lse = log_sum(M, S);
+                            }
                         }
                     }
                     if (half == 0 && lane == 0 && sh_last[x][wq]) *counter = 0;
@@ -1441,31 +1663,31 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     }
 }
 
-template <int NB, int NT, bool JOINED>
+template <int NB, int NT, int LAY>
 cudaError_t tc_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_tc_kernel<NB, NT, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<NB, NT>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_tc_kernel<NB, NT, LAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcGeo<NB, NT, LAY>::kSmem);
 }
-template <int NB, int NT, bool JOINED>
+template <int NB, int NT, int LAY>
 cudaError_t tc_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, const PageBoxes &bx, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_tc_kernel<NB, NT, JOINED>, dim3(sms), dim3(TcGeo<NB, NT>::kThreads), TcGeo<NB, NT>::kSmem, st,
+    cudaError_t e = launch_k(kv_attention_tc_kernel<NB, NT, LAY>, dim3(sms), dim3(TcGeo<NB, NT, LAY>::kThreads), TcGeo<NB, NT, LAY>::kSmem, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, bx);
     c->launches = 1;
     return note_err(c, e, "kv_attention_tc_kernel");
 }
 
-template <int NB, bool JOINED>
+template <int NB, int LAY>
 cudaError_t few_prepare()
 {
-    return cudaFuncSetAttribute(kv_attention_few_kernel<NB, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<NB>::kSmem);
+    return cudaFuncSetAttribute(kv_attention_few_kernel<NB, LAY>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewGeo<NB>::kSmem);
 }
-template <int NB, bool JOINED>
+template <int NB, int LAY>
 cudaError_t few_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, const PageBoxes &bx, cudaStream_t st)
 {
     const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
-    cudaError_t e = launch_k(kv_attention_few_kernel<NB, JOINED>, dim3(sms), dim3(FewGeo<NB>::kThreads), FewGeo<NB>::kSmem, st,
+    cudaError_t e = launch_k(kv_attention_few_kernel<NB, LAY>, dim3(sms), dim3(FewGeo<NB>::kThreads), FewGeo<NB>::kSmem, st,
                              !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, bx);
     c->launches = 1;
     return note_err(c, e, "kv_attention_few_kernel");
@@ -1538,26 +1760,40 @@ cudaError_t kv_tc_attach(Ctx *c)
     cudaDriverEntryPointQueryResult q;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
     if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
-    cudaError_t all[] = {few_prepare<1, false>(), few_prepare<2, false>(), few_prepare<4, false>(), few_prepare<2, true>(), few_prepare<4, true>(),
-                         tc_prepare<1, 1, false>(), tc_prepare<2, 1, false>(), tc_prepare<4, 1, false>(), tc_prepare<2, 1, true>(),
-                         tc_prepare<4, 1, true>(), tc_prepare<1, 2, false>(), tc_prepare<2, 2, false>()};
+    cudaError_t all[] = {few_prepare<1, kApart>(), few_prepare<2, kApart>(), few_prepare<4, kApart>(), few_prepare<2, kJoined>(), few_prepare<4, kJoined>(),
+                         tc_prepare<1, 1, kApart>(), tc_prepare<2, 1, kApart>(), tc_prepare<4, 1, kApart>(), tc_prepare<2, 1, kJoined>(),
+                         tc_prepare<4, 1, kJoined>(), tc_prepare<1, 2, kApart>(), tc_prepare<2, 2, kApart>(),
+                         tc_prepare<1, 1, kPacked>(), tc_prepare<2, 1, kPacked>(), tc_prepare<4, 1, kPacked>(), tc_prepare<1, 2, kPacked>(),
+                         tc_prepare<2, 2, kPacked>(),
+                         tc_prepare<1, 1, kCodes>(), tc_prepare<2, 1, kCodes>(), tc_prepare<4, 1, kCodes>(), tc_prepare<1, 2, kCodes>(),
+                         tc_prepare<2, 2, kCodes>()};
     for (cudaError_t one : all)
         if (one != cudaSuccess) return one;
     c->kv_encode = fn;
     return cudaSuccess;
 }
 
-cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
+static void place_parts(Ctx *c, AttnParams &p)
 {
     const size_t slots = (size_t)2 * kKvMaxSm * 2;
     p.part.counters = (int32_t *)c->kv_ws;
     p.part.ml = (float2 *)(c->kv_ws + kKvCounterBytes);
     p.part.o = (float *)(c->kv_ws + kKvCounterBytes + slots * 128 * 8);
+}
+// as many units of two row tiles as SMs, as far as the host knows
+static bool units_for_all(const Ctx *c, const AttnParams &p, const mrp_kv_batch &batch)
+{
+    return (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
+}
+
+cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
+{
+    place_parts(c, p);
     const long long rows = (long long)batch.max_new * p.g;
     const bool narrow = c->kv.head_dim <= 64, wide = c->kv.head_dim > 128;
     // Two row tiles share the stream of K and V where there are units for all SMs; with fewer the smaller units end sooner (512
     // tokens alone 28 against 27 us, 1024 44 against 36, 2048 74 against 78; 24 blocks of 33 behind 3000 102 against 120).
-    const bool two = rows > 128 && !wide && (long long)batch.n_seqs * p.Hk + (long long)batch.n_tokens * p.H / 256 > c->sm_count;
+    const bool two = rows > 128 && !wide && units_for_all(c, p, batch);
     CUtensorMap km, vm;
     PageBoxes bx;
     auto maps = [&](bool join) {
@@ -1571,9 +1807,9 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     if (e != cudaSuccess) return e;
     auto few = [&]() {
         p.lead = 2;                        // (24 single tokens 63, 61, 61 us at 1, 2, 3; 128 short caches 89, 86, 85)
-        if (narrow) return few_launch<1, false>(c, p, km, vm, bx, st);
-        if (bx.groups) return wide ? few_launch<4, true>(c, p, km, vm, bx, st) : few_launch<2, true>(c, p, km, vm, bx, st);
-        return wide ? few_launch<4, false>(c, p, km, vm, bx, st) : few_launch<2, false>(c, p, km, vm, bx, st);
+        if (narrow) return few_launch<1, kApart>(c, p, km, vm, bx, st);
+        if (bx.groups) return wide ? few_launch<4, kJoined>(c, p, km, vm, bx, st) : few_launch<2, kJoined>(c, p, km, vm, bx, st);
+        return wide ? few_launch<4, kApart>(c, p, km, vm, bx, st) : few_launch<2, kApart>(c, p, km, vm, bx, st);
     };
     // Rows a unit: 16, 128 or 256.  24 sequences of 200 to 6000 cached positions, 8 key heads of 128: 16 rows 61 us on the
     // transposed kernel, 75 on the 128-row one (one token of one sequence: 12.6 against 24); a transposed one for 32 or 64 rows
@@ -1596,12 +1832,90 @@ cudaError_t launch_paged_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch 
     if (two && bx.groups && (e = maps(false)) != cudaSuccess) return e;
     // (what a unit costs besides its tiles, in tiles: three 1000- to 2000-token prompts 235, 181, 159, 153 us at 1, 2, 3, 4)
     p.lead = two ? 4 : 3;
-    if (two) e = narrow ? tc_launch<1, 2, false>(c, p, km, vm, bx, st) : tc_launch<2, 2, false>(c, p, km, vm, bx, st);
-    else if (narrow) e = tc_launch<1, 1, false>(c, p, km, vm, bx, st);
-    else if (bx.groups) e = wide ? tc_launch<4, 1, true>(c, p, km, vm, bx, st) : tc_launch<2, 1, true>(c, p, km, vm, bx, st);
-    else e = wide ? tc_launch<4, 1, false>(c, p, km, vm, bx, st) : tc_launch<2, 1, false>(c, p, km, vm, bx, st);
+    if (two) e = narrow ? tc_launch<1, 2, kApart>(c, p, km, vm, bx, st) : tc_launch<2, 2, kApart>(c, p, km, vm, bx, st);
+    else if (narrow) e = tc_launch<1, 1, kApart>(c, p, km, vm, bx, st);
+    else if (bx.groups) e = wide ? tc_launch<4, 1, kJoined>(c, p, km, vm, bx, st) : tc_launch<2, 1, kJoined>(c, p, km, vm, bx, st);
+    else e = wide ? tc_launch<4, 1, kApart>(c, p, km, vm, bx, st) : tc_launch<2, 1, kApart>(c, p, km, vm, bx, st);
     c->launches += launches;
     return e;
+}
+
+// ---- pages of 8 bits, rows beside the queries ---------------------------------------------------------------------------
+bool kv_tc_takes_q8(const mrp_config &cfg, const mrp_kv_config &kv)
+{
+    // (a box is whole 16-byte runs of a row's codes, strides are multiples of 16 bytes)
+    return kv_tc_any(cfg, kv) && kv.n_pages > 0 && tc_box_rows(kv.page_size) > 0 && kv.head_dim % 16 == 0 && kv.page_stride % 16 == 0 &&
+           kv.page_stride < (1ll << 40) && (long long)kv.page_size * kv.head_dim < (1ll << 40);
+}
+
+cudaError_t launch_paged_attention_q8_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
+{
+    place_parts(c, p);
+    const mrp_kv_config &kv = c->kv;
+    const long long rows = (long long)batch.max_new * p.g;
+    const bool narrow = kv.head_dim <= 64, wide = kv.head_dim > 128;
+    const bool two = rows > 128 && !wide && units_for_all(c, p, batch);
+    PageBoxes bx = {};
+    bx.rows = tc_box_rows(kv.page_size);
+    CUtensorMap km, vm;
+    const cuuint64_t D = (cuuint64_t)kv.head_dim;
+    const cuuint64_t dims[4] = {D, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
+    const cuuint64_t strides[3] = {D, (cuuint64_t)kv.page_size * D, (cuuint64_t)kv.page_stride};
+    const cuuint32_t box[4] = {(cuuint32_t)(kv.head_dim < 128 ? kv.head_dim : 128), (cuuint32_t)bx.rows, 1, 1}, es[4] = {1, 1, 1, 1};
+    const void *pools[2] = {p.k, p.v};
+    for (int i = 0; i < 2; ++i)
+        if (((EncodeTiledFn)c->kv_encode)(i ? &vm : &km, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pools[i]), dims, strides, box, es,
+                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    cudaError_t e;
+    int launches = 0;
+    auto one = [&]() {
+        p.lead = 3;
+        return narrow ? tc_launch<1, 1, kCodes>(c, p, km, vm, bx, st) : wide ? tc_launch<4, 1, kCodes>(c, p, km, vm, bx, st) : tc_launch<2, 1, kCodes>(c, p, km, vm, bx, st);
+    };
+    if (two) {
+        p.rows_upto = kFewRows;
+        if ((e = one()) != cudaSuccess) return e;
+        launches = c->launches;
+        p.rows_above = kFewRows;
+        p.rows_upto = INT_MAX;
+        p.lead = 4;
+        e = narrow ? tc_launch<1, 2, kCodes>(c, p, km, vm, bx, st) : tc_launch<2, 2, kCodes>(c, p, km, vm, bx, st);
+    } else {
+        e = one();
+    }
+    c->launches += launches;
+    return e;
+}
+
+bool kv_tc_takes_rows(const mrp_config &cfg, const mrp_kv_config &kv, const mrp_packed_kv &rows)
+{
+    return kv_tc_any(cfg, kv) && rows.k_stride < (1ll << 39) && rows.v_stride < (1ll << 39);
+}
+
+cudaError_t launch_packed_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st)
+{
+    place_parts(c, p);
+    const bool narrow = p.D <= 64, wide = p.D > 128;
+    const bool two = (long long)batch.max_new * p.g > 128 && !wide && units_for_all(c, p, batch);
+    PageBoxes bx = {};
+    bx.rows = kTcTile;
+    CUtensorMap km, vm;
+    const void *ptr[2] = {p.k, p.v};
+    const int64_t stride[2] = {p.k_stride, p.v_stride};
+    for (int i = 0; i < 2; ++i) {
+        const cuuint64_t dims[4] = {(cuuint64_t)p.D, (cuuint64_t)batch.n_tokens, (cuuint64_t)p.Hk, 1};
+        const cuuint64_t strides[3] = {(cuuint64_t)stride[i] * 2, (cuuint64_t)p.D * 2, (cuuint64_t)stride[i] * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)bx.rows, 1, 1}, es[4] = {1, 1, 1, 1};
+        if (((EncodeTiledFn)c->kv_encode)(i ? &vm : &km, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(ptr[i]), dims, strides, box, es,
+                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    }
+    p.lead = two ? 4 : 3;
+    if (two) return narrow ? tc_launch<1, 2, kPacked>(c, p, km, vm, bx, st) : tc_launch<2, 2, kPacked>(c, p, km, vm, bx, st);
+    return narrow ? tc_launch<1, 1, kPacked>(c, p, km, vm, bx, st) : wide ? tc_launch<4, 1, kPacked>(c, p, km, vm, bx, st) : tc_launch<2, 1, kPacked>(c, p, km, vm, bx, st);
 }
 
 }  // namespace mrp
