@@ -1,0 +1,658 @@
+// Attention over pages of 8 bits, up to 16 query rows a sequence and key head: kv_attention_few_kernel (kv_attention_tc.cu, whose
+// mathematics, roles and units' ends these are) with half the bytes to read, which leaves half the time for everything else.
+//
+//   S^T = K Q^T on the codes as they lie: K's tile is the A operand in e4m3 (kind::f8f6f4), and a query row is two e4m3 rows of B,
+//   q = 2^E (hi + lo / 16): eight significant bits, which is all of a bf16 (elements below 2^-13 of their row's largest: to 2^-21 of
+//   that).  The thread that has a key takes its score times 2^E of the row times the key's scale.
+//   O^T += V^T P^T in bf16: four warps turn the codes of V times their scales into bf16 (exact) in two stages of their own.  In 8 bits
+//   P would need three parts or more, and lose the tail of a long cache, whose many small probabilities lie below what e4m3 holds.
+//   Turning K too would move 3 bytes more through shared memory for each of its codes, which then bounds the kernel instead of
+//   memory: TMA, warps and MMAs move 88 of 128 bytes a cycle at the memory's rate as it is.
+#include "kv_tile.cuh"
+
+namespace mrp {
+namespace {
+
+// A head is HB blocks of 128 features; a unit has up to ROWS query rows, 8 or 16.
+template <int HB, int ROWS> struct FewQ8Geo {
+    static constexpr int NR = ROWS;
+    static constexpr int kCols = 2 * NR;                   // columns of S (hi, lo of Q), of P (hi, lo) and of an accumulator
+    static constexpr int kKStages = 3, kRawStages = HB == 1 ? 4 : 3;       // of 128 keys, 128 codes
+    static constexpr int kRawAt = kKStages * 16384;
+    static constexpr int kVAt = kRawAt + kRawStages * 16384;               // two stages of bf16 V
+    static constexpr int kP = 128 * 128;                   // P of a warpgroup: 128 keys, rows of 128 bytes
+    static constexpr int kQ = HB * kCols * 128;            // queries of a unit, two of them
+    static constexpr int kPAt = kVAt + 2 * 32768, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
+    static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
+    static constexpr int kTmem = HB == 2 ? 512 : 256;      // of which 2 kCols + 4 HB kCols are used
+    static constexpr int kThreads = 640;
+    static constexpr int kWide = HB * 128;                 // features of a row of partial results
+};
+
+// The unit's query rows as two e4m3 parts each (row r: hi, row NR + r: lo), K-major blocks of 128 features, and what their scores
+// are multiplied by: 2^E scale log2(e), NaN for a row that is not finite.  64 threads, 64 / NR a row.
+template <int HB, int NR>
+__device__ __forceinline__ void load_query_parts(const AttnParams &p, int start, int h, int r0, int rows, uint32_t sq, float *factor, int tid)
+{
+    constexpr int kParts = 64 / NR, kChunks = 16 * HB / kParts;            // threads a row; runs of 8 features a thread
+    const int r = tid / kParts, part = tid % kParts;
+    const int rr = r0 + min(r, rows - 1), tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
+    const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)(start + tok) * p.q_stride + (int64_t)(h * p.g + hg) * p.D;
+    uint4 x[kChunks];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = part + kParts * i;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (r < rows && c * 8 < p.D) x[i] = __ldg(reinterpret_cast<const uint4 *>(src) + c);
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) top = max(top, max((w[y] << 16) & 0x7FFFFFFFu, w[y] & 0x7FFF0000u));
+    }
+#pragma unroll
+    for (int w = 1; w < kParts; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const uint32_t s = q8_scale(top);
+    const bool fine = s != kQ8NaN;
+    const float inv = q8_inverse(fine ? s : 127u);
+    if (part == 0) factor[r] = q8_factor(s) * p.scale_log2;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = part + kParts * i;
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            float f[4] = {__uint_as_float(w[2 * y] << 16), __uint_as_float(w[2 * y] & 0xFFFF0000u), __uint_as_float(w[2 * y + 1] << 16),
+                          __uint_as_float(w[2 * y + 1] & 0xFFFF0000u)};
+#pragma unroll
+            for (int z = 0; z < 4; ++z) f[z] = fine ? f[z] * inv : 0.f;
+            hi[y] = q8_codes(f[0], f[1], f[2], f[3]);
+            const float2 a = q8_values(hi[y] & 0xFFFFu, 1.f), b = q8_values(hi[y] >> 16, 1.f);
+            lo[y] = q8_codes((f[0] - a.x) * 16.f, (f[1] - a.y) * 16.f, (f[2] - b.x) * 16.f, (f[3] - b.y) * 16.f);
+        }
+        // features 8 c .. of a block of 128: half of a 16-byte chunk, swizzled by the row (rows r and NR + r alike)
+        const int cb = c & 15;
+        const uint32_t at = sq + (c >> 4) * (2 * NR * 128) + r * 128 + ((((cb >> 1) ^ (r & 7)) << 4) | ((cb & 1) << 3));
+        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(hi[0]), "r"(hi[1]) : "memory");
+        asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at + NR * 128), "r"(lo[0]), "r"(lo[1]) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+template <int HB, int NR>
+__global__ void __launch_bounds__(640, 1)
+kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
+                        const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
+{
+    typedef FewQ8Geo<HB, NR> G;
+    constexpr int DB = 2;
+    typedef RowTile<NR, kTcTile> Tile;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ long long sh_find[G::kThreads / 32 + 2];
+    __shared__ Suspects suspects[2];
+    __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
+    __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR], sh_rf[2][NR];   // maximum in use (unit, warpgroup), factor to it; a unit's rows' factors
+    __shared__ float sh_wm[2][4][NR], sh_wl[2][2][4][NR];  // row maxima and (of a unit) sums of the warps
+    __shared__ float sh_f[2][NR];                          // the unit's end: factors of the accumulators,
+    __shared__ int64_t sh_out[NR];                         //   where the rows go
+    __shared__ int sh_last;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bars = base + G::kBars;
+    auto k_at = [&](int s) { return base + s * 16384; };           // codes of K: operand stages
+    auto r_at = [&](int s) { return base + G::kRawAt + s * 16384; };       // codes of V, raw
+    auto v_at = [&](int s) { return base + G::kVAt + s * 32768; };         // V in bf16
+    auto k_full = [&](int s) { return bars + 8 * s; };
+    auto k_empty = [&](int s) { return bars + 8 * (4 + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (8 + s); };
+    auto raw_empty = [&](int s) { return bars + 8 * (12 + s); };
+    auto v_full = [&](int s) { return bars + 8 * (16 + s); };
+    auto v_empty = [&](int s) { return bars + 8 * (18 + s); };
+    auto s_full = [&](int x) { return bars + 8 * (32 + x); };
+    auto p_ready = [&](int x) { return bars + 8 * (34 + x); };
+    auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
+    auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
+    auto unit_end = [&](int x) { return bars + 8 * (40 + x); };    // the unit is written: everything of it may be reused
+    auto acc_full = [&](int x) { return bars + 8 * (42 + x); };    // the unit's sums, maxima and accumulators are there
+    unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 44);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    const WaitStatus ws = {p.b.status, p.b.user_status};
+
+    if (tid == 0) {
+        for (int s = 0; s < G::kKStages; ++s) {
+            mbar_init(k_full(s), 1);
+            mbar_init(k_empty(s), 1);
+        }
+        for (int s = 0; s < G::kRawStages; ++s) {
+            mbar_init(raw_full(s), 1);
+            mbar_init(raw_empty(s), 4);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(v_full(x), 4);
+            mbar_init(v_empty(x), 1);
+            mbar_init(s_full(x), 1);
+            mbar_init(p_ready(x), 4);
+            mbar_init(pv_done(x), 1);
+            mbar_init(q_ready(x), 64);
+            mbar_init(unit_end(x), 4);
+            mbar_init(acc_full(x), 8);
+        }
+        *abort_flag = 0;
+        prefetch_tmap(&kmap);
+        prefetch_tmap(&vmap);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"((uint32_t)G::kTmem) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators of two units
+    auto s_at = [&](int x) { return tmem + x * G::kCols; };        // (columns: the upper parts of the rows, the lower ones)
+    auto o_at = [&](int u, int x) { return tmem + 2 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
+    pdl_wait();
+    pdl_trigger();
+
+    Cursor<NR, kTcTile> cur;
+    long long per;
+    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
+                                            : find_piece<NR, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    if (len == 0) cur.at = 0;
+    const long long piece_end = len > 0 ? cur.at + len : 0;
+
+    if (warp == 0) {
+        // ================================ K and V tiles ================================
+        int ks = 0, rs = 0;
+        uint32_t k_phase = 0, r_phase = 0;
+        bool ok = true;
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+            auto fetch_k = [&](const PageRef &r) {
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(k_empty(ks), k_phase ^ 1u);
+                    if (!ok) return;
+                    fetch_codes(p, &kmap, bx, r, cur.h, 128 * y, 128, k_at(ks), k_full(ks), lane);
+                    if (++ks == G::kKStages) { ks = 0; k_phase ^= 1u; }
+                }
+            };
+            auto fetch_v = [&](const PageRef &r) {
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(raw_empty(rs), r_phase ^ 1u);
+                    if (!ok) return;
+                    fetch_codes(p, &vmap, bx, r, cur.h, 128 * y, min(p.D, 128), r_at(rs), raw_full(rs), lane);
+                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
+                }
+            };
+            PageRef now = look_up<kCodes>(p, bx, cur.t, begin, cur.s, cur.start, lane), next = now, then = now;
+            if (count > 1) next = look_up<kCodes>(p, bx, cur.t, begin + 1, cur.s, cur.start, lane);
+            fetch_k(now);
+            for (int n = 0; n < count; ++n) {
+                if (n + 2 < count) then = look_up<kCodes>(p, bx, cur.t, begin + n + 2, cur.s, cur.start, lane);
+                if (n + 1 < count) fetch_k(next);
+                fetch_v(now);
+                now = next;
+                next = then;
+            }
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else if (warp == 1) {
+        // ================================ MMAs ================================
+        int ks = 0, vs = 0;
+        uint32_t k_phase = 0, v_phase = 0, k = 0, unit = 0;
+        bool ok = true;
+        const uint32_t idesc_s = make_idesc_e4m3(G::kCols), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
+        typedef TileAt<DB, kApart> lay;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const uint32_t sq = base + G::kQAt + (unit & 1u) * G::kQ;
+            wait(q_ready(unit & 1u), (unit >> 1) & 1u);
+            if (!ok) break;
+            Suspects &sus = suspects[unit & 1];            // (the unit before the last is written: see the query warps)
+            if (lane == 0) sus.n = 0;
+            __syncwarp();
+            auto scores = [&](uint32_t kk) {               // S^T of tile kk from the stages at hand
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(k_full(ks), k_phase);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint32_t a = k_at(ks), q = sq + y * (G::kCols * 128);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)        // 32 features
+                            umma_f8(s_at(kk & 1u), make_smem_desc(a + c * 32), make_smem_desc(q + c * 32), idesc_s, y + c > 0);
+                        if (y + 1 == HB) umma_commit(s_full(kk & 1u));
+                        umma_commit(k_empty(ks));
+                    }
+                    __syncwarp();
+                    if (++ks == G::kKStages) { ks = 0; k_phase ^= 1u; }
+                }
+            };
+            scores(k);
+            for (int n = 0; n < count && ok; ++n, ++k) {
+                if (n + 1 < count) scores(k + 1);
+                const uint32_t ps = base + G::kPAt + (k & 1u) * G::kP;
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(v_full(vs), v_phase);
+                    if (!ok) break;
+                    const uint32_t va = v_at(vs);
+                    clean_tile<DB, kApart>(t, all, key_tile(t, begin + n) * kTcTile, va, sus, lane);
+                    if (y == 0) wait(p_ready(k & 1u), (k >> 1) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            umma_bf16(o_at(unit & 1u, k & 1u) + y * G::kCols, mn_desc(va + c * 2 * lay::group, lay::block, lay::group), mn_desc(ps + c * 2048, 0, 1024), idesc_o,
+                                      n >= 2 || c > 0);
+                        if (y + 1 == HB) umma_commit(pv_done(k & 1u));
+                        umma_commit(v_empty(vs));
+                    }
+                    __syncwarp();
+                    if ((vs ^= 1) == 0) v_phase ^= 1u;
+                }
+            }
+            ++unit;
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else if (warp < 4) {
+        // ================================ queries, a unit ahead ================================
+        uint32_t unit = 0;
+        bool ok = true;
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            if (part.count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const int u = unit & 1;
+            if (unit >= 2) {
+                ok = __all_sync(0xffffffffu, mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws));
+                if (!ok) break;
+            }
+            load_query_parts<HB, NR>(p, cur.start, cur.h, t.r0, t.rows, base + G::kQAt + u * G::kQ, sh_rf[u], tid - 64);
+            for (int r = tid - 64; r < NR; r += 64) {
+                const int pos = cur.pre + fast_div(t.r0 + min(r, t.rows - 1), p.gdiv);
+                sh_hi[u][r] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
+                sh_lo[u][r] = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            }
+            mbar_arrive(q_ready(u));
+            ++unit;
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else if (warp < 12) {
+        // ================================ softmax: a thread per key, two warpgroups in turn ================================
+        const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
+        const int bar_id = 1 + x;
+        const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+        const uint32_t s_tm = s_at(x) + lanes;
+        const uint32_t p_row = base + G::kPAt + x * G::kP + wt * 128;
+        uint32_t k0 = 0, unit = 0;
+        bool ok = true;
+        float l[NR];
+        while (cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const int u = unit & 1;
+            const uint32_t o_tm = o_at(u, x) + lanes;
+            float *sh_m = sh_ms[u][x];
+            if (unit >= 2) ok = mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws);
+            if (wg_any(bar_id, !ok)) break;
+            if (wt < NR) sh_m[wt] = kNone;
+            wg_sync(bar_id);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) l[r] = 0.f;
+            const int n0 = (int)((k0 & 1u) ^ (uint32_t)x); // this warpgroup's tiles: n0, n0 + 2, ..
+            // the key's scale, one of the warpgroup's tiles ahead; its page, two
+            auto find = [&](int n) { return find_keys<1>(p, t, n < count, begin + n, cur.s, wq * 32, lane); };
+            uint32_t scale_now[1], scale_next[1];
+            KeyPlaces<1> place = find(n0);
+            load_scales(p, p.k_scale, place, cur.h, scale_now);
+            place = find(n0 + 2);
+            for (int n = n0; n < count; n += 2) {
+                const uint32_t k = k0 + n;
+                load_scales(p, p.k_scale, place, cur.h, scale_next);
+                place = find(n + 4);
+                ok = mbar_wait(s_full(x), (k >> 1) & 1u, abort_flag, ws);
+                __syncwarp();
+                tc_fence_after();
+                const float kf = q8_factor(scale_now[0] & 255u);           // (a key that no row sees: any)
+                scale_now[0] = scale_next[0];
+                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + wt;
+                const bool whole = j0 >= all.all_lo && j0 + kTcTile <= all.all_hi;
+                uint32_t seen = 0;                         // by which rows, where not by all
+                if (!whole) {
+                    if (all.differ) {
+#pragma unroll 1
+                        for (int r = 0; r < NR; ++r) seen |= (uint32_t)sees(j, sh_hi[u][r], sh_lo[u][r], p.sinks) << r;
+                    } else {
+                        seen = sees(j, all.all_hi, all.all_lo, p.sinks) ? ~0u : 0u;
+                    }
+                }
+                float s[NR];
+                auto load = [&]() {                        // the key's scores, both parts of the queries
+                    float v[2 * NR];
+                    tmem_ld_n<2 * NR>(s_tm, v);
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) s[i] = fmaf(v[NR + i], 0.0625f, v[i]);
+                };
+                auto hide = [&]() {                        // what a row does not see: -inf
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < NR; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
+                    }
+                };
+                auto against_max = [&]() {                 // exponents; rows and keys have their powers of two
+#pragma unroll
+                    for (int i = 0; i < NR; i += 4) {
+                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[i]), f = *reinterpret_cast<const float4 *>(&sh_rf[u][i]);
+                        s[i] = fmaf(s[i], f.x * kf, -m.x); s[i + 1] = fmaf(s[i + 1], f.y * kf, -m.y);
+                        s[i + 2] = fmaf(s[i + 2], f.z * kf, -m.z); s[i + 3] = fmaf(s[i + 3], f.w * kf, -m.w);
+                    }
+                    hide();
+                };
+                bool grown = true;                         // (the warpgroup's first tile of the unit sets the maxima)
+                if (n >= 2) {
+                    load();
+                    against_max();
+                    float top = s[0];
+#pragma unroll
+                    for (int i = 1; i < NR; ++i) top = fmaxf(top, s[i]);
+                    grown = wg_any(bar_id, top > 8.f || !ok);
+                }
+                if (grown) {
+                    // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
+                    if (wg_any(bar_id, !ok)) { ok = false; break; }
+                    load();
+#pragma unroll
+                    for (int i = 0; i < NR; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(&sh_rf[u][i]);
+                        s[i] *= f.x * kf; s[i + 1] *= f.y * kf; s[i + 2] *= f.z * kf; s[i + 3] *= f.w * kf;
+                    }
+                    hide();
+                    {
+                        const float top = reduce_rows<NR, true>(s, lane);
+                        if (lane < NR) sh_wm[x][wq][lane] = top;
+                    }
+                    wg_sync(bar_id);
+                    if (wt < NR) {
+                        const float top = fmaxf(fmaxf(sh_wm[x][0][wt], sh_wm[x][1][wt]), fmaxf(sh_wm[x][2][wt], sh_wm[x][3][wt]));
+                        const float m = sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
+                        sh_c[x][wt] = nm == m ? 1.f : ex2f(m - nm);
+                        sh_m[wt] = nm;
+                    }
+                    wg_sync(bar_id);
+                    if (n >= 2) {
+#pragma unroll
+                        for (int r = 0; r < NR; r += 4) {
+                            const float4 c = *reinterpret_cast<const float4 *>(&sh_c[x][r]);
+                            l[r] *= c.x; l[r + 1] *= c.y; l[r + 2] *= c.z; l[r + 3] *= c.w;
+                        }
+                        // (the product of this warpgroup's last tile is done: S of this one came after it)
+#pragma unroll 1
+                        for (int r0 = 0; r0 < HB * G::kCols; r0 += 16) {
+                            float o[16];
+                            tmem_ld_n<16>(o_tm + r0, o);
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * sh_c[x][(r0 + i) & (NR - 1)]);
+                            tmem_st16(o_tm + r0, w);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                // ---- probabilities of the key -> its row of P
+                if (grown) {
+                    load();
+                    against_max();
+                }
+#pragma unroll
+                for (int c = 0; c < NR / 8; ++c) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 8 * c + 2 * i;
+                        const float a = ex2f(s[r]), b = ex2f(s[r + 1]);
+                        l[r] += a;
+                        l[r + 1] += b;
+                        split_bf16(a, b, hi[i], lo[i]);
+                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready(x));
+            }
+            if (!ok) break;
+            // ---- the unit's end: sums over the warp's keys, the last product
+            const float sum = reduce_rows<NR, false>(l, lane);
+            if (lane < NR) sh_wl[u][x][wq][lane] = sum;
+            if (n0 < count) {
+                const uint32_t last = k0 + (uint32_t)(n0 + ((count - 1 - n0) & ~1));
+                ok = mbar_wait(pv_done(x), (last >> 1) & 1u, abort_flag, ws);
+            }
+            if (wg_any(bar_id, !ok)) break;
+            tc_fence_before();
+            if (lane == 0) mbar_arrive(acc_full(u));
+            k0 += (uint32_t)count;
+            ++unit;
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else if (warp >= 16) {
+        // ================================ V: codes -> bf16 ================================
+        const int key0 = (warp - 16) * 32;
+        int rs = 0, vs = 0;
+        uint32_t r_phase = 0, v_phase = 0;
+        bool ok = true;
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            auto find = [&](int n) { return find_keys<1>(p, t, n < count, begin + n, cur.s, key0, lane); };
+            uint32_t now[1], next[1];
+            KeyPlaces<1> place = find(0);
+            load_scales(p, p.v_scale, place, cur.h, now);
+            place = find(1);
+            for (int n = 0; n < count && ok; ++n) {
+                load_scales(p, p.v_scale, place, cur.h, next);
+                place = find(n + 2);
+#pragma unroll 1
+                for (int y = 0; y < HB; ++y) {
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(raw_full(rs), r_phase, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(v_empty(vs), v_phase ^ 1u, abort_flag, ws));
+                    if (!ok) break;
+                    turn_stage<DB, 1>(r_at(rs), v_at(vs), key0, min(p.D, 128), p.D - 128 * y, now, lane);
+                    if (lane == 0) {
+                        mbar_arrive(v_full(vs));
+                        mbar_arrive(raw_empty(rs));
+                    }
+                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
+                    if ((vs ^= 1) == 0) v_phase ^= 1u;
+                }
+                now[0] = next[0];
+            }
+            leave_unit(p, cur, part.places, piece_end);
+        }
+    } else {
+        // ================================ units' ends: both accumulators joined, written, pieces joined ================================
+        const int wq = warp & 3, wt = wq * 32 + lane;
+        const int bar_id = 3;
+        const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+        uint32_t k0 = 0, unit = 0;
+        bool ok = true;
+        while (cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const Tile t = cur.t;
+            const int u = unit & 1;
+            ok = mbar_wait(acc_full(u), (unit >> 1) & 1u, abort_flag, ws);
+            if (wg_any(bar_id, !ok)) break;
+            bool has[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) has[y] = (int)((k0 & 1u) ^ (uint32_t)y) < count;
+            tc_fence_after();
+            const bool whole_unit = count == t.tiles;
+            const int slot = 2 * (int)blockIdx.x + (begin == 0 ? 1 : 0);
+            const int rows = t.rows;
+            if (wt < NR) {
+                float lw[2], mw[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    lw[y] = sh_wl[u][y][0][wt] + sh_wl[u][y][1][wt] + sh_wl[u][y][2][wt] + sh_wl[u][y][3][wt];
+                    mw[y] = sh_ms[u][y][wt];
+                }
+                const float M = fmaxf(mw[0], mw[1]);
+                const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
+                const float L = lw[0] * f0 + lw[1] * f1;
+                float inv = whole_unit ? inverse(L) : 1.f;
+                // (the row's features, in a part of them too; its log-sum-exp knows nothing of values)
+                if (suspects[u].n > 0 && suspects_hit(suspects[u], sh_hi[u][wt], sh_lo[u][wt], p.sinks)) inv = __int_as_float(0x7FC00000);
+                sh_f[0][wt] = f0 * inv;
+                sh_f[1][wt] = f1 * inv;
+                if (wt < rows) {
+                    const int rr = t.r0 + wt, tok = fast_div(rr, p.gdiv), head = cur.h * p.g + rr - tok * p.g;
+                    if (!whole_unit) {
+                        __stcg(p.part.ml + (size_t)slot * NR + wt, make_float2(M, L));
+                    } else {
+                        sh_out[wt] = (int64_t)(cur.start + tok) * p.out_stride + (int64_t)head * p.D;
+                        if (p.lse) p.lse[(int64_t)(cur.start + tok) * p.H + head] = log_sum(M, L);
+                    }
+                }
+            }
+            wg_sync(bar_id);
+#pragma unroll
+            for (int y = 0; y < HB; ++y) {             // a thread per feature, of each 128
+                const int f = y * 128 + wt;
+                float a[NR];
+#pragma unroll
+                for (int i = 0; i < NR; ++i) a[i] = 0.f;
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    if (has[z]) {
+                        float o[2 * NR];
+                        tmem_ld_n<2 * NR>(o_at(u, z) + y * G::kCols + lanes, o);
+#pragma unroll
+                        for (int i = 0; i < NR; ++i) a[i] = fmaf(o[i] + o[NR + i], sh_f[z][i], a[i]);
+                    }
+                if (f < p.D && whole_unit) {
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) reinterpret_cast<__nv_bfloat16 *>(p.out)[sh_out[i] + f] = __float2bfloat16_rn(a[i]);
+                } else if (f < p.D) {
+                    float *to = p.part.o + (size_t)slot * NR * G::kWide + f;
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (i < rows) __stcg(to + i * G::kWide, a[i]);
+                }
+            }
+            tc_fence_before();
+            if (!whole_unit) {
+                // ---- the pieces of the unit meet: the CTA that arrives last joins them in order
+                int c0, c1;
+                unit_pieces(p, cur, per, c0, c1);
+                wg_sync(bar_id);
+                if (wt == 0) sh_last = arrive_acq_rel(p.part.counters + c0) == c1 - c0;
+                wg_sync(bar_id);
+                if (sh_last) {
+                    const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
+                    if (rows <= 4) join_rows<NR, G::kWide, 1, 8>(ja, wq, lane);
+                    else join_rows<NR, G::kWide, 2, 4>(ja, wq, lane);
+                    if (wt == 0) p.part.counters[c0] = 0;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(unit_end(u));
+            wg_sync(bar_id);                           // sh_f, sh_out and sh_last are read
+            k0 += (uint32_t)count;
+            ++unit;
+            leave_unit(p, cur, part.places, piece_end);
+        }
+        if (wt == 0)                                   // (units are left over only where a wait gave up)
+            settle_arrivals(p, cur, per, piece_end, [&](const Cursor<NR, kTcTile> &, int c0, int c1) {
+                if (arrive_acq_rel(p.part.counters + c0) == c1 - c0) p.part.counters[c0] = 0;
+            });
+    }
+
+    __syncthreads();
+    if (*abort_flag) {
+        // a wait gave up: give copies still in flight time to land before the CTA leaves
+        const long long t0 = clock64();
+        while (clock64() - t0 < 200000) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)G::kTmem) : "memory");
+    }
+}
+
+template <int HB, int NR>
+cudaError_t few_q8_launch(Ctx *c, const AttnParams &p, const CUtensorMap &km, const CUtensorMap &vm, const PageBoxes &bx, cudaStream_t st)
+{
+    const int sms = c->sm_count < kKvMaxSm ? c->sm_count : kKvMaxSm;
+    cudaError_t e = launch_k(kv_attention_few_q8_kernel<HB, NR>, dim3(sms), dim3(FewQ8Geo<HB, NR>::kThreads), FewQ8Geo<HB, NR>::kSmem, st,
+                             !(c->cfg.flags & MRP_FLAG_NO_PDL), p, km, vm, bx);
+    c->launches = 1;
+    return note_err(c, e, "kv_attention_few_q8_kernel");
+}
+
+}  // namespace
+
+// box_rows: rows of a box; 8-bit pools of the geometry attached.  `swizzled`: as an operand, rows of 128 bytes; else raw.
+bool codes_map(Ctx *c, CUtensorMap *map, const void *pool, int box_rows, bool swizzled)
+{
+    const mrp_kv_config &kv = c->kv;
+    const cuuint64_t D = (cuuint64_t)kv.head_dim;
+    const cuuint64_t dims[4] = {D, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
+    const cuuint64_t strides[3] = {D, (cuuint64_t)kv.page_size * D, (cuuint64_t)kv.page_stride};
+    const cuuint32_t box[4] = {(cuuint32_t)(swizzled || kv.head_dim > 128 ? 128 : kv.head_dim), (cuuint32_t)box_rows, 1, 1}, es[4] = {1, 1, 1, 1};
+    return ((EncodeTiledFn)c->kv_encode)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pool), dims, strides, box, es,
+                                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HB, int NR> static cudaError_t few_q8_prepare()
+{
+    return cudaFuncSetAttribute(kv_attention_few_q8_kernel<HB, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewQ8Geo<HB, NR>::kSmem);
+}
+cudaError_t kv_few_q8_prepare()
+{
+    cudaError_t all[] = {few_q8_prepare<1, 8>(), few_q8_prepare<1, 16>(), few_q8_prepare<2, 8>(), few_q8_prepare<2, 16>()};
+    for (cudaError_t one : all)
+        if (one != cudaSuccess) return one;
+    return cudaSuccess;
+}
+
+// Sequences of up to 16 rows (p.rows_above, p.rows_upto say which), mostly of up to 8 if `eight`; p.part is in place.
+cudaError_t launch_few_q8(Ctx *c, AttnParams &p, int box_rows, bool eight, cudaStream_t st)
+{
+    CUtensorMap km, vm;
+    if (!codes_map(c, &km, p.k, box_rows, true) || !codes_map(c, &vm, p.v, box_rows, false)) return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    PageBoxes bx = {};
+    bx.rows = box_rows;
+    p.lead = 2;
+    if (eight) return p.D <= 128 ? few_q8_launch<1, 8>(c, p, km, vm, bx, st) : few_q8_launch<2, 8>(c, p, km, vm, bx, st);
+    return p.D <= 128 ? few_q8_launch<1, 16>(c, p, km, vm, bx, st) : few_q8_launch<2, 16>(c, p, km, vm, bx, st);
+}
+
+}  // namespace mrp

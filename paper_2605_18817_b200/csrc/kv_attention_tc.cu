@@ -32,30 +32,10 @@
 // used, and V rows that no row of the tile sees are zeroed in shared memory before the product (0 * NaN).  A V row with
 // an infinity or NaN that only some rows of a tile see (later tokens of a prompt) is zeroed too and makes the output of
 // the rows that do see it NaN, all features, instead of that of the rows that do not.
-#include <cuda_fp16.h>
-
-#include "kv_attention.cuh"
-#include "kv_q8.cuh"
-#include "tc_common.cuh"
+#include "kv_tile.cuh"
 
 namespace mrp {
 namespace {
-
-constexpr int kTcTile = 128;               // keys of a tile, rows of a row tile
-constexpr int kMaxSuspects = 16;           // boundary tiles of a unit that are remembered for values that are not finite
-
-struct WaitStatus {
-    int32_t *status, *user_status;
-};
-
-// A head is NB blocks of 64 features (1, 2 or 4); a ring stage holds DB of them (1 or 2) of a K or V tile, HB stages a tile.
-template <int NB> struct Blocks {
-    static constexpr int DB = NB >= 2 ? 2 : 1, HB = NB / DB;
-    static constexpr int kStageBytes = DB * 128 * 128;
-};
-// How the keys and values lie (see TileAt, PageBoxes): pages, a box a 64-feature block (kApart) or two (kJoined); rows beside the
-// queries (kPacked); pages of 8 bits (kCodes).
-enum { kApart = 0, kJoined = 1, kPacked = 2, kCodes = 3 };
 
 template <int NB, int NT, int LAY> struct TcGeo {
     typedef Blocks<NB> B;
@@ -76,71 +56,6 @@ template <int NB, int NT, int LAY> struct TcGeo {
     static_assert(NT == 1 || NB <= 2, "tensor memory: two row tiles of accumulators of at most 128 features");
 };
 
-struct Suspects {                          // boundary tiles with V rows that were zeroed for what they held
-    int n;
-    int base[kMaxSuspects];
-    uint32_t keys[kMaxSuspects][4];
-};
-
-__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
-}
-// D[tmem] (+)= A[tmem] * B[smem], bf16
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t db, uint32_t idesc, uint32_t acc)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(db), "r"(idesc), "r"(acc) : "memory");
-}
-// 32 columns of the warp's 32 lanes; no wait
-__device__ __forceinline__ void tmem_ld32(uint32_t a, float *v)
-{
-    uint32_t *r = reinterpret_cast<uint32_t *>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(a) : "memory");
-}
-__device__ __forceinline__ void tmem_ld16_go(uint32_t a, float *v)         // 16 columns; no wait
-{
-    uint32_t *r = reinterpret_cast<uint32_t *>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void tmem_landed16(float *v)
-{
-    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
-                      "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r)
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-        ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-// Behind the wait: the compiler sees no other tie between the wait and the registers the loads fill, and may use them early.
-__device__ __forceinline__ void tmem_landed32(float *v)
-{
-    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                     "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
-                     "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
-                     "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31]) :: "memory");
-}
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 // ======================================================================================================================
 // Few rows (decoding, blocks): everything transposed.  S^T = K Q^T puts the 128 keys of a tile on the tensor-memory lanes
 // and the 16 query rows on the columns, O^T += V^T P^T the features on the lanes: the MMAs and the exponentials do the work of
@@ -159,7 +74,6 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // single tokens 165 us against 158 for the bytes; 24 sequences of 200 to 6000 positions, one token 61 and four 64 against 48;
 // one token behind 2047 positions, 16 heads: 13, of which the launch, the cut and the joining of 16 pieces are most).  Caches of
 // one or two tiles are bound by a unit's chain instead, about 6 us an SM: 256 sequences of 20 to 300 positions 118 against 27.
-constexpr int kFewRows = 16;
 template <int NB> struct FewGeo {
     typedef Blocks<NB> B;
     static constexpr int NR = kFewRows;
@@ -174,364 +88,6 @@ template <int NB> struct FewGeo {
     static constexpr int kThreads = 512;
     static constexpr int kWide = B::HB * 128;              // features of a row of partial results
 };
-constexpr float kNone = -3.4028234e38f;    // the maximum of a row that has seen nothing
-
-template <int N> __device__ __forceinline__ void tmem_ld_n(uint32_t a, float *v);
-template <> __device__ __forceinline__ void tmem_ld_n<32>(uint32_t a, float *v)
-{
-    tmem_ld32(a, v);
-    tmem_wait_ld();
-    tmem_landed32(v);
-}
-template <> __device__ __forceinline__ void tmem_ld_n<16>(uint32_t a, float *v)
-{
-    tmem_ld16_go(a, v);
-    tmem_wait_ld();
-    tmem_landed16(v);
-}
-__device__ __forceinline__ void wg_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ bool any_of(int id, int threads, bool x)        // barrier of `threads` threads, true where any one's x is
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)x) : "memory");
-    return r != 0;
-}
-__device__ __forceinline__ bool wg_any(int id, bool x) { return any_of(id, 128, x); }
-// Reduces W rows (a value per lane each) over the warp; lane i returns row i (i % W).  Each step halves the rows a lane goes
-// on with: W - 1 exchanges instead of 5 W.
-template <int W, bool MAX> __device__ __forceinline__ float reduce_rows(float (&s)[W], int lane)
-{
-    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
-#pragma unroll
-    for (int h = W / 2; h > 0; h >>= 1) {
-        const bool up = (lane & h) != 0;
-#pragma unroll
-        for (int i = 0; i < h; ++i) {
-            const float keep = up ? s[i + h] : s[i], send = up ? s[i] : s[i + h];
-            s[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, h));
-        }
-    }
-    float r = s[0];
-#pragma unroll
-    for (int h = W; h < 32; h <<= 1) r = op(r, __shfl_xor_sync(0xffffffffu, r, h));
-    return r;
-}
-
-// Two fp32 operations in one instruction: (a, b) * s + c, (a, b) + (c, d)
-__device__ __forceinline__ void fma2(float &a, float &b, float s, float c)
-{
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
-        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(s), "f"(c));
-}
-__device__ __forceinline__ void add2(float &a, float &b, float c, float d)
-{
-    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
-        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
-}
-// bits lo..hi-1 of 32
-__device__ __forceinline__ uint32_t bit_range(int lo, int hi)
-{
-    const uint32_t h = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u, l = lo >= 32 ? ~0u : lo <= 0 ? 0u : (1u << lo) - 1u;
-    return h & ~l;
-}
-
-// K as an operand whose contraction runs along its rows (features), groups of 8 rows `group` bytes apart
-__device__ __forceinline__ uint64_t k_desc(uint32_t saddr, uint32_t group)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)1 << 16;
-    d |= (uint64_t)(group >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-// V^T as the A operand, V or P as the B operand: rows (keys) of 128 bytes, MN-major; `block` bytes to the next 64 features,
-// `group` to the next 8 keys
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t block, uint32_t group)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(block >> 4) << 16;
-    d |= (uint64_t)(group >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-
-// How pages become tiles.  A box is `rows` rows of one page and key head: 64 features wide, a box per 64-feature block, the
-// blocks of a tile 16 KB apart; or JOINED, where a page holds whole blocks of 128 features: 128 features wide (the pool seen
-// as [groups of 8 rows][64-feature block][row of the group][64 features]), the two blocks of a group of 8 rows side by side.
-// Half as many boxes of twice the size: with small pages their number is what bounds the stream.
-struct PageBoxes {
-    int rows;
-    int page_groups, head_groups, groups;  // joined (else 0): groups of 8 rows from page to page, head to head, in all
-};
-template <int DB, int LAY> struct TileAt {                 // of a tile: bytes to the next 64-feature block, the next group of 8 keys
-    static constexpr uint32_t block = LAY == kJoined ? 1024 : 128 * 128, group = LAY == kJoined ? DB * 1024 : 1024;
-};
-
-// The box of a tile's keys that is the lane's: where it lies in the pool.  Looked up a tile ahead of its use.
-struct PageRef {
-    bool need;                 // holds visible positions
-    int entry, row;            // page, row in it
-};
-template <int LAY, typename Tile>
-__device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes &bx, const Tile &t, int n, int s, int start, int lane)
-{
-    const int j = key_tile(t, n) * kTcTile + lane * bx.rows;
-    PageRef r;
-    r.need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
-    r.entry = r.row = 0;
-    if (LAY == kPacked) {
-        r.row = start + j;                                 // (rows behind the sequence's: not seen, whatever they are)
-    } else if (r.need) {
-        const int pg = fast_div(j, p.b.page);
-        r.row = j - pg * p.b.page.d;
-        r.entry = __ldg(p.b.page_table + (size_t)s * p.b.max_pages + pg);
-    }
-    return r;
-}
-
-// The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
-template <int DB, int LAY>
-__device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
-                                           uint32_t dst, uint32_t bar, int lane)
-{
-    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, r.need));
-    if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * 128u * DB);
-    __syncwarp();
-    if (r.need) {
-        const bool bad = LAY != kPacked && (unsigned)r.entry >= (unsigned)p.b.n_pages;
-        if (bad) kv_bad_index(p.b);
-        dst += lane * (bx.rows >> 3) * TileAt<DB, LAY>::group;
-        // (a page that is not one: outside the map, zeros arrive)
-        if (LAY == kJoined) {
-            const int g = bad ? bx.groups : r.entry * bx.page_groups + h * bx.head_groups + (r.row >> 3);
-            tma_load_page(dst, map, 0, 0, feature >> 6, g, bar);
-        } else {
-#pragma unroll
-            for (int x = 0; x < DB; ++x)
-                tma_load_page(dst + x * (128 * 128), map, feature + 64 * x, r.row, h, bad ? p.b.n_pages : r.entry, bar);
-        }
-    }
-}
-
-// 8 bits: the same, 128 keys of `pitch` codes from `feature` on, one row after the other, -> a raw stage.
-__device__ __forceinline__ void fetch_codes(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
-                                            int pitch, uint32_t dst, uint32_t bar, int lane)
-{
-    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, r.need));
-    if (lane == 0) mbar_expect_tx(bar, boxes * bx.rows * (uint32_t)pitch);
-    __syncwarp();
-    if (r.need) {
-        const bool bad = (unsigned)r.entry >= (unsigned)p.b.n_pages;
-        if (bad) kv_bad_index(p.b);
-        tma_load_page(dst + lane * bx.rows * pitch, map, feature, r.row, h, bad ? p.b.n_pages : r.entry, bar);
-    }
-}
-
-// 16 codes times the scale with byte s -> 16 bf16.  A code's bits, moved to a bf16's sign, lower exponent and upper mantissa bits, are
-// its value times 2^-120 (subnormal codes: subnormal bf16), so one exact product with 2^(s - 7) is all; scales above 2^7 take two.
-struct Turn {
-    __nv_bfloat162 f, g;
-};
-__device__ __forceinline__ Turn turn_of(uint32_t s, bool seen)             // a key's factors; 0 where no row sees it
-{
-    const uint32_t a = !seen ? 0u : s == kQ8NaN ? 0x7FC0u : (min(s, 134u) + 120u) << 7, b = s > 134u && s != kQ8NaN ? (s - 7u) << 7 : 0x3F80u;
-    const uint32_t f = a | a << 16, g = b | b << 16;
-    return Turn{*reinterpret_cast<const __nv_bfloat162 *>(&f), *reinterpret_cast<const __nv_bfloat162 *>(&g)};
-}
-__device__ __forceinline__ uint32_t turn_two(uint32_t bytes, const Turn &t, bool large)    // [0, code, 0, code]
-{
-    const uint32_t h = (bytes & 0x80008000u) | ((bytes >> 4) & 0x07F007F0u);
-    __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&h), t.f);
-    if (large) x = __hmul2(x, t.g);
-    return *reinterpret_cast<const uint32_t *>(&x);
-}
-
-// Query rows r0.. of a tile (those below `rows`; zeros beyond, and beyond the head's features) -> shared memory, as K-major
-// blocks of 64 features.  THREADS threads, all copies in flight together.
-template <int NB, int ROWS, int THREADS>
-__device__ __forceinline__ void load_queries(const AttnParams &p, int start, int h, int r0, int rows, uint32_t sq, int tid)
-{
-    constexpr int kRow = 8 * NB, kStep = THREADS / kRow;   // 16-byte chunks of a row; rows a round
-    static_assert(THREADS % kRow == 0 && ROWS % kStep == 0, "whole rounds");
-    const int ch = tid % kRow;
-    const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)start * p.q_stride + (int64_t)h * p.g * p.D;
-    const bool wide = ch * 8 < p.D;
-    int r = tid / kRow, tok = fast_div(r0 + r, p.gdiv), hg = r0 + r - tok * p.g;
-    const int dt = fast_div(kStep, p.gdiv), dh = kStep - dt * p.g;
-    uint32_t a = sq + (ch >> 3) * (ROWS * 128) + r * 128;
-#pragma unroll 4
-    for (int i = 0; i < ROWS / kStep; ++i) {
-        const bool on = wide & (r < rows);
-        const __nv_bfloat16 *q = on ? src + (int64_t)tok * p.q_stride + hg * p.D + ch * 8 : src;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(a + (((ch & 7) ^ (r & 7)) << 4)), "l"(q), "r"(on ? 16 : 0) : "memory");
-        r += kStep;
-        a += kStep * 128;
-        tok += dt;
-        hg += dh;
-        if (hg >= p.g) { hg -= p.g; ++tok; }
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-
-// What a unit's rows see together, for the V rows that must not reach a product: rows no row sees -> zeros; rows some
-// see that hold what is not finite -> zeros, remembered.  One warp, on a V tile that has landed.
-struct Seen {
-    int all_lo, all_hi;
-    bool differ;
-};
-template <typename Tile>
-__device__ __forceinline__ Seen seen_by_all(const AttnParams &p, const Tile &t, int pre)
-{
-    const int i0 = fast_div(t.r0, p.gdiv), i1 = fast_div(t.r0 + t.rows - 1, p.gdiv);
-    Seen s;
-    s.differ = i0 != i1 && (p.mask == MRP_ATTN_CAUSAL || p.window > 0);
-    s.all_hi = p.mask == MRP_ATTN_CAUSAL ? pre + i0 + 1 : t.hi;
-    s.all_lo = p.window > 0 ? max(0, pre + i1 + 1 - p.window) : 0;
-    return s;
-}
-template <int DB, int LAY, typename Tile>
-__device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0, uint32_t vs, Suspects &sus, int lane)
-{
-    typedef TileAt<DB, LAY> lay;
-    if ((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) {
-        if (!a.differ || (j0 >= a.all_lo && j0 + kTcTile <= a.all_hi)) return;
-    }
-    uint32_t found[4];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const int row = w * 32 + lane, j = j0 + row;
-        const uint32_t at = vs + (row >> 3) * lay::group + (row & 7) * 128;
-        const bool seen = j < t.hi && (j >= t.lo || j < t.s1);
-        bool bad = false;
-        if (seen && a.differ && !(j >= a.all_lo && j < a.all_hi)) {
-            for (int c = 0; c < 8 * DB; ++c) {
-                uint32_t u[4];
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                             : "r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)) : "memory");
-#pragma unroll
-                for (int y = 0; y < 4; ++y) bad |= (u[y] & 0x7F800000u) == 0x7F800000u || (u[y] & 0x7F80u) == 0x7F80u;
-            }
-        }
-        found[w] = __ballot_sync(0xffffffffu, bad);
-        if (!seen || bad)
-            for (int c = 0; c < 8 * DB; ++c)
-                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
-                             ::"r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
-    }
-    if (lane == 0 && (found[0] | found[1] | found[2] | found[3])) {
-        const int at_n = sus.n;
-        if (at_n < kMaxSuspects) {
-            sus.base[at_n] = j0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) sus.keys[at_n][w] = found[w];
-        }
-        sus.n = at_n + 1;
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-}
-__device__ __forceinline__ bool suspects_hit(const Suspects &sus, int hi, int lo, int sinks)
-{
-    bool hit = sus.n > kMaxSuspects;
-    for (int y = 0; y < min(sus.n, kMaxSuspects); ++y)
-        for (int w = 0; w < 4; ++w)
-            for (uint32_t bits = sus.keys[y][w]; bits; bits &= bits - 1) {
-                const int j = sus.base[y] + w * 32 + __ffs(bits) - 1;
-                hit |= sees(j, hi, lo, sinks);
-            }
-    return hit;
-}
-
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }      // (NaN goes through)
-__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
-
-// Joins the pieces c0..c1 of a unit in their order, with a running maximum: warp w of four takes every fourth row, RG rows
-// and U pieces of each in flight, a lane four features.
-struct JoinArgs {
-    const float2 *ml;
-    const float *o;
-    __nv_bfloat16 *out;                    // of the unit's sequence and key head
-    float *lse;
-    int64_t out_stride;
-    int H, D, g;
-    FastDiv gdiv;
-    int r0, rows, c0, c1;
-};
-__device__ __forceinline__ JoinArgs join_args(const AttnParams &p, int start, int h, int r0, int rows, int c0, int c1)
-{
-    JoinArgs a;
-    a.ml = p.part.ml;
-    a.o = p.part.o;
-    a.out = reinterpret_cast<__nv_bfloat16 *>(p.out) + (int64_t)start * p.out_stride + (int64_t)h * p.g * p.D;
-    a.lse = p.lse ? p.lse + (int64_t)start * p.H + h * p.g : nullptr;
-    a.out_stride = p.out_stride;
-    a.H = p.H; a.D = p.D; a.g = p.g; a.gdiv = p.gdiv;
-    a.r0 = r0; a.rows = rows; a.c0 = c0; a.c1 = c1;
-    return a;
-}
-template <int NR, int WIDE, int RG, int U>
-__device__ __forceinline__ void join_rows(const JoinArgs &p, int w, int lane)
-{
-    const int rows = p.rows, c0 = p.c0, c1 = p.c1;
-#pragma unroll 1
-    for (int f0 = 0; f0 < WIDE; f0 += 128) {
-        const bool mine = f0 + 4 * lane < p.D;
-#pragma unroll 1
-        for (int rb = w; rb < rows; rb += 4 * RG) {
-            float M[RG], L[RG];
-            float4 a[RG];
-#pragma unroll
-            for (int y = 0; y < RG; ++y) { M[y] = kNone; L[y] = 0.f; a[y] = make_float4(0.f, 0.f, 0.f, 0.f); }
-#pragma unroll 1
-            for (int cb = c0; cb <= c1; cb += U) {
-                float2 ml[RG][U];
-                float4 o[RG][U];
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int c = min(cb + i, c1);
-                    const size_t sl = (size_t)(2 * c + (c == c0)) * NR;
-#pragma unroll
-                    for (int y = 0; y < RG; ++y) {
-                        const int r = min(rb + 4 * y, rows - 1);
-                        ml[y][i] = __ldcg(p.ml + sl + r);
-                        o[y][i] = __ldcg(reinterpret_cast<const float4 *>(p.o + (sl + r) * WIDE) + (mine ? f0 / 4 + lane : 0));
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (cb + i <= c1) {
-#pragma unroll
-                        for (int y = 0; y < RG; ++y) {
-                            const float nm = fmaxf(M[y], ml[y][i].x);
-                            const float f = M[y] == nm ? 1.f : ex2f(M[y] - nm), e = ml[y][i].x == nm ? 1.f : ex2f(ml[y][i].x - nm);
-                            M[y] = nm;
-                            L[y] = fmaf(e, ml[y][i].y, L[y] * f);
-                            a[y].x = fmaf(e, o[y][i].x, a[y].x * f); a[y].y = fmaf(e, o[y][i].y, a[y].y * f);
-                            a[y].z = fmaf(e, o[y][i].z, a[y].z * f); a[y].w = fmaf(e, o[y][i].w, a[y].w * f);
-                        }
-                    }
-            }
-#pragma unroll
-            for (int y = 0; y < RG; ++y) {
-                const int r = rb + 4 * y;
-                if (r < rows && mine) {
-                    const float inv = inverse(L[y]);
-                    const int rr = p.r0 + r, tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
-                    __nv_bfloat16 *dst = p.out + (int64_t)tok * p.out_stride + (int64_t)hg * p.D + f0 + 4 * lane;
-                    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(a[y].x * inv, a[y].y * inv), pack_bf16(a[y].z * inv, a[y].w * inv));
-                    if (f0 + lane == 0 && p.lse) p.lse[(int64_t)tok * p.H + hg] = log_sum(M[y], L[y]);
-                }
-            }
-    }
-    }
-}
-
 template <int NB, int LAY>
 __global__ void __launch_bounds__(512, 1)
 kv_attention_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
@@ -1222,108 +778,24 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         }
     } else if (LAY == kCodes && warp >= 2 + 8 * NT) {
         // ================================ 8 bits: raw stages -> stages of the ring ================================
-        // A warp has KW keys of every tile and a lane 16 codes at a time: four lanes a key, 64 features, and of two features blocks
-        // neighbouring keys take different ones, so that loads and (swizzled) stores touch all banks once.
-        constexpr int KW = G::kTurners ? 128 / (G::kTurners ? G::kTurners : 1) : 128, KR = KW / 32;
-        const int w = warp - (2 + 8 * NT), kk = lane >> 2, q = lane & 3;
-        const int pitch = min(p.D, 128);
+        constexpr int KR = G::kTurners ? 4 / (G::kTurners ? G::kTurners : 1) : 1;      // of every tile, a warp has 32 KR keys
+        const int key0 = (warp - (2 + 8 * NT)) * 32 * KR;
         int stage = 0, raw = 0;
         uint32_t phase = 0, raw_phase = 0;
         bool ok = true;
-        struct Place {                                     // a lane's keys in the scales (-1: not seen, or no page)
-            int entry[KR], row[KR];
-        };
-        struct Bytes {
-            uint32_t k[KR], v[KR];
-            bool seen[KR];
-        };
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
             if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
-            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
-            auto peek = [&](int n, Place &a) {
-#pragma unroll
-                for (int i = 0; i < KR; ++i) {
-                    a.entry[i] = -1;
-                    a.row[i] = 0;
-                    if (n < count) {
-                        const int j = key_tile(t, begin + n) * kTcTile + w * KW + i * 32 + lane;
-                        if (j < t.hi && (j >= t.lo || j < t.s1)) {
-                            const int pg = fast_div(j, p.b.page);
-                            a.row[i] = j - pg * p.b.page.d;
-                            a.entry[i] = __ldg(table + pg);
-                        }
-                    }
-                }
-            };
-            auto fetch = [&](const Place &a, Bytes &b) {
-#pragma unroll
-                for (int i = 0; i < KR; ++i) {
-                    b.seen[i] = (unsigned)a.entry[i] < (unsigned)p.b.n_pages;
-                    const int64_t at = b.seen[i] ? ((int64_t)a.entry[i] * p.Hk + cur.h) * p.b.page.d + a.row[i] : 0;
-                    b.k[i] = __ldg(p.k_scale + at);
-                    b.v[i] = __ldg(p.v_scale + at);
-                }
-            };
-            auto turn = [&](const uint32_t (&bytes)[KR], const bool (&seen)[KR]) {
-                bool any = false;
-#pragma unroll
-                for (int i = 0; i < KR; ++i) any |= seen[i] && bytes[i] > 134u && bytes[i] != kQ8NaN;
-                const bool large = __any_sync(0xffffffffu, any);
+            auto find = [&](int n) { return find_keys<KR>(p, t, n < count, begin + n, cur.s, key0, lane); };
+            auto turn = [&](const uint32_t (&bytes)[KR]) {
 #pragma unroll 1
                 for (int y = 0; y < HB; ++y) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(raw_full(raw), raw_phase, abort_flag, ws));
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
-                    const uint32_t from = base + G::kRaw + raw * G::kRawStage, to = ring + stage * G::B::kStageBytes;
-                    const int wide = p.D - 128 * y;        // features of this stage, less than 64 DB at a head's end
-#pragma unroll
-                    for (int i = 0; i < KR; ++i)
-#pragma unroll 1
-                        for (int e = 0; e < 4; ++e) {      // 8 keys
-                            const Turn f = turn_of(__shfl_sync(0xffffffffu, bytes[i], e * 8 + kk), __shfl_sync(0xffffffffu, (int)seen[i], e * 8 + kk));
-                            const int key = w * KW + i * 32 + e * 8 + kk;
-                            const uint32_t row = to + (key >> 3) * 1024 + (key & 7) * 128;
-                            uint4 c[DB];
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                const int ch = q + (DB == 2 ? 4 * (d ^ (kk & 1)) : 0);
-                                c[d] = make_uint4(0, 0, 0, 0);
-                                if (ch * 16 < wide)
-                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[d].x), "=r"(c[d].y), "=r"(c[d].z), "=r"(c[d].w)
-                                                 : "r"(from + key * pitch + ch * 16) : "memory");
-                            }
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                const int ch = q + (DB == 2 ? 4 * (d ^ (kk & 1)) : 0);
-                                const uint32_t x[4] = {c[d].x, c[d].y, c[d].z, c[d].w};
-                                uint32_t o[8];
-                                if (!large) {
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) {
-                                        o[2 * z] = turn_two(__byte_perm(x[z], 0, 0x1404), f, false);
-                                        o[2 * z + 1] = turn_two(__byte_perm(x[z], 0, 0x3424), f, false);
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) {
-                                        o[2 * z] = turn_two(__byte_perm(x[z], 0, 0x1404), f, true);
-                                        o[2 * z + 1] = turn_two(__byte_perm(x[z], 0, 0x3424), f, true);
-                                    }
-                                }
-                                // (beyond the head's features: zeros, also in a row of NaN)
-                                if (ch * 16 >= wide)
-#pragma unroll
-                                    for (int z = 0; z < 8; ++z) o[z] = 0u;
-                                const uint32_t at = row + (ch >> 2) * TileAt<DB, LAY>::block, sw = key & 7;
-                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * q) ^ sw) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * q + 1) ^ sw) << 4)), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
-                            }
-                        }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
+                    turn_stage<DB, KR>(base + G::kRaw + raw * G::kRawStage, ring + stage * G::B::kStageBytes, key0, min(p.D, 128), p.D - 128 * y, bytes, lane);
                     if (lane == 0) {
                         mbar_arrive(full_bar(stage));
                         mbar_arrive(raw_empty(raw));
@@ -1333,22 +805,24 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 }
             };
             // scales a tile ahead of their use, their pages another tile
-            Place at;
-            Bytes now, next, then;
-            peek(0, at);
-            fetch(at, now);
-            peek(1, at);
-            fetch(at, next);
-            peek(2, at);
-            turn(now.k, now.seen);
+            uint32_t kn[KR], vn[KR], k1[KR], v1[KR], k2[KR], v2[KR];
+            KeyPlaces<KR> at = find(0);
+            load_scales(p, p.k_scale, at, cur.h, kn);
+            load_scales(p, p.v_scale, at, cur.h, vn);
+            at = find(1);
+            load_scales(p, p.k_scale, at, cur.h, k1);
+            load_scales(p, p.v_scale, at, cur.h, v1);
+            at = find(2);
+            turn(kn);
             for (int n = 0; n < count && ok; ++n) {        // the order in which the MMA warp takes them
-                fetch(at, then);
-                peek(n + 3, at);
-                if (NT == 2) turn(now.v, now.seen);
-                if (n + 1 < count) turn(next.k, next.seen);
-                if (NT == 1) turn(now.v, now.seen);
-                now = next;
-                next = then;
+                load_scales(p, p.k_scale, at, cur.h, k2);
+                load_scales(p, p.v_scale, at, cur.h, v2);
+                at = find(n + 3);
+                if (NT == 2) turn(vn);
+                if (n + 1 < count) turn(k1);
+                if (NT == 1) turn(vn);
+#pragma unroll
+                for (int y = 0; y < KR; ++y) { vn[y] = v1[y]; k1[y] = k2[y]; v1[y] = v2[y]; }
             }
             leave_unit(p, cur, part.places, piece_end);
         }
@@ -1594,7 +1068,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                     if (half == 0 && lane == 0) sh_last[x][wq] = arrive_acq_rel(counter) == c1 - c0;
                     any_of(pair, 64, false);
                     if (sh_last[x][wq] && live) {
-                        constexpr int U = NT == 1 ? 2 : 1;             // pieces in flight (registers)
+                        constexpr int U = NT == 1 && LAY != kCodes ? 2 : 1;      // pieces in flight (registers)
                         auto slot_of = [&](int c) { return (size_t)((2 * c + (c == c0)) * NT + x); };
 #pragma unroll 1
                         for (int f = 0; f < NB; ++f) {
@@ -1769,6 +1243,7 @@ cudaError_t kv_tc_attach(Ctx *c)
                          tc_prepare<2, 2, kCodes>()};
     for (cudaError_t one : all)
         if (one != cudaSuccess) return one;
+    if ((e = kv_few_q8_prepare()) != cudaSuccess) return e;
     c->kv_encode = fn;
     return cudaSuccess;
 }
@@ -1857,17 +1332,9 @@ cudaError_t launch_paged_attention_q8_tc(Ctx *c, AttnParams &p, const mrp_kv_bat
     const bool two = rows > 128 && !wide && units_for_all(c, p, batch);
     PageBoxes bx = {};
     bx.rows = tc_box_rows(kv.page_size);
+    if (rows <= kFewRows) return launch_few_q8(c, p, bx.rows, rows <= 8, st);
     CUtensorMap km, vm;
-    const cuuint64_t D = (cuuint64_t)kv.head_dim;
-    const cuuint64_t dims[4] = {D, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
-    const cuuint64_t strides[3] = {D, (cuuint64_t)kv.page_size * D, (cuuint64_t)kv.page_stride};
-    const cuuint32_t box[4] = {(cuuint32_t)(kv.head_dim < 128 ? kv.head_dim : 128), (cuuint32_t)bx.rows, 1, 1}, es[4] = {1, 1, 1, 1};
-    const void *pools[2] = {p.k, p.v};
-    for (int i = 0; i < 2; ++i)
-        if (((EncodeTiledFn)c->kv_encode)(i ? &vm : &km, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pools[i]), dims, strides, box, es,
-                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    if (!codes_map(c, &km, p.k, bx.rows, false) || !codes_map(c, &vm, p.v, bx.rows, false)) return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     cudaError_t e;
     int launches = 0;
     auto one = [&]() {
@@ -1876,7 +1343,7 @@ cudaError_t launch_paged_attention_q8_tc(Ctx *c, AttnParams &p, const mrp_kv_bat
     };
     if (two) {
         p.rows_upto = kFewRows;
-        if ((e = one()) != cudaSuccess) return e;
+        if ((e = launch_few_q8(c, p, bx.rows, p.g <= 8, st)) != cudaSuccess) return e;
         launches = c->launches;
         p.rows_above = kFewRows;
         p.rows_upto = INT_MAX;
