@@ -1,13 +1,20 @@
 // Attention over pages of 8 bits, up to 16 query rows a sequence and key head: kv_attention_few_kernel (kv_attention_tc.cu, whose
-// mathematics, roles and units' ends these are) with half the bytes to read, which leaves half the time for everything else.
+// mathematics and units' ends these are) with half the bytes to read, which leaves half the time for everything else.
 //
 //   S^T = K Q^T on the codes as they lie: K's tile is the A operand in e4m3 (kind::f8f6f4), and a query row is two e4m3 rows of B,
 //   q = 2^E (hi + lo / 16): eight significant bits, which is all of a bf16 (elements below 2^-13 of their row's largest: to 2^-21 of
 //   that).  The thread that has a key takes its score times 2^E of the row times the key's scale.
-//   O^T += V^T P^T in bf16: four warps turn the codes of V times their scales into bf16 (exact) in two stages of their own.  In 8 bits
+//   O^T += V^T P^T in bf16: warps turn the codes of V times their scales into bf16 (exact) in two stages of their own.  In 8 bits
 //   P would need three parts or more, and lose the tail of a long cache, whose many small probabilities lie below what e4m3 holds.
 //   Turning K too would move 3 bytes more through shared memory for each of its codes, which then bounds the kernel instead of
 //   memory: TMA, warps and MMAs move 88 of 128 bytes a cycle at the memory's rate as it is.
+//
+//   warp 0   K and V tiles by TMA      warp 1   S MMAs      warp 2   PV MMAs      warp 3   the tiles' scales
+//   warps 4-7, 8-11   softmax: two warpgroups that take tiles in turn, a thread per key
+//   warps 12-15   queries, a unit ahead, and units' ends          from warp 16 on   V's codes -> bf16 (8 rows: two groups of four warps, a stage each)
+// Instructions bound it next to memory, so each role's loop is short: the roles of an SM quarter share its instruction cache and
+// its issue slots.  (One warp for both kinds of MMAs, scales looked up by the warps that use them, turning unrolled: 64 ragged
+// single tokens 266 us; the turning rolled and 8 rows instead of 16: 159.)
 #include "kv_tile.cuh"
 
 namespace mrp {
@@ -24,27 +31,31 @@ template <int HB, int ROWS> struct FewQ8Geo {
     static constexpr int kQ = HB * kCols * 128;            // queries of a unit, two of them
     static constexpr int kPAt = kVAt + 2 * 32768, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
-    static constexpr int kTmem = HB == 2 ? 512 : 256;      // of which 2 kCols + 4 HB kCols are used
-    static constexpr int kThreads = 640;
+    static constexpr int kTmem = HB == 2 && NR == 16 ? 512 : 256;          // of which 4 kCols (S) + 4 HB kCols are used
+    static constexpr int kTurners = NR == 8 ? 8 : 4;       // warps (16 rows: the softmax needs the registers)
+    static constexpr int kThreads = 512 + 32 * kTurners;
     static constexpr int kWide = HB * 128;                 // features of a row of partial results
 };
 
 // The unit's query rows as two e4m3 parts each (row r: hi, row NR + r: lo), K-major blocks of 128 features, and what their scores
-// are multiplied by: 2^E scale log2(e), NaN for a row that is not finite.  64 threads, 64 / NR a row.
+// are multiplied by: 2^E scale log2(e), NaN for a row that is not finite.  128 threads, 128 / NR a row.
 template <int HB, int NR>
 __device__ __forceinline__ void load_query_parts(const AttnParams &p, int start, int h, int r0, int rows, uint32_t sq, float *factor, int tid)
 {
-    constexpr int kParts = 64 / NR, kChunks = 16 * HB / kParts;            // threads a row; runs of 8 features a thread
+    constexpr int kParts = 128 / NR, kChunks = 16 * HB / kParts;           // threads a row; runs of 8 features a thread
     const int r = tid / kParts, part = tid % kParts;
     const int rr = r0 + min(r, rows - 1), tok = fast_div(rr, p.gdiv), hg = rr - tok * p.g;
-    const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)(start + tok) * p.q_stride + (int64_t)(h * p.g + hg) * p.D;
+    const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(p.q) + (int64_t)(start + tok) * p.q_stride + (int64_t)(h * p.g + hg) * p.D);
+    const int have = r < rows ? p.D / 8 : 0;
     uint4 x[kChunks];
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
         const int c = part + kParts * i;
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows && c * 8 < p.D) x[i] = __ldg(reinterpret_cast<const uint4 *>(src) + c);
+        x[i] = c < have ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
         for (int y = 0; y < 4; ++y) top = max(top, max((w[y] << 16) & 0x7FFFFFFFu, w[y] & 0x7FFF0000u));
@@ -79,19 +90,49 @@ __device__ __forceinline__ void load_query_parts(const AttnParams &p, int start,
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// The scale bytes of a lane's four keys of V at a boundary of what is seen: see the scales' warp.
+template <typename Tile>
+__device__ __noinline__ uint32_t mend_scales(const Tile &t, const Seen &a, int j0, uint32_t w, Suspects &sus, int lane)
+{
+    uint32_t keep = 0, bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int j = j0 + lane * 4 + e;
+        const bool seen = j < t.hi && (j >= t.lo || j < t.s1), nan = ((w >> (8 * e)) & 255u) == kQ8NaN;
+        const bool some = seen && nan && a.differ && !(j >= a.all_lo && j < a.all_hi);
+        bad |= (uint32_t)some << e;
+        keep |= seen && !some ? 255u << (8 * e) : 0u;
+    }
+    if (__any_sync(0xffffffffu, bad != 0)) {
+        const int slot = sus.n;
+        __syncwarp();
+        if (lane == 0) sus.n = slot + 1;
+        if (slot < kMaxSuspects) {
+            if (lane == 0) sus.base[slot] = j0;
+            uint32_t word = bad << (4 * (lane & 7));       // 32 keys, of eight lanes
+#pragma unroll
+            for (int x = 1; x < 8; x <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, x);
+            if ((lane & 7) == 0) sus.keys[slot][lane >> 3] = word;
+        }
+        __syncwarp();
+    }
+    return w & keep;
+}
+
 template <int HB, int NR>
-__global__ void __launch_bounds__(640, 1)
+__global__ void __launch_bounds__(FewQ8Geo<HB, NR>::kThreads, 1)
 kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
-                        const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
+                           const __grid_constant__ CUtensorMap vmap, const PageBoxes bx)
 {
     typedef FewQ8Geo<HB, NR> G;
-    constexpr int DB = 2;
     typedef RowTile<NR, kTcTile> Tile;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ long long sh_find[G::kThreads / 32 + 2];
+    __shared__ Cursor<NR, kTcTile> sh_cur;                 // where this CTA's piece of the line begins, its length, a full piece's
+    __shared__ long long sh_len, sh_per;
     __shared__ Suspects suspects[2];
+    __shared__ uint32_t sh_ks[4][32], sh_vs[G::kRawStages][32];            // scale bytes of the keys of a tile's K (by S buffer), of a raw stage
     __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
-    __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR], sh_rf[2][NR];   // maximum in use (unit, warpgroup), factor to it; a unit's rows' factors
+    __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR], sh_rf[2][NR];     // maximum in use (unit, warpgroup), factor to it; rows' factors
     __shared__ float sh_wm[2][4][NR], sh_wl[2][2][4][NR];  // row maxima and (of a unit) sums of the warps
     __shared__ float sh_f[2][NR];                          // the unit's end: factors of the accumulators,
     __shared__ int64_t sh_out[NR];                         //   where the rows go
@@ -105,18 +146,19 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     auto v_at = [&](int s) { return base + G::kVAt + s * 32768; };         // V in bf16
     auto k_full = [&](int s) { return bars + 8 * s; };
     auto k_empty = [&](int s) { return bars + 8 * (4 + s); };
-    auto raw_full = [&](int s) { return bars + 8 * (8 + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (8 + s); };     // the codes, and their scales
     auto raw_empty = [&](int s) { return bars + 8 * (12 + s); };
     auto v_full = [&](int s) { return bars + 8 * (16 + s); };
     auto v_empty = [&](int s) { return bars + 8 * (18 + s); };
-    auto s_full = [&](int x) { return bars + 8 * (32 + x); };
-    auto p_ready = [&](int x) { return bars + 8 * (34 + x); };
-    auto pv_done = [&](int x) { return bars + 8 * (36 + x); };
-    auto q_ready = [&](int x) { return bars + 8 * (38 + x); };
-    auto unit_end = [&](int x) { return bars + 8 * (40 + x); };    // the unit is written: everything of it may be reused
-    auto acc_full = [&](int x) { return bars + 8 * (42 + x); };    // the unit's sums, maxima and accumulators are there
+    auto s_full = [&](int b) { return bars + 8 * (20 + b); };      // the scores of a tile, and the keys' scales
+    auto s_free = [&](int b) { return bars + 8 * (24 + b); };
+    auto p_ready = [&](int x) { return bars + 8 * (28 + x); };
+    auto pv_done = [&](int x) { return bars + 8 * (30 + x); };
+    auto q_ready = [&](int x) { return bars + 8 * (32 + x); };
+    auto unit_end = [&](int x) { return bars + 8 * (34 + x); };    // the unit is written: everything of it may be reused
+    auto acc_full = [&](int x) { return bars + 8 * (36 + x); };    // the unit's sums, maxima and accumulators are there
     unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 44);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 40);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     const WaitStatus ws = {p.b.status, p.b.user_status};
 
@@ -126,16 +168,19 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             mbar_init(k_empty(s), 1);
         }
         for (int s = 0; s < G::kRawStages; ++s) {
-            mbar_init(raw_full(s), 1);
+            mbar_init(raw_full(s), 2);
             mbar_init(raw_empty(s), 4);
+        }
+        for (int b = 0; b < 4; ++b) {
+            mbar_init(s_full(b), 2);
+            mbar_init(s_free(b), 4);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(v_full(x), 4);
             mbar_init(v_empty(x), 1);
-            mbar_init(s_full(x), 1);
             mbar_init(p_ready(x), 4);
             mbar_init(pv_done(x), 1);
-            mbar_init(q_ready(x), 64);
+            mbar_init(q_ready(x), 128);
             mbar_init(unit_end(x), 4);
             mbar_init(acc_full(x), 8);
         }
@@ -148,32 +193,41 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"((uint32_t)G::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (warp == 2) {
+        pdl_wait();
+        Cursor<NR, kTcTile> c;
+        long long full = 1;
+        c.at = 0;
+        const long long len = cut_line<NR>(p, c, full, blockIdx.x == 0);
+        if (lane == 0) {
+            sh_cur = c;
+            sh_len = len;
+            sh_per = full;
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;    // S of the two warpgroups, then their accumulators of two units
-    auto s_at = [&](int x) { return tmem + x * G::kCols; };        // (columns: the upper parts of the rows, the lower ones)
-    auto o_at = [&](int u, int x) { return tmem + 2 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
+    const uint32_t tmem = *tmem_holder;    // four buffers of S, then the warpgroups' accumulators of two units
+    auto s_at = [&](int b) { return tmem + b * G::kCols; };        // (columns: the upper parts of the rows, the lower ones)
+    auto o_at = [&](int u, int x) { return tmem + 4 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
     pdl_wait();
     pdl_trigger();
 
-    Cursor<NR, kTcTile> cur;
-    long long per;
-    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
-                                            : find_piece<NR, kTcTile, G::kThreads>(p, cur, per, sh_find);
-    if (len == 0) cur.at = 0;
-    const long long piece_end = len > 0 ? cur.at + len : 0;
+    Cursor<NR, kTcTile> cur = sh_cur;
+    const long long per = sh_per, piece_end = sh_len > 0 ? cur.at + sh_len : 0;
+    if (sh_len == 0) cur.at = 0;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag, ws)); };   // a warp's
 
     if (warp == 0) {
         // ================================ K and V tiles ================================
         int ks = 0, rs = 0;
         uint32_t k_phase = 0, r_phase = 0;
-        bool ok = true;
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
-            auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+            if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
             auto fetch_k = [&](const PageRef &r) {
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
@@ -195,72 +249,73 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             PageRef now = look_up<kCodes>(p, bx, cur.t, begin, cur.s, cur.start, lane), next = now, then = now;
             if (count > 1) next = look_up<kCodes>(p, bx, cur.t, begin + 1, cur.s, cur.start, lane);
             fetch_k(now);
-            for (int n = 0; n < count; ++n) {
+            for (int n = 0; n < count && ok; ++n) {
                 if (n + 2 < count) then = look_up<kCodes>(p, bx, cur.t, begin + n + 2, cur.s, cur.start, lane);
                 if (n + 1 < count) fetch_k(next);
                 fetch_v(now);
                 now = next;
                 next = then;
             }
-            leave_unit(p, cur, part.places, piece_end);
+            next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp == 1) {
-        // ================================ MMAs ================================
-        int ks = 0, vs = 0;
-        uint32_t k_phase = 0, v_phase = 0, k = 0, unit = 0;
-        bool ok = true;
-        const uint32_t idesc_s = make_idesc_e4m3(G::kCols), idesc_o = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
-        typedef TileAt<DB, kApart> lay;
-        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+        // ================================ S^T = K Q^T ================================
+        int ks = 0;
+        uint32_t k_phase = 0, k = 0, unit = 0;             // k: tiles done
+        const uint32_t idesc = make_idesc_e4m3(G::kCols);
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
-            const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
-            const Tile t = cur.t;
-            const Seen all = seen_by_all(p, t, cur.pre);
-            const uint32_t sq = base + G::kQAt + (unit & 1u) * G::kQ;
+            if (part.count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
+            const uint64_t q = make_smem_desc(base + G::kQAt + (unit & 1u) * G::kQ);
             wait(q_ready(unit & 1u), (unit >> 1) & 1u);
-            if (!ok) break;
-            Suspects &sus = suspects[unit & 1];            // (the unit before the last is written: see the query warps)
-            if (lane == 0) sus.n = 0;
-            __syncwarp();
-            auto scores = [&](uint32_t kk) {               // S^T of tile kk from the stages at hand
+            for (int n = 0; n < part.count && ok; ++n, ++k) {
+                const uint32_t b = k & 3u;
+                wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     wait(k_full(ks), k_phase);
-                    if (!ok) return;
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a = k_at(ks), q = sq + y * (G::kCols * 128);
+                    const uint64_t a = make_smem_desc(k_at(ks));
                     if (elect_one()) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)        // 32 features
-                            umma_f8(s_at(kk & 1u), make_smem_desc(a + c * 32), make_smem_desc(q + c * 32), idesc_s, y + c > 0);
-                        if (y + 1 == HB) umma_commit(s_full(kk & 1u));
+                        for (int c = 0; c < 4; ++c)        // 32 features each (a descriptor counts 16 bytes)
+                            umma_f8(s_at(b), a + 2 * c, q + (y * (G::kCols * 128) >> 4) + 2 * c, idesc, y + c > 0);
+                        if (y + 1 == HB) umma_commit(s_full(b));
                         umma_commit(k_empty(ks));
                     }
                     __syncwarp();
                     if (++ks == G::kKStages) { ks = 0; k_phase ^= 1u; }
                 }
-            };
-            scores(k);
-            for (int n = 0; n < count && ok; ++n, ++k) {
-                if (n + 1 < count) scores(k + 1);
-                const uint32_t ps = base + G::kPAt + (k & 1u) * G::kP;
+            }
+            ++unit;
+            next_unit(p, cur, part.places, piece_end);
+        }
+    } else if (warp == 2) {
+        // ================================ O^T += V^T P^T ================================
+        int vs = 0;
+        uint32_t v_phase = 0, k = 0, unit = 0;
+        const uint32_t idesc = make_idesc(G::kCols) | (1u << 15) | (1u << 16);
+        typedef TileAt<2, kApart> lay;
+        while (ok && cur.at < piece_end) {
+            const UnitPart part = unit_part(p, cur, piece_end);
+            if (part.count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
+            for (int n = 0; n < part.count && ok; ++n, ++k) {
+                const uint32_t x = k & 1u;
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     wait(v_full(vs), v_phase);
                     if (!ok) break;
-                    const uint32_t va = v_at(vs);
-                    clean_tile<DB, kApart>(t, all, key_tile(t, begin + n) * kTcTile, va, sus, lane);
-                    if (y == 0) wait(p_ready(k & 1u), (k >> 1) & 1u);
+                    if (y == 0) wait(p_ready(x), (k >> 1) & 1u);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint64_t a = mn_desc(v_at(vs), lay::block, lay::group), b = mn_desc(base + G::kPAt + x * G::kP, 0, 1024);
+                    const uint32_t d = o_at(unit & 1u, x) + y * G::kCols;
                     if (elect_one()) {
 #pragma unroll
-                        for (int c = 0; c < 8; ++c)
-                            umma_bf16(o_at(unit & 1u, k & 1u) + y * G::kCols, mn_desc(va + c * 2 * lay::group, lay::block, lay::group), mn_desc(ps + c * 2048, 0, 1024), idesc_o,
-                                      n >= 2 || c > 0);
-                        if (y + 1 == HB) umma_commit(pv_done(k & 1u));
+                        for (int c = 0; c < 8; ++c)        // 16 keys each
+                            umma_bf16(d, a + (c * 2 * lay::group >> 4), b + (c * 2048 >> 4), idesc, n >= 2 || c > 0);
+                        if (y + 1 == HB) umma_commit(pv_done(x));
                         umma_commit(v_empty(vs));
                     }
                     __syncwarp();
@@ -268,72 +323,104 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 }
             }
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
+            next_unit(p, cur, part.places, piece_end);
         }
-    } else if (warp < 4) {
-        // ================================ queries, a unit ahead ================================
-        uint32_t unit = 0;
-        bool ok = true;
+    } else if (warp == 3) {
+        // ================================ scales of the tiles ================================
+        // A lane's four keys of a tile lie in one page (page sizes are multiples of 8) and their scales in one word.  V rows that must
+        // not reach the product get scale byte 0 here (their probabilities are 0, and the codes times 2^-127 are finite): those no
+        // row sees, and rows of NaN that some see and others do not (remembered: the output of those that do is NaN).
+        uint32_t unit = 0, k = 0;
+        int rs = 0;
+        uint32_t r_phase = 0;
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
-            if (part.count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            const int begin = part.begin, count = part.count;
+            if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
-            const int u = unit & 1;
-            if (unit >= 2) {
-                ok = __all_sync(0xffffffffu, mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws));
-                if (!ok) break;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const int u = unit & 1, h = cur.h;
+            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
+            const int lo = all.differ ? max(t.lo, all.all_lo) : t.lo, hi = all.differ ? min(t.hi, all.all_hi) : t.hi;     // tiles in here: all is seen by all
+            auto find = [&](int n, int &row) {
+                const int j = n < count ? key_tile(t, begin + n) * kTcTile + lane * 4 : t.hi;
+                row = 0;
+                if (!((j < t.hi && j + 4 > t.lo) || j < t.s1)) return -1;
+                const int pg = fast_div(j, p.b.page);
+                row = j - pg * p.b.page.d;
+                return __ldg(table + pg);
+            };
+            auto load = [&](int entry, int row, uint32_t &kw, uint32_t &vw) {      // (no page: zeros, as its codes)
+                kw = vw = 0;
+                if ((unsigned)entry < (unsigned)p.b.n_pages) {
+                    const int64_t at = ((int64_t)entry * p.Hk + h) * p.b.page.d + row;
+                    kw = __ldg(reinterpret_cast<const uint32_t *>(p.k_scale + at));
+                    vw = __ldg(reinterpret_cast<const uint32_t *>(p.v_scale + at));
+                }
+            };
+            int row, entry = find(0, row);
+            uint32_t kw, vw, kn, vn;
+            load(entry, row, kw, vw);
+            entry = find(1, row);
+            if (unit >= 2) wait(unit_end(u), ((unit >> 1) - 1u) & 1u);             // (the suspects of the unit before the last)
+            if (lane == 0) suspects[u].n = 0;
+            __syncwarp();
+            for (int n = 0; n < count && ok; ++n, ++k) {
+                load(entry, row, kn, vn);
+                entry = find(n + 2, row);
+                const uint32_t b = k & 3u;
+                wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
+                sh_ks[b][lane] = kw;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_full(b));
+                const int j0 = key_tile(t, begin + n) * kTcTile;
+                if (j0 < lo || j0 + kTcTile > hi) vw = mend_scales(t, all, j0, vw, suspects[u], lane);
+#pragma unroll
+                for (int y = 0; y < HB; ++y) {
+                    wait(raw_empty(rs), r_phase ^ 1u);
+                    sh_vs[rs][lane] = vw;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(raw_full(rs));
+                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
+                }
+                kw = kn;
+                vw = vn;
             }
-            load_query_parts<HB, NR>(p, cur.start, cur.h, t.r0, t.rows, base + G::kQAt + u * G::kQ, sh_rf[u], tid - 64);
-            for (int r = tid - 64; r < NR; r += 64) {
-                const int pos = cur.pre + fast_div(t.r0 + min(r, t.rows - 1), p.gdiv);
-                sh_hi[u][r] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : t.hi;
-                sh_lo[u][r] = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
-            }
-            mbar_arrive(q_ready(u));
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
+            next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp < 12) {
         // ================================ softmax: a thread per key, two warpgroups in turn ================================
         const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
         const int bar_id = 1 + x;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t s_tm = s_at(x) + lanes;
         const uint32_t p_row = base + G::kPAt + x * G::kP + wt * 128;
         uint32_t k0 = 0, unit = 0;
-        bool ok = true;
         float l[NR];
         while (cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const int u = unit & 1;
             const uint32_t o_tm = o_at(u, x) + lanes;
             float *sh_m = sh_ms[u][x];
-            if (unit >= 2) ok = mbar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws);
+            if (unit >= 2) ok = bar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws);
             if (wg_any(bar_id, !ok)) break;
             if (wt < NR) sh_m[wt] = kNone;
             wg_sync(bar_id);
 #pragma unroll
             for (int r = 0; r < NR; ++r) l[r] = 0.f;
             const int n0 = (int)((k0 & 1u) ^ (uint32_t)x); // this warpgroup's tiles: n0, n0 + 2, ..
-            // the key's scale, one of the warpgroup's tiles ahead; its page, two
-            auto find = [&](int n) { return find_keys<1>(p, t, n < count, begin + n, cur.s, wq * 32, lane); };
-            uint32_t scale_now[1], scale_next[1];
-            KeyPlaces<1> place = find(n0);
-            load_scales(p, p.k_scale, place, cur.h, scale_now);
-            place = find(n0 + 2);
+#pragma unroll 1
             for (int n = n0; n < count; n += 2) {
-                const uint32_t k = k0 + n;
-                load_scales(p, p.k_scale, place, cur.h, scale_next);
-                place = find(n + 4);
-                ok = mbar_wait(s_full(x), (k >> 1) & 1u, abort_flag, ws);
+                const uint32_t k = k0 + n, b = k & 3u;
+                const uint32_t s_tm = s_at(b) + lanes;
+                ok = bar_wait(s_full(b), (k >> 2) & 1u, abort_flag, ws);
                 __syncwarp();
                 tc_fence_after();
-                const float kf = q8_factor(scale_now[0] & 255u);           // (a key that no row sees: any)
-                scale_now[0] = scale_next[0];
+                const float kf = q8_factor((sh_ks[b][wt >> 2] >> (8 * (wt & 3))) & 255u);
                 const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + wt;
                 const bool whole = j0 >= all.all_lo && j0 + kTcTile <= all.all_hi;
                 uint32_t seen = 0;                         // by which rows, where not by all
@@ -376,7 +463,9 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     for (int i = 1; i < NR; ++i) top = fmaxf(top, s[i]);
                     grown = wg_any(bar_id, top > 8.f || !ok);
                 }
-                if (grown) {
+                // the product of this warpgroup's tile before is done: P and the accumulator are its own again
+                if (k >= 2) ok = bar_wait(pv_done(x), ((k >> 1) - 1u) & 1u, abort_flag, ws) && ok;
+                if (__builtin_expect(grown, false)) {
                     // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
                     if (wg_any(bar_id, !ok)) { ok = false; break; }
                     load();
@@ -404,7 +493,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                             const float4 c = *reinterpret_cast<const float4 *>(&sh_c[x][r]);
                             l[r] *= c.x; l[r + 1] *= c.y; l[r + 2] *= c.z; l[r + 3] *= c.w;
                         }
-                        // (the product of this warpgroup's last tile is done: S of this one came after it)
+                        tc_fence_after();
 #pragma unroll 1
                         for (int r0 = 0; r0 < HB * G::kCols; r0 += 16) {
                             float o[16];
@@ -416,28 +505,28 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                         }
                         tmem_wait_st();
                     }
-                }
-                // ---- probabilities of the key -> its row of P
-                if (grown) {
                     load();
                     against_max();
                 }
+                // ---- the scores have been read; probabilities of the key -> its row of P
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_free(b));
 #pragma unroll
                 for (int c = 0; c < NR / 8; ++c) {
                     uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = 8 * c + 2 * i;
-                        const float a = ex2f(s[r]), b = ex2f(s[r + 1]);
+                        const float a = ex2f(s[r]), b2 = ex2f(s[r + 1]);
                         l[r] += a;
-                        l[r + 1] += b;
-                        split_bf16(a, b, hi[i], lo[i]);
+                        l[r + 1] += b2;
+                        split_bf16(a, b2, hi[i], lo[i]);
                     }
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_ready(x));
             }
@@ -447,65 +536,83 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             if (lane < NR) sh_wl[u][x][wq][lane] = sum;
             if (n0 < count) {
                 const uint32_t last = k0 + (uint32_t)(n0 + ((count - 1 - n0) & ~1));
-                ok = mbar_wait(pv_done(x), (last >> 1) & 1u, abort_flag, ws);
+                ok = bar_wait(pv_done(x), (last >> 1) & 1u, abort_flag, ws);
             }
             if (wg_any(bar_id, !ok)) break;
             tc_fence_before();
             if (lane == 0) mbar_arrive(acc_full(u));
             k0 += (uint32_t)count;
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
+            next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp >= 16) {
         // ================================ V: codes -> bf16 ================================
-        const int key0 = (warp - 16) * 32;
-        int rs = 0, vs = 0;
-        uint32_t r_phase = 0, v_phase = 0;
-        bool ok = true;
+        constexpr int kGroups = G::kTurners / 4;           // a group of four warps takes every kGroups-th stage
+        const int group = (warp - 16) >> 2, key0 = ((warp - 16) & 3) * 32;
+        uint32_t i = (uint32_t)group, end = 0;             // stages
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
-            const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
-            const Tile t = cur.t;
-            auto find = [&](int n) { return find_keys<1>(p, t, n < count, begin + n, cur.s, key0, lane); };
-            uint32_t now[1], next[1];
-            KeyPlaces<1> place = find(0);
-            load_scales(p, p.v_scale, place, cur.h, now);
-            place = find(1);
-            for (int n = 0; n < count && ok; ++n) {
-                load_scales(p, p.v_scale, place, cur.h, next);
-                place = find(n + 2);
+            const uint32_t begin = end;
+            end += (uint32_t)part.count * HB;
 #pragma unroll 1
-                for (int y = 0; y < HB; ++y) {
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(raw_full(rs), r_phase, abort_flag, ws));
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(v_empty(vs), v_phase ^ 1u, abort_flag, ws));
-                    if (!ok) break;
-                    turn_stage<DB, 1>(r_at(rs), v_at(vs), key0, min(p.D, 128), p.D - 128 * y, now, lane);
-                    if (lane == 0) {
-                        mbar_arrive(v_full(vs));
-                        mbar_arrive(raw_empty(rs));
-                    }
-                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
-                    if ((vs ^= 1) == 0) v_phase ^= 1u;
+            for (; i < end && ok; i += kGroups) {
+                const uint32_t rs = i % G::kRawStages, vs = i & 1u;
+                wait(raw_full(rs), (i / G::kRawStages) & 1u);
+                wait(v_empty(vs), ((i >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+                uint32_t scale[1] = {(sh_vs[rs][(key0 + lane) >> 2] >> (8 * (lane & 3))) & 255u};
+                turn_stage<2, 1>(r_at(rs), v_at(vs), key0, min(p.D, 128), HB == 1 ? p.D : p.D - 128 * (int)((i - begin) & 1u), scale, lane);
+                if (lane == 0) {
+                    mbar_arrive(v_full(vs));
+                    mbar_arrive(raw_empty(rs));
                 }
-                now[0] = next[0];
             }
-            leave_unit(p, cur, part.places, piece_end);
+            next_unit(p, cur, part.places, piece_end);
         }
     } else {
-        // ================================ units' ends: both accumulators joined, written, pieces joined ================================
+        // ================================ queries, a unit ahead; units' ends ================================
         const int wq = warp & 3, wt = wq * 32 + lane;
         const int bar_id = 3;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
         uint32_t k0 = 0, unit = 0;
-        bool ok = true;
-        while (cur.at < piece_end) {
+        auto to_tiles = [&](Cursor<NR, kTcTile> &c) {      // on to a unit that this piece has tiles of
+            while (c.at < piece_end) {
+                const UnitPart part = unit_part(p, c, piece_end);
+                if (part.count > 0) break;
+                next_unit(p, c, part.places, piece_end);
+            }
+        };
+        auto queries = [&](const Cursor<NR, kTcTile> &c, int u) {      // (the unit before the last has ended here: all of it may be reused)
+            load_query_parts<HB, NR>(p, c.start, c.h, c.t.r0, c.t.rows, base + G::kQAt + u * G::kQ, sh_rf[u], wt);
+            if (wt < NR) {
+                const int pos = c.pre + fast_div(c.t.r0 + min(wt, c.t.rows - 1), p.gdiv);
+                sh_hi[u][wt] = p.mask == MRP_ATTN_CAUSAL ? pos + 1 : c.t.hi;
+                sh_lo[u][wt] = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            }
+            mbar_arrive(q_ready(u));
+        };
+        to_tiles(cur);
+        Cursor<NR, kTcTile> ahead = cur;
+#pragma unroll 1
+        for (int first = 1; cur.at < piece_end; first = 0) {
+            if (!first) {
+                cur = ahead;
+                if (cur.at >= piece_end) break;
+            }
+            // (the first round loads the first unit's queries, every round the next one's)
+#pragma unroll 1
+            for (int y = first; y >= 0; --y) {
+                if (y == 0) {
+                    next_unit(p, ahead, unit_part(p, ahead, piece_end).places, piece_end);
+                    to_tiles(ahead);
+                }
+                if (ahead.at < piece_end) queries(ahead, (unit + 1 - y) & 1);
+            }
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const int u = unit & 1;
-            ok = mbar_wait(acc_full(u), (unit >> 1) & 1u, abort_flag, ws);
+            ok = bar_wait(acc_full(u), (unit >> 1) & 1u, abort_flag, ws);
             if (wg_any(bar_id, !ok)) break;
             bool has[2];
 #pragma unroll
@@ -575,8 +682,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 wg_sync(bar_id);
                 if (sh_last) {
                     const JoinArgs ja = join_args(p, cur.start, cur.h, t.r0, rows, c0, c1);
-                    if (rows <= 4) join_rows<NR, G::kWide, 1, 8>(ja, wq, lane);
-                    else join_rows<NR, G::kWide, 2, 4>(ja, wq, lane);
+                    join_rows<NR, G::kWide, 1, 4>(ja, wq, lane);          // (registers)
                     if (wt == 0) p.part.counters[c0] = 0;
                 }
             }
@@ -585,7 +691,6 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             wg_sync(bar_id);                           // sh_f, sh_out and sh_last are read
             k0 += (uint32_t)count;
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
         }
         if (wt == 0)                                   // (units are left over only where a wait gave up)
             settle_arrivals(p, cur, per, piece_end, [&](const Cursor<NR, kTcTile> &, int c0, int c1) {

@@ -26,6 +26,74 @@ template <int NB> struct Blocks {
 // queries (kPacked); pages of 8 bits (kCodes).
 enum { kApart = 0, kJoined = 1, kPacked = 2, kCodes = 3 };
 
+// What a role's loop does rarely stands outside of it: the loops of all roles have to stay in the instruction caches together.
+__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, int32_t *user_status)
+{
+    const WaitStatus ws = {status, user_status};
+    return mbar_wait(bar, parity, abort_flag, ws);
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, const WaitStatus &ws)
+{
+    return mbar_try_wait(bar, parity) || wait_longer(bar, parity, abort_flag, ws.status, ws.user_status);
+}
+template <int ROWS>
+__device__ __noinline__ void next_unit(const AttnParams &p, Cursor<ROWS, kTcTile> &c, int places, long long piece_end) { leave_unit(p, c, places, piece_end); }
+
+// find_piece for a warp on its own, of any number of sequences, in little code (twice through them).
+template <int ROWS>
+__device__ __noinline__ long long cut_line(const AttnParams &p, Cursor<ROWS, kTcTile> &c, long long &per, bool report)
+{
+    const int lane = threadIdx.x & 31;
+    auto tiles_of = [&](int s, bool tell) {
+        if (s >= p.b.n_seqs) return 0ll;
+        return sequence_tiles<ROWS, kTcTile>(p, s, tell);
+    };
+    long long total = 0, begin = 0, end = 0, done = 0;
+    c.s = -1;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+        for (int s0 = 0; s0 < p.b.n_seqs && c.s < 0; s0 += 32) {
+            const long long mine = tiles_of(s0 + lane, pass == 0 && report);
+            long long x = mine;            // inclusive sum over the lanes
+#pragma unroll
+            for (int w = 1; w < 32; w <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, w);
+                if (lane >= w) x += y;
+            }
+            const long long before = done + x - mine;
+            const uint32_t hit = __ballot_sync(0xffffffffu, pass == 1 && mine > 0 && before <= begin && begin < before + mine);
+            if (hit) {
+                c.s = s0 + __ffs(hit) - 1;
+                c.at = __shfl_sync(0xffffffffu, before, __ffs(hit) - 1);
+            }
+            done += __shfl_sync(0xffffffffu, x, 31);
+        }
+        if (pass == 0) {
+            total = done;
+            done = 0;
+            per = div_line(total + gridDim.x - 1, gridDim.x);
+            begin = per * blockIdx.x;
+            end = min(total, begin + per);
+            if (begin >= end) return 0;
+        }
+    }
+    kv_sequence(p.b, c.s, c.start, c.n, c.pre);
+    c.rt = -1;
+    long long next = c.at;
+    do {                                   // the row tile
+        c.at = next;
+        c.t = row_tile<ROWS, kTcTile>(p, c.n, c.pre, ++c.rt);
+        next = c.at + (long long)(c.t.tiles + p.lead) * p.Hk;
+    } while (next <= begin);
+    const int in = (int)(begin - c.at);
+    c.h = in / (c.t.tiles + p.lead);
+    c.i = in - c.h * (c.t.tiles + p.lead);
+    c.at = begin;
+    c.unit = begin - c.i;
+    return end - begin;
+}
+
 struct Suspects {                          // boundary tiles with V rows that were zeroed for what they held
     int n;
     int base[kMaxSuspects];
@@ -338,35 +406,29 @@ __device__ __forceinline__ void turn_stage(uint32_t from, uint32_t to, int key0,
     }
     const uint32_t s0 = ((2 * q) ^ kk) << 4, s1 = ((2 * q + 1) ^ kk) << 4;
     // (a short loop: the roles of a kernel share the instruction caches.  Unrolled it took twice as long)
-    uint32_t c[DB][4], next[DB][4];
-    auto load = [&](uint32_t off) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(next[d][0]), "=r"(next[d][1]), "=r"(next[d][2]), "=r"(next[d][3]) : "r"(load_at[d] + off) : "memory");
-    };
-    load(0);
-    uint32_t off = 0;
 #pragma unroll 1
-    for (int r = 0; r < N; ++r) {
+    for (int r = 0; r < N; r += 2) {
+        uint32_t c[2][DB][4], f[2];
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) c[d][z] = next[d][z];
-        off += r + 1 < N ? 8 * pitch : 0;
-        load(off);
-        uint32_t f = own[0].f;
-        if (KR == 2) f = r < 4 ? own[0].f : own[KR - 1].f;
-        f = __shfl_sync(0xffffffffu, f, (r & 3) * 8 + kk);
+            for (int d = 0; d < DB; ++d)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[e][d][0]), "=r"(c[e][d][1]), "=r"(c[e][d][2]), "=r"(c[e][d][3])
+                             : "r"(load_at[d] + (r + e) * 8 * pitch) : "memory");
+        const uint32_t fo = KR == 2 && r >= 4 ? own[KR - 1].f : own[0].f;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            const uint32_t fd = in[d] ? f : 0u;
-            uint32_t o[8];
+        for (int e = 0; e < 2; ++e) f[e] = __shfl_sync(0xffffffffu, fo, ((r + e) & 3) * 8 + kk);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) turn_four(c[d][z], fd, o[2 * z], o[2 * z + 1]);
-            const uint32_t at = store_at[d] + r * 1024;
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + s0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + s1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
-        }
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const uint32_t fd = in[d] ? f[e] : 0u, at = store_at[d] + (r + e) * 1024;
+                uint32_t o[8];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) turn_four(c[e][d][z], fd, o[2 * z], o[2 * z + 1]);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + s0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + s1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+            }
     }
     if (large) {                                           // the second factor, over what this lane has stored
 #pragma unroll 1
@@ -468,6 +530,52 @@ __device__ __forceinline__ void clean_tile(const Tile &t, const Seen &a, int j0,
             for (int w = 0; w < 4; ++w) sus.keys[at_n][w] = found[w];
         }
         sus.n = at_n + 1;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+// The same as a short function, for apart tiles.
+template <int DB, typename Tile>
+__device__ __noinline__ void clean_rarely(const Tile &t, const Seen &a, int j0, uint32_t vs, Suspects &sus, int lane)
+{
+    typedef TileAt<DB, kApart> lay;
+    if (((j0 >= t.lo && j0 + kTcTile <= t.hi) || j0 + kTcTile <= t.s1) && (!a.differ || (j0 >= a.all_lo && j0 + kTcTile <= a.all_hi))) return;
+    int slot = -1;
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+        const int row = w * 32 + lane, j = j0 + row;
+        const uint32_t at = vs + (row >> 3) * lay::group + (row & 7) * 128;
+        const bool seen = j < t.hi && (j >= t.lo || j < t.s1);
+        bool bad = false;
+        if (seen && a.differ && !(j >= a.all_lo && j < a.all_hi)) {
+#pragma unroll 2
+            for (int c = 0; c < 8 * DB; ++c) {
+                uint32_t u[4];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                             : "r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)) : "memory");
+#pragma unroll
+                for (int y = 0; y < 4; ++y) bad |= (u[y] & 0x7F800000u) == 0x7F800000u || (u[y] & 0x7F80u) == 0x7F80u;
+            }
+        }
+        const uint32_t found = __ballot_sync(0xffffffffu, bad);
+        if (!seen || bad)
+#pragma unroll 2
+            for (int c = 0; c < 8 * DB; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at + (c >> 3) * lay::block + (((c + lane) & 7) << 4)), "r"(0u) : "memory");
+        if (found) {
+            if (slot < 0) {
+                slot = sus.n;
+                __syncwarp();
+                if (lane == 0) {
+                    if (slot < kMaxSuspects) {
+                        sus.base[slot] = j0;
+                        sus.keys[slot][0] = sus.keys[slot][1] = sus.keys[slot][2] = sus.keys[slot][3] = 0;
+                    }
+                    sus.n = slot + 1;
+                }
+            }
+            if (lane == 0 && slot < kMaxSuspects) sus.keys[slot][w] = found;
+        }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
