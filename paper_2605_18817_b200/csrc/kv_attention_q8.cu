@@ -90,9 +90,16 @@ __device__ __forceinline__ void load_query_parts(const AttnParams &p, int start,
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// 4 bytes to shared memory, which arrive at the barrier when they are there (zeros where !on)
+__device__ __forceinline__ void copy_word(uint32_t dst, const void *src, bool on, uint32_t bar)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // The scale bytes of a lane's four keys of V at a boundary of what is seen: see the scales' warp.
 template <typename Tile>
-__device__ __noinline__ uint32_t mend_scales(const Tile &t, const Seen &a, int j0, uint32_t w, Suspects &sus, int lane)
+__device__ __noinline__ uint32_t mend_scales(const Tile &t, const Seen &a, int j0, uint32_t w, Suspects &sus, int lane, bool tell)
 {
     uint32_t keep = 0, bad = 0;
 #pragma unroll
@@ -103,7 +110,7 @@ __device__ __noinline__ uint32_t mend_scales(const Tile &t, const Seen &a, int j
         bad |= (uint32_t)some << e;
         keep |= seen && !some ? 255u << (8 * e) : 0u;
     }
-    if (__any_sync(0xffffffffu, bad != 0)) {
+    if (tell && __any_sync(0xffffffffu, bad != 0)) {
         const int slot = sus.n;
         __syncwarp();
         if (lane == 0) sus.n = slot + 1;
@@ -168,11 +175,11 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             mbar_init(k_empty(s), 1);
         }
         for (int s = 0; s < G::kRawStages; ++s) {
-            mbar_init(raw_full(s), 2);
+            mbar_init(raw_full(s), 33);
             mbar_init(raw_empty(s), 4);
         }
         for (int b = 0; b < 4; ++b) {
-            mbar_init(s_full(b), 2);
+            mbar_init(s_full(b), 33);
             mbar_init(s_free(b), 4);
         }
         for (int x = 0; x < 2; ++x) {
@@ -246,15 +253,29 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
                 }
             };
-            PageRef now = look_up<kCodes>(p, bx, cur.t, begin, cur.s, cur.start, lane), next = now, then = now;
-            if (count > 1) next = look_up<kCodes>(p, bx, cur.t, begin + 1, cur.s, cur.start, lane);
+            const Tile t = cur.t;
+            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
+            PageRun run = {INT_MIN, 0, 0};
+            auto find = [&](int n) {                       // the lane's box of a tile
+                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + lane * bx.rows, pg = fast_div(j, p.b.page);
+                const int entry = page_entry(p, table, run, fast_div(j0, p.b.page), pg, lane);
+                PageRef r;
+                r.need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
+                r.row = j - pg * p.b.page.d;
+                r.entry = entry;
+                return r;
+            };
+            PageRef now = find(0);
             fetch_k(now);
+#pragma unroll 1
             for (int n = 0; n < count && ok; ++n) {
-                if (n + 2 < count) then = look_up<kCodes>(p, bx, cur.t, begin + n + 2, cur.s, cur.start, lane);
-                if (n + 1 < count) fetch_k(next);
+                PageRef next = now;
+                if (n + 1 < count) {
+                    next = find(n + 1);
+                    fetch_k(next);
+                }
                 fetch_v(now);
                 now = next;
-                next = then;
             }
             next_unit(p, cur, part.places, piece_end);
         }
@@ -327,7 +348,8 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         }
     } else if (warp == 3) {
         // ================================ scales of the tiles ================================
-        // A lane's four keys of a tile lie in one page (page sizes are multiples of 8) and their scales in one word.  V rows that must
+        // A lane's four keys of a tile lie in one page (page sizes are multiples of 8) and their scales in one word, copied
+        // asynchronously (loaded into registers they cost their latency a tile: 64 ragged 151 us).  V rows that must
         // not reach the product get scale byte 0 here (their probabilities are 0, and the codes times 2^-127 are finite): those no
         // row sees, and rows of NaN that some see and others do not (remembered: the output of those that do is NaN).
         uint32_t unit = 0, k = 0;
@@ -342,49 +364,32 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             const int u = unit & 1, h = cur.h;
             const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
             const int lo = all.differ ? max(t.lo, all.all_lo) : t.lo, hi = all.differ ? min(t.hi, all.all_hi) : t.hi;     // tiles in here: all is seen by all
-            auto find = [&](int n, int &row) {
-                const int j = n < count ? key_tile(t, begin + n) * kTcTile + lane * 4 : t.hi;
-                row = 0;
-                if (!((j < t.hi && j + 4 > t.lo) || j < t.s1)) return -1;
-                const int pg = fast_div(j, p.b.page);
-                row = j - pg * p.b.page.d;
-                return __ldg(table + pg);
-            };
-            auto load = [&](int entry, int row, uint32_t &kw, uint32_t &vw) {      // (no page: zeros, as its codes)
-                kw = vw = 0;
-                if ((unsigned)entry < (unsigned)p.b.n_pages) {
-                    const int64_t at = ((int64_t)entry * p.Hk + h) * p.b.page.d + row;
-                    kw = __ldg(reinterpret_cast<const uint32_t *>(p.k_scale + at));
-                    vw = __ldg(reinterpret_cast<const uint32_t *>(p.v_scale + at));
-                }
-            };
-            int row, entry = find(0, row);
-            uint32_t kw, vw, kn, vn;
-            load(entry, row, kw, vw);
-            entry = find(1, row);
+            PageRun run = {INT_MIN, 0, 0};
             if (unit >= 2) wait(unit_end(u), ((unit >> 1) - 1u) & 1u);             // (the suspects of the unit before the last)
             if (lane == 0) suspects[u].n = 0;
             __syncwarp();
+#pragma unroll 1
             for (int n = 0; n < count && ok; ++n, ++k) {
-                load(entry, row, kn, vn);
-                entry = find(n + 2, row);
+                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + lane * 4, pg = fast_div(j, p.b.page);
+                const int entry = page_entry(p, table, run, fast_div(j0, p.b.page), pg, lane);
+                const bool on = ((j < t.hi && j + 4 > t.lo) || j < t.s1) && (unsigned)entry < (unsigned)p.b.n_pages;    // (no page: zeros, as its codes)
+                const int64_t at = on ? ((int64_t)entry * p.Hk + h) * p.b.page.d + (j - pg * p.b.page.d) : 0;
                 const uint32_t b = k & 3u;
                 wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
-                sh_ks[b][lane] = kw;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(s_full(b));
-                const int j0 = key_tile(t, begin + n) * kTcTile;
-                if (j0 < lo || j0 + kTcTile > hi) vw = mend_scales(t, all, j0, vw, suspects[u], lane);
+                copy_word(smem_u32(&sh_ks[b][lane]), p.k_scale + at, on, s_full(b));
+                const bool inside = j0 >= lo && j0 + kTcTile <= hi;
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     wait(raw_empty(rs), r_phase ^ 1u);
-                    sh_vs[rs][lane] = vw;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(raw_full(rs));
+                    if (inside) {
+                        copy_word(smem_u32(&sh_vs[rs][lane]), p.v_scale + at, on, raw_full(rs));
+                    } else {
+                        uint32_t w = on ? __ldg(reinterpret_cast<const uint32_t *>(p.v_scale + at)) : 0u;
+                        sh_vs[rs][lane] = mend_scales(t, all, j0, w, suspects[u], lane, y == 0);
+                        mbar_arrive(raw_full(rs));
+                    }
                     if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
                 }
-                kw = kn;
-                vw = vn;
             }
             ++unit;
             next_unit(p, cur, part.places, piece_end);
