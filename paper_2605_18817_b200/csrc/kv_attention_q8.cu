@@ -9,7 +9,7 @@
 //   Turning K too would move 3 bytes more through shared memory for each of its codes, which then bounds the kernel instead of
 //   memory: TMA, warps and MMAs move 88 of 128 bytes a cycle at the memory's rate as it is.
 //
-//   warp 0   K and V tiles by TMA      warp 1   S MMAs      warp 2   PV MMAs      warp 3   the tiles' scales
+//   warp 0   K by TMA, and its scales      warp 1   S MMAs      warp 2   PV MMAs      warp 3   V and its scales
 //   warps 4-7, 8-11   softmax: two warpgroups that take tiles in turn, a thread per key
 //   warps 12-15   queries, a unit ahead, and units' ends          from warp 16 on   V's codes -> bf16 (8 rows: two groups of four warps, a stage each)
 // Instructions bound it next to memory, so each role's loop is short: the roles of an SM quarter share its instruction cache and
@@ -227,56 +227,94 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag, ws)); };   // a warp's
 
-    if (warp == 0) {
-        // ================================ K and V tiles ================================
-        int ks = 0, rs = 0;
-        uint32_t k_phase = 0, r_phase = 0;
+    if (warp == 0 || warp == 3) {
+        // ================================ K (warp 0), V (warp 3): tiles and their scales ================================
+        // A lane has a box of one of the next tiles (32 lanes: 2 to 32 tiles), so that what it takes to find a page, and its latency,
+        // comes once a box and not once a lane and tile (64 ragged single tokens 137 us so).  Scales go a word of four keys a lane,
+        // copied asynchronously.  V rows that must not reach the product get scale byte 0 here (their probabilities are 0, and the
+        // codes times 2^-127 are finite): those no row sees, and rows of NaN that some see and others do not (remembered: the
+        // output of those that do is NaN).
+        const bool v = warp == 3;
+        const uint8_t *scale = v ? p.v_scale : p.k_scale;
+        const int pitch = v ? min(p.D, 128) : 128, stages = v ? G::kRawStages : G::kKStages;
+        const uint32_t at = v ? r_at(0) : k_at(0), full = v ? raw_full(0) : k_full(0), empty = v ? raw_empty(0) : k_empty(0);
+        const int log_rows = 31 - __clz(bx.rows), log_boxes = 7 - log_rows, boxes = 1 << log_boxes, tiles = 32 >> log_boxes;
+        const int my_tile = lane >> log_boxes, my_box = lane & (boxes - 1);
+        uint32_t unit = 0, k = 0, phase = 0;
+        int stage = 0;
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
             if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
-            auto fetch_k = [&](const PageRef &r) {
-#pragma unroll
-                for (int y = 0; y < HB; ++y) {
-                    wait(k_empty(ks), k_phase ^ 1u);
-                    if (!ok) return;
-                    fetch_codes(p, &kmap, bx, r, cur.h, 128 * y, 128, k_at(ks), k_full(ks), lane);
-                    if (++ks == G::kKStages) { ks = 0; k_phase ^= 1u; }
-                }
-            };
-            auto fetch_v = [&](const PageRef &r) {
-#pragma unroll
-                for (int y = 0; y < HB; ++y) {
-                    wait(raw_empty(rs), r_phase ^ 1u);
-                    if (!ok) return;
-                    fetch_codes(p, &vmap, bx, r, cur.h, 128 * y, min(p.D, 128), r_at(rs), raw_full(rs), lane);
-                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
-                }
-            };
             const Tile t = cur.t;
+            const Seen all = seen_by_all(p, t, cur.pre);
+            const int u = unit & 1, h = cur.h;
             const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
-            PageRun run = {INT_MIN, 0, 0};
-            auto find = [&](int n) {                       // the lane's box of a tile
-                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + lane * bx.rows, pg = fast_div(j, p.b.page);
-                const int entry = page_entry(p, table, run, fast_div(j0, p.b.page), pg, lane);
-                PageRef r;
-                r.need = lane * bx.rows < kTcTile && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1);
-                r.row = j - pg * p.b.page.d;
-                r.entry = entry;
-                return r;
+            const int lo = all.differ ? max(t.lo, all.all_lo) : t.lo, hi = all.differ ? min(t.hi, all.all_hi) : t.hi;     // tiles in here: all is seen by all
+            struct Box {
+                int entry, row;                            // entry -1: not needed
             };
-            PageRef now = find(0);
-            fetch_k(now);
-#pragma unroll 1
-            for (int n = 0; n < count && ok; ++n) {
-                PageRef next = now;
-                if (n + 1 < count) {
-                    next = find(n + 1);
-                    fetch_k(next);
+            auto find = [&](int n) {                       // the lane's box of tiles n ..
+                const int j = key_tile(t, begin + n + my_tile) * kTcTile + (my_box << log_rows);
+                Box b = {-1, 0};
+                if (n + my_tile < count && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1)) {
+                    const int pg = fast_div(j, p.b.page);
+                    b.row = j - pg * p.b.page.d;
+                    b.entry = __ldg(table + pg);
+                    if (b.entry < 0) b.entry = p.b.n_pages;
                 }
-                fetch_v(now);
-                now = next;
+                return b;
+            };
+            Box next = find(0);
+            if (v) {
+                if (unit >= 2) wait(unit_end(u), ((unit >> 1) - 1u) & 1u);         // (the suspects of the unit before the last)
+                if (lane == 0) suspects[u].n = 0;
+                __syncwarp();
             }
+#pragma unroll 1
+            for (int n0 = 0; n0 < count && ok; n0 += tiles) {
+                const Box box = next;
+                const bool need = box.entry >= 0, fine = need && box.entry < p.b.n_pages;
+                if (need && !fine) kv_bad_index(p.b);
+                const int page = fine ? box.entry : p.b.n_pages;                   // (a page that is not one: outside the map, zeros arrive)
+                const int64_t scales = fine ? ((int64_t)box.entry * p.Hk + h) * p.b.page.d + box.row : -1;
+                const uint32_t needed = __ballot_sync(0xffffffffu, need);
+                if (n0 + tiles < count) next = find(n0 + tiles);
+#pragma unroll 1
+                for (int i = 0; i < min(tiles, count - n0) && ok; ++i, ++k) {
+                    const uint32_t here = (needed >> (i << log_boxes)) & (uint32_t)((1ull << boxes) - 1);
+                    // the word of the lane's keys 4 l .. 4 l + 3 (no page, not needed: zeros, as its codes or whatever they are)
+                    const int64_t from = __shfl_sync(0xffffffffu, scales, (i << log_boxes) | ((lane * 4) >> log_rows));
+                    const uint8_t *word = scale + (from < 0 ? 0 : from + ((lane * 4) & (bx.rows - 1)));
+                    if (!v) {
+                        const uint32_t b = k & 3u;
+                        wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
+                        copy_word(smem_u32(&sh_ks[b][lane]), word, from >= 0, s_full(b));
+                    }
+#pragma unroll
+                    for (int y = 0; y < HB; ++y) {
+                        const uint32_t bar = full + 8 * stage;
+                        wait(empty + 8 * stage, phase ^ 1u);
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect_tx(bar, __popc(here) * (uint32_t)(bx.rows * pitch));
+                        __syncwarp();
+                        if (my_tile == i && need)
+                            tma_load_page(at + stage * 16384 + (my_box << log_rows) * pitch, v ? &vmap : &kmap, 128 * y, box.row, h, page, bar);
+                        if (v) {
+                            const int j0 = key_tile(t, begin + n0 + i) * kTcTile;
+                            if (j0 >= lo && j0 + kTcTile <= hi) {
+                                copy_word(smem_u32(&sh_vs[stage][lane]), word, from >= 0, bar);
+                            } else {
+                                const uint32_t w = from >= 0 ? __ldg(reinterpret_cast<const uint32_t *>(word)) : 0u;
+                                sh_vs[stage][lane] = mend_scales(t, all, j0, w, suspects[u], lane, y == 0);
+                                mbar_arrive(bar);
+                            }
+                        }
+                        if (++stage == stages) { stage = 0; phase ^= 1u; }
+                    }
+                }
+            }
+            ++unit;
             next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp == 1) {
@@ -341,54 +379,6 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     }
                     __syncwarp();
                     if ((vs ^= 1) == 0) v_phase ^= 1u;
-                }
-            }
-            ++unit;
-            next_unit(p, cur, part.places, piece_end);
-        }
-    } else if (warp == 3) {
-        // ================================ scales of the tiles ================================
-        // A lane's four keys of a tile lie in one page (page sizes are multiples of 8) and their scales in one word, copied
-        // asynchronously (loaded into registers they cost their latency a tile: 64 ragged 151 us).  V rows that must
-        // not reach the product get scale byte 0 here (their probabilities are 0, and the codes times 2^-127 are finite): those no
-        // row sees, and rows of NaN that some see and others do not (remembered: the output of those that do is NaN).
-        uint32_t unit = 0, k = 0;
-        int rs = 0;
-        uint32_t r_phase = 0;
-        while (ok && cur.at < piece_end) {
-            const UnitPart part = unit_part(p, cur, piece_end);
-            const int begin = part.begin, count = part.count;
-            if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
-            const Tile t = cur.t;
-            const Seen all = seen_by_all(p, t, cur.pre);
-            const int u = unit & 1, h = cur.h;
-            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
-            const int lo = all.differ ? max(t.lo, all.all_lo) : t.lo, hi = all.differ ? min(t.hi, all.all_hi) : t.hi;     // tiles in here: all is seen by all
-            PageRun run = {INT_MIN, 0, 0};
-            if (unit >= 2) wait(unit_end(u), ((unit >> 1) - 1u) & 1u);             // (the suspects of the unit before the last)
-            if (lane == 0) suspects[u].n = 0;
-            __syncwarp();
-#pragma unroll 1
-            for (int n = 0; n < count && ok; ++n, ++k) {
-                const int j0 = key_tile(t, begin + n) * kTcTile, j = j0 + lane * 4, pg = fast_div(j, p.b.page);
-                const int entry = page_entry(p, table, run, fast_div(j0, p.b.page), pg, lane);
-                const bool on = ((j < t.hi && j + 4 > t.lo) || j < t.s1) && (unsigned)entry < (unsigned)p.b.n_pages;    // (no page: zeros, as its codes)
-                const int64_t at = on ? ((int64_t)entry * p.Hk + h) * p.b.page.d + (j - pg * p.b.page.d) : 0;
-                const uint32_t b = k & 3u;
-                wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
-                copy_word(smem_u32(&sh_ks[b][lane]), p.k_scale + at, on, s_full(b));
-                const bool inside = j0 >= lo && j0 + kTcTile <= hi;
-#pragma unroll
-                for (int y = 0; y < HB; ++y) {
-                    wait(raw_empty(rs), r_phase ^ 1u);
-                    if (inside) {
-                        copy_word(smem_u32(&sh_vs[rs][lane]), p.v_scale + at, on, raw_full(rs));
-                    } else {
-                        uint32_t w = on ? __ldg(reinterpret_cast<const uint32_t *>(p.v_scale + at)) : 0u;
-                        sh_vs[rs][lane] = mend_scales(t, all, j0, w, suspects[u], lane, y == 0);
-                        mbar_arrive(raw_full(rs));
-                    }
-                    if (++rs == G::kRawStages) { rs = 0; r_phase ^= 1u; }
                 }
             }
             ++unit;

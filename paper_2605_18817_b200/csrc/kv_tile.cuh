@@ -280,24 +280,6 @@ __device__ __forceinline__ PageRef look_up(const AttnParams &p, const PageBoxes 
     return r;
 }
 
-// The page entries of a sequence, 64 of them in a warp's registers, so that no tile waits for its own: lane l has entries base + l and
-// base + 32 + l, the second 32 loaded while the first are in use.  For whole warps; a tile lies in 17 pages at most.
-struct PageRun {
-    int base, now, next;
-};
-__device__ __forceinline__ int page_entry(const AttnParams &p, const int32_t *table, PageRun &r, int first, int page, int lane)
-{
-    if ((unsigned)(first - r.base) >= 32u) {               // `first`: the tile's first page
-        const bool on = (unsigned)(first - r.base) < 64u;
-        r.base = on ? r.base + 32 : first;
-        r.now = on ? r.next : __ldg(table + min(first + lane, p.b.max_pages - 1));
-        r.next = __ldg(table + min(r.base + 32 + lane, p.b.max_pages - 1));
-    }
-    const int i = page - r.base;
-    const int a = __shfl_sync(0xffffffffu, r.now, i & 31), b = __shfl_sync(0xffffffffu, r.next, i & 31);
-    return i < 32 ? a : b;
-}
-
 // The pages of a K or V tile's visible positions, 64 DB features from `feature` on -> a ring stage; the whole warp.
 template <int DB, int LAY>
 __device__ __forceinline__ void fetch_tile(const AttnParams &p, const CUtensorMap *map, const PageBoxes &bx, const PageRef &r, int h, int feature,
