@@ -24,14 +24,15 @@ namespace {
 template <int HB, int ROWS> struct FewQ8Geo {
     static constexpr int NR = ROWS;
     static constexpr int kCols = 2 * NR;                   // columns of S (hi, lo of Q), of P (hi, lo) and of an accumulator
-    static constexpr int kKStages = 3, kRawStages = HB == 1 ? 4 : 3;       // of 128 keys, 128 codes
+    // of 128 keys, 128 codes: as much in flight as there is room for (three and four: 64 ragged 139 us)
+    static constexpr int kKStages = 4, kRawStages = HB + NR / 8 == 2 ? 5 : HB + NR / 8 == 3 ? 4 : 3;
     static constexpr int kRawAt = kKStages * 16384;
     static constexpr int kVAt = kRawAt + kRawStages * 16384;               // two stages of bf16 V
-    static constexpr int kP = 128 * 128;                   // P of a warpgroup: 128 keys, rows of 128 bytes
+    static constexpr int kPRow = kCols * 2, kP = 128 * kPRow;              // P of a warpgroup: 128 keys, rows of 32 or 64 swizzled bytes
     static constexpr int kQ = HB * kCols * 128;            // queries of a unit, two of them
     static constexpr int kPAt = kVAt + 2 * 32768, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
-    static constexpr int kTmem = HB == 2 && NR == 16 ? 512 : 256;          // of which 4 kCols (S) + 4 HB kCols are used
+    static constexpr int kTmem = NR == 16 ? 512 : 256;     // of which 8 kCols (S) + 4 HB kCols are used
     static constexpr int kTurners = NR == 8 ? 8 : 4;       // warps (16 rows: the softmax needs the registers)
     static constexpr int kThreads = 512 + 32 * kTurners;
     static constexpr int kWide = HB * 128;                 // features of a row of partial results
@@ -90,6 +91,12 @@ __device__ __forceinline__ void load_query_parts(const AttnParams &p, int start,
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// P^T as the B operand: rows (keys) of 32 or 64 bytes, MN-major, swizzled over as many
+template <int ROW> __device__ __forceinline__ uint64_t p_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(8 * ROW >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)(ROW == 32 ? 6 : 4) << 61;
+}
+
 // 4 bytes to shared memory, which arrive at the barrier when they are there (zeros where !on)
 __device__ __forceinline__ void copy_word(uint32_t dst, const void *src, bool on, uint32_t bar)
 {
@@ -137,7 +144,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     __shared__ Cursor<NR, kTcTile> sh_cur;                 // where this CTA's piece of the line begins, its length, a full piece's
     __shared__ long long sh_len, sh_per;
     __shared__ Suspects suspects[2];
-    __shared__ uint32_t sh_ks[4][32], sh_vs[G::kRawStages][32];            // scale bytes of the keys of a tile's K (by S buffer), of a raw stage
+    __shared__ uint32_t sh_ks[8][32], sh_vs[G::kRawStages][32];            // scale bytes of the keys of a tile's K (by S buffer), of a raw stage
     __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
     __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR], sh_rf[2][NR];     // maximum in use (unit, warpgroup), factor to it; rows' factors
     __shared__ float sh_wm[2][4][NR], sh_wl[2][2][4][NR];  // row maxima and (of a unit) sums of the warps
@@ -154,18 +161,18 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     auto k_full = [&](int s) { return bars + 8 * s; };
     auto k_empty = [&](int s) { return bars + 8 * (4 + s); };
     auto raw_full = [&](int s) { return bars + 8 * (8 + s); };     // the codes, and their scales
-    auto raw_empty = [&](int s) { return bars + 8 * (12 + s); };
-    auto v_full = [&](int s) { return bars + 8 * (16 + s); };
-    auto v_empty = [&](int s) { return bars + 8 * (18 + s); };
-    auto s_full = [&](int b) { return bars + 8 * (20 + b); };      // the scores of a tile, and the keys' scales
-    auto s_free = [&](int b) { return bars + 8 * (24 + b); };
+    auto raw_empty = [&](int s) { return bars + 8 * (14 + s); };
+    auto v_full = [&](int s) { return bars + 8 * (20 + s); };
+    auto v_empty = [&](int s) { return bars + 8 * (22 + s); };
+    auto s_full = [&](int b) { return bars + 8 * (40 + b); };      // the scores of a tile, and the keys' scales
+    auto s_free = [&](int b) { return bars + 8 * (48 + b); };
     auto p_ready = [&](int x) { return bars + 8 * (28 + x); };
     auto pv_done = [&](int x) { return bars + 8 * (30 + x); };
     auto q_ready = [&](int x) { return bars + 8 * (32 + x); };
     auto unit_end = [&](int x) { return bars + 8 * (34 + x); };    // the unit is written: everything of it may be reused
     auto acc_full = [&](int x) { return bars + 8 * (36 + x); };    // the unit's sums, maxima and accumulators are there
     unsigned char *gbars = smem_raw + (base - smem_u32(smem_raw)) + G::kBars;
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 40);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(gbars + 8 * 56);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     const WaitStatus ws = {p.b.status, p.b.user_status};
 
@@ -178,7 +185,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             mbar_init(raw_full(s), 33);
             mbar_init(raw_empty(s), 4);
         }
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < 8; ++b) {
             mbar_init(s_full(b), 33);
             mbar_init(s_free(b), 4);
         }
@@ -189,7 +196,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             mbar_init(pv_done(x), 1);
             mbar_init(q_ready(x), 128);
             mbar_init(unit_end(x), 4);
-            mbar_init(acc_full(x), 8);
+            mbar_init(acc_full(x), 9);
         }
         *abort_flag = 0;
         prefetch_tmap(&kmap);
@@ -215,9 +222,9 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;    // four buffers of S, then the warpgroups' accumulators of two units
+    const uint32_t tmem = *tmem_holder;    // eight buffers of S, then the warpgroups' accumulators of two units
     auto s_at = [&](int b) { return tmem + b * G::kCols; };        // (columns: the upper parts of the rows, the lower ones)
-    auto o_at = [&](int u, int x) { return tmem + 4 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
+    auto o_at = [&](int u, int x) { return tmem + 8 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
     pdl_wait();
     pdl_trigger();
 
@@ -225,6 +232,13 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     const long long per = sh_per, piece_end = sh_len > 0 ? cur.at + sh_len : 0;
     if (sh_len == 0) cur.at = 0;
     bool ok = true;
+    auto to_tiles = [&](Cursor<NR, kTcTile> &c) {          // on to a unit that this piece has tiles of
+        while (c.at < piece_end) {
+            const UnitPart part = unit_part(p, c, piece_end);
+            if (part.count > 0) break;
+            next_unit(p, c, part.places, piece_end);
+        }
+    };
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag, ws)); };   // a warp's
 
     if (warp == 0 || warp == 3) {
@@ -242,30 +256,30 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         const int my_tile = lane >> log_boxes, my_box = lane & (boxes - 1);
         uint32_t unit = 0, k = 0, phase = 0;
         int stage = 0;
+        struct Box {
+            int entry, row;                                // entry -1: not needed
+        };
+        auto find = [&](const Cursor<NR, kTcTile> &c, const UnitPart &part, int n) {       // the lane's box of tiles n ..
+            const int j = key_tile(c.t, part.begin + n + my_tile) * kTcTile + (my_box << log_rows);
+            Box b = {-1, 0};
+            if (n + my_tile < part.count && ((j < c.t.hi && j + bx.rows > c.t.lo) || j < c.t.s1)) {
+                const int pg = fast_div(j, p.b.page);
+                b.row = j - pg * p.b.page.d;
+                b.entry = __ldg(p.b.page_table + (size_t)c.s * p.b.max_pages + pg);
+                if (b.entry < 0) b.entry = p.b.n_pages;
+            }
+            return b;
+        };
+        to_tiles(cur);
+        Box next = {-1, 0};
+        if (cur.at < piece_end) next = find(cur, unit_part(p, cur, piece_end), 0);
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { next_unit(p, cur, part.places, piece_end); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const int u = unit & 1, h = cur.h;
-            const int32_t *table = p.b.page_table + (size_t)cur.s * p.b.max_pages;
             const int lo = all.differ ? max(t.lo, all.all_lo) : t.lo, hi = all.differ ? min(t.hi, all.all_hi) : t.hi;     // tiles in here: all is seen by all
-            struct Box {
-                int entry, row;                            // entry -1: not needed
-            };
-            auto find = [&](int n) {                       // the lane's box of tiles n ..
-                const int j = key_tile(t, begin + n + my_tile) * kTcTile + (my_box << log_rows);
-                Box b = {-1, 0};
-                if (n + my_tile < count && ((j < t.hi && j + bx.rows > t.lo) || j < t.s1)) {
-                    const int pg = fast_div(j, p.b.page);
-                    b.row = j - pg * p.b.page.d;
-                    b.entry = __ldg(table + pg);
-                    if (b.entry < 0) b.entry = p.b.n_pages;
-                }
-                return b;
-            };
-            Box next = find(0);
             if (v) {
                 if (unit >= 2) wait(unit_end(u), ((unit >> 1) - 1u) & 1u);         // (the suspects of the unit before the last)
                 if (lane == 0) suspects[u].n = 0;
@@ -279,7 +293,13 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 const int page = fine ? box.entry : p.b.n_pages;                   // (a page that is not one: outside the map, zeros arrive)
                 const int64_t scales = fine ? ((int64_t)box.entry * p.Hk + h) * p.b.page.d + box.row : -1;
                 const uint32_t needed = __ballot_sync(0xffffffffu, need);
-                if (n0 + tiles < count) next = find(n0 + tiles);
+                if (n0 + tiles < count) {
+                    next = find(cur, part, n0 + tiles);
+                } else {                                   // (the next unit's first boxes: their pages are known before this one's last tiles go)
+                    next_unit(p, cur, part.places, piece_end);
+                    to_tiles(cur);
+                    if (cur.at < piece_end) next = find(cur, unit_part(p, cur, piece_end), 0);
+                }
 #pragma unroll 1
                 for (int i = 0; i < min(tiles, count - n0) && ok; ++i, ++k) {
                     const uint32_t here = (needed >> (i << log_boxes)) & (uint32_t)((1ull << boxes) - 1);
@@ -287,8 +307,8 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     const int64_t from = __shfl_sync(0xffffffffu, scales, (i << log_boxes) | ((lane * 4) >> log_rows));
                     const uint8_t *word = scale + (from < 0 ? 0 : from + ((lane * 4) & (bx.rows - 1)));
                     if (!v) {
-                        const uint32_t b = k & 3u;
-                        wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
+                        const uint32_t b = k & 7u;
+                        wait(s_free(b), ((k >> 3) & 1u) ^ 1u);
                         copy_word(smem_u32(&sh_ks[b][lane]), word, from >= 0, s_full(b));
                     }
 #pragma unroll
@@ -315,7 +335,6 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 }
             }
             ++unit;
-            next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp == 1) {
         // ================================ S^T = K Q^T ================================
@@ -328,8 +347,8 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             const uint64_t q = make_smem_desc(base + G::kQAt + (unit & 1u) * G::kQ);
             wait(q_ready(unit & 1u), (unit >> 1) & 1u);
             for (int n = 0; n < part.count && ok; ++n, ++k) {
-                const uint32_t b = k & 3u;
-                wait(s_free(b), ((k >> 2) & 1u) ^ 1u);
+                const uint32_t b = k & 7u;
+                wait(s_free(b), ((k >> 3) & 1u) ^ 1u);
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
                     wait(k_full(ks), k_phase);
@@ -368,14 +387,15 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     if (y == 0) wait(p_ready(x), (k >> 1) & 1u);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t a = mn_desc(v_at(vs), lay::block, lay::group), b = mn_desc(base + G::kPAt + x * G::kP, 0, 1024);
+                    const uint64_t a = mn_desc(v_at(vs), lay::block, lay::group), b = p_desc<G::kPRow>(base + G::kPAt + x * G::kP);
                     const uint32_t d = o_at(unit & 1u, x) + y * G::kCols;
                     if (elect_one()) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c)        // 16 keys each
-                            umma_bf16(d, a + (c * 2 * lay::group >> 4), b + (c * 2048 >> 4), idesc, n >= 2 || c > 0);
+                            umma_bf16(d, a + (c * 2 * lay::group >> 4), b + (c * 16 * G::kPRow >> 4), idesc, n >= 2 || c > 0);
                         if (y + 1 == HB) umma_commit(pv_done(x));
                         umma_commit(v_empty(vs));
+                        if (n + 1 == part.count && y + 1 == HB) umma_commit(acc_full(unit & 1u));
                     }
                     __syncwarp();
                     if ((vs ^= 1) == 0) v_phase ^= 1u;
@@ -389,7 +409,8 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
         const int bar_id = 1 + x;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t p_row = base + G::kPAt + x * G::kP + wt * 128;
+        const uint32_t p_row = base + G::kPAt + x * G::kP + wt * G::kPRow;
+        const int p_sw = NR == 8 ? (wt >> 2) & 1 : (wt >> 1) & 3;
         uint32_t k0 = 0, unit = 0;
         float l[NR];
         while (cur.at < piece_end) {
@@ -401,18 +422,16 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             const int u = unit & 1;
             const uint32_t o_tm = o_at(u, x) + lanes;
             float *sh_m = sh_ms[u][x];
-            if (unit >= 2) ok = bar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws);
-            if (wg_any(bar_id, !ok)) break;
-            if (wt < NR) sh_m[wt] = kNone;
-            wg_sync(bar_id);
+            if (unit >= 2) ok = bar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws) && ok;
 #pragma unroll
             for (int r = 0; r < NR; ++r) l[r] = 0.f;
             const int n0 = (int)((k0 & 1u) ^ (uint32_t)x); // this warpgroup's tiles: n0, n0 + 2, ..
+            if (n0 >= count && wt < NR) sh_m[wt] = kNone;
 #pragma unroll 1
             for (int n = n0; n < count; n += 2) {
-                const uint32_t k = k0 + n, b = k & 3u;
+                const uint32_t k = k0 + n, b = k & 7u;
                 const uint32_t s_tm = s_at(b) + lanes;
-                ok = bar_wait(s_full(b), (k >> 2) & 1u, abort_flag, ws);
+                ok = bar_wait(s_full(b), (k >> 3) & 1u, abort_flag, ws) && ok;
                 __syncwarp();
                 tc_fence_after();
                 const float kf = q8_factor((sh_ks[b][wt >> 2] >> (8 * (wt & 3))) & 255u);
@@ -462,7 +481,6 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 if (k >= 2) ok = bar_wait(pv_done(x), ((k >> 1) - 1u) & 1u, abort_flag, ws) && ok;
                 if (__builtin_expect(grown, false)) {
                     // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
-                    if (wg_any(bar_id, !ok)) { ok = false; break; }
                     load();
 #pragma unroll
                     for (int i = 0; i < NR; i += 4) {
@@ -474,10 +492,10 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                         const float top = reduce_rows<NR, true>(s, lane);
                         if (lane < NR) sh_wm[x][wq][lane] = top;
                     }
-                    wg_sync(bar_id);
+                    if (wg_any(bar_id, !ok)) { ok = false; break; }
                     if (wt < NR) {
                         const float top = fmaxf(fmaxf(sh_wm[x][0][wt], sh_wm[x][1][wt]), fmaxf(sh_wm[x][2][wt], sh_wm[x][3][wt]));
-                        const float m = sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
+                        const float m = n < 2 ? kNone : sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
                         sh_c[x][wt] = nm == m ? 1.f : ex2f(m - nm);
                         sh_m[wt] = nm;
                     }
@@ -518,23 +536,18 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                         l[r + 1] += b2;
                         split_bf16(a, b2, hi[i], lo[i]);
                     }
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ (wt & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ (wt & 7)) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ p_sw) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ p_sw) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_ready(x));
             }
-            if (!ok) break;
-            // ---- the unit's end: sums over the warp's keys, the last product
+            // ---- the unit's end: sums over the warp's keys
+            if (wg_any(bar_id, !ok)) break;
             const float sum = reduce_rows<NR, false>(l, lane);
             if (lane < NR) sh_wl[u][x][wq][lane] = sum;
-            if (n0 < count) {
-                const uint32_t last = k0 + (uint32_t)(n0 + ((count - 1 - n0) & ~1));
-                ok = bar_wait(pv_done(x), (last >> 1) & 1u, abort_flag, ws);
-            }
-            if (wg_any(bar_id, !ok)) break;
-            tc_fence_before();
+            __syncwarp();
             if (lane == 0) mbar_arrive(acc_full(u));
             k0 += (uint32_t)count;
             ++unit;
@@ -570,13 +583,6 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         const int bar_id = 3;
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
         uint32_t k0 = 0, unit = 0;
-        auto to_tiles = [&](Cursor<NR, kTcTile> &c) {      // on to a unit that this piece has tiles of
-            while (c.at < piece_end) {
-                const UnitPart part = unit_part(p, c, piece_end);
-                if (part.count > 0) break;
-                next_unit(p, c, part.places, piece_end);
-            }
-        };
         auto queries = [&](const Cursor<NR, kTcTile> &c, int u) {      // (the unit before the last has ended here: all of it may be reused)
             load_query_parts<HB, NR>(p, c.start, c.h, c.t.r0, c.t.rows, base + G::kQAt + u * G::kQ, sh_rf[u], wt);
             if (wt < NR) {
@@ -750,7 +756,7 @@ cudaError_t launch_few_q8(Ctx *c, AttnParams &p, int box_rows, bool eight, cudaS
     if (!codes_map(c, &km, p.k, box_rows, true) || !codes_map(c, &vm, p.v, box_rows, false)) return note_err(c, cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     PageBoxes bx = {};
     bx.rows = box_rows;
-    p.lead = 2;
+    p.lead = 5;
     if (eight) return p.D <= 128 ? few_q8_launch<1, 8>(c, p, km, vm, bx, st) : few_q8_launch<2, 8>(c, p, km, vm, bx, st);
     return p.D <= 128 ? few_q8_launch<1, 16>(c, p, km, vm, bx, st) : few_q8_launch<2, 16>(c, p, km, vm, bx, st);
 }

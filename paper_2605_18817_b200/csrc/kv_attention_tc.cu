@@ -556,7 +556,11 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     constexpr int DB = G::B::DB, HB = G::B::HB;
     constexpr int kRows = G::kRows;
     typedef RowTile<kRows, kTcTile> Tile;
+    // With the warps that turn codes there are roles enough to overrun the instruction caches: what a loop does rarely stands outside
+    // of it then (prompt chunk 830 -> 632 us; packed prompts, with a role less, 468 -> 494).
+    constexpr bool kShort = LAY == kCodes;
     extern __shared__ unsigned char smem_raw[];
+    __shared__ Cursor<kRows, kTcTile> sh_cur;
     __shared__ long long sh_find[G::kThreads / 32 + 2];
     __shared__ Suspects suspects[2];
     __shared__ float sh_top[2][NT][2][128], sh_sum[NT][2][128];    // what the halves of a row tell each other
@@ -606,6 +610,18 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (kShort && warp == 2) {
+        pdl_wait();
+        Cursor<kRows, kTcTile> c;
+        long long full = 1;
+        c.at = 0;
+        const long long piece = cut_line<kRows>(p, c, full, blockIdx.x == 0);
+        if (lane == 0) {
+            sh_cur = c;
+            sh_find[0] = piece;
+            sh_find[1] = full;
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -614,11 +630,24 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
     pdl_trigger();
 
     Cursor<kRows, kTcTile> cur;
-    long long per;
-    const long long len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0)
-                                            : find_piece<kRows, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    long long per, len;
+    if constexpr (kShort) {
+        cur = sh_cur;
+        len = sh_find[0];
+        per = sh_find[1];
+    } else {
+        len = p.b.n_seqs <= 128 ? find_piece_warp(p, cur, per, blockIdx.x == 0 && warp == 0) : find_piece<kRows, kTcTile, G::kThreads>(p, cur, per, sh_find);
+    }
     if (len == 0) cur.at = 0;
     const long long piece_end = len > 0 ? cur.at + len : 0;
+    auto hold = [](uint32_t bar, uint32_t parity, volatile int *flag, const WaitStatus &w) {
+        if constexpr (kShort) return bar_wait(bar, parity, flag, w);
+        else return mbar_wait(bar, parity, flag, w);
+    };
+    auto go_on = [&](Cursor<kRows, kTcTile> &c, int places) {
+        if constexpr (kShort) next_unit(p, c, places, piece_end);
+        else leave_unit(p, c, places, piece_end);
+    };
 
     if (warp == 0) {
         // ================================ TMA producer ================================
@@ -628,12 +657,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            if (count == 0) { go_on(cur, part.places); continue; }
             const Tile t = cur.t;
             auto fetch = [&](const PageRef &r, int which) {
 #pragma unroll
                 for (int y = 0; y < HB; ++y) {
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(LAY == kCodes ? raw_empty(stage) : empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, hold(LAY == kCodes ? raw_empty(stage) : empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
                     if constexpr (LAY == kCodes)
                         fetch_codes(p, which ? &vmap : &kmap, bx, r, cur.h, 128 * y, min(p.D, 128), base + G::kRaw + stage * G::kRawStage, raw_full(stage), lane);
@@ -653,7 +682,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 now = next;
                 next = then;
             }
-            leave_unit(p, cur, part.places, piece_end);
+            go_on(cur, part.places);
         }
     } else if (warp == 1) {
         // ================================ MMA issuer ================================
@@ -662,7 +691,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         bool ok = true, two_parts = false;
         const uint32_t idesc_s = make_idesc(128), idesc_o = make_idesc(DB * 64) | (1u << 16);
         typedef TileAt<DB, LAY> lay;
-        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ws)); };
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, hold(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         auto mma_s = [&](int x, int row_tile, uint32_t ks, int y) {        // S buffer x (+)= Q_row_tile K^T, features 128 y ..
             if (elect_one()) {
@@ -697,14 +726,19 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            if (count == 0) { go_on(cur, part.places); continue; }
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             two_parts = NT == 1 && LAY != kPacked && t.rows <= kFewRows;
             Suspects &sus = suspects[unit & 1];
             if (lane == 0) sus.n = 0;
             __syncwarp();
-            auto clean = [&](int n, uint32_t vs) { clean_tile<DB, LAY>(t, all, key_tile(t, begin + n) * kTcTile, vs, sus, lane); };
+            const int fine_to = p.window > 0 ? 0 : all.differ ? min(t.hi, all.all_hi) : t.hi;      // tiles up to here hold nothing to clean
+            auto clean = [&](int n, uint32_t vs) {
+                const int j0 = key_tile(t, begin + n) * kTcTile;
+                if constexpr (!kShort) clean_tile<DB, LAY>(t, all, j0, vs, sus, lane);
+                else if (j0 + kTcTile > fine_to) clean_rarely<DB>(t, all, j0, vs, sus, lane);
+            };
             auto at_stage = [&](int s) { return ring + s * G::B::kStageBytes; };
 #pragma unroll
             for (int x = 0; x < NT; ++x) wait(q_ready(x), unit & 1u);
@@ -774,7 +808,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 }
             }
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
+            go_on(cur, part.places);
         }
     } else if (LAY == kCodes && warp >= 2 + 8 * NT) {
         // ================================ 8 bits: raw stages -> stages of the ring ================================
@@ -786,14 +820,14 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         while (ok && cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            if (count == 0) { go_on(cur, part.places); continue; }
             const Tile t = cur.t;
             auto find = [&](int n) { return find_keys<KR>(p, t, n < count, begin + n, cur.s, key0, lane); };
             auto turn = [&](const uint32_t (&bytes)[KR]) {
 #pragma unroll 1
                 for (int y = 0; y < HB; ++y) {
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(raw_full(raw), raw_phase, abort_flag, ws));
-                    ok = ok && __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, hold(raw_full(raw), raw_phase, abort_flag, ws));
+                    ok = ok && __all_sync(0xffffffffu, hold(empty_bar(stage), phase ^ 1u, abort_flag, ws));
                     if (!ok) return;
                     turn_stage<DB, KR>(base + G::kRaw + raw * G::kRawStage, ring + stage * G::B::kStageBytes, key0, min(p.D, 128), p.D - 128 * y, bytes, lane);
                     if (lane == 0) {
@@ -824,7 +858,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
 #pragma unroll
                 for (int y = 0; y < KR; ++y) { vn[y] = v1[y]; k1[y] = k2[y]; v1[y] = v2[y]; }
             }
-            leave_unit(p, cur, part.places, piece_end);
+            go_on(cur, part.places);
         }
     } else {
         // ================================ softmax: two threads per row ================================
@@ -839,12 +873,12 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         // P V of tile kk done.  A barrier may be one phase behind what is waited for, not two: with two S buffers the
         // softmax can finish a tile while the product before the last still runs, so each buffer has its own.
         auto wait_pv = [&](uint32_t kk) {
-            return NT == 2 ? mbar_wait(pv_done(x), kk & 1u, abort_flag, ws) : mbar_wait(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
+            return NT == 2 ? hold(pv_done(x), kk & 1u, abort_flag, ws) : hold(pv_done(kk & 1u), (kk >> 1) & 1u, abort_flag, ws);
         };
         while (cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
-            if (count == 0) { leave_unit(p, cur, part.places, piece_end); continue; }
+            if (count == 0) { go_on(cur, part.places); continue; }
             const Tile t = cur.t;
             const int rows = min(128, t.rows - x * 128);   // of this row tile (can be negative)
             const bool two_parts = NT == 1 && LAY != kPacked && t.rows <= kFewRows;
@@ -874,7 +908,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
             for (int n = 0; n < count; ++n, ++k) {
                 const int buf = NT == 2 ? x : (int)(k & 1u);
                 const uint32_t s_tm = tmem + buf * 128 + half * 64 + lanes;        // this half's scores, then its P
-                ok = mbar_wait(s_full(buf), NT == 2 ? k & 1u : (k >> 1) & 1u, abort_flag, ws);
+                ok = hold(s_full(buf), NT == 2 ? k & 1u : (k >> 1) & 1u, abort_flag, ws);
                 __syncwarp();
                 tc_fence_after();
                 if (!warp_live) {
@@ -1114,7 +1148,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
                 }
             }
             ++unit;
-            leave_unit(p, cur, part.places, piece_end);
+            go_on(cur, part.places);
         }
         if (half == 0 && lane == 0)                    // (units are left over only where a wait gave up)
             settle_arrivals(p, cur, per, piece_end, [&](const Cursor<kRows, kTcTile> &c, int c0, int c1) {

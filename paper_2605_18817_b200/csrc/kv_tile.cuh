@@ -44,25 +44,27 @@ template <int ROWS>
 __device__ __noinline__ long long cut_line(const AttnParams &p, Cursor<ROWS, kTcTile> &c, long long &per, bool report)
 {
     const int lane = threadIdx.x & 31;
-    auto tiles_of = [&](int s, bool tell) {
-        if (s >= p.b.n_seqs) return 0ll;
-        return sequence_tiles<ROWS, kTcTile>(p, s, tell);
-    };
-    long long total = 0, begin = 0, end = 0, done = 0;
+    long long begin = 0, end = 0, done = 0, mine = 0;
     c.s = -1;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
         for (int s0 = 0; s0 < p.b.n_seqs && c.s < 0; s0 += 32) {
-            const long long mine = tiles_of(s0 + lane, pass == 0 && report);
-            long long x = mine;            // inclusive sum over the lanes
+            if (pass == 0 || p.b.n_seqs > 32) mine = s0 + lane < p.b.n_seqs ? sequence_tiles<ROWS, kTcTile>(p, s0 + lane, pass == 0 && report) : 0;
+            long long x = mine;
+            if (pass == 0) {
 #pragma unroll
-            for (int w = 1; w < 32; w <<= 1) {
+                for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
+                done += x;
+                continue;
+            }
+#pragma unroll
+            for (int w = 1; w < 32; w <<= 1) {             // inclusive sum over the lanes
                 const long long y = __shfl_up_sync(0xffffffffu, x, w);
                 if (lane >= w) x += y;
             }
             const long long before = done + x - mine;
-            const uint32_t hit = __ballot_sync(0xffffffffu, pass == 1 && mine > 0 && before <= begin && begin < before + mine);
+            const uint32_t hit = __ballot_sync(0xffffffffu, mine > 0 && before <= begin && begin < before + mine);
             if (hit) {
                 c.s = s0 + __ffs(hit) - 1;
                 c.at = __shfl_sync(0xffffffffu, before, __ffs(hit) - 1);
@@ -70,12 +72,11 @@ __device__ __noinline__ long long cut_line(const AttnParams &p, Cursor<ROWS, kTc
             done += __shfl_sync(0xffffffffu, x, 31);
         }
         if (pass == 0) {
-            total = done;
-            done = 0;
-            per = div_line(total + gridDim.x - 1, gridDim.x);
+            per = div_line(done + gridDim.x - 1, gridDim.x);
             begin = per * blockIdx.x;
-            end = min(total, begin + per);
+            end = min(done, begin + per);
             if (begin >= end) return 0;
+            done = 0;
         }
     }
     kv_sequence(p.b, c.s, c.start, c.n, c.pre);
