@@ -106,7 +106,7 @@ template <typename T, int DP, int SRC> struct Smem {
     static constexpr int kRedPitch = DP + 4;               // floats
     // 8 bits: a ring of raw stages (codes of K and V, the 4-byte words their scales lie in, the bytes in those), and one
     // stage of values, which at the end of a unit takes the warp's parts
-    static constexpr int kLoads = SRC != kFromQ8 ? G::kStages : DP <= 128 ? 3 : 2;
+    static constexpr int kLoads = SRC != kFromQ8 ? G::kStages : DP <= (sizeof(T) == 2 ? 128 : 64) ? 3 : 2;        // (f32 of 128 features: two CTAs an SM)
     static constexpr int kRaw = 2 * kWarpKeys * DP + 2 * kWarpKeys * 4 + 2 * kWarpKeys;
     static constexpr int kParts = kRows * kRedPitch * 4;
     static constexpr int kValues = kStage > kParts ? kStage : kParts;
@@ -361,6 +361,15 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) load_tile(s);
 
+    // (what 8 bits stand for has four significant bits: one tf32 part is all of it, and a product less is needed)
+    auto split_key = [](float x, uint32_t &hi, uint32_t &lo) {
+        if (SRC == kFromQ8) {
+            hi = __float_as_uint(x);
+            lo = 0;
+        } else {
+            split_tf32(x, hi, lo);
+        }
+    };
     const long long piece_end = cur.at + len;
     int stage = 0;
     long long at = cur.at;
@@ -462,10 +471,10 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                             float2 kb;
                             asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(kb.x), "=f"(kb.y) : "r"(sk + (x * 8 + gid) * G::kPitchK + at) : "memory");
                             uint32_t bh[2], bl[2];
-                            split_tf32(kb.x, bh[0], bl[0]);
-                            split_tf32(kb.y, bh[1], bl[1]);
+                            split_key(kb.x, bh[0], bl[0]);
+                            split_key(kb.y, bh[1], bl[1]);
                             mma8(d[x], al, bh[0], bh[1]);
-                            mma8(d[x], ah, bl[0], bl[1]);
+                            if (SRC != kFromQ8) mma8(d[x], ah, bl[0], bl[1]);
                             mma8(d[x], ah, bh[0], bh[1]);
                         }
                     }
@@ -548,10 +557,10 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v0) : "r"(a0) : "memory");
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v1) : "r"(a0 + G::kPitchV) : "memory");
                         uint32_t bh[2], bl[2];
-                        split_tf32(v0, bh[0], bl[0]);
-                        split_tf32(v1, bh[1], bl[1]);
+                        split_key(v0, bh[0], bl[0]);
+                        split_key(v1, bh[1], bl[1]);
                         mma8(d, al[x], bh[0], bh[1]);
-                        mma8(d, ah[x], bl[0], bl[1]);
+                        if (SRC != kFromQ8) mma8(d, ah[x], bl[0], bl[1]);
                         mma8(d, ah[x], bh[0], bh[1]);
                     }
 #pragma unroll

@@ -42,7 +42,7 @@ template <int NB, int NT, int LAY> struct TcGeo {
     // 8 bits: raw stages (128 rows of up to 128 codes) beside the ring, and warps that turn them into stages of it
     static constexpr int kRawStage = LAY == kCodes ? B::kStageBytes / 2 : 0;
     static constexpr int kRawStages = LAY != kCodes ? 0 : B::DB == 1 ? 4 : NT == 1 && B::HB == 1 ? 3 : 2;
-    static constexpr int kTurners = LAY != kCodes ? 0 : NT == 1 ? 4 : 2;
+    static constexpr int kTurners = LAY != kCodes ? 0 : NT == 1 ? 4 : 2;           // (eight with one row tile: blocks of 32 55 -> 61 us)
     static constexpr int kStages = LAY == kCodes ? (B::DB == 1 ? 8 : B::HB == 2 || NT == 2 ? 3 : 4)
                                                  : B::DB == 1 ? 10 : B::HB == 2 || NT == 2 ? 4 : 5;
     static constexpr int kQTile = NB * 128 * 128;          // queries of a row tile
@@ -694,9 +694,14 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, hold(bar, parity, abort_flag, ws)); };
         auto step = [&]() { if (++stage == G::kStages) { stage = 0; phase ^= 1u; } };
         auto mma_s = [&](int x, int row_tile, uint32_t ks, int y) {        // S buffer x (+)= Q_row_tile K^T, features 128 y ..
+            // (descriptors that are added to instead of made anew: the issue of an MMA is about as long as its work)
+            const uint64_t qd = make_smem_desc(sq + row_tile * G::kQTile + y * G::B::kStageBytes), kd = k_desc(ks, lay::group);
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4 * DB; ++c) {
+                    if constexpr (LAY >= kPacked)
+                        umma_bf16(tmem + x * 128, qd + (((c >> 2) * (128 * 128) + (c & 3) * 32) >> 4), kd + (((c >> 2) * lay::block + (c & 3) * 32) >> 4), idesc_s, y + c > 0);
+                    else
                     umma_bf16(tmem + x * 128, make_smem_desc(sq + row_tile * G::kQTile + y * G::B::kStageBytes + (c >> 2) * (128 * 128) + (c & 3) * 32),
                               k_desc(ks + (c >> 2) * lay::block + (c & 3) * 32, lay::group), idesc_s, y + c > 0);
                 }
@@ -706,9 +711,13 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         };
         // O_row_tile += P_x V, keys 16 c0 .. 16 c0 + 63, features 128 y ..
         auto mma_o = [&](int x, int row_tile, uint32_t vs, int y, int c0, bool first) {
+            const uint64_t vd = mn_desc(vs + c0 * 2 * lay::group, lay::block, lay::group);
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
+                    if constexpr (LAY >= kPacked)
+                        umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, vd + (c * 2 * lay::group >> 4), idesc_o, !first || c0 + c > 0);
+                    else
                     umma_ts(tmem + 256 + (row_tile + y) * 128, tmem + x * 128 + c0 * 16 + c * 8, mn_desc(vs + (c0 + c) * 2 * lay::group, lay::block, lay::group), idesc_o, !first || c0 + c > 0);
                 if (two_parts) {
 #pragma unroll
@@ -812,7 +821,7 @@ kv_attention_tc_kernel(const __grid_constant__ AttnParams p, const __grid_consta
         }
     } else if (LAY == kCodes && warp >= 2 + 8 * NT) {
         // ================================ 8 bits: raw stages -> stages of the ring ================================
-        constexpr int KR = G::kTurners ? 4 / (G::kTurners ? G::kTurners : 1) : 1;      // of every tile, a warp has 32 KR keys
+        constexpr int KR = G::kTurners ? 4 / (G::kTurners ? G::kTurners : 1) : 1;                // of a stage, a warp has 32 KR keys
         const int key0 = (warp - (2 + 8 * NT)) * 32 * KR;
         int stage = 0, raw = 0;
         uint32_t phase = 0, raw_phase = 0;
