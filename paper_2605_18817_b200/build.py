@@ -10,7 +10,7 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libmrp_b200.so")
 SOURCES = ["mrp_api.cu", "simt_kernels.cu", "select_verify.cu", "tc_kernels.cu", "tc_skinny.cu", "tc_chain.cu",
-           "kv_rows.cu", "kv_read.cu", "kv_attention.cu", "kv_attention_tc.cu", "kv_attention_q8.cu"]
+           "kv_rows.cu", "kv_read.cu", "kv_attention.cu", "kv_attention_tc.cu", "kv_attention_q8.cu", "kv_attention_short.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17"]
 
 

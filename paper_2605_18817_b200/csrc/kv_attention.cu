@@ -684,6 +684,9 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
     cp_wait<0>();
 }
 
+// Packed sequences of up to so many tokens, as far as the host knows, go without tiles of 128 rows.
+constexpr int kShortNew = 128;
+
 size_t slot_bytes() { return (size_t)kRows * (256 * 4 + 8); }
 
 template <typename T, int DP, int SRC>
@@ -788,7 +791,8 @@ cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp
     p.k = kv.k; p.v = kv.v;
     p.k_stride = kv.k_stride; p.v_stride = kv.v_stride;
     p.join = kv.join != 0;
-    return kv_tc_takes_rows(c->cfg, c->kv, kv) ? launch_packed_attention_tc(c, p, batch, st) : launch<kFromRows>(c, p, st);
+    if (!kv_tc_takes_rows(c->cfg, c->kv, kv)) return launch<kFromRows>(c, p, st);
+    return batch.max_new <= kShortNew ? launch_packed_attention_short(c, p, batch, st) : launch_packed_attention_tc(c, p, batch, st);
 }
 
 }  // namespace mrp

@@ -417,6 +417,8 @@ cudaError_t launch_paged_attention_q8_tc(Ctx *c, AttnParams &p, const mrp_kv_bat
 cudaError_t kv_few_q8_prepare();
 cudaError_t launch_few_q8(Ctx *c, AttnParams &p, int box_rows, bool eight, cudaStream_t st);    // (kv_attention_q8.cu)
 bool kv_tc_takes_rows(const mrp_config &cfg, const mrp_kv_config &kv, const mrp_packed_kv &rows);
+cudaError_t kv_short_prepare();
+cudaError_t launch_packed_attention_short(Ctx *c, const AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);      // (kv_attention_short.cu)
 cudaError_t launch_packed_attention_tc(Ctx *c, AttnParams &p, const mrp_kv_batch &batch, cudaStream_t st);
 
 }  // namespace mrp

@@ -1286,7 +1286,7 @@ cudaError_t kv_tc_attach(Ctx *c)
                          tc_prepare<2, 2, kCodes>()};
     for (cudaError_t one : all)
         if (one != cudaSuccess) return one;
-    if ((e = kv_few_q8_prepare()) != cudaSuccess) return e;
+    if ((e = kv_few_q8_prepare()) != cudaSuccess || (e = kv_short_prepare()) != cudaSuccess) return e;
     c->kv_encode = fn;
     return cudaSuccess;
 }
