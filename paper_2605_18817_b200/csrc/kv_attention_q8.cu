@@ -10,8 +10,9 @@
 //   memory: TMA, warps and MMAs move 88 of 128 bytes a cycle at the memory's rate as it is.
 //
 //   warp 0   K by TMA, and its scales      warp 1   S MMAs      warp 2   PV MMAs      warp 3   V and its scales
-//   warps 4-7, 8-11   softmax: two warpgroups that take tiles in turn, a thread per key
-//   warps 12-15   queries, a unit ahead, and units' ends          from warp 16 on   V's codes -> bf16 (8 rows: two groups of four warps, a stage each)
+//   warps 4-7, 8-11   softmax, a thread per key and eight rows: two warpgroups that take tiles in turn (8 rows; maxima, sums and
+//            accumulators of their own, joined at the unit's end) or the same tiles' rows by halves (16 rows: @@SPLIT@@)
+//   warps 12-15   queries, a unit ahead, and units' ends          from warp 16 on   V's codes -> bf16 (two groups of four warps, a stage each)
 // Instructions bound it next to memory, so each role's loop is short: the roles of an SM quarter share its instruction cache and
 // its issue slots.  (One warp for both kinds of MMAs, scales looked up by the warps that use them, turning unrolled: 64 ragged
 // single tokens 266 us; the turning rolled and 8 rows instead of 16: 159.)
@@ -33,7 +34,8 @@ template <int HB, int ROWS> struct FewQ8Geo {
     static constexpr int kPAt = kVAt + 2 * 32768, kQAt = kPAt + 2 * kP, kBars = kQAt + 2 * kQ;
     static constexpr int kSmem = kBars + 1024 + 1024;      // + alignment of the base
     static constexpr int kTmem = NR == 16 ? 512 : 256;     // of which 8 kCols (S) + 4 HB kCols are used
-    static constexpr int kTurners = NR == 8 ? 8 : 4;       // warps (16 rows: the softmax needs the registers)
+    static constexpr int kTurners = 8;                     // warps
+    static constexpr bool kSplit = NR == 16;               // both warpgroups take every tile, eight rows each
     static constexpr int kThreads = 512 + 32 * kTurners;
     static constexpr int kWide = HB * 128;                 // features of a row of partial results
 };
@@ -91,6 +93,24 @@ __device__ __forceinline__ void load_query_parts(const AttnParams &p, int start,
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// 8 columns each of the warp's 32 lanes, from two places
+__device__ __forceinline__ void tmem_ld8_two(uint32_t a, uint32_t b, float *v, float *w)
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v), *s = reinterpret_cast<uint32_t *>(w);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(a) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(s[0]), "=r"(s[1]), "=r"(s[2]), "=r"(s[3]), "=r"(s[4]), "=r"(s[5]), "=r"(s[6]), "=r"(s[7]) : "r"(b) : "memory");
+    tmem_wait_ld();
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                      "+f"(w[0]), "+f"(w[1]), "+f"(w[2]), "+f"(w[3]), "+f"(w[4]), "+f"(w[5]), "+f"(w[6]), "+f"(w[7]) :: "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t a, const float *v)
+{
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 // P^T as the B operand: rows (keys) of 32 or 64 bytes, MN-major, swizzled over as many
 template <int ROW> __device__ __forceinline__ uint64_t p_desc(uint32_t saddr)
 {
@@ -146,8 +166,10 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     __shared__ Suspects suspects[2];
     __shared__ uint32_t sh_ks[8][32], sh_vs[G::kRawStages][32];            // scale bytes of the keys of a tile's K (by S buffer), of a raw stage
     __shared__ int sh_hi[2][NR], sh_lo[2][NR];             // what a row sees: [lo, hi) and the first positions
-    __shared__ __align__(16) float sh_ms[2][2][NR], sh_c[2][NR], sh_rf[2][NR];     // maximum in use (unit, warpgroup), factor to it; rows' factors
-    __shared__ float sh_wm[2][4][NR], sh_wl[2][2][4][NR];  // row maxima and (of a unit) sums of the warps
+    constexpr int kR = 8;                                  // rows of a warpgroup
+    constexpr int kStep = G::kSplit ? 1 : 2;               // from one of its tiles to the next
+    __shared__ __align__(16) float sh_ms[2][2][kR], sh_c[2][kR], sh_rf[2][NR];     // maximum in use (unit, warpgroup), factor to it; rows' factors
+    __shared__ float sh_wm[2][4][kR], sh_wl[2][2][4][kR];  // row maxima and (of a unit) sums of the warps
     __shared__ float sh_f[2][NR];                          // the unit's end: factors of the accumulators,
     __shared__ int64_t sh_out[NR];                         //   where the rows go
     __shared__ int sh_last;
@@ -187,12 +209,12 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
         }
         for (int b = 0; b < 8; ++b) {
             mbar_init(s_full(b), 33);
-            mbar_init(s_free(b), 4);
+            mbar_init(s_free(b), G::kSplit ? 8 : 4);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(v_full(x), 4);
             mbar_init(v_empty(x), 1);
-            mbar_init(p_ready(x), 4);
+            mbar_init(p_ready(x), G::kSplit ? 8 : 4);
             mbar_init(pv_done(x), 1);
             mbar_init(q_ready(x), 128);
             mbar_init(unit_end(x), 4);
@@ -222,7 +244,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;    // eight buffers of S, then the warpgroups' accumulators of two units
+    const uint32_t tmem = *tmem_holder;    // eight buffers of S, then accumulators of two units (8 rows: of each warpgroup)
     auto s_at = [&](int b) { return tmem + b * G::kCols; };        // (columns: the upper parts of the rows, the lower ones)
     auto o_at = [&](int u, int x) { return tmem + 8 * G::kCols + (2 * u + x) * HB * G::kCols; };    // (HB accumulators of 128 features)
     pdl_wait();
@@ -388,11 +410,11 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t a = mn_desc(v_at(vs), lay::block, lay::group), b = p_desc<G::kPRow>(base + G::kPAt + x * G::kP);
-                    const uint32_t d = o_at(unit & 1u, x) + y * G::kCols;
+                    const uint32_t d = o_at(unit & 1u, G::kSplit ? 0 : x) + y * G::kCols;
                     if (elect_one()) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c)        // 16 keys each
-                            umma_bf16(d, a + (c * 2 * lay::group >> 4), b + (c * 16 * G::kPRow >> 4), idesc, n >= 2 || c > 0);
+                            umma_bf16(d, a + (c * 2 * lay::group >> 4), b + (c * 16 * G::kPRow >> 4), idesc, n >= kStep || c > 0);
                         if (y + 1 == HB) umma_commit(pv_done(x));
                         umma_commit(v_empty(vs));
                         if (n + 1 == part.count && y + 1 == HB) umma_commit(acc_full(unit & 1u));
@@ -405,14 +427,15 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             next_unit(p, cur, part.places, piece_end);
         }
     } else if (warp < 12) {
-        // ================================ softmax: a thread per key, two warpgroups in turn ================================
+        // ================================ softmax: a thread per key ================================
         const int x = (warp - 4) >> 2, wq = warp & 3, wt = wq * 32 + lane;
         const int bar_id = 1 + x;
+        const int row0 = G::kSplit ? 8 * x : 0;            // of the warpgroup's rows: also their first column of S, P and the accumulator
         const uint32_t lanes = (uint32_t)(wq * 32) << 16;
-        const uint32_t p_row = base + G::kPAt + x * G::kP + wt * G::kPRow;
         const int p_sw = NR == 8 ? (wt >> 2) & 1 : (wt >> 1) & 3;
+        const uint32_t p_row = base + G::kPAt + wt * G::kPRow, p_hi = (uint32_t)(((row0 / 8) ^ p_sw) << 4), p_lo = (uint32_t)(((row0 / 8 + NR / 8) ^ p_sw) << 4);
         uint32_t k0 = 0, unit = 0;
-        float l[NR];
+        float l[kR];
         while (cur.at < piece_end) {
             const UnitPart part = unit_part(p, cur, piece_end);
             const int begin = part.begin, count = part.count;
@@ -420,17 +443,17 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             const Tile t = cur.t;
             const Seen all = seen_by_all(p, t, cur.pre);
             const int u = unit & 1;
-            const uint32_t o_tm = o_at(u, x) + lanes;
+            const uint32_t o_tm = o_at(u, G::kSplit ? 0 : x) + lanes + row0;
             float *sh_m = sh_ms[u][x];
             if (unit >= 2) ok = bar_wait(unit_end(u), ((unit >> 1) - 1u) & 1u, abort_flag, ws) && ok;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) l[r] = 0.f;
-            const int n0 = (int)((k0 & 1u) ^ (uint32_t)x); // this warpgroup's tiles: n0, n0 + 2, ..
-            if (n0 >= count && wt < NR) sh_m[wt] = kNone;
+            for (int r = 0; r < kR; ++r) l[r] = 0.f;
+            const int n0 = G::kSplit ? 0 : (int)((k0 & 1u) ^ (uint32_t)x);         // this warpgroup's tiles: n0, n0 + kStep, ..
+            if (n0 >= count && wt < kR) sh_m[wt] = kNone;
 #pragma unroll 1
-            for (int n = n0; n < count; n += 2) {
+            for (int n = n0; n < count; n += kStep) {
                 const uint32_t k = k0 + n, b = k & 7u;
-                const uint32_t s_tm = s_at(b) + lanes;
+                const uint32_t s_tm = s_at(b) + lanes + row0;
                 ok = bar_wait(s_full(b), (k >> 3) & 1u, abort_flag, ws) && ok;
                 __syncwarp();
                 tc_fence_after();
@@ -441,80 +464,83 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 if (!whole) {
                     if (all.differ) {
 #pragma unroll 1
-                        for (int r = 0; r < NR; ++r) seen |= (uint32_t)sees(j, sh_hi[u][r], sh_lo[u][r], p.sinks) << r;
+                        for (int r = 0; r < kR; ++r) seen |= (uint32_t)sees(j, sh_hi[u][row0 + r], sh_lo[u][row0 + r], p.sinks) << r;
                     } else {
                         seen = sees(j, all.all_hi, all.all_lo, p.sinks) ? ~0u : 0u;
                     }
                 }
-                float s[NR];
+                float s[kR];
                 auto load = [&]() {                        // the key's scores, both parts of the queries
-                    float v[2 * NR];
-                    tmem_ld_n<2 * NR>(s_tm, v);
+                    float v[2][8];
+                    tmem_ld8_two(s_tm, s_tm + NR, v[0], v[1]);
 #pragma unroll
-                    for (int i = 0; i < NR; ++i) s[i] = fmaf(v[NR + i], 0.0625f, v[i]);
+                    for (int i = 0; i < kR; ++i) s[i] = fmaf(v[1][i], 0.0625f, v[0][i]);
                 };
                 auto hide = [&]() {                        // what a row does not see: -inf
                     if (!whole) {
 #pragma unroll
-                        for (int i = 0; i < NR; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
+                        for (int i = 0; i < kR; ++i) s[i] = (seen >> i) & 1u ? s[i] : -INFINITY;
                     }
                 };
                 auto against_max = [&]() {                 // exponents; rows and keys have their powers of two
 #pragma unroll
-                    for (int i = 0; i < NR; i += 4) {
-                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[i]), f = *reinterpret_cast<const float4 *>(&sh_rf[u][i]);
+                    for (int i = 0; i < kR; i += 4) {
+                        const float4 m = *reinterpret_cast<const float4 *>(&sh_m[i]), f = *reinterpret_cast<const float4 *>(&sh_rf[u][row0 + i]);
                         s[i] = fmaf(s[i], f.x * kf, -m.x); s[i + 1] = fmaf(s[i + 1], f.y * kf, -m.y);
                         s[i + 2] = fmaf(s[i + 2], f.z * kf, -m.z); s[i + 3] = fmaf(s[i + 3], f.w * kf, -m.w);
                     }
                     hide();
                 };
                 bool grown = true;                         // (the warpgroup's first tile of the unit sets the maxima)
-                if (n >= 2) {
+                if (n >= kStep) {
                     load();
                     against_max();
                     float top = s[0];
 #pragma unroll
-                    for (int i = 1; i < NR; ++i) top = fmaxf(top, s[i]);
+                    for (int i = 1; i < kR; ++i) top = fmaxf(top, s[i]);
                     grown = wg_any(bar_id, top > 8.f || !ok);
                 }
-                // the product of this warpgroup's tile before is done: P and the accumulator are its own again
-                if (k >= 2) ok = bar_wait(pv_done(x), ((k >> 1) - 1u) & 1u, abort_flag, ws) && ok;
+                // the product of the tile before the last is done: its P may be overwritten (and, tiles in turn, the accumulator scaled)
+                if (k >= 2) ok = bar_wait(pv_done(k & 1u), ((k >> 1) - 1u) & 1u, abort_flag, ws) && ok;
                 if (__builtin_expect(grown, false)) {
                     // ---- some row's maximum has grown: new maxima, sums and accumulator brought to them
+                    if (G::kSplit && n >= 1) ok = bar_wait(pv_done((k - 1) & 1u), ((k - 1) >> 1) & 1u, abort_flag, ws) && ok;
                     load();
 #pragma unroll
-                    for (int i = 0; i < NR; i += 4) {
-                        const float4 f = *reinterpret_cast<const float4 *>(&sh_rf[u][i]);
+                    for (int i = 0; i < kR; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(&sh_rf[u][row0 + i]);
                         s[i] *= f.x * kf; s[i + 1] *= f.y * kf; s[i + 2] *= f.z * kf; s[i + 3] *= f.w * kf;
                     }
                     hide();
                     {
-                        const float top = reduce_rows<NR, true>(s, lane);
-                        if (lane < NR) sh_wm[x][wq][lane] = top;
+                        const float top = reduce_rows<kR, true>(s, lane);
+                        if (lane < kR) sh_wm[x][wq][lane] = top;
                     }
                     if (wg_any(bar_id, !ok)) { ok = false; break; }
-                    if (wt < NR) {
+                    if (wt < kR) {
                         const float top = fmaxf(fmaxf(sh_wm[x][0][wt], sh_wm[x][1][wt]), fmaxf(sh_wm[x][2][wt], sh_wm[x][3][wt]));
-                        const float m = n < 2 ? kNone : sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
+                        const float m = n < kStep ? kNone : sh_m[wt], nm = top > m + 8.f || (m == kNone && top > kNone) ? top : m;
                         sh_c[x][wt] = nm == m ? 1.f : ex2f(m - nm);
                         sh_m[wt] = nm;
                     }
                     wg_sync(bar_id);
-                    if (n >= 2) {
+                    if (n >= kStep) {
 #pragma unroll
-                        for (int r = 0; r < NR; r += 4) {
+                        for (int r = 0; r < kR; r += 4) {
                             const float4 c = *reinterpret_cast<const float4 *>(&sh_c[x][r]);
                             l[r] *= c.x; l[r + 1] *= c.y; l[r + 2] *= c.z; l[r + 3] *= c.w;
                         }
                         tc_fence_after();
 #pragma unroll 1
-                        for (int r0 = 0; r0 < HB * G::kCols; r0 += 16) {
-                            float o[16];
-                            tmem_ld_n<16>(o_tm + r0, o);
-                            uint32_t w[16];
+                        for (int y = 0; y < HB; ++y) {
+                            float o[2][8];
+                            tmem_ld8_two(o_tm + y * G::kCols, o_tm + y * G::kCols + NR, o[0], o[1]);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * sh_c[x][(r0 + i) & (NR - 1)]);
-                            tmem_st16(o_tm + r0, w);
+                            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) o[z][i] *= sh_c[x][i];
+                            tmem_st8(o_tm + y * G::kCols, o[0]);
+                            tmem_st8(o_tm + y * G::kCols + NR, o[1]);
                         }
                         tmem_wait_st();
                     }
@@ -525,28 +551,25 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_free(b));
+                uint32_t hi[4], lo[4];
 #pragma unroll
-                for (int c = 0; c < NR / 8; ++c) {
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 8 * c + 2 * i;
-                        const float a = ex2f(s[r]), b2 = ex2f(s[r + 1]);
-                        l[r] += a;
-                        l[r + 1] += b2;
-                        split_bf16(a, b2, hi[i], lo[i]);
-                    }
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + ((c ^ p_sw) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_row + (((c + NR / 8) ^ p_sw) << 4)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                for (int i = 0; i < 4; ++i) {
+                    const float a = ex2f(s[2 * i]), b2 = ex2f(s[2 * i + 1]);
+                    l[2 * i] += a;
+                    l[2 * i + 1] += b2;
+                    split_bf16(a, b2, hi[i], lo[i]);
                 }
+                const uint32_t to = p_row + (k & 1u) * G::kP;
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + p_hi), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + p_lo), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready(x));
+                if (lane == 0) mbar_arrive(p_ready(k & 1u));
             }
             // ---- the unit's end: sums over the warp's keys
             if (wg_any(bar_id, !ok)) break;
-            const float sum = reduce_rows<NR, false>(l, lane);
-            if (lane < NR) sh_wl[u][x][wq][lane] = sum;
+            const float sum = reduce_rows<kR, false>(l, lane);
+            if (lane < kR) sh_wl[u][x][wq][lane] = sum;
             __syncwarp();
             if (lane == 0) mbar_arrive(acc_full(u));
             k0 += (uint32_t)count;
@@ -615,7 +638,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
             const int u = unit & 1;
             ok = bar_wait(acc_full(u), (unit >> 1) & 1u, abort_flag, ws);
             if (wg_any(bar_id, !ok)) break;
-            bool has[2];
+            bool has[2];                               // tiles in turn: the warpgroup had one
 #pragma unroll
             for (int y = 0; y < 2; ++y) has[y] = (int)((k0 & 1u) ^ (uint32_t)y) < count;
             tc_fence_after();
@@ -626,9 +649,11 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 float lw[2], mw[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    lw[y] = sh_wl[u][y][0][wt] + sh_wl[u][y][1][wt] + sh_wl[u][y][2][wt] + sh_wl[u][y][3][wt];
-                    mw[y] = sh_ms[u][y][wt];
+                    const int x = G::kSplit ? wt >> 3 : y;     // rows by halves: the row's warpgroup alone
+                    lw[y] = sh_wl[u][x][0][wt & 7] + sh_wl[u][x][1][wt & 7] + sh_wl[u][x][2][wt & 7] + sh_wl[u][x][3][wt & 7];
+                    mw[y] = sh_ms[u][x][wt & 7];
                 }
+                if (G::kSplit) lw[1] = 0.f;
                 const float M = fmaxf(mw[0], mw[1]);
                 const float f0 = mw[0] == M ? 1.f : ex2f(mw[0] - M), f1 = mw[1] == M ? 1.f : ex2f(mw[1] - M);
                 const float L = lw[0] * f0 + lw[1] * f1;
@@ -655,8 +680,8 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
 #pragma unroll
                 for (int i = 0; i < NR; ++i) a[i] = 0.f;
 #pragma unroll
-                for (int z = 0; z < 2; ++z)
-                    if (has[z]) {
+                for (int z = 0; z < (G::kSplit ? 1 : 2); ++z)
+                    if (G::kSplit || has[z]) {
                         float o[2 * NR];
                         tmem_ld_n<2 * NR>(o_at(u, z) + y * G::kCols + lanes, o);
 #pragma unroll
