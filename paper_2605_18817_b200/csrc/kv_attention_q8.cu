@@ -315,13 +315,7 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 const int page = fine ? box.entry : p.b.n_pages;                   // (a page that is not one: outside the map, zeros arrive)
                 const int64_t scales = fine ? ((int64_t)box.entry * p.Hk + h) * p.b.page.d + box.row : -1;
                 const uint32_t needed = __ballot_sync(0xffffffffu, need);
-                if (n0 + tiles < count) {
-                    next = find(cur, part, n0 + tiles);
-                } else {                                   // (the next unit's first boxes: their pages are known before this one's last tiles go)
-                    next_unit(p, cur, part.places, piece_end);
-                    to_tiles(cur);
-                    if (cur.at < piece_end) next = find(cur, unit_part(p, cur, piece_end), 0);
-                }
+                if (n0 + tiles < count) next = find(cur, part, n0 + tiles);
 #pragma unroll 1
                 for (int i = 0; i < min(tiles, count - n0) && ok; ++i, ++k) {
                     const uint32_t here = (needed >> (i << log_boxes)) & (uint32_t)((1ull << boxes) - 1);
@@ -357,6 +351,9 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
                 }
             }
             ++unit;
+            next_unit(p, cur, part.places, piece_end);     // (while this one's last tiles are on their way)
+            to_tiles(cur);
+            if (cur.at < piece_end) next = find(cur, unit_part(p, cur, piece_end), 0);
         }
     } else if (warp == 1) {
         // ================================ S^T = K Q^T ================================
