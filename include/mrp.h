@@ -504,7 +504,8 @@ int mrp_paged_attention(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_modul
  *                        other: the row is its codes times 2^(s - 127); 255: NaN in all features
  * Half the bytes of a bf16 cache to hold and to read (head_dim + 1 a row).  A power of two as the scale costs no precision
  * that a finer one would keep, codes being floating point themselves, and makes every row exact in bf16.  Codes 0x7F and
- * 0xFF (NaN) are never written; in a row that is seen, mrp_paged_attention_q8 may read them as any value.
+ * 0xFF (NaN) and scale bytes 248 to 254 are never written; where a row that is seen has one, the output of its sequence may be
+ * anything.
  */
 typedef struct {
     uint8_t *k, *v;
@@ -514,8 +515,8 @@ typedef struct {
 /*
  * mrp_kv_append into such a cache: k normalised and rotated on the way, then k and v row by row to codes.  E = s - 127 is the
  * smallest integer with max |row| <= 448 * 2^E (at least -127; 0 for a row of zeros), codes are rounded to nearest, ties to
- * even: once, from the fp32 result (k) or from the values themselves (v).  A row with a value that is not finite becomes a
- * row of NaN.  Everything else as in mrp_kv_append.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * even: once, from the fp32 result (k) or from the values themselves (v); of the largest rows (E = 120) codes stop at 240, so
+ * that they stay finite.  A row with a value that is not finite becomes a row of NaN.  Everything else as in mrp_kv_append.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 int mrp_kv_append_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_qkv_rows *rows,
                      void *cuda_stream);

@@ -97,14 +97,15 @@ def attention(q, k_pages, v_pages, seq_start, prefix_len, page_table, page_size,
 
 def q8_rows(x):
     """Rows x [.., D] -> (e4m3 codes uint8 [.., D], scale bytes uint8 [..]): row = codes * 2^(byte - 127), the exponent the
-    smallest one >= -127 with max |row| <= 448 * 2^E, 0 for a row of zeros; byte 255 (codes 0) where a value is not finite."""
+    smallest one >= -127 with max |row| <= 448 * 2^E, 0 for a row of zeros, codes of rows with E = 120 at most 240; byte 255 (codes 0) where a value is not finite."""
     from oracle import fp8
     x = np.asarray(x, np.float64)
     flat = x.reshape(-1, x.shape[-1])
     bad = ~np.isfinite(flat).all(-1)
     flat = np.where(bad[:, None], 0.0, flat)
     scale = np.maximum(fp8.row_scales(flat), 2.0 ** -127)
-    codes = fp8.encode(flat / scale[:, None])
+    top = np.where(scale == 2.0 ** 120, 240.0, 448.0)[:, None]             # (256 * 2^120 is infinite in fp32 and bf16)
+    codes = fp8.encode(np.clip(flat / scale[:, None], -top, top))
     byte = np.where(bad, 255, np.frexp(scale)[1] - 1 + 127).astype(np.uint8)
     return codes.reshape(x.shape), byte.reshape(x.shape[:-1])
 

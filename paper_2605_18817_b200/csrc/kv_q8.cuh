@@ -5,6 +5,7 @@
 namespace mrp {
 
 constexpr uint32_t kQ8NaN = 255;           // the scale byte of a row with a value that is not finite
+constexpr uint32_t kQ8Last = 247;          // the largest one else: the largest fp32 lies below 256 * 2^120
 
 // Where rows of the pools and their scales lie (elements are bytes).
 struct PoolQ8 {

@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
         step *= NG;
         const bool codes = Q8 && kind > 0;
         // 8 bits: the row's scale from its largest magnitude, then the lane's codes and the row's byte
-        auto put_codes = [&](const float *f, int i) {
+        auto put_codes = [&](float *f, int i) {
             uint32_t top = 0;
 #pragma unroll
             for (int y = 0; y < 8; ++y) top = max(top, __float_as_uint(f[y]) & 0x7FFFFFFFu);
@@ -169,10 +169,15 @@ __global__ void __launch_bounds__(kRowThreads, 4) qk_rows_kernel(const __grid_co
             const uint32_t sc = q8_scale(top);
             const bool fine = sc != kQ8NaN;
             const float inv = q8_inverse(fine ? sc : 127u);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) f[y] *= inv;
+            if (sc == kQ8Last)                             // (256 * 2^120 would be infinite: the row stays finite)
+#pragma unroll
+                for (int y = 0; y < 8; ++y) f[y] = fminf(fmaxf(f[y], -240.f), 240.f);
             if (store && i * NG < n) {
                 uint8_t *to = reinterpret_cast<uint8_t *>(p.dst[kind]) + page_off + (int64_t)(h0 + i * NG) * head_out;
-                *reinterpret_cast<uint32_t *>(to + e0) = fine ? q8_codes(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv) : 0u;
-                *reinterpret_cast<uint32_t *>(to + e1) = fine ? q8_codes(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv) : 0u;
+                *reinterpret_cast<uint32_t *>(to + e0) = fine ? q8_codes(f[0], f[1], f[2], f[3]) : 0u;
+                *reinterpret_cast<uint32_t *>(to + e1) = fine ? q8_codes(f[4], f[5], f[6], f[7]) : 0u;
                 if (gl == 0) p.scale[kind - 1][scale_off + (int64_t)(h0 + i * NG) * p.b.page.d] = (uint8_t)sc;
             }
         };

@@ -13,6 +13,7 @@ def test_codes_and_scales_of_rows():
     v = ref.q8_values(codes, byte)
     assert np.isnan(v[5:7]).all() and (codes[5:7] == 0).all()
     assert v[0].tolist() == [0, 0, 0] and v[1].tolist() == [448.0, -1.0, 2.0 ** -9] and v[3].tolist() == [3.5, -3.5, 0.0]
+    assert v[7].tolist() == [240 * 2.0 ** 120, 0.0, -240 * 2.0 ** 120] and np.isfinite(np.float32(v[7])).all()
     assert v[2].tolist() == [448.0, 0.0, 1.0] and v[4, 0] in (0.0, 2.0 ** -136)
     r = np.random.default_rng(1).standard_normal((200, 64)) * np.exp(np.random.default_rng(2).standard_normal((200, 1)) * 5)
     codes, byte = ref.q8_rows(r)
