@@ -25,8 +25,11 @@ namespace {
 template <int HB, int ROWS> struct FewQ8Geo {
     static constexpr int NR = ROWS;
     static constexpr int kCols = 2 * NR;                   // columns of S (hi, lo of Q), of P (hi, lo) and of an accumulator
-    // of 128 keys, 128 codes: as much in flight as there is room for (three and four: 64 ragged 139 us)
-    static constexpr int kKStages = 4, kRawStages = HB + NR / 8 == 2 ? 5 : HB + NR / 8 == 3 ? 4 : 3;
+    // of 128 keys, 128 codes: as much in flight as there is room for (three and four: 64 ragged 139 us).  Raw stages are even in number:
+    // a stage belongs to one group of the turning warps then, which waits for every one of its phases.  With an odd number a group
+    // could come to a stage whose phase before, the other group's, is still open, and take it for its own.
+    static constexpr int kKStages = HB + NR / 8 == 3 ? 4 : 5, kRawStages = HB + NR / 8 == 4 ? 2 : 4;
+    static_assert(kRawStages % 2 == 0, "a group of turning warps a raw stage");
     static constexpr int kRawAt = kKStages * 16384;
     static constexpr int kVAt = kRawAt + kRawStages * 16384;               // two stages of bf16 V
     static constexpr int kPRow = kCols * 2, kP = 128 * kPRow;              // P of a warpgroup: 128 keys, rows of 32 or 64 swizzled bytes
@@ -181,9 +184,9 @@ kv_attention_few_q8_kernel(const __grid_constant__ AttnParams p, const __grid_co
     auto r_at = [&](int s) { return base + G::kRawAt + s * 16384; };       // codes of V, raw
     auto v_at = [&](int s) { return base + G::kVAt + s * 32768; };         // V in bf16
     auto k_full = [&](int s) { return bars + 8 * s; };
-    auto k_empty = [&](int s) { return bars + 8 * (4 + s); };
-    auto raw_full = [&](int s) { return bars + 8 * (8 + s); };     // the codes, and their scales
-    auto raw_empty = [&](int s) { return bars + 8 * (14 + s); };
+    auto k_empty = [&](int s) { return bars + 8 * (6 + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (12 + s); };    // the codes, and their scales
+    auto raw_empty = [&](int s) { return bars + 8 * (16 + s); };
     auto v_full = [&](int s) { return bars + 8 * (20 + s); };
     auto v_empty = [&](int s) { return bars + 8 * (22 + s); };
     auto s_full = [&](int b) { return bars + 8 * (40 + b); };      // the scores of a tile, and the keys' scales
