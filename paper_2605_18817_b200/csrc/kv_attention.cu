@@ -782,6 +782,7 @@ cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const m
     p.k = pool.k; p.v = pool.v;
     p.k_scale = pool.k_scale; p.v_scale = pool.v_scale;
     p.scale_bytes = (int64_t)c->kv.n_pages * c->kv.n_kv_heads * c->kv.page_size;
+    if (a.mask == MRP_ATTN_PREFIX) p.b.beyond = 0x7fffffff - p.b.cap;      // (the block's own keys lie elsewhere)
     return kv_tc_takes_q8(c->cfg, c->kv) ? launch_paged_attention_q8_tc(c, p, batch, st) : launch<kFromQ8>(c, p, st);
 }
 

@@ -38,6 +38,7 @@ struct KvBatch {
     const int32_t *seq_start, *prefix_len, *page_table, *positions;
     int n_seqs, n_tokens, n_pages, max_pages;
     int cap;                   // positions a sequence can hold
+    int beyond = 0;            // how far new tokens may lie behind them: 0, or any way where they need no place in the cache
     FastDiv page;              // page_size
     int64_t page_stride;       // elements
     int32_t *status, *user_status;
@@ -75,7 +76,7 @@ __device__ __forceinline__ bool kv_sequence(const KvBatch &b, int s, int &start,
     const int end = __ldg(b.seq_start + s + 1);
     pre = b.prefix_len ? __ldg(b.prefix_len + s) : 0;     // (no cache: nothing lies in front of the rows)
     n = end - start;
-    return start >= 0 && end >= start && end <= b.n_tokens && pre >= 0 && pre <= b.cap && n <= b.cap - pre;
+    return start >= 0 && end >= start && end <= b.n_tokens && pre >= 0 && pre <= b.cap && n <= b.cap + b.beyond - pre;
 }
 
 // ---- workspace: arrival counters, then (max, sum) pairs and rows of partial results -----------------------------------

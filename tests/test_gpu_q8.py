@@ -539,3 +539,29 @@ def test_refusals_on_the_host():
         assert fn(None, None, None, None, None) == 1
     with pytest.raises(TypeError):
         b.KvPoolQ8(*(torch.zeros((2, 1, 4, 8), dtype=torch.uint8) for _ in range(4)))
+
+
+@gpu
+@pytest.mark.parametrize("dtype,H,Hk,D,P,lens", [
+    ("f32", 4, 2, 64, 16, [(30, 40), (5, 90)]), ("f32", 3, 1, 8, 1, [(2, 9)]), ("bf16", 3, 1, 80, 7, [(20, 33), (0, 40)]),
+    ("bf16", 2, 2, 128, 8, [(64, 16), (32, 12)]), ("bf16", 4, 2, 128, 16, [(60, 32), (64, 64)]), ("bf16", 2, 2, 64, 32, [(90, 200), (0, 300)])],
+    ids=str)
+def test_the_cache_alone_needs_no_room_for_the_block(dtype, H, Hk, D, P, lens):
+    c = CacheQ8(dtype, H, Hk, D, P, [(p, 0) for p, _ in lens], seed=D)
+    cap = c.max_pages * P
+    c.T = sum(n for _, n in lens)
+    c.lens, c.start_np = lens, np.concatenate([[0], np.cumsum([n for _, n in lens])]).astype(np.int32)
+    c.seq_start = torch.from_numpy(c.start_np).to(DEV)
+    c.batch = c.b.KvBatch(c.seq_start, c.prefix_len, c.table, c.T, max(n for _, n in lens), None, c.status)
+    over = [p + n > cap for p, n in lens]
+    q = c.rand(c.T, H, D)
+    out, lse = c.attend(q, mask=c.b.MRP_ATTN_BLOCK)                # (elsewhere the rule stays)
+    assert int(c.status) != 0 and any(over)
+    c.status.zero_()
+    for (p, n), s in zip(lens, c.start_np):
+        assert p + n <= cap or bool((out[s:s + n] == 7).all() and (lse[s:s + n] == 7).all())
+    c.max_pages = 1 << 20                                          # what the plain form refuses by
+    for window in (0, 50):
+        out, lse = c.attend(q, mask=c.b.MRP_ATTN_PREFIX, window=window)
+        close(c, q, out, lse, mask=2, window=window)
+    assert int(c.status) == 0
