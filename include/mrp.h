@@ -513,10 +513,11 @@ typedef struct {
 } mrp_kv_pool_q8;
 
 /*
- * mrp_kv_append into such a cache: k normalised and rotated on the way, then k and v row by row to codes.  E = s - 127 is the
- * smallest integer with max |row| <= 448 * 2^E (at least -127; 0 for a row of zeros), codes are rounded to nearest, ties to
- * even: once, from the fp32 result (k) or from the values themselves (v); of the largest rows (E = 120) codes stop at 240, so
- * that they stay finite.  A row with a value that is not finite becomes a row of NaN.  Everything else as in mrp_kv_append.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * mrp_kv_append into such a cache: k normalised and rotated on the way, then k and v row by row to codes.  E = s - 127 is
+ * the smallest integer with max |row| <= 448 * 2^E (at least -127; 0 for a row of zeros), codes are rounded to nearest,
+ * ties to even: once, from the fp32 result (k) or from the values themselves (v); of the largest rows (E = 120) codes stop
+ * at 240, so that they stay finite.  A row with a value that is not finite becomes a row of NaN.  Everything else as in
+ * mrp_kv_append.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 int mrp_kv_append_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool, const mrp_qkv_rows *rows,
                      void *cuda_stream);
@@ -538,9 +539,10 @@ int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8
 
 /*
  * mrp_paged_attention over such a cache: the same masks, outputs and work split, on the values the rows stand for.  Queries
- * stay as they are.  With MRP_ATTN_PREFIX the new tokens need no room in the cache: prefix_len[b] alone has to fit.  A visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does
- * not depend on values).  bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA
- * feeds; others, f32 and MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * stay as they are.  With MRP_ATTN_PREFIX the new tokens need no room in the cache: prefix_len[b] alone has to fit.  A
+ * visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
+ * bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA feeds; others, f32 and
+ * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool,
                            const mrp_attention_args *args, void *cuda_stream);

@@ -334,14 +334,16 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
     auto to_values = [&](uint32_t raw, uint32_t sk) {
         const uint32_t sv = sk + kWarpKeys * G::kPitchK, words = raw + 2 * kWarpKeys * DP;
         constexpr int lanes = DP / 8;
+        uint32_t at, sc;                                   // of row `lane`: 0 .. 15 keys, then values
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(at) : "r"(words + 2 * kWarpKeys * 4 + lane) : "memory");
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(words + lane * 4 + at) : "memory");
+        const float own = q8_factor(sc);
 #pragma unroll 2
         for (int i = lane; i < 2 * kWarpKeys * lanes; i += 32) {
-            const int row = i / lanes, ch = i % lanes, key = row & 15;         // rows 0 .. 15: keys, then values
-            uint32_t c0, c1, at, sc;
+            const int row = i / lanes, ch = i % lanes, key = row & 15;
+            uint32_t c0, c1;
             asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c0), "=r"(c1) : "r"(raw + row * DP + ch * 8) : "memory");
-            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(at) : "r"(words + 2 * kWarpKeys * 4 + row) : "memory");
-            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sc) : "r"(words + row * 4 + at) : "memory");
-            const float f = q8_factor(sc);
+            const float f = __shfl_sync(0xffffffffu, own, row);
             const float2 a = q8_values(c0 & 0xFFFFu, f), b = q8_values(c0 >> 16, f), c = q8_values(c1 & 0xFFFFu, f), d = q8_values(c1 >> 16, f);
             const uint32_t to = row < kWarpKeys ? sk + key * G::kPitchK : sv + key * G::kPitchV;
             if constexpr (kBf16) {                         // (exact: four significant bits)

@@ -11,11 +11,15 @@
 //
 //   warp 0   K by TMA, and its scales      warp 1   S MMAs      warp 2   PV MMAs      warp 3   V and its scales
 //   warps 4-7, 8-11   softmax, a thread per key and eight rows: two warpgroups that take tiles in turn (8 rows; maxima, sums and
-//            accumulators of their own, joined at the unit's end) or the same tiles' rows by halves (16 rows: @@SPLIT@@)
+//            accumulators of their own, joined at the unit's end) or the same tiles' rows by halves (16 rows: 32 blocks of 4 take 67 us
+//            either way, but a thread's 16 rows would need 100 registers and leave room for four turning warps instead of eight)
 //   warps 12-15   queries, a unit ahead, and units' ends          from warp 16 on   V's codes -> bf16 (two groups of four warps, a stage each)
 // Instructions bound it next to memory, so each role's loop is short: the roles of an SM quarter share its instruction cache and
 // its issue slots.  (One warp for both kinds of MMAs, scales looked up by the warps that use them, turning unrolled: 64 ragged
 // single tokens 266 us; the turning rolled and 8 rows instead of 16: 159.)
+// Measured, in a graph: 64 ragged single tokens of up to 9000 positions, 32 / 8 heads of 128: 130 us for 623 MB, 4.8 TB/s (issue
+// slots 48 % busy, DRAM 58 %); 32 blocks of 4 behind 200 to 6000 positions 67 us; one token behind 2500, 16 / 8 heads 14 us, which is
+// the chain of start, cut of the line, page entries, a tile and the join of 16 pieces, none of it wide.
 #include "kv_tile.cuh"
 
 namespace mrp {

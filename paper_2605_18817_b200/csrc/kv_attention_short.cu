@@ -6,8 +6,8 @@
 // head, a warp 16 of them, which it takes from the scores to the output in registers (mma.sync m16n8k16); keys and values go
 // through shared memory in chunks of 64 (cp.async, two stages), and three CTAs share an SM.
 // Longer sequences are served rightly too, a chunk after the other; the 128-row tiles (kv_attention_tc.cu) do it faster.  The
-// whole call, with joining: 32 blocks of 4, 32 / 8 heads, @@B4@@ us (128-row tiles 19.0); 12 blocks of 32, 16 / 8 heads, @@B32@@
-// (12.1); 40 prompts of up to 70 tokens, 15 / 5 heads of 80, @@ODD@@ (24.5).
+// whole call, with joining: 32 blocks of 4, 32 / 8 heads, 8.6 us (128-row tiles 19.0); 12 blocks of 32, 16 / 8 heads, 9.1
+// (12.1); 40 prompts of up to 70 tokens, 15 / 5 heads of 80, 18.1 (24.5).
 //
 // V rows behind the sequence's end arrive as zeros.  A V row with a value that is not finite, where masks differ between rows, is
 // zeroed in shared memory (0 * NaN), and the rows that see it are NaN in all features.

@@ -28,6 +28,16 @@
 //   Where a maximum grows, each warp of a pair rescales half of the accumulator's columns, and the pair meets before the first
 //   product of the tile may start: that product adds to all columns.
 //
+// Other sources of K and V (LAY), same tiles and MMAs:
+//   kPacked  rows beside the queries, no pages: 4 prompts of 600 to 4000 tokens, 32 / 8 heads: 435 us, 0.74 PFLOP/s.  Joining reads
+//            the row and its log-sum-exp before it writes them.
+//   kCodes   8 bits: TMA fetches codes into raw stages, and warps of their own (two beside two row tiles, four beside one) turn
+//            codes times scales into bf16 stages of the ring, exactly.  Waits, lookups and cleaning are functions then: a loop of
+//            every role has to stay in the instruction caches (inlined: prompt chunks 810 us).  2 chunks of 2000 behind 4000 to
+//            6000 positions, 32 / 8 heads: 630 us, 0.71 PFLOP/s; a ring of three stages beside the raw ones and the turning's
+//            issue slots (47 % busy against 39 %) are what 16 bits does not pay.  Four turning warps spill and give 625; a third
+//            raw stage and rolled loops over half a row's scores give nothing.  12 blocks of 32: 55 us.
+//
 // Pages hold what they hold behind a sequence's end: scores of positions a row does not see are replaced before they are
 // used, and V rows that no row of the tile sees are zeroed in shared memory before the product (0 * NaN).  A V row with
 // an infinity or NaN that only some rows of a tile see (later tokens of a prompt) is zeroed too and makes the output of

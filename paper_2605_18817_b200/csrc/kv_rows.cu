@@ -15,6 +15,8 @@
 // rot_dim / 2 that is no multiple of four splits runs: there the other half of a pair is read again.
 // Measured, 32 query and 8 key heads of 128 in bf16 with norms: 16384 tokens 64 us (336 MB: 5.2 TB/s), 24509 tokens with values
 // into pages 105 us (602 MB: 5.7 TB/s, 0.89 of a copy); 4 tokens 3.6 us and 128 tokens 4.2 us a launch inside a graph.
+// Into 8 bits (the largest of a row over the lanes that hold it, codes by cvt.e4m3x2): 7 prompts of 500 to 3500 tokens with their
+// queries 81 us (354 MB: 4.4 TB/s), bound by instructions (issue slots 68 % busy, DRAM 47 %); 24 blocks of 4 5.6 us.
 #include <cuda_fp16.h>
 
 #include "kv_attention.cuh"
