@@ -16,12 +16,17 @@
 //
 // bf16: mma.sync m16n8k16, operands by ldmatrix from XOR-swizzled rows, probabilities as bf16 hi + lo.
 // f32:  mma.sync m16n8k8 on tf32 operands split into two (x = hi + lo, three products: relative 2^-21).
+// f32 on 8 bits: keys and values are exact in bf16, so m16n8k16 with queries and probabilities in three bf16 parts (2^-24): half the
+// products, no splits of keys and half the stage.  24 sequences as below, 128 features 143 us (tf32, one part of K and V: 174),
+// 256 features 364 (466); 7 of up to 9 tokens behind a window, heads of 72: 35 (38).  What is left is a tile's chain at two CTAs an SM.
 //
 // What bounds it: the instructions around the products (f32: splitting K and V, three conversions and a subtraction a value and
 // row of the tile), not memory.  24 sequences of 200 to 6000 positions, one token each, 32 / 8 heads: bf16 of 128 features in
 // pages of 20 rows 100 us (48 for the bytes); f32 107 (48) at 64 features, 184 (97) at 128, 530 (193) at 256.  Two CTAs an SM
 // count more than a second stage: f32 of 128 features 235 us with two stages of one CTA.  Rows beyond 16 take a unit per 16.
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "kv_attention.cuh"
 #include "kv_q8.cuh"
@@ -79,6 +84,18 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint3
     const __nv_bfloat162 l = __floats2bfloat162_rn(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
     lo = *reinterpret_cast<const uint32_t *>(&l);
 }
+// The same for 32 bits in three parts: two cut off (so that none becomes infinite), the last rounded: below 2^-24 of x is left out
+__device__ __forceinline__ void split3_bf16(float a, float b, uint32_t (&part)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        part[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+        a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+    }
+    const __nv_bfloat162 l = __floats2bfloat162_rn(a, b);
+    part[2] = *reinterpret_cast<const uint32_t *>(&l);
+}
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
@@ -102,17 +119,21 @@ template <int DP> struct Geo<float, DP> {
 };
 template <typename T, int DP, int SRC> struct Smem {
     typedef Geo<T, DP> G;
-    static constexpr int kStage = kWarpKeys * (G::kPitchK + G::kPitchV);
+    // f32 on 8 bits: keys and values are exact in bf16, queries and probabilities go in three bf16 parts
+    static constexpr bool kThree = sizeof(T) == 4 && SRC == kFromQ8;
+    typedef typename std::conditional<kThree, __nv_bfloat16, T>::type Held;        // what a stage holds
+    typedef Geo<Held, DP> GH;
+    static constexpr int kStage = kWarpKeys * (GH::kPitchK + GH::kPitchV);
     static constexpr int kRedPitch = DP + 4;               // floats
     // 8 bits: a ring of raw stages (codes of K and V, the 4-byte words their scales lie in, the bytes in those), and one
     // stage of values, which at the end of a unit takes the warp's parts
-    static constexpr int kLoads = SRC != kFromQ8 ? G::kStages : DP <= (sizeof(T) == 2 ? 128 : 64) ? 3 : 2;        // (f32 of 128 features: two CTAs an SM)
+    static constexpr int kLoads = SRC != kFromQ8 ? G::kStages : DP <= 128 ? 3 : 2;
     static constexpr int kRaw = 2 * kWarpKeys * DP + 2 * kWarpKeys * 4 + 2 * kWarpKeys;
     static constexpr int kParts = kRows * kRedPitch * 4;
     static constexpr int kValues = kStage > kParts ? kStage : kParts;
     static constexpr int kWarp = SRC == kFromQ8 ? kLoads * kRaw + kValues : kLoads * kStage;
     static constexpr int kRing = kWarps * kWarp;
-    static constexpr int kQ = kRows * G::kPitchQ;
+    static constexpr int kQPart = kRows * GH::kPitchQ, kQ = (kThree ? 3 : 1) * kQPart;
     static constexpr int kRed = SRC == kFromQ8 ? 0 : kWarps * kParts;
     static constexpr int kMl = 2 * kWarps * kRows * 4;
     static constexpr int kTotal = kRing + kQ + kRed + kMl;
@@ -181,7 +202,9 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
 {
     typedef Geo<T, DP> G;
     typedef Smem<T, DP, SRC> S;
-    constexpr bool kBf16 = sizeof(T) == 2;
+    typedef typename S::Held Held;
+    typedef Geo<Held, DP> GH;
+    constexpr bool kBf16 = sizeof(T) == 2, kThree = S::kThree;
     constexpr int kStages = S::kLoads;
     constexpr int NF = DP / 8;                             // 8-feature blocks of the accumulator
     constexpr bool kQRegs = kBf16 && DP <= 128;
@@ -332,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
     };
     // 8 bits: a landed raw stage -> values, as a stage of the other kinds holds them
     auto to_values = [&](uint32_t raw, uint32_t sk) {
-        const uint32_t sv = sk + kWarpKeys * G::kPitchK, words = raw + 2 * kWarpKeys * DP;
+        const uint32_t sv = sk + kWarpKeys * GH::kPitchK, words = raw + 2 * kWarpKeys * DP;
         constexpr int lanes = DP / 8;
         uint32_t at, sc;                                   // of row `lane`: 0 .. 15 keys, then values
         asm volatile("ld.shared.u8 %0, [%1];" : "=r"(at) : "r"(words + 2 * kWarpKeys * 4 + lane) : "memory");
@@ -345,17 +368,13 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
             asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c0), "=r"(c1) : "r"(raw + row * DP + ch * 8) : "memory");
             const float f = __shfl_sync(0xffffffffu, own, row);
             const float2 a = q8_values(c0 & 0xFFFFu, f), b = q8_values(c0 >> 16, f), c = q8_values(c1 & 0xFFFFu, f), d = q8_values(c1 >> 16, f);
-            const uint32_t to = row < kWarpKeys ? sk + key * G::kPitchK : sv + key * G::kPitchV;
-            if constexpr (kBf16) {                         // (exact: four significant bits)
-                const __nv_bfloat162 w0 = __floats2bfloat162_rn(a.x, a.y), w1 = __floats2bfloat162_rn(b.x, b.y),
-                                     w2 = __floats2bfloat162_rn(c.x, c.y), w3 = __floats2bfloat162_rn(d.x, d.y);
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + ((ch ^ (key & 7)) << 4)), "r"(*reinterpret_cast<const uint32_t *>(&w0)),
-                             "r"(*reinterpret_cast<const uint32_t *>(&w1)), "r"(*reinterpret_cast<const uint32_t *>(&w2)),
-                             "r"(*reinterpret_cast<const uint32_t *>(&w3)) : "memory");
-            } else {
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + ch * 32), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y) : "memory");
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + ch * 32 + 16), "f"(c.x), "f"(c.y), "f"(d.x), "f"(d.y) : "memory");
-            }
+            const uint32_t to = row < kWarpKeys ? sk + key * GH::kPitchK : sv + key * GH::kPitchV;
+            // (exact: four significant bits; below 2^-133 rounded)
+            const __nv_bfloat162 w0 = __floats2bfloat162_rn(a.x, a.y), w1 = __floats2bfloat162_rn(b.x, b.y),
+                                 w2 = __floats2bfloat162_rn(c.x, c.y), w3 = __floats2bfloat162_rn(d.x, d.y);
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + ((ch ^ (key & 7)) << 4)), "r"(*reinterpret_cast<const uint32_t *>(&w0)),
+                         "r"(*reinterpret_cast<const uint32_t *>(&w1)), "r"(*reinterpret_cast<const uint32_t *>(&w2)),
+                         "r"(*reinterpret_cast<const uint32_t *>(&w3)) : "memory");
         }
         __syncwarp();
     };
@@ -363,15 +382,6 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) load_tile(s);
 
-    // (what 8 bits stand for has four significant bits: one tf32 part is all of it, and a product less is needed)
-    auto split_key = [](float x, uint32_t &hi, uint32_t &lo) {
-        if (SRC == kFromQ8) {
-            hi = __float_as_uint(x);
-            lo = 0;
-        } else {
-            split_tf32(x, hi, lo);
-        }
-    };
     const long long piece_end = cur.at + len;
     int stage = 0;
     long long at = cur.at;
@@ -389,8 +399,17 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                 x = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.q) + (int64_t)(cur.start + tok) * p.q_stride +
                                                           (int64_t)(cur.h * p.g + hg) * p.D) + ch);
             }
-            const uint32_t a = sq + r * G::kPitchQ + ((G::kSwizzle ? ch ^ (r & 7) : ch) << 4);
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+            if constexpr (kThree) {
+                uint32_t u[3], w[3];
+                split3_bf16(__uint_as_float(x.x), __uint_as_float(x.y), u);
+                split3_bf16(__uint_as_float(x.z), __uint_as_float(x.w), w);
+#pragma unroll
+                for (int y = 0; y < 3; ++y)
+                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(chunk_at<DP>(sq + y * S::kQPart, r, ch >> 1) + (ch & 1) * 8), "r"(u[y]), "r"(w[y]) : "memory");
+            } else {
+                const uint32_t a = sq + r * G::kPitchQ + ((G::kSwizzle ? ch ^ (r & 7) : ch) << 4);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+            }
         }
         if (SRC == kFromRows && p.join && tid < t.rows) {
             const int row = t.r0 + tid, tok = row / p.g;
@@ -426,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
             load_tile((stage + kStages - 1) % kStages);
             cp_wait<kStages - 1>();
             __syncwarp();
-            const uint32_t sk = SRC == kFromQ8 ? ring + kStages * S::kRaw : ring + stage * S::kStage, sv = sk + kWarpKeys * G::kPitchK;
+            const uint32_t sk = SRC == kFromQ8 ? ring + kStages * S::kRaw : ring + stage * S::kStage, sv = sk + kWarpKeys * GH::kPitchK;
             if constexpr (SRC == kFromQ8) to_values(ring + stage * S::kRaw, sk);
             const int j0 = key_tile(t, begin_tile + n) * kTile + warp * kWarpKeys;
             float s[2][4];
@@ -447,6 +466,32 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                     }
                     mma16(s[0], a, b[0], b[1]);
                     mma16(s[1], a, b[2], b[3]);
+                }
+            } else if constexpr (kThree) {
+                // (32 features at a time, added here: see below; the smallest parts first)
+#pragma unroll 1
+                for (int k2 = 0; k2 < DP / 32; ++k2) {
+                    float d[2][4];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) d[x][y] = 0.f;
+                    uint32_t b[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) ldsm4(chunk_at<DP>(sk, ((lane >> 4) << 3) + (lane & 7), 4 * k2 + 2 * i + ((lane >> 3) & 1)), b[i]);
+#pragma unroll
+                    for (int y = 2; y >= 0; --y)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t a[4];
+                            ldsm4(chunk_at<DP>(sq + y * S::kQPart, lane & 15, 4 * k2 + 2 * i + (lane >> 4)), a);
+                            mma16(d[0], a, b[i][0], b[i][1]);
+                            mma16(d[1], a, b[i][2], b[i][3]);
+                        }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) s[x][y] += d[x][y];
                 }
             } else {
                 // the tensor pipe cuts its sums off instead of rounding them: 32 products at a time, added here
@@ -473,10 +518,10 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                             float2 kb;
                             asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(kb.x), "=f"(kb.y) : "r"(sk + (x * 8 + gid) * G::kPitchK + at) : "memory");
                             uint32_t bh[2], bl[2];
-                            split_key(kb.x, bh[0], bl[0]);
-                            split_key(kb.y, bh[1], bl[1]);
+                            split_tf32(kb.x, bh[0], bl[0]);
+                            split_tf32(kb.y, bh[1], bl[1]);
                             mma8(d[x], al, bh[0], bh[1]);
-                            if (SRC != kFromQ8) mma8(d[x], ah, bl[0], bl[1]);
+                            mma8(d[x], ah, bl[0], bl[1]);
                             mma8(d[x], ah, bh[0], bh[1]);
                         }
                     }
@@ -523,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                     s[x][y] = exp2_fast(fmaf(s[x][y], p.scale_log2, -mm[y >> 1]));
                     l[y >> 1] += s[x][y];
                 }
-            if (!whole && differ) patch_nonfinite<T, DP, NF>(sv, s, o, lane);
+            if (!whole && differ) patch_nonfinite<Held, DP, NF>(sv, s, o, lane);
             if constexpr (kBf16) {
                 // probabilities as bf16 hi + lo (2^-17 together): with few rows the second product costs nothing that shows
                 uint32_t a[4], al[4];
@@ -539,6 +584,30 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                     mma16(o[f + 1], al, b[2], b[3]);
                     mma16(o[f], a, b[0], b[1]);
                     mma16(o[f + 1], a, b[2], b[3]);
+                }
+            } else if constexpr (kThree) {
+                uint32_t a[3][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; y += 2) {
+                        uint32_t w[3];
+                        split3_bf16(s[x][y], s[x][y + 1], w);
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) a[i][2 * x + (y >> 1)] = w[i];
+                    }
+#pragma unroll
+                for (int f = 0; f < NF; f += 2) {
+                    uint32_t b[4];
+                    ldsm4t(chunk_at<DP>(sv, (((lane >> 3) & 1) << 3) + (lane & 7), f + (lane >> 4)), b);
+                    float d[2][4] = {};
+#pragma unroll
+                    for (int i = 2; i >= 0; --i) {
+                        mma16(d[0], a[i], b[0], b[1]);
+                        mma16(d[1], a[i], b[2], b[3]);
+                    }
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) { o[f][y] += d[0][y]; o[f + 1][y] += d[1][y]; }
                 }
             } else {
                 uint32_t ah[2][4], al[2][4];               // keys 2 tig, 2 tig + 1 stand for k = tig, tig + 4
@@ -559,10 +628,10 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v0) : "r"(a0) : "memory");
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v1) : "r"(a0 + G::kPitchV) : "memory");
                         uint32_t bh[2], bl[2];
-                        split_key(v0, bh[0], bl[0]);
-                        split_key(v1, bh[1], bl[1]);
+                        split_tf32(v0, bh[0], bl[0]);
+                        split_tf32(v1, bh[1], bl[1]);
                         mma8(d, al[x], bh[0], bh[1]);
-                        if (SRC != kFromQ8) mma8(d, ah[x], bl[0], bl[1]);
+                        mma8(d, ah[x], bl[0], bl[1]);
                         mma8(d, ah[x], bh[0], bh[1]);
                     }
 #pragma unroll
