@@ -542,8 +542,8 @@ int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8
  * stay as they are.  With MRP_ATTN_PREFIX the new tokens need no room in the cache: prefix_len[b] alone has to fit.  A
  * visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
  * bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA feeds; others, f32 and
- * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Values below 2^-133 are rounded to multiples of it (f32 too).  Errors:
- * INVALID_ARG, UNSUPPORTED, CUDA.
+ * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Values below 2^-126 may lose bits (f32 too).  Errors: INVALID_ARG,
+ * UNSUPPORTED, CUDA.
  */
 int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool,
                            const mrp_attention_args *args, void *cuda_stream);
