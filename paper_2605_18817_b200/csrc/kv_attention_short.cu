@@ -9,8 +9,9 @@
 // whole call, with joining: 32 blocks of 4, 32 / 8 heads, 8.6 us (128-row tiles 19.0); 12 blocks of 32, 16 / 8 heads, 9.1
 // (12.1); 40 prompts of up to 70 tokens, 15 / 5 heads of 80, 18.1 (24.5).
 //
-// V rows behind the sequence's end arrive as zeros.  A V row with a value that is not finite, where masks differ between rows, is
-// zeroed in shared memory (0 * NaN), and the rows that see it are NaN in all features.
+// Keys that no row of the CTA sees (behind the sequence's end or the diagonal, before the window) are not read and count as zeros: 0 *
+// NaN must not reach a product.  A V row with a value that is not finite that some rows of the CTA see and others do not is zeroed in
+// shared memory, and the rows that see it are NaN in all features.
 #include "kv_attention.cuh"
 
 namespace mrp {
@@ -90,7 +91,7 @@ __device__ __forceinline__ void short_rows(const AttnParams &p, int start, int n
         const int fill = min(kChunk, (n - c * kChunk + 15) & ~15) * C;         // (sixteen keys at a time are read)
         for (int i = tid; i < fill; i += kShortThreads) {
             const int row = i / C, ch = i % C, j = c * kChunk + row;
-            const bool on = j < n && ch * 8 < p.D;
+            const bool on = j < end && (j >= lo || j < p.sinks) && ch * 8 < p.D;
             copy16(row_chunk<DP>(sk, row, ch), kp + (on ? (int64_t)j * p.k_stride + ch * 8 : 0), on);
             copy16(row_chunk<DP>(sv, row, ch), vp + (on ? (int64_t)j * p.v_stride + ch * 8 : 0), on);
         }
