@@ -410,9 +410,9 @@ int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t
  * (any number, also none), at positions prefix_len[b], prefix_len[b] + 1, ... behind the prefix_len[b] positions the
  * sequence has in the cache already.  All arrays DEVICE; the lengths are read on the device, so a captured call serves
  * other lengths on replay.  A sequence whose rows or positions do not fit (0 <= seq_start[b] <= seq_start[b + 1] <=
- * n_tokens, 0 <= prefix_len[b], prefix_len[b] + new tokens <= max_pages * page_size) raises MRP_DEV_BAD_INDEX and is
- * skipped: nothing of it is stored or written.  Rows that belong to no sequence are left alone.  The rows of two
- * sequences must not overlap.
+ * n_tokens, 0 <= prefix_len[b], prefix_len[b] + new tokens <= max_pages * page_size, with MRP_ATTN_PREFIX prefix_len[b]
+ * alone <= that) raises MRP_DEV_BAD_INDEX and is skipped: nothing of it is stored or written.  Rows that belong to no
+ * sequence are left alone.  The rows of two sequences must not overlap.
  */
 typedef struct {
     const int32_t *seq_start;   /* [n_seqs + 1]                                                      */
@@ -466,7 +466,7 @@ int mrp_kv_append(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_module_kv *
 typedef enum {
     MRP_ATTN_CAUSAL = 0,        /* 0 .. p                                                             */
     MRP_ATTN_BLOCK = 1,         /* 0 .. prefix_len[b] + new tokens - 1: the block sees itself whole   */
-    MRP_ATTN_PREFIX = 2         /* 0 .. prefix_len[b] - 1: the cache alone                            */
+    MRP_ATTN_PREFIX = 2         /* 0 .. prefix_len[b] - 1: the cache alone, which needs no room for the new tokens */
 } mrp_attention_mask;
 
 typedef struct {
@@ -539,8 +539,7 @@ int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8
 
 /*
  * mrp_paged_attention over such a cache: the same masks, outputs and work split, on the values the rows stand for.  Queries
- * stay as they are.  With MRP_ATTN_PREFIX the new tokens need no room in the cache: prefix_len[b] alone has to fit.  A
- * visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
+ * stay as they are.  A visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
  * bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA feeds; others, f32 and
  * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Values below 2^-126 may lose bits (f32 too).  Errors: INVALID_ARG,
  * UNSUPPORTED, CUDA.

@@ -811,6 +811,7 @@ AttnParams attn_params(Ctx *c, const mrp_kv_batch &batch, const mrp_attention_ar
     p.H = kv.n_heads; p.Hk = kv.n_kv_heads; p.g = kv.n_heads / kv.n_kv_heads; p.D = kv.head_dim;
     p.gdiv = make_fastdiv(p.g);
     p.mask = a.mask; p.window = a.window; p.sinks = a.window > 0 ? a.sinks : 0;
+    if (a.mask == MRP_ATTN_PREFIX) p.b.beyond = 0x7fffffff - p.b.cap;      // (the new tokens' own keys lie elsewhere)
     p.rows_upto = 0x7fffffff;
     p.scale_log2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)kv.head_dim)) * 1.4426950408889634f;
     return p;
@@ -853,7 +854,6 @@ cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const m
     p.k = pool.k; p.v = pool.v;
     p.k_scale = pool.k_scale; p.v_scale = pool.v_scale;
     p.scale_bytes = (int64_t)c->kv.n_pages * c->kv.n_kv_heads * c->kv.page_size;
-    if (a.mask == MRP_ATTN_PREFIX) p.b.beyond = 0x7fffffff - p.b.cap;      // (the block's own keys lie elsewhere)
     return kv_tc_takes_q8(c->cfg, c->kv) ? launch_paged_attention_q8_tc(c, p, batch, st) : launch<kFromQ8>(c, p, st);
 }
 
