@@ -381,7 +381,7 @@ typedef struct {
                                     [h g, (h + 1) g), g = n_heads / n_kv_heads, read key head h               */
     int32_t head_dim;            /* multiple of 8, at most 256                                               */
     int32_t page_size;           /* rows per page, >= 1                                                      */
-    int32_t n_pages;             /* pages of a pool (0: no cache, mrp_qk_norm_rotate only)                   */
+    int32_t n_pages;             /* pages of a pool (0: no cache, mrp_qk_norm_rotate and mrp_packed_attention only) */
     int32_t max_pages;           /* entries of a page table row: a sequence holds at most max_pages *
                                     page_size <= 2^30 positions                                              */
     int64_t page_stride;         /* elements from a page to the next, a multiple of 8; 0 = pages one after
@@ -393,12 +393,16 @@ typedef struct {
     float norm_eps;              /* epsilon of the per-head RMSNorm                                          */
 } mrp_kv_config;
 
-/* Bytes of additional device workspace (0 on a bad configuration). */
+/*
+ * Bytes of additional device workspace (0 on a bad configuration): what every call can use.  On a bf16 context whose pages are
+ * read in tiles of 16 rows (n_pages 0, or page_size no multiple of 8) only mrp_packed_attention uses all of it: the bytes of
+ * the same configuration with MRP_FLAG_FORCE_SIMT serve too, and packed attention beyond short sequences is slower with them.
+ */
 size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv);
 
 /*
  * Attach a cache geometry to a context (workspace borrowed until mrp_destroy or the next attach: DEVICE, 256-byte
- * aligned, at least mrp_kv_workspace_bytes; it must not serve another context too).  Like mrp_create this call may
+ * aligned, mrp_kv_workspace_bytes or what is said there; it must not serve another context too).  Like mrp_create this call may
  * block (it clears the workspace's arrival counters, on the legacy stream); make it outside of any stream capture, with no
  * call on the context in flight and nothing pending on any stream that writes the workspace.  The three calls below run on the context's device and, like every call on a context, one after the
  * other: a captured graph of them counts as a call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.

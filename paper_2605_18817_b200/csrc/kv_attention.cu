@@ -819,11 +819,15 @@ AttnParams attn_params(Ctx *c, const mrp_kv_batch &batch, const mrp_attention_ar
 
 }  // namespace
 
-size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv)
+static size_t workspace_for(bool large_tiles)
 {
     const size_t few = kKvCounterBytes + (size_t)4 * kKvMaxSm * slot_bytes();
-    return kv_tc_any(cfg, kv) && kv_tc_workspace_bytes() > few ? kv_tc_workspace_bytes() : few;
+    return large_tiles && kv_tc_workspace_bytes() > few ? kv_tc_workspace_bytes() : few;
 }
+size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv) { return workspace_for(kv_tc_any(cfg, kv)); }
+// Packed attention alone has large tiles on a geometry whose pages have none: what is smaller serves everything else.
+size_t kv_workspace_least(const mrp_config &cfg, const mrp_kv_config &kv) { return workspace_for(kv_tc_takes(cfg, kv)); }
+static bool large_tiles_fit(const Ctx *c) { return c->kv_ws_bytes >= kv_tc_workspace_bytes(); }
 
 cudaError_t kv_attach(Ctx *c)
 {
@@ -854,7 +858,7 @@ cudaError_t launch_paged_attention_q8(Ctx *c, const mrp_kv_batch &batch, const m
     p.k = pool.k; p.v = pool.v;
     p.k_scale = pool.k_scale; p.v_scale = pool.v_scale;
     p.scale_bytes = (int64_t)c->kv.n_pages * c->kv.n_kv_heads * c->kv.page_size;
-    return kv_tc_takes_q8(c->cfg, c->kv) ? launch_paged_attention_q8_tc(c, p, batch, st) : launch<kFromQ8>(c, p, st);
+    return kv_tc_takes_q8(c->cfg, c->kv) && large_tiles_fit(c) ? launch_paged_attention_q8_tc(c, p, batch, st) : launch<kFromQ8>(c, p, st);
 }
 
 cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp_packed_kv &kv, const mrp_attention_args &a, cudaStream_t st)
@@ -866,7 +870,8 @@ cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp
     p.k_stride = kv.k_stride; p.v_stride = kv.v_stride;
     p.join = kv.join != 0;
     if (!kv_tc_takes_rows(c->cfg, c->kv, kv)) return launch<kFromRows>(c, p, st);
-    return packed_short(p, batch.max_new) ? launch_packed_attention_short(c, p, batch, st) : launch_packed_attention_tc(c, p, batch, st);
+    if (packed_short(p, batch.max_new)) return launch_packed_attention_short(c, p, batch, st);
+    return large_tiles_fit(c) ? launch_packed_attention_tc(c, p, batch, st) : launch<kFromRows>(c, p, st);
 }
 
 }  // namespace mrp

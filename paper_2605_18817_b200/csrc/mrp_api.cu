@@ -476,7 +476,7 @@ int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t
 {
     if (!ctx || !workspace || ((uintptr_t)workspace & 255u) || !kv_ok(kv)) return MRP_ERR_INVALID_ARG;
     Ctx &c = ctx->c;
-    if (workspace_bytes < kv_workspace_bytes(c.cfg, *kv)) return MRP_ERR_NOMEM;
+    if (workspace_bytes < kv_workspace_least(c.cfg, *kv)) return MRP_ERR_NOMEM;
     DeviceGuard guard(c.cfg.device);
     if (guard.err != cudaSuccess) return MRP_ERR_CUDA;
     c.err[0] = 0;
@@ -490,6 +490,7 @@ int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t
         c.kv_turn[j] = turns >= 1.0 ? 0 : (uint64_t)(turns * 18446744073709551616.0);
     }
     c.kv_ws = (char *)workspace;
+    c.kv_ws_bytes = workspace_bytes;
     const cudaError_t e = kv_attach(&c);
     if (e != cudaSuccess) {
         note_err(&c, e, "mrp_kv_attach");

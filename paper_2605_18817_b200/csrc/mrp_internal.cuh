@@ -106,6 +106,7 @@ struct Ctx {
     mrp_kv_config kv;
     uint64_t kv_turn[128];     // 2^64 / (2 pi) * inv_freq[j] mod 2^64: position * kv_turn[j] is the exact angle in turns
     char *kv_ws;
+    size_t kv_ws_bytes;
     void *kv_encode;           // cuTensorMapEncodeTiled, or nullptr where the geometry does not take the TMA kernel
     char err[192];             // detail of the last failure ("" if none)
     bool prof_enabled;
@@ -289,6 +290,7 @@ size_t module_att_offset(const mrp_config &cfg);   // the clean-prefix attention
 
 // ---- the paged key / value cache (kv_rows.cu, kv_read.cu, kv_attention.cu, kv_attention_tc.cu) ------
 size_t kv_workspace_bytes(const mrp_config &cfg, const mrp_kv_config &kv);
+size_t kv_workspace_least(const mrp_config &cfg, const mrp_kv_config &kv);   // with which packed attention may be slower
 cudaError_t kv_attach(Ctx *c);               // after the kv fields are set: clears the counters, sets kernel attributes
 cudaError_t launch_qk_rows(Ctx *c, const mrp_kv_batch *batch, const mrp_module_kv *pages, const int32_t *positions,
                            int n_tokens, const mrp_qkv_rows &rows, cudaStream_t st);
