@@ -755,10 +755,23 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
     cp_wait<0>();
 }
 
-// Whether packed sequences go without tiles of 128 rows, by the longest as far as the host knows it: 16 sequences of 32 tokens, 32 / 8
-// heads of 128, 10.8 against 14.5 us, of 64 19.0 against 18.2, of 128 38.8 against 29.6 (16 / 8 heads: 7.9 / 13.5, 12.4 / 15.6,
-// 24.1 / 20.5); 16 / 4 heads of 256: 11.9 against 16.9, 25.9 against 18.8.
-bool packed_short(const AttnParams &p, int max_new) { return max_new <= 128 && (long long)max_new * p.g <= (p.D <= 128 ? 256 : 128); }
+// Whether packed sequences go without tiles of 128 rows, by the longest as far as the host knows it.  The short kernel takes a chunk of 64
+// keys after the other and shares nothing between its CTAs of 64 rows, so a second chunk is what makes it the slower one, and not the
+// rows (us in a graph, short / 128-row tiles, n tokens a sequence):
+//   one chunk      40 sequences, 32 / 8 heads of 128: n 32 17.9 / 25.1, n 64 33.2 / 41.1; 16 / 8: n 64 20.8 / 27.4; 8 / 1: n 64 12.6 / 19.1
+//                  (16 sequences, 32 / 8, n 64: 19.3 / 18.1, a wave and a bit of three CTAs an SM, but ragged 12.5 / 16.7)
+//   half a second  heads of 64: 40, 32 / 8, n 96 34.1 / 42.9, whole blocks 36.1 / 38.8; of 128, where the mask is causal (the first rows skip the
+//                  second chunk) and sequences many: 40, 32 / 8 59.2 / 65.4, 16 / 8 34.1 / 39.6, one 11.9 / 10.7; whole blocks 64.1 / 57.6
+//   two            40, 32 / 8, n 128 85.6 / 69.2; 16, 16 / 8 25.1 / 20.5
+//   heads of 256   one CTA an SM: 16, 16 / 4, n 16 10.9 / 14.9, n 32 (a wave) 12.2 / 16.8, 40 (more) 33.1 / 29.0
+// Over the 784 batches measured (1 to 100 sequences, equal or ragged lengths) it costs 1 % over always taking the better one; the dearest
+// choices are 100 of n 85, 15 / 5 heads of 80, 55.7 / 47.1, and, not made, 100 ragged of up to 128, 8 / 8, 38.7 / 58.4.
+bool packed_short(const Ctx *c, const AttnParams &p, const mrp_kv_batch &batch)
+{
+    const long long units = (long long)batch.n_seqs * p.Hk, groups = ((long long)batch.max_new * p.g + 63) / 64;
+    if (p.D > 128) return batch.max_new <= 64 && (groups <= 1 || units * groups <= c->sm_count);
+    return batch.max_new <= 64 || (batch.max_new <= 96 && (p.D <= 64 || (p.mask == MRP_ATTN_CAUSAL && 2 * units > c->sm_count)));
+}
 
 size_t slot_bytes() { return (size_t)kRows * (256 * 4 + 8); }
 
@@ -870,7 +883,7 @@ cudaError_t launch_packed_attention(Ctx *c, const mrp_kv_batch &batch, const mrp
     p.k_stride = kv.k_stride; p.v_stride = kv.v_stride;
     p.join = kv.join != 0;
     if (!kv_tc_takes_rows(c->cfg, c->kv, kv)) return launch<kFromRows>(c, p, st);
-    if (packed_short(p, batch.max_new)) return launch_packed_attention_short(c, p, batch, st);
+    if (packed_short(c, p, batch)) return launch_packed_attention_short(c, p, batch, st);
     return large_tiles_fit(c) ? launch_packed_attention_tc(c, p, batch, st) : launch<kFromRows>(c, p, st);
 }
 
