@@ -1,8 +1,9 @@
 """Packed attention: a value that is not finite reaches only the rows that see it, wherever the borders of a kernel's tiles of query rows
 and keys fall: before a window, behind the diagonal, between the first tokens and the window.
 
-Rows that do not see the key give the bits that they give without it: its probability is 0 and its row counts as zeros, and adding
-0 changes no sum.  Rows that see it are not finite where it is not."""
+A value: rows that do not see it give the bits that they give without it, since its probability is 0 and its row counts as zeros, and
+adding 0 changes no sum; rows that see it are not finite where it is not.  A key: rows that do not see it are as close to the definition
+as ever (the rows of a warp raise their maxima together, so they may round in other places); rows that see it are NaN."""
 import pytest
 import torch
 
@@ -46,6 +47,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(case, flags):
     kw = dict(mask=mask, window=window, sinks=sinks)
     prior, pl = c.rand(c.T, H, D), c.rand(c.T, H).float()
     starts = [int(s) for s in c.start_np]
+    mine = torch.arange(c.T, device=DEV) < starts[-1]
     for hint in (max(new), 1, 10000):                      # each kernel, whichever the lengths would choose
         c.batch.c.max_new = hint
         plain, lse = c.attend(**kw)
@@ -71,6 +73,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(case, flags):
                 c.k[s + j] = float("nan")
                 out, l2 = c.attend(**kw)
                 c.k[s + j] = good
-                assert torch.equal(out[~hit], plain[~hit]) and torch.equal(l2[~hit], lse[~hit]), (hint, b, j)
+                c.close(out, l2, rows=~hit & mine, **kw)
+                assert (out[~mine] == 7).all() and (l2[~mine] == 7).all(), (hint, b, j)
                 assert torch.isnan(out[hit].float()).all() and torch.isnan(l2[hit]).all()
     assert int(c.status.item()) == 0
