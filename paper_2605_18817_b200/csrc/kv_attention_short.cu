@@ -88,7 +88,7 @@ __device__ __forceinline__ void short_rows(const AttnParams &p, int start, int n
     };
     auto load = [&](int c, int stage) {
         const uint32_t sk = smem + stage * 2 * kPart, sv = sk + kPart;
-        const int fill = min(kChunk, (n - c * kChunk + 15) & ~15) * C;         // (sixteen keys at a time are read)
+        const int fill = min(kChunk, (end - c * kChunk + 15) & ~15) * C;       // (sixteen keys at a time are read)
         for (int i = tid; i < fill; i += kShortThreads) {
             const int row = i / C, ch = i % C, j = c * kChunk + row;
             const bool on = j < end && (j >= lo || j < p.sinks) && ch * 8 < p.D;
@@ -160,7 +160,7 @@ __device__ __forceinline__ void short_rows(const AttnParams &p, int start, int n
             __syncthreads();
             const int key = tid >> 1;      // two threads a key
             bool mine = false;
-            for (int ch = tid & 1; ch < C && j0 + key < n; ch += 2) {
+            for (int ch = tid & 1; ch < C && j0 + key < end; ch += 2) {
                 uint32_t w[4];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(row_chunk<DP>(sv, key, ch)) : "memory");
 #pragma unroll
@@ -178,7 +178,7 @@ __device__ __forceinline__ void short_rows(const AttnParams &p, int start, int n
             __syncthreads();
         }
         if (warp_live) {
-            const int keys = n - j0;       // of the chunk, or more
+            const int keys = end - j0;     // of the chunk, or more
             float s[8][4];
 #pragma unroll
             for (int t = 0; t < 8; ++t)
