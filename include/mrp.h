@@ -404,8 +404,9 @@ size_t mrp_kv_workspace_bytes(const mrp_config *cfg, const mrp_kv_config *kv);
  * Attach a cache geometry to a context (workspace borrowed until mrp_destroy or the next attach: DEVICE, 256-byte
  * aligned, mrp_kv_workspace_bytes or what is said there; it must not serve another context too).  Like mrp_create this call may
  * block (it clears the workspace's arrival counters, on the legacy stream); make it outside of any stream capture, with no
- * call on the context in flight and nothing pending on any stream that writes the workspace.  The three calls below run on the context's device and, like every call on a context, one after the
- * other: a captured graph of them counts as a call on its context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
+ * call on the context in flight and nothing pending on any stream that writes the workspace.  The calls below run on the
+ * context's device and, like every call on a context, one after the other: a captured graph of them counts as a call on its
+ * context while it is replayed.  Errors: INVALID_ARG, NOMEM, CUDA.
  */
 int mrp_kv_attach(mrp_ctx *ctx, const mrp_kv_config *kv, void *workspace, size_t workspace_bytes);
 
@@ -542,11 +543,13 @@ int mrp_kv_read_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8
                    void *cuda_stream);
 
 /*
- * mrp_paged_attention over such a cache: the same masks, outputs and work split, on the values the rows stand for.  Queries
- * stay as they are.  A visible row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
+ * mrp_paged_attention over such a cache: the same masks, outputs and work split, on the values the rows stand for.  A visible
+ * row of NaN makes the scores of those that see it NaN (k), or their output (v; its lse does not depend on values).
  * bf16 with head_dim a multiple of 16, page_size of 8 and page_stride of 16 runs on tiles that TMA feeds; others, f32 and
- * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Values below 2^-126 may lose bits (f32 too).  Errors: INVALID_ARG,
- * UNSUPPORTED, CUDA.
+ * MRP_FLAG_FORCE_SIMT on tiles of 16 rows.  Values below 2^-126 may lose bits (f32 too).  Queries enter the products as they
+ * are, but in batches of up to 16 rows on the tiles that TMA feeds, or in the launch that serves the sequences of up to 16 rows of
+ * longer ones: there as two e4m3 parts, which hold all of a bf16 but of elements below 2^-13 of their row's largest, and those to
+ * 2^-21 of that largest.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv_pool_q8 *pool,
                            const mrp_attention_args *args, void *cuda_stream);
@@ -559,7 +562,10 @@ int mrp_paged_attention_q8(mrp_ctx *ctx, const mrp_kv_batch *batch, const mrp_kv
  * join != 0: out and lse hold the result of a pass over OTHER keys for the same queries (a block's cached prefix:
  * mrp_paged_attention or _q8 with MRP_ATTN_PREFIX) and become the result over both sets, so a block that is decoded again
  * and again attends to its own keys as they are and stores them only once it is committed.  Where lse holds -inf, out is
- * not read.  out is a result rounded to the context dtype, so a joined row carries that rounding beside its own.
+ * not read.  out is a result rounded to the context dtype, so a joined row carries that rounding beside its own.  `sinks` counts
+ * from a sequence's first row here: for one window over cache and rows take the window in both passes and sinks = 0 in this
+ * one, which is exact where prefix_len >= sinks.  A sequence that the first pass reported and skipped is joined with whatever
+ * out and lse held.
  * Of the batch, prefix_len, page_table and positions are not read and may be NULL; needs a geometry (mrp_kv_attach; n_pages
  * may be 0), whose workspace it uses.  A token that sees nothing, scores, sums, values that are not finite, streams and
  * repeats as in mrp_paged_attention; probabilities are rounded to bf16 once on the tiles that TMA feeds (all bf16 contexts
