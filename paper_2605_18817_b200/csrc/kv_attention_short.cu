@@ -6,8 +6,8 @@
 // head, a warp 16 of them, which it takes from the scores to the output in registers (mma.sync m16n8k16); keys and values go
 // through shared memory in chunks of 64 (cp.async, two stages), and three CTAs share an SM.
 // Longer sequences are served rightly too, a chunk after the other; the 128-row tiles (kv_attention_tc.cu) do it faster.  The
-// whole call, with joining: 32 blocks of 4, 32 / 8 heads, 8.6 us (128-row tiles 19.0); 12 blocks of 32, 16 / 8 heads, 9.1
-// (12.1); 40 prompts of up to 70 tokens, 15 / 5 heads of 80, 18.1 (24.5).
+// whole call, with joining: 32 blocks of 4, 32 / 8 heads, 8.8 us (128-row tiles 19.0); 12 blocks of 32, 16 / 8 heads, 9.4
+// (12.1); 40 prompts of up to 70 tokens, 15 / 5 heads of 80, 17.8 (24.5).
 //
 // Keys that no row of the CTA sees (behind the sequence's end or the diagonal, before the window) are not read and count as zeros: 0 *
 // NaN must not reach a product.  A V row with a value that is not finite that some rows of the CTA see and others do not is zeroed in
@@ -241,7 +241,8 @@ __device__ __forceinline__ void short_rows(const AttnParams &p, int start, int n
 #pragma unroll
                         for (int x = 0; x < 2; ++x) spoiled[x] |= sees(j0 + e, hi_r[x], lo_r[x], p.sinks);
             }
-            // ---- O += P V, P as bf16 (2^-8 of each at most; the sum takes the unrounded values)
+            // ---- O += P V, P as bf16 (2^-8 of each at most; the sum takes the unrounded values): half the products of two parts,
+            // and what the 128-row tiles do, so that a sequence's precision does not depend on which kernel its batch takes
 #pragma unroll
             for (int t = 0; t < 8; t += 2) {
                 if (t * 8 >= keys) break;

@@ -29,7 +29,7 @@
 //   product of the tile may start: that product adds to all columns.
 //
 // Other sources of K and V (LAY), same tiles and MMAs:
-//   kPacked  rows beside the queries, no pages: 4 prompts of 600 to 4000 tokens, 32 / 8 heads: 435 us, 0.74 PFLOP/s.  Joining reads
+//   kPacked  rows beside the queries, no pages: 4 prompts of 600 to 4000 tokens, 32 / 8 heads: 437 us, 0.74 PFLOP/s.  Joining reads
 //            the row and its log-sum-exp before it writes them.
 //   kCodes   8 bits: TMA fetches codes into raw stages, and warps of their own (two beside two row tiles, four beside one) turn
 //            codes times scales into bf16 stages of the ring, exactly.  Waits, lookups and cleaning are functions then: a loop of
