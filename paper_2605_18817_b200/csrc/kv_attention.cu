@@ -758,14 +758,14 @@ __global__ void __launch_bounds__(kThreads, Smem<T, DP, SRC>::kCtas) kv_attentio
 // Whether packed sequences go without tiles of 128 rows, by the longest as far as the host knows it.  The short kernel takes a chunk of 64
 // keys after the other and shares nothing between its CTAs of 64 rows, so a second chunk is what makes it the slower one, and not the
 // rows (us in a graph, short / 128-row tiles, n tokens a sequence):
-//   one chunk      40 sequences, 32 / 8 heads of 128: n 32 17.9 / 25.1, n 64 33.2 / 41.1; 16 / 8: n 64 20.8 / 27.4; 8 / 1: n 64 12.6 / 19.1
-//                  (16 sequences, 32 / 8, n 64: 19.3 / 18.1, a wave and a bit of three CTAs an SM, but ragged 12.5 / 16.7)
-//   half a second  heads of 64: 40, 32 / 8, n 96 34.1 / 42.9, whole blocks 36.1 / 38.8; of 128, where the mask is causal (the first rows skip the
-//                  second chunk) and sequences many: 40, 32 / 8 59.2 / 65.4, 16 / 8 34.1 / 39.6, one 11.9 / 10.7; whole blocks 64.1 / 57.6
-//   two            40, 32 / 8, n 128 85.6 / 69.2; 16, 16 / 8 25.1 / 20.5
-//   heads of 256   one CTA an SM: 16, 16 / 4, n 16 10.9 / 14.9, n 32 (a wave) 12.2 / 16.8, 40 (more) 33.1 / 29.0
+//   one chunk      40 sequences, 32 / 8 heads of 128: n 32 17.6 / 24.9, n 64 30.4 / 41.0; 16 / 8: n 64 19.1 / 27.3; 8 / 1: n 64 12.0 / 18.8
+//                  (16 whole blocks, 32 / 8, n 64: 16.9 / 15.7, a wave and a bit of three CTAs an SM; ragged prompts 11.3 / 16.6)
+//   half a second  heads of 64: 40, 32 / 8, n 96 32.2 / 42.6, whole blocks 36.1 / 38.6; of 128, where the mask is causal (the first rows skip the
+//                  second chunk) and sequences many: 40, 32 / 8 54.3 / 65.1, 16 / 8 32.0 / 39.5, one 11.6 / 10.8; whole blocks 62.3 / 57.5
+//   two            40, 32 / 8, n 128 77.7 / 69.3; 16, 16 / 8 23.6 / 20.5
+//   heads of 256   one CTA an SM: 16, 16 / 4, n 16 10.9 / 14.8, n 32 (a wave) 12.2 / 16.8, 40 (more) 31.5 / 28.8
 // Over the 784 batches measured (1 to 100 sequences, equal or ragged lengths) it costs 1 % over always taking the better one; the dearest
-// choices are 100 of n 85, 15 / 5 heads of 80, 55.7 / 47.1, and, not made, 100 ragged of up to 128, 8 / 8, 38.7 / 58.4.
+// choices are 100 of n 85, 15 / 5 heads of 80, 53.1 / 47.0, and, not made, 100 ragged of up to 128, 8 / 8, 37.7 / 57.8.
 bool packed_short(const Ctx *c, const AttnParams &p, const mrp_kv_batch &batch)
 {
     const long long units = (long long)batch.n_seqs * p.Hk, groups = ((long long)batch.max_new * p.g + 63) / 64;
